@@ -412,10 +412,141 @@ STLITE_API stlite_status stlite_decode_attention_layers(const stlite_shape* shap
 STLITE_API stlite_status stlite_decode_layers_workspace_size(const stlite_shape* shape, int32_t n_layers,
                                                              size_t* bytes);
 
+/* ---- paged caches ----------------------------------------------------------
+ * A server keeps many sessions' caches, each of its own length after
+ * compression, in pages.  A page holds page_rows consecutive cached rows of
+ * one layer, laid out as the library's caches are; a layer's page pools are
+ *     k_pages, v_pages  [n_pages][page_rows][Hkv][d]   (shape->dtype)
+ * and row r of sequence s is row r % page_rows of page
+ * table[s][r / page_rows].  All layers of a model may share one table.  The
+ * int32 arrays are device memory, 4-byte aligned, and are read when the
+ * kernels run: a captured call follows whatever they hold at replay.  Kernels
+ * check every entry: a row whose page lies outside [0, n_pages), or that lies
+ * outside [0, max_pages * page_rows), is neither read nor written.
+ * n_pages * page_rows, n_seqs * max_pages and max_pages * page_rows each fit
+ * an int32. */
+typedef struct {
+  int32_t n_seqs;        /* S >= 1 */
+  int32_t n_pages;       /* pages of each pool, >= 1 */
+  int32_t page_rows;     /* cached rows of a page, >= 1 */
+  int32_t max_pages;     /* entries of table for each sequence, >= 1 */
+  const int32_t* table;  /* device [S][max_pages] */
+  const int32_t* len;    /* device [S]: cached rows of each sequence, the step's new tokens included
+                            (stlite_compact_paged, stlite_compress_layers_paged: not read, may be NULL) */
+  const int32_t* cu_new; /* device [S + 1], or NULL: sequence s owns the packed new tokens
+                            [cu_new[s], cu_new[s + 1]), non-decreasing from 0; NULL: every sequence has
+                            shape->window of them, T = S * window */
+} stlite_pages;
+
+/* Rotary position encoding.  Pair i (0 .. 63) of a head turns by the angle
+ * p * inv_freq[i], p the token's position on the pair's axis: the first
+ * section[0] pairs use axis 0, the next section[1] axis 1, the last section[2]
+ * axis 2 (temporal, row and column positions of a vision-language model).
+ * section = {64, 0, 0} has one axis.  The angle is taken modulo whole turns in
+ * 64-bit integers, so that it keeps its precision at any position. */
+typedef struct {
+  double inv_freq[STLITE_HEAD_DIM / 2]; /* radians per position, within +-2^32 */
+  int32_t section[3];                   /* each >= 0, together 64 */
+  int32_t interleaved;                  /* 0: pair i is elements (i, i + 64); 1: (2 i, 2 i + 1) */
+} stlite_rope;
+
+/* inv_freq[i] = base^(-2 i / d), section {64, 0, 0}, not interleaved.  Host
+ * only.  STLITE_EINVAL unless base is finite and > 0. */
+STLITE_API stlite_status stlite_rope_init(double base, stlite_rope* rope);
+
+/* T = shape->n_tokens packed tokens as the projections leave them (device):
+ * q [T][Hq][d], k and v [T][Hkv][d], each token's heads packed and tokens
+ * *_stride elements apart (0: packed; otherwise a multiple of 16 bytes, at
+ * least the heads' extent), so that the three may be slices of one
+ * projection's output. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v; /* stlite_paged_append only */
+  int64_t q_stride, k_stride, v_stride;
+  const void* q_norm; /* [d] weights (shape->dtype) of each query head's RMS norm, or NULL: none */
+  const void* k_norm; /* the same for key heads */
+  float eps;          /* of the norms: finite, >= 0 */
+  const int32_t* pos; /* device, 4-byte aligned: [T] positions where section = {64, 0, 0}, else [3][T] */
+} stlite_tokens;
+
+/* Rotated queries and keys of a prompt, what stlite_score and
+ * stlite_compress_layer take: for every head x of q and k,
+ *   y = x / sqrt(mean(x^2) + eps) * norm      (norm given; else y = x)
+ *   out = y rotated by its token's position   (see stlite_rope)
+ * in fp32, rounded once.  q_out [T][Hq][d], k_out [T][Hkv][d], packed.
+ * q_out may be x->q, and k_out x->k, where those are packed; other overlap of
+ * inputs and outputs is not allowed.  shape->window is not used (any valid
+ * value). */
+STLITE_API stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
+                                          void* q_out, void* k_out, void* stream);
+
+/* The new tokens of a serving step (a token of every session, drafts, or
+ * chunks of prompts) into the pages: q_out [T][Hq][d] and the cached keys are
+ * the rotated heads of stlite_rotate_qk, values are copied.  Token i of the n_s
+ * new ones of sequence s becomes row len[s] - n_s + i.  Tokens behind
+ * cu_new[S] are padding: they and their rows of q_out are left alone.  A row
+ * that lies outside its sequence's pages or names a page outside the pool is
+ * not written (its q_out is).  Rows that two sequences share are not to be
+ * written by both.  q_out may be x->q where that is packed.
+ * shape: n_tokens = T; window = tokens of each sequence where cu_new is NULL
+ *   (otherwise not used). */
+STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope,
+                                             const stlite_tokens* x, const stlite_pages* pages, void* q_out,
+                                             void* k_pages, void* v_pages, void* stream);
+
+/* Attention of every session's new tokens over its cache (the paged form of
+ * stlite_decode_attention, for a batch): new token i of the n_s of sequence s
+ * attends to rows j < len[s] - (n_s - 1 - i), that is to everything before
+ * it and itself,
+ *   out[t][g][:] = sum_j softmax_j(q[t][g] . k_j / sqrt(d)) v_j
+ * with the rows of KV head g / (Hq/Hkv).  A token that sees no row (an idle
+ * session of length 0) gets zeros.  Rows past a sequence's length, and
+ * whatever they hold, take no part.  A page outside the pool, or a length past
+ * max_pages * page_rows, leaves those rows out and records STLITE_EINVAL in
+ * the workspace error word.
+ * shape: n_tokens = T; window = the most new tokens of a sequence (cu_new NULL:
+ *   of each), 1 .. 16 (further tokens of a sequence are left unwritten);
+ *   Hq / Hkv <= 16.
+ * q, out [T][Hq][d] (shape->dtype), packed; rows behind cu_new[S] are left
+ *   alone.  ws: at least stlite_paged_workspace_size bytes, zero-filled before
+ *   its first use (its first word is the error word of
+ *   stlite_device_status).  The work is divided over the GPU by the lengths as
+ *   they are when the kernels run, so one capture serves growing caches. */
+STLITE_API stlite_status stlite_paged_attention(const stlite_shape* shape, const stlite_pages* pages, const void* q,
+                                                const void* k_pages, const void* v_pages, void* out, void* ws,
+                                                size_t ws_bytes, void* stream);
+
+/* Workspace bytes of stlite_paged_attention. */
+STLITE_API stlite_status stlite_paged_workspace_size(const stlite_shape* shape, const stlite_pages* pages,
+                                                     size_t* bytes);
+
+/* stlite_compact into pages, for n_layers layers: row r of head h of sequence
+ * `seq` becomes k[idx[h][r]][h], r < budget.  layers: HOST array; each
+ * entry's k and v are the layer's cache [N][Hkv][d] (v may be page-locked host
+ * memory), k_out and v_out its page POOLS, idx_out (read) its device int32
+ * [Hkv][budget]; q is not used.  A row whose index lies outside [0, N), or
+ * whose page is not one, is left unwritten.  pages->len is the caller's to
+ * set. */
+STLITE_API stlite_status stlite_compact_paged(const stlite_shape* shape, int32_t budget, const stlite_pages* pages,
+                                              int32_t seq, int32_t n_layers, const stlite_layer_io* layers,
+                                              void* stream);
+
+/* stlite_compress_layers whose compaction writes the kept rows into sequence
+ * `seq`'s pages: k_out and v_out of each layer are its page POOLS.  The B kept
+ * rows have to fit the sequence's table (STLITE_EINVAL where B > max_pages *
+ * page_rows).  Everything else as for stlite_compress_layers. */
+STLITE_API stlite_status stlite_compress_layers_paged(const stlite_shape* shape, const stlite_frames* frames,
+                                                      const stlite_params* params, const stlite_pages* pages,
+                                                      int32_t seq, int32_t n_layers, const stlite_layer_io* layers,
+                                                      int32_t* budget_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Reads and clears the workspace's device error word (synchronises `stream`).
  * *status receives STLITE_OK, STLITE_ETIMEOUT if a kernel's bounded wait ran
- * out since the last read, or STLITE_ECUDA if a kernel found its launch
- * configuration unusable (it then returned without touching its outputs).
+ * out since the last read, STLITE_ECUDA if a kernel found its launch
+ * configuration unusable (it then returned without touching its outputs), or
+ * STLITE_EINVAL if stlite_paged_attention met a page or a length outside its
+ * bounds.
  * ws = NULL reads the error word of stlite_score_noalloc's fixed scratch on
  * the current device instead. */
 STLITE_API stlite_status stlite_device_status(void* ws, void* stream, stlite_status* status);

@@ -425,6 +425,13 @@ void select_variants(SelectArgs& a, const stlite_params* params, const Problem& 
   a.a_norm_max = params->abase_norm == STLITE_ABASE_MAX ? 1 : 0;
 }
 
+// Pages and sequence that the kept rows of a call go to, in place of dense
+// outputs, and every layer's budget.
+struct PagedRows {
+  PageView pages;
+  int seq, budget;
+};
+
 // Algorithm 1 for a batch of layers (steps 1-5), every stage one launch.
 // Layer l keeps io.budget[l] tokens per KV head.  With a second stream
 // (aux_stream), step 1 runs on it beside steps 2-3: CSS and TSG are enqueued
@@ -433,7 +440,8 @@ void select_variants(SelectArgs& a, const stlite_params* params, const Problem& 
 // CSS's inverse norms but not Phi, so with the tensor-core CSS its second
 // kernel (Phi from the dots) goes last on the second stream, after an event
 // that marks the dots done: TSG starts as soon as the dots are written.
-stlite_status compress_batch(const Ctx& c, const stlite_params* params, const LayerPtrs& io) {
+stlite_status compress_batch(const Ctx& c, const stlite_params* params, const LayerPtrs& io,
+                             const PagedRows* to = nullptr) {
   const bool tsg = params->tsg_enable && c.ft.n_frames >= 2;
   const bool window = params->base_scorer == STLITE_BASE_WINDOW;
   Strided<float> a_base = c.view<float>(c.plan.a_base);
@@ -484,7 +492,7 @@ stlite_status compress_batch(const Ctx& c, const stlite_params* params, const La
   a.write_stages = 0;  // rho, gate and S stay on chip: only the indices leave
   for (int l = 0; l < c.p.L; ++l) a.idx[l] = io.idx[l];
   if ((e = launch_select(c.p, c.ft, a, c.st)) != cudaSuccess) return STLITE_ECUDA;
-  return cuda_status(launch_gather(c.p, io, c.st));
+  return cuda_status(to ? launch_gather_paged(c.p, io, to->pages, to->seq, c.st) : launch_gather(c.p, io, c.st));
 }
 
 }  // namespace
@@ -637,14 +645,15 @@ stlite_status stlite_compress_layer(const stlite_shape* shape, const stlite_fram
 namespace {
 
 // Algorithm 1 over n_layers layers, layer l keeping budgets[l] tokens per
-// KV head; every budget is checked before anything is enqueued.  The pointer
+// KV head (to->budget where the kept rows go to pages); every budget is checked before anything is enqueued.  The pointer
 // checks are skipped for a packed batch's per-sequence offsets (their bases
 // were checked; an index block there starts on a 4-byte boundary, which the
 // kernels' scalar index accesses need).
 stlite_status compress_layers_impl(const stlite_shape* shape, const stlite_frames* frames,
                                    const stlite_params* params, int32_t n_layers,
                                    const stlite_layer_io* layers, const int32_t* budgets, void* ws,
-                                   size_t ws_bytes, void* stream, bool check_pointers = true) {
+                                   size_t ws_bytes, void* stream, bool check_pointers = true,
+                                   const PagedRows* to = nullptr) {
   Ctx c;
   stlite_status s = prepare(shape, frames, ws, ws_bytes, n_layers, stream, &c);
   if (s != STLITE_OK) return s;
@@ -656,7 +665,7 @@ stlite_status compress_layers_impl(const stlite_shape* shape, const stlite_frame
           !aligned16(x.v_out) || !aligned16(x.idx_out))
         return STLITE_EINVAL;
     }
-    if (budgets[l] < 1 || budgets[l] > c.p.n) return STLITE_EINVAL;
+    if (!to && (budgets[l] < 1 || budgets[l] > c.p.n)) return STLITE_EINVAL;
   }
   // one launch per stage for up to kMaxLayers layers at a time
   for (int l0 = 0; l0 < n_layers; l0 += kMaxLayers) {
@@ -674,9 +683,9 @@ stlite_status compress_layers_impl(const stlite_shape* shape, const stlite_frame
       io.k_out[l] = x.k_out;
       io.v_out[l] = x.v_out;
       io.idx[l] = x.idx_out;
-      io.budget[l] = budgets[l0 + l];
+      io.budget[l] = to ? to->budget : budgets[l0 + l];
     }
-    if ((s = compress_batch(cb, params, io)) != STLITE_OK) return s;
+    if ((s = compress_batch(cb, params, io, to)) != STLITE_OK) return s;
   }
   return STLITE_OK;
 }
@@ -999,6 +1008,243 @@ stlite_status stlite_decode_attention_layers(const stlite_shape* shape, int32_t 
   return STLITE_OK;
 }
 
+// ---- paged caches -----------------------------------------------------------
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// The page geometry and table; need_len: the call reads the lengths.
+stlite_status check_pages(const stlite_pages* pg, bool need_len) {
+  if (!pg || !pg->table || !aligned4(pg->table)) return STLITE_EINVAL;
+  if (pg->n_seqs < 1 || pg->n_pages < 1 || pg->page_rows < 1 || pg->max_pages < 1) return STLITE_EINVAL;
+  if (need_len && (!pg->len || !aligned4(pg->len) || !aligned4(pg->cu_new))) return STLITE_EINVAL;
+  const long long most = 0x7fffffffLL;
+  if ((long long)pg->n_pages * pg->page_rows > most || (long long)pg->n_seqs * pg->max_pages > most ||
+      (long long)pg->max_pages * pg->page_rows > most)
+    return STLITE_EUNSUPPORTED;
+  return STLITE_OK;
+}
+
+// Without cu_new every sequence has w new tokens.
+stlite_status check_new(const stlite_shape* s, const stlite_pages* pg) {
+  if (!pg->cu_new && (long long)pg->n_seqs * s->window != s->n_tokens) return STLITE_EINVAL;
+  return STLITE_OK;
+}
+
+PageView page_view(const stlite_pages* pg, int w) {
+  PageView v;
+  v.table = pg->table;
+  v.len = pg->len;
+  v.cu = pg->cu_new;
+  v.n_seqs = pg->n_seqs;
+  v.n_pages = pg->n_pages;
+  v.page_rows = pg->page_rows;
+  v.max_pages = pg->max_pages;
+  v.w = w;
+  return v;
+}
+
+stlite_status check_rope(const stlite_rope* r) {
+  if (!r) return STLITE_EINVAL;
+  if (r->interleaved != 0 && r->interleaved != 1) return STLITE_EINVAL;
+  long long pairs = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (r->section[a] < 0) return STLITE_EINVAL;
+    pairs += r->section[a];
+  }
+  if (pairs != kD / 2) return STLITE_EINVAL;
+  for (int i = 0; i < kD / 2; ++i)
+    if (!(std::fabs(r->inv_freq[i]) <= 4294967296.0)) return STLITE_EINVAL;
+  return STLITE_OK;
+}
+
+RopeView rope_view(const stlite_rope* r) {
+  RopeView v;
+  for (int i = 0; i < kD / 2; ++i) {
+    // f / (2 pi) modulo 1 in 64 bits: 1 / (2 pi) as a sum of two doubles, the
+    // first product's rounding error recovered by fma.  (A 53-bit turn would be
+    // 1.5e-6 radians off at position 2^31.)
+    const double f = r->inv_freq[i], hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;
+    double x = f * hi;
+    const double e = std::fma(f, hi, -x) + f * lo;
+    x -= std::trunc(x);  // exact
+    const double y = std::fabs(x), top = std::floor(y * 0x1p32);
+    uint64_t turn = ((uint64_t)top << 32) + (uint64_t)((y * 0x1p32 - top) * 0x1p32);
+    if (x < 0.0) turn = 0 - turn;
+    v.turn[i] = turn + (uint64_t)(int64_t)std::rint(e * 0x1p64);
+  }
+  v.end0 = r->section[0];
+  v.end1 = r->section[0] + r->section[1];
+  v.interleaved = r->interleaved;
+  return v;
+}
+
+// A token stride: the heads' extent where 0, else checked against it.
+stlite_status token_stride(int64_t given, int heads, int esize, long long* out) {
+  const int64_t packed = (int64_t)heads * kD;
+  if (given == 0) given = packed;
+  if (given < packed || given % (16 / esize) != 0 || given > ((int64_t)1 << 40)) return STLITE_EINVAL;
+  *out = given;
+  return STLITE_OK;
+}
+
+stlite_status token_view(const stlite_shape* s, const stlite_rope* rope, const stlite_tokens* x, bool need_v,
+                         TokenView* v) {
+  stlite_status st = check_rope(rope);
+  if (st != STLITE_OK) return st;
+  if (!x || !x->q || !x->k || (need_v && !x->v) || !x->pos) return STLITE_EINVAL;
+  if (!aligned16(x->q) || !aligned16(x->k) || (need_v && !aligned16(x->v)) || !aligned16(x->q_norm) ||
+      !aligned16(x->k_norm) || !aligned4(x->pos))
+    return STLITE_EINVAL;
+  if ((x->q_norm || x->k_norm) && !(std::isfinite(x->eps) && x->eps >= 0.f)) return STLITE_EINVAL;
+  const int esize = s->dtype == STLITE_BF16 ? 2 : 4;
+  if ((st = token_stride(x->q_stride, s->n_q_heads, esize, &v->q_stride)) != STLITE_OK) return st;
+  if ((st = token_stride(x->k_stride, s->n_kv_heads, esize, &v->k_stride)) != STLITE_OK) return st;
+  if ((st = token_stride(need_v ? x->v_stride : 0, s->n_kv_heads, esize, &v->v_stride)) != STLITE_OK) return st;
+  v->q = x->q;
+  v->k = x->k;
+  v->v = x->v;
+  v->q_norm = x->q_norm;
+  v->k_norm = x->k_norm;
+  v->eps = x->eps;
+  v->pos = x->pos;
+  v->n = s->n_tokens;
+  v->hq = s->n_q_heads;
+  v->hkv = s->n_kv_heads;
+  return STLITE_OK;
+}
+
+// An output that is its input has to be packed as the output is.
+bool in_place_ok(const void* in, long long stride, int heads, const void* out) {
+  return in != out || stride == (long long)heads * kD;
+}
+
+stlite_status check_paged_attention(const stlite_shape* shape, const stlite_pages* pages) {
+  stlite_status s = check_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, true)) != STLITE_OK) return s;
+  if ((s = check_new(shape, pages)) != STLITE_OK) return s;
+  if (shape->window > kPagedMaxNew || shape->n_q_heads / shape->n_kv_heads > kDecMaxG) return STLITE_EUNSUPPORTED;
+  return STLITE_OK;
+}
+
+DType to_dtype(const stlite_shape* s) { return s->dtype == STLITE_BF16 ? kBF16 : kF32; }
+
+}  // namespace
+
+stlite_status stlite_rope_init(double base, stlite_rope* rope) {
+  if (!rope || !std::isfinite(base) || !(base > 0.0)) return STLITE_EINVAL;
+  for (int i = 0; i < kD / 2; ++i) rope->inv_freq[i] = std::pow(base, -2.0 * i / kD);
+  rope->section[0] = kD / 2;
+  rope->section[1] = rope->section[2] = 0;
+  rope->interleaved = 0;
+  return STLITE_OK;
+}
+
+stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
+                               void* q_out, void* k_out, void* stream) {
+  stlite_status s = check_shape(shape);
+  if (s != STLITE_OK) return s;
+  TokenView v;
+  if ((s = token_view(shape, rope, x, false, &v)) != STLITE_OK) return s;
+  if (!q_out || !k_out || !aligned16(q_out) || !aligned16(k_out)) return STLITE_EINVAL;
+  if (!in_place_ok(x->q, v.q_stride, v.hq, q_out) || !in_place_ok(x->k, v.k_stride, v.hkv, k_out))
+    return STLITE_EINVAL;
+  return cuda_status(launch_rotate(to_dtype(shape), v, rope_view(rope), nullptr, q_out, k_out, nullptr,
+                                   static_cast<cudaStream_t>(stream)));
+}
+
+stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
+                                  const stlite_pages* pages, void* q_out, void* k_pages, void* v_pages,
+                                  void* stream) {
+  stlite_status s = check_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, true)) != STLITE_OK) return s;
+  if ((s = check_new(shape, pages)) != STLITE_OK) return s;
+  TokenView v;
+  if ((s = token_view(shape, rope, x, true, &v)) != STLITE_OK) return s;
+  if (!q_out || !k_pages || !v_pages || !aligned16(q_out) || !aligned16(k_pages) || !aligned16(v_pages))
+    return STLITE_EINVAL;
+  if (!in_place_ok(x->q, v.q_stride, v.hq, q_out)) return STLITE_EINVAL;
+  const PageView pg = page_view(pages, shape->window);
+  return cuda_status(launch_rotate(to_dtype(shape), v, rope_view(rope), &pg, q_out, k_pages, v_pages,
+                                   static_cast<cudaStream_t>(stream)));
+}
+
+stlite_status stlite_paged_workspace_size(const stlite_shape* shape, const stlite_pages* pages, size_t* bytes) {
+  if (!bytes) return STLITE_EINVAL;
+  const stlite_status s = check_paged_attention(shape, pages);
+  if (s != STLITE_OK) return s;
+  *bytes = paged_workspace_bytes(to_dtype(shape), page_view(pages, shape->window), shape->n_q_heads, shape->n_kv_heads);
+  return STLITE_OK;
+}
+
+stlite_status stlite_paged_attention(const stlite_shape* shape, const stlite_pages* pages, const void* q,
+                                     const void* k_pages, const void* v_pages, void* out, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  const stlite_status s = check_paged_attention(shape, pages);
+  if (s != STLITE_OK) return s;
+  if (!q || !k_pages || !v_pages || !out || !ws) return STLITE_EINVAL;
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(ws))
+    return STLITE_EINVAL;
+  const PageView pg = page_view(pages, shape->window);
+  const DType dt = to_dtype(shape);
+  if (ws_bytes < paged_workspace_bytes(dt, pg, shape->n_q_heads, shape->n_kv_heads)) return STLITE_EWORKSPACE;
+  return cuda_status(launch_paged_attention(dt, pg, q, k_pages, v_pages, out, shape->n_tokens, shape->n_q_heads,
+                                            shape->n_kv_heads, ws, static_cast<cudaStream_t>(stream)));
+}
+
+stlite_status stlite_compact_paged(const stlite_shape* shape, int32_t budget, const stlite_pages* pages, int32_t seq,
+                                   int32_t n_layers, const stlite_layer_io* layers, void* stream) {
+  stlite_status s = check_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, false)) != STLITE_OK) return s;
+  if (n_layers < 1 || !layers || seq < 0 || seq >= pages->n_seqs) return STLITE_EINVAL;
+  if (budget < 1 || budget > shape->n_tokens || budget > (long long)pages->max_pages * pages->page_rows)
+    return STLITE_EINVAL;
+  for (int l = 0; l < n_layers; ++l) {
+    const stlite_layer_io& x = layers[l];
+    if (!x.k || !x.v || !x.k_out || !x.v_out || !x.idx_out) return STLITE_EINVAL;
+    if (!aligned16(x.k) || !aligned16(x.v) || !aligned16(x.k_out) || !aligned16(x.v_out) || !aligned16(x.idx_out))
+      return STLITE_EINVAL;
+  }
+  const PageView pg = page_view(pages, 1);
+  for (int l0 = 0; l0 < n_layers; l0 += kMaxLayers) {
+    const int L = n_layers - l0 < kMaxLayers ? n_layers - l0 : kMaxLayers;
+    LayerPtrs io;
+    memset(&io, 0, sizeof(io));
+    for (int l = 0; l < L; ++l) {
+      const stlite_layer_io& x = layers[l0 + l];
+      io.k[l] = x.k;
+      io.v[l] = x.v;
+      io.k_out[l] = x.k_out;
+      io.v_out[l] = x.v_out;
+      io.idx[l] = x.idx_out;
+      io.budget[l] = budget;
+    }
+    s = cuda_status(launch_gather_paged(to_problem(shape, L), io, pg, seq, static_cast<cudaStream_t>(stream)));
+    if (s != STLITE_OK) return s;
+  }
+  return STLITE_OK;
+}
+
+stlite_status stlite_compress_layers_paged(const stlite_shape* shape, const stlite_frames* frames,
+                                           const stlite_params* params, const stlite_pages* pages, int32_t seq,
+                                           int32_t n_layers, const stlite_layer_io* layers, int32_t* budget_out,
+                                           void* ws, size_t ws_bytes, void* stream) {
+  if (n_layers < 1 || !layers || !shape) return STLITE_EINVAL;
+  stlite_status s = check_params(params);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, false)) != STLITE_OK) return s;
+  if (seq < 0 || seq >= pages->n_seqs) return STLITE_EINVAL;
+  const int32_t budget = stlite_budget(shape->n_tokens, params->beta, params->k_override);
+  if (budget < 1 || budget > (long long)pages->max_pages * pages->page_rows) return STLITE_EINVAL;
+  const PagedRows to = {page_view(pages, 1), seq, budget};
+  s = compress_layers_impl(shape, frames, params, n_layers, layers, nullptr, ws, ws_bytes, stream, true, &to);
+  if (s == STLITE_OK && budget_out) *budget_out = budget;
+  return s;
+}
+
 stlite_status stlite_device_status(void* ws, void* stream, stlite_status* status) {
   if (!status || (ws && !aligned16(ws))) return STLITE_EINVAL;
   if (!ws) {  // the error word of stlite_score_noalloc's fixed scratch on the current device
@@ -1011,7 +1257,10 @@ stlite_status stlite_device_status(void* ws, void* stream, stlite_status* status
   if (cudaMemcpyAsync(&word, ws, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess) return STLITE_ECUDA;
   if (cudaStreamSynchronize(st) != cudaSuccess) return STLITE_ECUDA;
   if (cudaMemsetAsync(ws, 0, 4, st) != cudaSuccess) return STLITE_ECUDA;
-  *status = (word & kErrTimeout) ? STLITE_ETIMEOUT : (word ? STLITE_ECUDA : STLITE_OK);
+  *status = (word & kErrTimeout) ? STLITE_ETIMEOUT
+            : word == kErrInput  ? STLITE_EINVAL
+            : word               ? STLITE_ECUDA
+                                 : STLITE_OK;
   return STLITE_OK;
 }
 

@@ -15,6 +15,7 @@ constexpr int kTsgTile = 128;      // historical tokens per TSG row tile
 // Device error word bits (first 32-bit word of the workspace).
 constexpr uint32_t kErrTimeout = 1u;  // a bounded wait ran out
 constexpr uint32_t kErrLaunch = 2u;   // a kernel found its launch configuration unusable
+constexpr uint32_t kErrInput = 4u;    // a page table or a length names rows that do not exist
 
 // Bounded waits give up after this many nanoseconds of %globaltimer.
 constexpr uint64_t kWaitLimitNs = 1000000000ull;

@@ -269,4 +269,44 @@ size_t decode_workspace_bytes(int n, int hq, int hkv, int w, int layers);
 cudaError_t launch_decode(DType dt, const DecBatch& b, int layers, int n, int hq, int hkv, int w, void* ws,
                           cudaStream_t st);
 
+// ---- paged caches -----------------------------------------------------------
+// Where a sequence's rows are: row r of sequence s is row r % page_rows of page
+// table[s * max_pages + r / page_rows] of a layer's pools
+// [n_pages][page_rows][hkv][128].
+struct PageView {
+  const int32_t* table;
+  const int32_t* len;  // [n_seqs]
+  const int32_t* cu;   // [n_seqs + 1], or null: w new tokens per sequence
+  int n_seqs, n_pages, page_rows, max_pages, w;
+};
+// Rotation by position: pair i turns by turn[i] * 2^-64 of a turn per
+// position (what exceeds a turn falls off the top of 64 bits) on axis 0, 1 or
+// 2 for i < end0, < end1 or beyond.
+struct RopeView {
+  uint64_t turn[kD / 2];
+  int end0, end1;
+  int interleaved;
+};
+// Packed tokens of T * (hq + 2 hkv) heads; strides in elements.
+struct TokenView {
+  const void *q, *k, *v;
+  long long q_stride, k_stride, v_stride;
+  const void *q_norm, *k_norm;
+  float eps;
+  const int32_t* pos;  // [axes][n]
+  int n, hq, hkv;
+};
+// Rotated q to q_out and rotated k to k_out, both packed (pages null), or k
+// and v to the pages.
+cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, const PageView* pages, void* q_out,
+                          void* k_out, void* v_out, cudaStream_t st);
+// launch_gather with row r going to row r of sequence seq's pages: io.k_out
+// and io.v_out are the layers' pools.
+cudaError_t launch_gather_paged(const Problem& p, const LayerPtrs& io, const PageView& pages, int seq, cudaStream_t st);
+// Attention of pages.w (at most) new tokens of each sequence over its rows.
+constexpr int kPagedMaxNew = 16;
+size_t paged_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv);
+cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
+                                   void* out, int n, int hq, int hkv, void* ws, cudaStream_t st);
+
 }  // namespace stl

@@ -33,7 +33,9 @@ EXPORTED = ("stlite_budget", "stlite_workspace_size", "stlite_score", "stlite_ga
             "stlite_compress_layers_budgets", "stlite_hierarchical_budgets", "stlite_spatial_saliency_size",
             "stlite_compress_varlen_layers", "stlite_prompt_score", "stlite_prompt_workspace_size",
             "stlite_decode_attention_layers", "stlite_decode_layers_workspace_size",
-            "stlite_selftest_wait_timeout")
+            "stlite_selftest_wait_timeout", "stlite_rope_init", "stlite_rotate_qk", "stlite_paged_append",
+            "stlite_paged_attention", "stlite_paged_workspace_size", "stlite_compact_paged",
+            "stlite_compress_layers_paged")
 
 
 class Shape(ctypes.Structure):
@@ -67,6 +69,22 @@ class LayerIO(ctypes.Structure):
 
 class DecodeIO(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("cu_new", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_double * 64), ("section", ctypes.c_int32 * 3), ("interleaved", ctypes.c_int32)]
+
+
+class Tokens(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float), ("pos", ctypes.c_void_p)]
 
 
 class KernelTime(ctypes.Structure):
@@ -121,6 +139,19 @@ _sig = {
     "stlite_decode_attention_layers": (_S, [ctypes.POINTER(Shape), ctypes.c_int32, _P, _P, ctypes.c_size_t, _P]),
     "stlite_decode_layers_workspace_size": (_S, [ctypes.POINTER(Shape), ctypes.c_int32,
                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "stlite_rope_init": (_S, [ctypes.c_double, ctypes.POINTER(Rope)]),
+    "stlite_rotate_qk": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(Tokens), _P, _P, _P]),
+    "stlite_paged_append": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(Tokens),
+                                 ctypes.POINTER(Pages), _P, _P, _P, _P]),
+    "stlite_paged_attention": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Pages), _P, _P, _P, _P, _P,
+                                    ctypes.c_size_t, _P]),
+    "stlite_paged_workspace_size": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Pages),
+                                         ctypes.POINTER(ctypes.c_size_t)]),
+    "stlite_compact_paged": (_S, [ctypes.POINTER(Shape), ctypes.c_int32, ctypes.POINTER(Pages), ctypes.c_int32,
+                                  ctypes.c_int32, _P, _P]),
+    "stlite_compress_layers_paged": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Frames), ctypes.POINTER(Params),
+                                          ctypes.POINTER(Pages), ctypes.c_int32, ctypes.c_int32, _P,
+                                          ctypes.POINTER(ctypes.c_int32), _P, ctypes.c_size_t, _P]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -451,6 +482,181 @@ def decode_attention_layers(qs, ks, vs, stream=None):
     outs = [torch.empty(q.shape, dtype=torch.float32, device=ks[0].device) for q in qs]
     stlite_decode_attention_layers(list(zip(qs, ks, vs, outs)), ws, stream)
     return outs, ws
+
+
+# ------------------------------------------------------------ paged caches
+
+def make_rope(base=10000.0, section=(64, 0, 0), interleaved=False, inv_freq=None) -> Rope:
+    """Rotary frequencies base^(-2 i / 128), or inv_freq (64 values, for
+    scaled ones); section: pairs turned by each of the three position axes."""
+    rope = Rope()
+    _check(_lib.stlite_rope_init(float(base), ctypes.byref(rope)), "stlite_rope_init")
+    if inv_freq is not None:
+        rope.inv_freq[:] = [float(x) for x in inv_freq]
+    rope.section[:] = [int(x) for x in section]
+    rope.interleaved = int(interleaved)
+    return rope
+
+
+class PageTable:
+    """stlite_pages of int32 device tensors (kept alive with it): table
+    [S][max_pages], length [S], cu_new [S + 1] or None.  max_new: the most
+    new tokens of a sequence (of every sequence where cu_new is None)."""
+
+    def __init__(self, n_pages, page_rows, table, length=None, cu_new=None, max_new=1):
+        for t, n in ((table, 2), (length, 1), (cu_new, 1)):
+            if t is not None and (t.dtype != torch.int32 or t.dim() != n or not t.is_contiguous()):
+                raise ValueError("table, length and cu_new are contiguous int32 tensors")
+        n_seqs = table.shape[0]
+        if (length is not None and length.shape[0] != n_seqs) or (cu_new is not None and cu_new.shape[0] != n_seqs + 1):
+            raise ValueError("length is [S] and cu_new [S + 1] for a table [S][max_pages]")
+        self.table, self.length, self.cu_new, self.max_new = table, length, cu_new, int(max_new)
+        self.c = Pages(n_seqs, int(n_pages), int(page_rows), table.shape[1], _ptr(table), _ptr(length), _ptr(cu_new))
+
+
+def make_pages(n_pages, page_rows, table, length=None, cu_new=None, max_new=1) -> PageTable:
+    return PageTable(n_pages, page_rows, table, length, cu_new, max_new)
+
+
+def _check_pools(pages, hkv, dtype, *pools):
+    want = (pages.c.n_pages, pages.c.page_rows, hkv, 128)
+    for p in pools:
+        if p.shape != want or p.dtype != dtype or not p.is_contiguous():
+            raise ValueError("a page pool is a contiguous tensor %s of the cache's type" % (want,))
+
+
+def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps):
+    """stlite_tokens of q, k, v [T][H][128], each token's heads packed."""
+    n = q.shape[0]
+    strides = []
+    for x in (q, k, v):
+        if x is None:
+            strides.append(0)
+            continue
+        if x.dim() != 3 or x.shape[0] != n or x.shape[2] != 128 or x.dtype != q.dtype:
+            raise ValueError("q, k and v are [T][H][128] of one type")
+        s = x.stride()
+        if s[2] != 1 or (x.shape[1] > 1 and s[1] != 128):
+            raise ValueError("a token's heads are packed")
+        strides.append(s[0] if n > 1 else 0)
+    for w in (q_norm, k_norm):
+        if w is not None and (w.shape != (128,) or w.dtype != q.dtype or not w.is_contiguous()):
+            raise ValueError("a norm's weights are [128] of q's type")
+    axes = 1 if rope.section[0] == 64 else 3
+    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != axes * n:
+        raise ValueError("pos is a contiguous int32 [%sT]" % ("" if axes == 1 else "3]["))
+    return Tokens(q.data_ptr(), k.data_ptr(), _ptr(v), strides[0], strides[1], strides[2], _ptr(q_norm), _ptr(k_norm),
+                  eps, pos.data_ptr())
+
+
+def _check_packed(shape, dtype, *outs):
+    for o in outs:
+        if o.shape != shape or o.dtype != dtype or not o.is_contiguous():
+            raise ValueError("an output is a contiguous %s of q's type" % (tuple(shape),))
+
+
+def stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
+    """Norm (where weights are given) and rotation of every head of q
+    [T][Hq][128] and k [T][Hkv][128] (each may be a slice of one projection's
+    output) into q_out and k_out; pos: int32 [T], or [3][T] for three axes."""
+    _check_packed(q.shape, q.dtype, q_out)
+    _check_packed(k.shape, q.dtype, k_out)
+    x = _tokens(q, k, None, pos, rope, q_norm, k_norm, eps)
+    sh = Shape(q.shape[0], q.shape[1], k.shape[1], 128, 1, _DTYPE[q.dtype])
+    _check(_lib.stlite_rotate_qk(sh, rope, x, q_out.data_ptr(), k_out.data_ptr(), _stream(stream)),
+           "stlite_rotate_qk")
+
+
+def rotate_qk(q, k, pos, rope, q_norm=None, k_norm=None, eps=1e-6, stream=None):
+    """Allocates the outputs and runs stlite_rotate_qk."""
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm, k_norm, eps, stream)
+    return q_out, k_out
+
+
+def stlite_paged_append(q, k, v, pos, rope, pages, q_out, k_pages, v_pages, q_norm=None, k_norm=None, eps=1e-6,
+                        stream=None):
+    """The new tokens' rotated keys and their values into the pages, the
+    rotated queries into q_out (see stlite_rotate_qk for q, k, v and pos)."""
+    _check_packed(q.shape, q.dtype, q_out)
+    _check_pools(pages, k.shape[1], q.dtype, k_pages, v_pages)
+    if v.shape != k.shape:
+        raise ValueError("k and v have one shape")
+    x = _tokens(q, k, v, pos, rope, q_norm, k_norm, eps)
+    sh = Shape(q.shape[0], q.shape[1], k.shape[1], 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[q.dtype])
+    _check(_lib.stlite_paged_append(sh, rope, x, pages.c, q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                    _stream(stream)), "stlite_paged_append")
+
+
+def _paged_shape(q, k_pages, pages) -> Shape:
+    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
+        raise ValueError("q is a contiguous [T][Hq][128]")
+    return Shape(q.shape[0], q.shape[1], k_pages.shape[2], 128, pages.max_new, _DTYPE[q.dtype])
+
+
+def stlite_paged_workspace_size(shape: Shape, pages: PageTable) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.stlite_paged_workspace_size(ctypes.byref(shape), ctypes.byref(pages.c), ctypes.byref(out)),
+           "stlite_paged_workspace_size")
+    return int(out.value)
+
+
+def paged_workspace(q, k_pages, pages):
+    """Zero-filled workspace tensor of stlite_paged_attention."""
+    return torch.zeros(stlite_paged_workspace_size(_paged_shape(q, k_pages, pages), pages), dtype=torch.uint8,
+                       device=q.device)
+
+
+def stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream=None):
+    """Attention of the new tokens q [T][Hq][128] over their sequences'
+    pages into out (q's shape and type)."""
+    sh = _paged_shape(q, k_pages, pages)
+    _check_packed(q.shape, q.dtype, out)
+    _check_pools(pages, sh.n_kv_heads, q.dtype, k_pages, v_pages)
+    _check(_lib.stlite_paged_attention(sh, pages.c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                       out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)),
+           "stlite_paged_attention")
+
+
+def paged_attention(q, k_pages, v_pages, pages, stream=None):
+    """Allocates the output and the workspace and runs stlite_paged_attention."""
+    out = torch.empty_like(q)
+    stlite_paged_attention(q, k_pages, v_pages, pages, out, paged_workspace(q, k_pages, pages), stream)
+    return out
+
+
+def _paged_layer_table(layers, pages, budget):
+    for k, v, kp, vp, ix in layers:
+        _check_pools(pages, k.shape[1], k.dtype, kp, vp)
+        if k.shape != layers[0][0].shape or v.shape != k.shape or ix.shape != (k.shape[1], budget):
+            raise ValueError("k and v are [N][Hkv][128] and idx [Hkv][budget] in every layer")
+    return _layer_table([(k, k, v, kp, vp, ix) for k, v, kp, vp, ix in layers])
+
+
+def stlite_compact_paged(layers, budget, pages, seq, stream=None):
+    """The kept rows of every layer into sequence seq's pages; layers: list
+    of (k, v, k_pages, v_pages, idx)."""
+    n, hkv, d = layers[0][0].shape
+    sh = Shape(n, hkv, hkv, d, 1, _DTYPE[layers[0][0].dtype])
+    arr = _paged_layer_table(layers, pages, int(budget))
+    _check(_lib.stlite_compact_paged(sh, int(budget), pages.c, int(seq), len(layers), _address(arr),
+                                     _stream(stream)), "stlite_compact_paged")
+
+
+def stlite_compress_layers_paged(layers, frames, params, pages, seq, ws, stream=None) -> int:
+    """stlite_compress_layers with the kept rows in sequence seq's pages;
+    layers: list of (q, k, v, k_pages, v_pages, idx_out)."""
+    sh = make_shape(layers[0][0], layers[0][1])
+    for _, _, _, kp, vp, _ in layers:
+        _check_pools(pages, sh.n_kv_heads, layers[0][1].dtype, kp, vp)
+    fs = _frames(frames)
+    arr = _layer_table(layers)
+    b = ctypes.c_int32(0)
+    _check(_lib.stlite_compress_layers_paged(sh, fs.c, params, pages.c, int(seq), len(layers), _address(arr),
+                                             ctypes.byref(b), _ptr(ws), ws.numel(), _stream(stream)),
+           "stlite_compress_layers_paged")
+    return int(b.value)
 
 
 def stlite_selftest_wait_timeout(ws, limit_ns: int, stream=None):
