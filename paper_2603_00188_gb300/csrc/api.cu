@@ -1125,6 +1125,10 @@ stlite_status check_paged_attention(const stlite_shape* shape, const stlite_page
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
   if (shape->window > kPagedMaxNew || shape->n_q_heads / shape->n_kv_heads > kDecMaxG) return STLITE_EUNSUPPORTED;
+  // block and item numbers of a session fit an int32 in the kernels
+  const long long rows = (long long)pages->max_pages * pages->page_rows * shape->n_kv_heads;
+  const long long items = (long long)pages->n_seqs * shape->n_kv_heads * kPagedMaxNew;
+  if (rows > (1LL << 30) || items > (1LL << 30)) return STLITE_EUNSUPPORTED;
   return STLITE_OK;
 }
 

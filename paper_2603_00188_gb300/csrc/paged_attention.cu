@@ -1,47 +1,535 @@
 // Attention of a serving step's new tokens over paged caches:
 //   out[t][g] = sum_j softmax_j(q_{t,g} . k_{j,h} / sqrt(d)) v_{j,h}, h = g / G,
 // over the rows j < len - (n - 1 - i) of the session, t its i-th of n new
-// tokens.
+// tokens.  Every cached row is read once per row chunk: the bytes of K and V
+// bound it.
+//
+// Work is divided by what the sessions hold when the kernel runs.  An item is
+// (session, KV head, chunk of query rows); its cache is cut into blocks of 16
+// rows, and the blocks of all items, laid end to end, into equal ranges, one
+// per CTA.  A CTA computes the parts of the few items that its range meets: an
+// item that lies inside one range is finished there, the parts of others are
+// merged by a second kernel.
 #include <type_traits>
 
 #include "kernels.cuh"
+#include "ptx.cuh"
 
 namespace stl {
 
-constexpr int kPatThreads = 256;
-constexpr int kPatWarps = kPatThreads / 32;
-constexpr int kPatRows = 16;  // query rows of a CTA: (new token, query head) pairs of one KV head
 constexpr float kPatLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float pat_weight(float a, float m) { return a == -CUDART_INF_F ? 0.f : exp2f(a - m); }
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_f(float x, float* y) { *y = x; }
 __device__ __forceinline__ void from_f(float x, __nv_bfloat16* y) { *y = __float2bfloat16_rn(x); }
 
-// One CTA per (session, KV head, 16 query rows); a warp takes every eighth row
-// of the cache, a lane four dimensions.
-template <typename T>
-__global__ void __launch_bounds__(kPatThreads) k_paged_attention(const __grid_constant__ PageView pg, const T* q,
-                                                                 const T* k, const T* v, T* out, int n, int hq,
-                                                                 int hkv, uint32_t* err) {
-  __shared__ float wo[kPatWarps][kD];
-  __shared__ float2 wml[kPatWarps];
+// ---------------------------------------------------------------- the split
+constexpr int kPatBlock = 16;  // cached rows of a block
+
+// What a session asks for.
+struct SeqWork {
+  int first, fresh;  // its packed tokens: first .. first + fresh
+  int len;           // cached rows
+  int blocks;        // blocks of one item
+  int chunks;        // items of one KV head
+};
+__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int G, int chunk_rows) {
+  SeqWork w;
+  w.first = pg.cu ? pg.cu[s] : s * pg.w;
+  w.fresh = pg.cu ? pg.cu[s + 1] - w.first : pg.w;
+  w.len = max(0, min(pg.len[s], pg.max_pages * pg.page_rows));
+  w.blocks = max(1, (w.len + kPatBlock - 1) / kPatBlock);  // an empty session's zeros are one block's work
+  w.chunks = (max(0, min(w.fresh, pg.w)) * G + chunk_rows - 1) / chunk_rows;
+  return w;
+}
+
+// A position in the sequence of all blocks: session s begins at block `base`.
+struct Cursor {
+  long long base;
+  int s;
+  SeqWork w;
+  __device__ __forceinline__ long long cost(int hkv) const { return (long long)w.blocks * w.chunks * hkv; }
+};
+
+// A CTA's range of blocks and where it starts.
+struct Range {
+  long long b0, b1, total;
+  int ctas;  // that have one
+  Cursor at;
+};
+
+// Threads' block costs are summed over the sessions, and the range's first
+// session found by the thread that holds it.  Whole CTA; `scratch` is 8
+// 64-bit words for each warp and two more.
+template <int THREADS>
+__device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int min_blocks, uint32_t* err,
+                            long long* scratch) {
+  constexpr int kWarps = THREADS / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (pg.n_seqs + THREADS - 1) / THREADS, s0 = min(pg.n_seqs, tid * per), s1 = min(pg.n_seqs, s0 + per);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) {
+    Cursor c;
+    c.w = seq_work(pg, s, G, chunk_rows);
+    mine += c.cost(hkv);
+    if (blockIdx.x == 0 && c.w.len != pg.len[s]) record_error(err, kErrInput);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) scratch[warp] = incl;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const long long x = scratch[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  Range r;
+  r.total = total;
+  const long long most = (total + min_blocks - 1) / min_blocks;
+  r.ctas = (int)(most < gridDim.x ? most : gridDim.x);
+  const int c = blockIdx.x;
+  if (c >= r.ctas) {
+    r.b0 = r.b1 = 0;
+    return r;  // the same for every thread
+  }
+  r.b0 = total * c / r.ctas;
+  r.b1 = total * (c + 1) / r.ctas;
+  incl += before;
+  if (mine > 0 && incl - mine <= r.b0 && r.b0 < incl) {
+    long long base = incl - mine;
+    int s = s0;
+    for (; s < s1; ++s) {
+      Cursor x;
+      x.w = seq_work(pg, s, G, chunk_rows);
+      if (r.b0 < base + x.cost(hkv)) break;
+      base += x.cost(hkv);
+    }
+    scratch[kWarps] = base;
+    scratch[kWarps + 1] = s;
+  }
+  __syncthreads();
+  r.at.base = scratch[kWarps];
+  r.at.s = (int)scratch[kWarps + 1];
+  r.at.w = seq_work(pg, r.at.s, G, chunk_rows);
+  return r;
+}
+
+// Moves on to the session of block b.
+__device__ __forceinline__ void advance(Cursor& c, long long b, const PageView& pg, int G, int chunk_rows, int hkv) {
+  while (b >= c.base + c.cost(hkv)) {
+    c.base += c.cost(hkv);
+    c.w = seq_work(pg, ++c.s, G, chunk_rows);
+  }
+}
+
+// Which part of which item is left for the second kernel: `desc` has an entry
+// for each item, or for each CTA where those are fewer, of the item that
+// starts there.
+struct PartDesc {
+  int item;     // (session * hkv + head) * chunks of a full session + chunk; -1: nothing to merge
+  int c0, c1;   // CTAs with a part: slot 2 c0 + 1, then slots 2 c for c = c0 + 1 .. c1
+  int pad;
+};
+
+constexpr int kPatMaxCtas = 1024;
+
+__device__ __forceinline__ void cp_async16_fill(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// ---------------------------------------------------------------------- bf16
+// Each warp streams its own blocks (every kWarps-th of the range) through its
+// own ring of stages in shared memory: 16 rows of keys and of values by
+// asynchronous 16-byte copies (any page size: a lane looks up its row's page
+// one block ahead; rows that do not count are filled with zeros and
+// masked).  No warp
+// waits for another until an item ends.  Both products run on the warp's
+// tensor cores (m16n8k16, fp32 accumulation), as a single new token is at
+// most 16 query rows, below the smallest tile of tcgen05:
+//   S (16 rows x 8 queries) = K Q^T, the queries' fragments in registers,
+//   O^T (128 dims x 8 queries) += V^T P^T, P transposed in registers by
+//   movmatrix and taken as P = hi + lo, two bf16 parts (16 bits of it: with one
+//   part the weights' rounding would be as large as the result's).
+constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
+constexpr int kPmCtas = 2;                          // per SM
+constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
+constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
+__host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
+__host__ __device__ constexpr int pm_smem(int nt) {
+  return kPmWarps * pm_stages(nt) * 2 * kPmHalf + kPmWarps * 8 * nt * (kPmPitch * 4 + 8) + 8 * (kPmWarps + 2);
+}
+
+__device__ __forceinline__ void pm_ldsm_x4(uint32_t addr, uint32_t (&a)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void pm_ldsm_x4_trans(uint32_t addr, uint32_t (&a)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void pm_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The 8 x 8 matrix of 16-bit values held two to a lane, transposed.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Byte of the 16-byte chunk c of row r of a half stage, swizzled so that eight
+// rows' chunks lie in eight different bank groups.
+__device__ __forceinline__ uint32_t pm_off(int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 7)) << 4)); }
+
+// The cached row of lane % 16 in a block: its slot, or -1 where it does not count.
+__device__ __forceinline__ int block_slot(const PageView& pg, const Cursor& c, int blk, uint32_t* err) {
+  const int j = blk * kPatBlock + (threadIdx.x & (kPatBlock - 1));
+  if (j >= c.w.len) return -1;
+  const int i = j / pg.page_rows, page = pg.table[(size_t)c.s * pg.max_pages + i];
+  if (page < 0 || page >= pg.n_pages) {
+    record_error(err, kErrInput);
+    return -1;
+  }
+  return page * pg.page_rows + (j - i * pg.page_rows);
+}
+
+template <int NT>
+__global__ void __launch_bounds__(kPmThreads, kPmCtas)
+    k_paged_mma(const __grid_constant__ PageView pg, const __nv_bfloat16* q, const __nv_bfloat16* k,
+                const __nv_bfloat16* v, __nv_bfloat16* out, int n, int hq, int hkv, int by_item, int chunks,
+                PartDesc* desc, float2* part_ml, float* part_o, uint32_t* err) {
+  constexpr int kStages = pm_stages(NT), kRows = 8 * NT;
+  extern __shared__ uint4 pat_smem[];
+  float* wo = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(pat_smem) + kPmWarps * kStages * 2 * kPmHalf);
+  float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * kRows * kPmPitch);
+  long long* scratch = reinterpret_cast<long long*>(wml + kPmWarps * kRows);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
+  const int G = hq / hkv, cta = blockIdx.x;
+  const uint32_t ring = smem_u32(pat_smem) + warp * kStages * 2 * kPmHalf;
   pdl_trigger();
   pdl_wait();
-  const int s = blockIdx.x, h = blockIdx.y, r0 = blockIdx.z * kPatRows, G = hq / hkv;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int first = pg.cu ? pg.cu[s] : s * pg.w, fresh = pg.cu ? pg.cu[s + 1] - first : pg.w;
-  const int cap = pg.max_pages * pg.page_rows, asked = pg.len[s], len = max(0, min(asked, cap));
-  if (asked != len && threadIdx.x == 0) record_error(err, kErrInput);
+  const Range rg = find_range<kPmThreads>(pg, G, kRows, hkv, kPmWarps, err, scratch);
+  if (!by_item && tid == 0) desc[cta].item = -1;
+  if (cta >= rg.ctas) return;
+
+  // fetching: the cursor of the block whose slots were looked up last
+  Cursor ahead = rg.at;
+  long long fb = rg.b0 + warp;  // next block to look up
+  int slot = -1, head = 0;
+  bool more = false;
+  uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
+  auto look_up = [&]() {
+    more = fb < rg.b1;
+    if (!more) return;
+    advance(ahead, fb, pg, G, kRows, hkv);
+    const int local = (int)(fb - ahead.base), item = local / ahead.w.blocks;
+    head = item / ahead.w.chunks;
+    slot = block_slot(pg, ahead, local - item * ahead.w.blocks, err);
+    fb += kPmWarps;
+  };
+  auto fetch = [&](int stage) {
+    if (more) {
+      const uint64_t ok = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
+      counts = (counts & ~(0xffffull << (16 * stage))) | ok << (16 * stage);
+      const uint32_t dst = ring + stage * 2 * kPmHalf;
+      const int c = lane & 15;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = 2 * i + (lane >> 4), sl = __shfl_sync(0xffffffffu, slot, r);
+        const size_t at = ((size_t)max(sl, 0) * hkv + head) * kD + 8 * c;
+        cp_async16_fill(dst + pm_off(r, c), k + at, sl >= 0);
+        cp_async16_fill(dst + kPmHalf + pm_off(r, c), v + at, sl >= 0);
+      }
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int st = 0; st < kStages; ++st) {
+    look_up();
+    fetch(st);
+  }
+
   const float scale = kPatLog2e * rsqrtf((float)kD);
-  for (int rr = r0; rr < min(r0 + kPatRows, min(fresh, pg.w) * G); ++rr) {
-    const int i = rr / G, g = h * G + rr % G, t = first + i;
+  Cursor cur = rg.at;
+  long long b = rg.b0 + warp;  // the warp's next block to compute
+  int stage = 0;
+  for (long long seg = rg.b0; seg < rg.b1;) {
+    // the part of one item that lies in the range: blocks seg .. seg_end
+    advance(cur, seg, pg, G, kRows, hkv);
+    const int item = (int)((seg - cur.base) / cur.w.blocks);
+    const int h = item / cur.w.chunks, chunk = item % cur.w.chunks;
+    const long long i0 = cur.base + (long long)item * cur.w.blocks, i1 = i0 + cur.w.blocks;
+    const long long seg_end = i1 < rg.b1 ? i1 : rg.b1;
+    const int row0 = chunk * kRows, rows = min(kRows, min(cur.w.fresh, pg.w) * G - row0);
+
+    // query fragments, and the rows that each of the lane's queries sees
+    uint32_t qb[8][NT][2];
+    int sees[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + 8 * nt + g8, t = cur.w.first + r / G;
+      const bool ok = 8 * nt + g8 < rows && t >= 0 && t < n;
+      const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + ((size_t)(ok ? t : 0) * hq + h * G + r % G) * kD);
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        qb[ks][nt][0] = ok ? qr[8 * ks + t4] : 0u;
+        qb[ks][nt][1] = ok ? qr[8 * ks + 4 + t4] : 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int x = 8 * nt + 2 * t4 + e;
+        sees[nt][e] = x < rows ? cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G) : 0;
+      }
+    }
+    // running state: queries 8 nt + 2 t4 + e; o[mt][nt][j] is dimension
+    // 16 mt + g8 + 8 (j >> 1) of query 8 nt + 2 t4 + (j & 1)
+    float m[NT][2], l[NT][2], o[8][NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -CUDART_INF_F;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
+    }
+    for (; b < seg_end; b += kPmWarps) {
+      cp_async_wait<kStages - 1>();
+      __syncwarp();
+      look_up();  // the block that will take this stage
+      const uint32_t kt = ring + stage * 2 * kPmHalf, vt = kt + kPmHalf;
+      const int base = (int)(b - i0) * kPatBlock;
+      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) >> g8;
+      float c[2][NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[0][nt][j] = c[1][nt][j] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        uint32_t a[4];
+        pm_ldsm_x4(kt + pm_off(lane & 15, 2 * ks + (lane >> 4)), a);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) pm_mma(c[ks & 1][nt], a, qb[ks][nt][0], qb[ks][nt][1]);
+      }
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[2][2], alpha[2];  // [row g8, g8 + 8][query]
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float x0 = (ok & 1u) && base + g8 < sees[nt][e] ? (c[0][nt][e] + c[1][nt][e]) * scale : -CUDART_INF_F;
+          const float x1 =
+              (ok & 256u) && base + g8 + 8 < sees[nt][e] ? (c[0][nt][2 + e] + c[1][nt][2 + e]) * scale : -CUDART_INF_F;
+          float mx = fmaxf(x0, x1);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float mn = fmaxf(m[nt][e], mx), ms = mn == -CUDART_INF_F ? 0.f : mn;
+          alpha[e] = ex2_approx(m[nt][e] - ms);
+          p[0][e] = ex2_approx(x0 - ms);
+          p[1][e] = ex2_approx(x1 - ms);
+          l[nt][e] = fmaf(l[nt][e], alpha[e], p[0][e] + p[1][e]);  // the lane's rows only
+          m[nt][e] = mn;
+        }
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[mt][nt][j] *= alpha[j & 1];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t hi = pack_bf16(p[x][0], p[x][1]);
+          const uint32_t lo = pack_bf16(p[x][0] - __uint_as_float(hi << 16), p[x][1] - __uint_as_float(hi & 0xffff0000u));
+          ph[nt][x] = transpose8x8(hi);
+          pl[nt][x] = transpose8x8(lo);
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) {
+        uint32_t a[4];
+        pm_ldsm_x4_trans(vt + pm_off((lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), a);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          pm_mma(o[mt][nt], a, ph[nt][0], ph[nt][1]);
+          pm_mma(o[mt][nt], a, pl[nt][0], pl[nt][1]);
+        }
+      }
+      __syncwarp();
+      fetch(stage);
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    // the warps' states of this item, merged in shared memory
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float s = l[nt][e];
+        s += __shfl_xor_sync(0xffffffffu, s, 4);
+        s += __shfl_xor_sync(0xffffffffu, s, 8);
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
+        const int x = 8 * nt + 2 * t4 + e;
+        if (g8 == 0) wml[warp * kRows + x] = make_float2(m[nt][e], s);
+        float* w = wo + (warp * kRows + x) * kPmPitch + g8;
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) {
+          w[16 * mt] = o[mt][nt][e];
+          w[16 * mt + 8] = o[mt][nt][2 + e];
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = seg == i0 && seg_end == i1;
+    const int part = 2 * cta + (seg == i0 ? 1 : 0);
+    for (int x = warp; x < rows; x += kPmWarps) {
+      float M = -CUDART_INF_F, L = 0.f, wt[kPmWarps];
+#pragma unroll
+      for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
+#pragma unroll
+      for (int w = 0; w < kPmWarps; ++w) {
+        const float2 ml = wml[w * kRows + x];
+        wt[w] = pat_weight(ml.x, M);
+        L = fmaf(ml.y, wt[w], L);
+      }
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kPmWarps; ++w) {
+        const float4 y = *reinterpret_cast<const float4*>(wo + (w * kRows + x) * kPmPitch + 4 * lane);
+        O.x = fmaf(y.x, wt[w], O.x);
+        O.y = fmaf(y.y, wt[w], O.y);
+        O.z = fmaf(y.z, wt[w], O.z);
+        O.w = fmaf(y.w, wt[w], O.w);
+      }
+      const int r = row0 + x, t = cur.w.first + r / G;
+      if (whole) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        if (t >= 0 && t < n)
+          *reinterpret_cast<uint2*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
+              make_uint2(pack_bf16(O.x * inv, O.y * inv), pack_bf16(O.z * inv, O.w * inv));
+      } else {
+        *reinterpret_cast<float4*>(part_o + ((size_t)part * 16 + x) * kD + 4 * lane) = O;
+        if (lane == 0) part_ml[part * 16 + x] = make_float2(M, L);
+      }
+    }
+    if (tid == 0 && seg == i0) {
+      const int id = (cur.s * hkv + h) * chunks + chunk;
+      PartDesc d = {whole ? -1 : id, cta, cta, 0};
+      // the CTA whose range holds the item's last block
+      while (!whole && rg.total * (d.c1 + 1) / rg.ctas < i1) ++d.c1;
+      if (by_item)
+        desc[id] = d;
+      else if (!whole)
+        desc[cta] = d;
+    }
+    seg = seg_end;
+    if (seg < rg.b1) __syncthreads();  // the merge buffer is free again
+  }
+  cp_async_wait<0>();
+}
+
+// out of the items that several CTAs had parts of.  grid (descriptors, rows):
+// four slices of 128 threads, a dimension each; the parts' weights are formed
+// in shared memory while the first partials are on their way.
+template <typename T>
+__global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ PageView pg, T* out, int n, int hq,
+                                                       int hkv, int chunks, int chunk_rows, int by_item,
+                                                       const PartDesc* desc, const float2* part_ml,
+                                                       const float* part_o) {
+  __shared__ float wts[2 * kPatMaxCtas];
+  __shared__ float red[2][16];
+  __shared__ float acc[3][kD];
+  pdl_trigger();
+  pdl_wait();
+  if (by_item) {  // items of sessions with fewer rows have no entry
+    const int s = blockIdx.x / (hkv * chunks);
+    const SeqWork w = seq_work(pg, s, hq / hkv, chunk_rows);
+    if ((int)blockIdx.x % chunks >= w.chunks) return;
+  }
+  const PartDesc d = desc[blockIdx.x];
+  if (d.item < 0) return;
+  const int G = hq / hkv, chunk = d.item % chunks, h = d.item / chunks % hkv, s = d.item / chunks / hkv;
+  const SeqWork w = seq_work(pg, s, G, chunk_rows);
+  const int x = blockIdx.y, r = chunk * chunk_rows + x;
+  if (r >= min(w.fresh, pg.w) * G) return;
+  const int tid = threadIdx.x, c = tid & (kD - 1), slice = tid / kD, lane = tid & 31, warp = tid >> 5;
+  const int parts = d.c1 - d.c0 + 1;
+  auto at = [&](int p) { return (p == 0 ? 2 * d.c0 + 1 : 2 * (d.c0 + p)) * 16 + x; };
+  float M = -CUDART_INF_F;
+  for (int p = tid; p < parts; p += 4 * kD) M = fmaxf(M, part_ml[at(p)].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  if (lane == 0) red[0][warp] = M;
+  __syncthreads();
+  for (int i = 0; i < 16; ++i) M = fmaxf(M, red[0][i]);
+  float L = 0.f;
+  for (int p = tid; p < parts; p += 4 * kD) {
+    const float2 ml = part_ml[at(p)];
+    const float a = pat_weight(ml.x, M);
+    wts[p] = a;
+    L = fmaf(ml.y, a, L);
+  }
+  L = warp_sum(L);
+  if (lane == 0) red[1][warp] = L;
+  __syncthreads();
+  L = 0.f;
+  for (int i = 0; i < 16; ++i) L += red[1][i];
+  float O = 0.f;
+#pragma unroll 4
+  for (int p = slice; p < parts; p += 4) O = fmaf(part_o[(size_t)at(p) * kD + c], wts[p], O);
+  if (slice > 0) acc[slice - 1][c] = O;
+  __syncthreads();
+  if (slice > 0) return;
+  O = (O + acc[0][c]) + (acc[1][c] + acc[2][c]);
+  const int t = w.first + r / G;
+  if (t >= 0 && t < n) from_f(L == 0.f ? 0.f : O / L, out + ((size_t)t * hq + h * G + r % G) * kD + c);
+}
+
+// ---------------------------------------------------------------------- fp32
+constexpr int kPfThreads = 256;
+constexpr int kPfWarps = kPfThreads / 32;
+constexpr int kPfRows = 16;  // query rows of a CTA: (new token, query head) pairs of one KV head
+
+// One CTA per (session, KV head, 16 query rows); a warp takes every eighth row
+// of the cache, a lane four dimensions.
+__global__ void __launch_bounds__(kPfThreads) k_paged_fp32(const __grid_constant__ PageView pg, const float* q,
+                                                           const float* k, const float* v, float* out, int n, int hq,
+                                                           int hkv, uint32_t* err) {
+  __shared__ float wo[kPfWarps][kD];
+  __shared__ float2 wml[kPfWarps];
+  pdl_trigger();
+  pdl_wait();
+  const int s = blockIdx.x, h = blockIdx.y, r0 = blockIdx.z * kPfRows, G = hq / hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const SeqWork sw = seq_work(pg, s, G, kPfRows);
+  if (sw.len != pg.len[s] && threadIdx.x == 0) record_error(err, kErrInput);
+  const float scale = kPatLog2e * rsqrtf((float)kD);
+  for (int rr = r0; rr < min(r0 + kPfRows, min(sw.fresh, pg.w) * G); ++rr) {
+    const int i = rr / G, g = h * G + rr % G, t = sw.first + i;
     if (t < 0 || t >= n) break;
     float qf[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -CUDART_INF_F, l = 0.f;
-    for (int e = 0; e < 4; ++e) qf[e] = to_f(q[((size_t)t * hq + g) * kD + 4 * lane + e]) * scale;
-    const int sees = len - (fresh - 1 - i);
-    for (int j = warp; j < sees; j += kPatWarps) {
+    for (int e = 0; e < 4; ++e) qf[e] = q[((size_t)t * hq + g) * kD + 4 * lane + e] * scale;
+    const int sees = sw.len - (sw.fresh - 1 - i);
+    for (int j = warp; j < sees; j += kPfWarps) {
       const int p = j / pg.page_rows, page = pg.table[(size_t)s * pg.max_pages + p];
       if (page < 0 || page >= pg.n_pages) {
         if (lane == 0) record_error(err, kErrInput);
@@ -49,20 +537,20 @@ __global__ void __launch_bounds__(kPatThreads) k_paged_attention(const __grid_co
       }
       const size_t at = (((size_t)page * pg.page_rows + (j - p * pg.page_rows)) * hkv + h) * kD + 4 * lane;
       float x = 0.f;
-      for (int e = 0; e < 4; ++e) x = fmaf(qf[e], to_f(k[at + e]), x);
+      for (int e = 0; e < 4; ++e) x = fmaf(qf[e], k[at + e], x);
       x = warp_sum(x);
       const float mn = fmaxf(m, x), a = pat_weight(m, mn), w = pat_weight(x, mn);
       l = l * a + w;
       m = mn;
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], a, w * to_f(v[at + e]));
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], a, w * v[at + e]);
     }
     for (int e = 0; e < 4; ++e) wo[warp][4 * lane + e] = o[e];
     if (lane == 0) wml[warp] = make_float2(m, l);
     __syncthreads();
     if (threadIdx.x < kD) {
       float M = -CUDART_INF_F, L = 0.f, O = 0.f;
-      for (int w = 0; w < kPatWarps; ++w) M = fmaxf(M, wml[w].x);
-      for (int w = 0; w < kPatWarps; ++w) {
+      for (int w = 0; w < kPfWarps; ++w) M = fmaxf(M, wml[w].x);
+      for (int w = 0; w < kPfWarps; ++w) {
         const float a = pat_weight(wml[w].x, M);
         L = fmaf(wml[w].y, a, L);
         O = fmaf(wo[w][threadIdx.x], a, O);
@@ -73,24 +561,60 @@ __global__ void __launch_bounds__(kPatThreads) k_paged_attention(const __grid_co
   }
 }
 
-size_t paged_workspace_bytes(DType, const PageView&, int, int) { return 256; }
+// -------------------------------------------------------------------- launch
+static int paged_ctas() {
+  int dev = 0, sms = 152;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return kPmCtas * sms < kPatMaxCtas ? kPmCtas * sms : kPatMaxCtas;
+}
+
+// Workspace: the error word, the descriptors (16 KB), then two parts of each
+// CTA: (max, sum) of 16 query rows, and their weighted values.
+constexpr size_t kPatHead = 256, kPatDescs = kPatMaxCtas * sizeof(PartDesc);
+size_t paged_workspace_bytes(DType, const PageView&, int, int) {
+  return kPatHead + kPatDescs + (size_t)2 * paged_ctas() * 16 * (sizeof(float2) + kD * sizeof(float));
+}
 
 cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
                                    void* out, int n, int hq, int hkv, void* ws, cudaStream_t st) {
-  const int chunks = (pages.w * (hq / hkv) + kPatRows - 1) / kPatRows;
   uint32_t* err = static_cast<uint32_t*>(ws);
-  TimingScope ts("paged_attention", st);
+  const int rows = pages.w * (hq / hkv);
   cudaError_t e = cudaSuccess;
-  auto run = [&](auto zero) {
-    typedef decltype(zero) T;
-    e = launch_after(k_paged_attention<T>, dim3(pages.n_seqs, hkv, chunks), kPatThreads, 0, st, pages,
-                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
-                     static_cast<T*>(out), n, hq, hkv, err);
-  };
-  if (dt == kBF16)
-    run(__nv_bfloat16());
-  else
-    run(float());
+  if (dt == kF32) {
+    TimingScope ts("paged_attention", st);
+    e = launch_after(k_paged_fp32, dim3(pages.n_seqs, hkv, (rows + kPfRows - 1) / kPfRows), kPfThreads, 0, st, pages,
+                     static_cast<const float*>(q), static_cast<const float*>(k), static_cast<const float*>(v),
+                     static_cast<float*>(out), n, hq, hkv, err);
+    return e != cudaSuccess ? e : cudaGetLastError();
+  }
+  const int ctas = paged_ctas(), chunk_rows = rows <= 8 ? 8 : 16, chunks = (rows + chunk_rows - 1) / chunk_rows;
+  const long long items = (long long)pages.n_seqs * hkv * chunks;
+  const int by_item = items <= ctas, descs = by_item ? (int)items : ctas;
+  uint8_t* at = static_cast<uint8_t*>(ws) + kPatHead;
+  PartDesc* desc = reinterpret_cast<PartDesc*>(at);
+  float2* part_ml = reinterpret_cast<float2*>(at + kPatDescs);
+  float* part_o = reinterpret_cast<float*>(part_ml + (size_t)2 * ctas * 16);
+  typedef __nv_bfloat16 B;
+  {
+    TimingScope ts("paged_attention", st);
+    auto run = [&](auto nt) {
+      constexpr int NT = decltype(nt)::value;
+      e = cudaFuncSetAttribute(k_paged_mma<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, pm_smem(NT));
+      if (e != cudaSuccess) return;
+      e = launch_after(k_paged_mma<NT>, dim3(ctas), kPmThreads, pm_smem(NT), st, pages, static_cast<const B*>(q),
+                       static_cast<const B*>(k), static_cast<const B*>(v), static_cast<B*>(out), n, hq, hkv, by_item,
+                       chunks, desc, part_ml, part_o, err);
+    };
+    if (chunk_rows == 8)
+      run(std::integral_constant<int, 1>());
+    else
+      run(std::integral_constant<int, 2>());
+    if (e != cudaSuccess) return e;
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  TimingScope ts("paged_merge", st);
+  e = launch_after(k_paged_merge<B>, dim3(descs, rows < chunk_rows ? rows : chunk_rows), 4 * kD, 0, st, pages,
+                   static_cast<B*>(out), n, hq, hkv, chunks, chunk_rows, by_item, desc, part_ml, part_o);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
