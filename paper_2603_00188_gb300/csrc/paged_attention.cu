@@ -33,11 +33,11 @@ struct SeqWork {
   int blocks;        // blocks of one item
   int chunks;        // items of one KV head
 };
-__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int G, int chunk_rows) {
+__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, int G, int chunk_rows) {
   SeqWork w;
   w.first = pg.cu ? pg.cu[s] : s * pg.w;
   w.fresh = pg.cu ? pg.cu[s + 1] - w.first : pg.w;
-  w.len = max(0, min(pg.len[s], pg.max_pages * pg.page_rows));
+  w.len = max(0, min(len, pg.max_pages * pg.page_rows));
   w.blocks = max(1, (w.len + kPatBlock - 1) / kPatBlock);  // an empty session's zeros are one block's work
   w.chunks = (max(0, min(w.fresh, pg.w)) * G + chunk_rows - 1) / chunk_rows;
   return w;
@@ -51,28 +51,54 @@ struct Cursor {
   __device__ __forceinline__ long long cost(int hkv) const { return (long long)w.blocks * w.chunks * hkv; }
 };
 
-// A CTA's range of blocks and where it starts.
+// x / d and x % d; quotients of up to 32-bit numbers, which is what comes, take
+// a tenth of the time of 64-bit ones.
+__device__ __forceinline__ long long div_mod(long long x, int d, int* rem) {
+  if (x < 0x100000000ll) {
+    const uint32_t y = (uint32_t)x / (uint32_t)d;
+    *rem = (int)((uint32_t)x - y * (uint32_t)d);
+    return y;
+  }
+  *rem = (int)(x % d);
+  return x / d;
+}
+
+// A CTA's range of blocks and where it starts.  All blocks are dealt to `ctas`
+// CTAs in ranges of `quota` blocks, the first `extra` one more.
 struct Range {
-  long long b0, b1, total;
-  int ctas;  // that have one
+  long long b0, b1;
+  long long quota;
+  int ctas, extra;
   Cursor at;
+  __device__ __forceinline__ long long start(int c) const { return c * quota + min(c, extra); }
+  __device__ __forceinline__ int cta_of(long long b) const {
+    const long long wide = extra * (quota + 1);
+    int rem;
+    return b < wide ? (int)div_mod(b, (int)(quota + 1), &rem) : extra + (int)div_mod(b - wide, (int)quota, &rem);
+  }
 };
 
 // Threads' block costs are summed over the sessions, and the range's first
-// session found by the thread that holds it.  Whole CTA; `scratch` is 8
-// 64-bit words for each warp and two more.
+// session found by the thread that holds it.  Whole CTA; min_blocks: the
+// fewest blocks that make a CTA of their own.
+template <int THREADS>
+struct RangeScratch {
+  long long warp_sum[THREADS / 32];
+  Cursor at;
+};
 template <int THREADS>
 __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int min_blocks, uint32_t* err,
-                            long long* scratch) {
+                            RangeScratch<THREADS>* scratch) {
   constexpr int kWarps = THREADS / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (pg.n_seqs + THREADS - 1) / THREADS, s0 = min(pg.n_seqs, tid * per), s1 = min(pg.n_seqs, s0 + per);
   long long mine = 0;
+  Cursor c;  // of the thread's last session, and its only one where there are no more than threads
   for (int s = s0; s < s1; ++s) {
-    Cursor c;
-    c.w = seq_work(pg, s, G, chunk_rows);
+    const int asked = pg.len[s];
+    c.w = seq_work(pg, s, asked, G, chunk_rows);
     mine += c.cost(hkv);
-    if (blockIdx.x == 0 && c.w.len != pg.len[s]) record_error(err, kErrInput);
+    if (blockIdx.x == 0 && c.w.len != asked) record_error(err, kErrInput);
   }
   long long incl = mine;
 #pragma unroll
@@ -80,43 +106,37 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
     const long long x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
-  if (lane == 31) scratch[warp] = incl;
+  if (lane == 31) scratch->warp_sum[warp] = incl;
   __syncthreads();
   long long before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    const long long x = scratch[w];
+    const long long x = scratch->warp_sum[w];
     if (w < warp) before += x;
     total += x;
   }
   Range r;
-  r.total = total;
   const long long most = (total + min_blocks - 1) / min_blocks;
   r.ctas = (int)(most < gridDim.x ? most : gridDim.x);
-  const int c = blockIdx.x;
-  if (c >= r.ctas) {
-    r.b0 = r.b1 = 0;
-    return r;  // the same for every thread
-  }
-  r.b0 = total * c / r.ctas;
-  r.b1 = total * (c + 1) / r.ctas;
+  if ((int)blockIdx.x >= r.ctas) return r;  // the same for every thread
+  r.quota = div_mod(total, r.ctas, &r.extra);
+  r.b0 = r.start(blockIdx.x);
+  r.b1 = r.start(blockIdx.x + 1);
   incl += before;
   if (mine > 0 && incl - mine <= r.b0 && r.b0 < incl) {
-    long long base = incl - mine;
-    int s = s0;
-    for (; s < s1; ++s) {
-      Cursor x;
-      x.w = seq_work(pg, s, G, chunk_rows);
-      if (r.b0 < base + x.cost(hkv)) break;
-      base += x.cost(hkv);
+    c.base = incl - mine;
+    c.s = s0;
+    if (per > 1) {
+      for (c.w = seq_work(pg, s0, pg.len[s0], G, chunk_rows); r.b0 >= c.base + c.cost(hkv);) {
+        c.base += c.cost(hkv);
+        ++c.s;
+        c.w = seq_work(pg, c.s, pg.len[c.s], G, chunk_rows);
+      }
     }
-    scratch[kWarps] = base;
-    scratch[kWarps + 1] = s;
+    scratch->at = c;
   }
   __syncthreads();
-  r.at.base = scratch[kWarps];
-  r.at.s = (int)scratch[kWarps + 1];
-  r.at.w = seq_work(pg, r.at.s, G, chunk_rows);
+  r.at = scratch->at;
   return r;
 }
 
@@ -124,7 +144,8 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
 __device__ __forceinline__ void advance(Cursor& c, long long b, const PageView& pg, int G, int chunk_rows, int hkv) {
   while (b >= c.base + c.cost(hkv)) {
     c.base += c.cost(hkv);
-    c.w = seq_work(pg, ++c.s, G, chunk_rows);
+    ++c.s;
+    c.w = seq_work(pg, c.s, pg.len[c.s], G, chunk_rows);
   }
 }
 
@@ -137,7 +158,7 @@ struct PartDesc {
   int pad;
 };
 
-constexpr int kPatMaxCtas = 1024;
+constexpr int kPatMaxCtas = 1024;  // two parts to a thread of the merge
 
 __device__ __forceinline__ void cp_async16_fill(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
@@ -167,7 +188,7 @@ constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a blo
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
 __host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
 __host__ __device__ constexpr int pm_smem(int nt) {
-  return kPmWarps * pm_stages(nt) * 2 * kPmHalf + kPmWarps * 8 * nt * (kPmPitch * 4 + 8) + 8 * (kPmWarps + 2);
+  return kPmWarps * pm_stages(nt) * 2 * kPmHalf + kPmWarps * 8 * nt * (kPmPitch * 4 + 8) + (int)sizeof(RangeScratch<kPmThreads>);
 }
 
 __device__ __forceinline__ void pm_ldsm_x4(uint32_t addr, uint32_t (&a)[4]) {
@@ -225,7 +246,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   extern __shared__ uint4 pat_smem[];
   float* wo = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(pat_smem) + kPmWarps * kStages * 2 * kPmHalf);
   float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * kRows * kPmPitch);
-  long long* scratch = reinterpret_cast<long long*>(wml + kPmWarps * kRows);
+  RangeScratch<kPmThreads>* scratch = reinterpret_cast<RangeScratch<kPmThreads>*>(wml + kPmWarps * kRows);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
   const int G = hq / hkv, cta = blockIdx.x;
   const uint32_t ring = smem_u32(pat_smem) + warp * kStages * 2 * kPmHalf;
@@ -433,9 +454,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     }
     if (tid == 0 && seg == i0) {
       const int id = (cur.s * hkv + h) * chunks + chunk;
-      PartDesc d = {whole ? -1 : id, cta, cta, 0};
-      // the CTA whose range holds the item's last block
-      while (!whole && rg.total * (d.c1 + 1) / rg.ctas < i1) ++d.c1;
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
       if (by_item)
         desc[id] = d;
       else if (!whole)
@@ -455,47 +474,72 @@ __global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ 
                                                        int hkv, int chunks, int chunk_rows, int by_item,
                                                        const PartDesc* desc, const float2* part_ml,
                                                        const float* part_o) {
-  __shared__ float wts[2 * kPatMaxCtas];
+  __shared__ float wts[kPatMaxCtas];
   __shared__ float red[2][16];
   __shared__ float acc[3][kD];
   pdl_trigger();
   pdl_wait();
   if (by_item) {  // items of sessions with fewer rows have no entry
     const int s = blockIdx.x / (hkv * chunks);
-    const SeqWork w = seq_work(pg, s, hq / hkv, chunk_rows);
+    const SeqWork w = seq_work(pg, s, 0, hq / hkv, chunk_rows);
     if ((int)blockIdx.x % chunks >= w.chunks) return;
   }
   const PartDesc d = desc[blockIdx.x];
   if (d.item < 0) return;
   const int G = hq / hkv, chunk = d.item % chunks, h = d.item / chunks % hkv, s = d.item / chunks / hkv;
-  const SeqWork w = seq_work(pg, s, G, chunk_rows);
+  const SeqWork w = seq_work(pg, s, 0, G, chunk_rows);
   const int x = blockIdx.y, r = chunk * chunk_rows + x;
   if (r >= min(w.fresh, pg.w) * G) return;
   const int tid = threadIdx.x, c = tid & (kD - 1), slice = tid / kD, lane = tid & 31, warp = tid >> 5;
   const int parts = d.c1 - d.c0 + 1;
   auto at = [&](int p) { return (p == 0 ? 2 * d.c0 + 1 : 2 * (d.c0 + p)) * 16 + x; };
-  float M = -CUDART_INF_F;
-  for (int p = tid; p < parts; p += 4 * kD) M = fmaxf(M, part_ml[at(p)].x);
+  constexpr int kAtOnce = 10;  // partials of a slice in flight
+  float y[kAtOnce];
+  auto load = [&](int p0) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int p = p0 + slice + 4 * u;
+      y[u] = p < parts ? part_o[(size_t)at(p) * kD + c] : 0.f;
+    }
+  };
+  load(0);
+  float2 ml[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int p = tid + 4 * kD * i;
+    ml[i] = p < parts ? part_ml[at(p)] : make_float2(-CUDART_INF_F, 0.f);
+  }
+  float M = fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   if (lane == 0) red[0][warp] = M;
   __syncthreads();
+#pragma unroll
   for (int i = 0; i < 16; ++i) M = fmaxf(M, red[0][i]);
   float L = 0.f;
-  for (int p = tid; p < parts; p += 4 * kD) {
-    const float2 ml = part_ml[at(p)];
-    const float a = pat_weight(ml.x, M);
-    wts[p] = a;
-    L = fmaf(ml.y, a, L);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float a = pat_weight(ml[i].x, M);
+    wts[tid + 4 * kD * i] = a;
+    L = fmaf(ml[i].y, a, L);
   }
   L = warp_sum(L);
   if (lane == 0) red[1][warp] = L;
   __syncthreads();
   L = 0.f;
+#pragma unroll
   for (int i = 0; i < 16; ++i) L += red[1][i];
   float O = 0.f;
-#pragma unroll 4
-  for (int p = slice; p < parts; p += 4) O = fmaf(part_o[(size_t)at(p) * kD + c], wts[p], O);
+  for (int p0 = 0;;) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int p = p0 + slice + 4 * u;
+      if (p < parts) O = fmaf(y[u], wts[p], O);
+    }
+    p0 += 4 * kAtOnce;
+    if (p0 >= parts) break;
+    load(p0);
+  }
   if (slice > 0) acc[slice - 1][c] = O;
   __syncthreads();
   if (slice > 0) return;
@@ -520,7 +564,7 @@ __global__ void __launch_bounds__(kPfThreads) k_paged_fp32(const __grid_constant
   pdl_wait();
   const int s = blockIdx.x, h = blockIdx.y, r0 = blockIdx.z * kPfRows, G = hq / hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const SeqWork sw = seq_work(pg, s, G, kPfRows);
+  const SeqWork sw = seq_work(pg, s, pg.len[s], G, kPfRows);
   if (sw.len != pg.len[s] && threadIdx.x == 0) record_error(err, kErrInput);
   const float scale = kPatLog2e * rsqrtf((float)kD);
   for (int rr = r0; rr < min(r0 + kPfRows, min(sw.fresh, pg.w) * G); ++rr) {
