@@ -1041,6 +1041,9 @@ PageView page_view(const stlite_pages* pg, int w) {
   v.page_rows = pg->page_rows;
   v.max_pages = pg->max_pages;
   v.w = w;
+  v.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (pg->page_rows == 1 << i) v.page_shift = i;
   return v;
 }
 
@@ -1129,6 +1132,7 @@ stlite_status check_paged_attention(const stlite_shape* shape, const stlite_page
   const long long rows = (long long)pages->max_pages * pages->page_rows * shape->n_kv_heads;
   const long long items = (long long)pages->n_seqs * shape->n_kv_heads * kPagedMaxNew;
   if (rows > (1LL << 30) || items > (1LL << 30)) return STLITE_EUNSUPPORTED;
+  if ((long long)pages->n_pages * pages->page_rows * shape->n_kv_heads > 0x7fffffffLL) return STLITE_EUNSUPPORTED;
   return STLITE_OK;
 }
 

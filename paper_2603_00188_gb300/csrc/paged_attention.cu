@@ -170,25 +170,30 @@ __device__ __forceinline__ void cp_async_wait() {
 }
 
 // ---------------------------------------------------------------------- bf16
-// Each warp streams its own blocks (every kWarps-th of the range) through its
+// Each warp streams its own blocks (every kPmWarps-th of the range) through its
 // own ring of stages in shared memory: 16 rows of keys and of values by
 // asynchronous 16-byte copies (any page size: a lane looks up its row's page
-// one block ahead; rows that do not count are filled with zeros and
-// masked).  No warp
-// waits for another until an item ends.  Both products run on the warp's
-// tensor cores (m16n8k16, fp32 accumulation), as a single new token is at
-// most 16 query rows, below the smallest tile of tcgen05:
-//   S (16 rows x 8 queries) = K Q^T, the queries' fragments in registers,
+// one block ahead; rows that do not count are filled with zeros and masked).
+// No warp waits for another until an item ends.  Both products run on the
+// warp's tensor cores (m16n8k16, fp32 accumulation), as a session's new tokens
+// make a few query rows, below the smallest tile of tcgen05:
+//   S (16 rows x 8 queries) = K Q^T,
 //   O^T (128 dims x 8 queries) += V^T P^T, P transposed in registers by
 //   movmatrix and taken as P = hi + lo, two bf16 parts (16 bits of it: with one
 //   part the weights' rounding would be as large as the result's).
+// NT: groups of eight queries that share one read of the cache: 1 or 2 with
+// their fragments in registers, 4 with them read from shared memory.
 constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
 constexpr int kPmCtas = 2;                          // per SM
 constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
 __host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
+__host__ __device__ constexpr int pm_ring(int nt) { return kPmWarps * pm_stages(nt) * 2 * kPmHalf; }
+__host__ __device__ constexpr int pm_queries(int nt) { return nt > 2 ? 8 * nt * kD * 2 : 0; }
+__host__ __device__ constexpr int pm_pass(int nt) { return nt > 2 ? 2 : nt; }  // groups merged at a time
 __host__ __device__ constexpr int pm_smem(int nt) {
-  return kPmWarps * pm_stages(nt) * 2 * kPmHalf + kPmWarps * 8 * nt * (kPmPitch * 4 + 8) + (int)sizeof(RangeScratch<kPmThreads>);
+  return pm_ring(nt) + pm_queries(nt) + kPmWarps * 8 * (pm_pass(nt) * kPmPitch * 4 + nt * 8) +
+         (int)sizeof(RangeScratch<kPmThreads>);
 }
 
 __device__ __forceinline__ void pm_ldsm_x4(uint32_t addr, uint32_t (&a)[4]) {
@@ -225,108 +230,134 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // rows' chunks lie in eight different bank groups.
 __device__ __forceinline__ uint32_t pm_off(int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 7)) << 4)); }
 
-// The cached row of lane % 16 in a block: its slot, or -1 where it does not count.
-__device__ __forceinline__ int block_slot(const PageView& pg, const Cursor& c, int blk, uint32_t* err) {
-  const int j = blk * kPatBlock + (threadIdx.x & (kPatBlock - 1));
-  if (j >= c.w.len) return -1;
-  const int i = j / pg.page_rows, page = pg.table[(size_t)c.s * pg.max_pages + i];
-  if (page < 0 || page >= pg.n_pages) {
-    record_error(err, kErrInput);
-    return -1;
-  }
-  return page * pg.page_rows + (j - i * pg.page_rows);
-}
-
 template <int NT>
 __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     k_paged_mma(const __grid_constant__ PageView pg, const __nv_bfloat16* q, const __nv_bfloat16* k,
                 const __nv_bfloat16* v, __nv_bfloat16* out, int n, int hq, int hkv, int by_item, int chunks,
-                PartDesc* desc, float2* part_ml, float* part_o, uint32_t* err) {
-  constexpr int kStages = pm_stages(NT), kRows = 8 * NT;
+                int chunk_rows, PartDesc* desc, float2* part_ml, float* part_o, uint32_t* err) {
+  constexpr int kStages = pm_stages(NT), kRows = 8 * NT, kPass = pm_pass(NT);
   extern __shared__ uint4 pat_smem[];
-  float* wo = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(pat_smem) + kPmWarps * kStages * 2 * kPmHalf);
-  float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * kRows * kPmPitch);
+  uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
+  float* wo = reinterpret_cast<float*>(sm + pm_ring(NT) + pm_queries(NT));
+  float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * 8 * kPass * kPmPitch);
   RangeScratch<kPmThreads>* scratch = reinterpret_cast<RangeScratch<kPmThreads>*>(wml + kPmWarps * kRows);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
   const int G = hq / hkv, cta = blockIdx.x;
-  const uint32_t ring = smem_u32(pat_smem) + warp * kStages * 2 * kPmHalf;
+  const uint32_t ring = smem_u32(sm) + warp * kStages * 2 * kPmHalf;
   pdl_trigger();
   pdl_wait();
-  const Range rg = find_range<kPmThreads>(pg, G, kRows, hkv, kPmWarps, err, scratch);
-  if (!by_item && tid == 0) desc[cta].item = -1;
+  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, err, scratch);
+  const bool describes = tid == kPmThreads - 32;  // the thread that writes the CTA's descriptor
+  if (!by_item && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  // fetching: the cursor of the block whose slots were looked up last
+  // Fetching.  look_up: lane % 16's row of the warp's next block, as a row of
+  // 128 elements of the pools seen as [rows][128], or -1 where it does not
+  // count.  fetch: its copies into a stage.
   Cursor ahead = rg.at;
-  long long fb = rg.b0 + warp;  // next block to look up
-  int slot = -1, head = 0;
-  bool more = false;
-  uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
-  auto look_up = [&]() {
-    more = fb < rg.b1;
-    if (!more) return;
-    advance(ahead, fb, pg, G, kRows, hkv);
-    const int local = (int)(fb - ahead.base), item = local / ahead.w.blocks;
-    head = item / ahead.w.chunks;
-    slot = block_slot(pg, ahead, local - item * ahead.w.blocks, err);
+  long long fb = rg.b0 + warp;
+  int ahead_blk = -1, ahead_head = 0;
+  auto look_up = [&]() -> int {
+    if (fb >= rg.b1) return -2;  // the range's end
+    if (ahead_blk < 0 || ahead_blk + kPmWarps >= ahead.w.blocks) {
+      advance(ahead, fb, pg, G, chunk_rows, hkv);
+      const int local = (int)(fb - ahead.base), item = local / ahead.w.blocks;
+      ahead_blk = local - item * ahead.w.blocks;
+      ahead_head = item / ahead.w.chunks;
+    } else {
+      ahead_blk += kPmWarps;
+    }
     fb += kPmWarps;
+    const int j = ahead_blk * kPatBlock + (lane & (kPatBlock - 1));
+    if (j >= ahead.w.len) return -1;
+    const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
+    const int page = pg.table[(size_t)ahead.s * pg.max_pages + i];
+    if (page < 0 || page >= pg.n_pages) {
+      record_error(err, kErrInput);
+      return -1;
+    }
+    return (page * pg.page_rows + (j - i * pg.page_rows)) * hkv + ahead_head;
   };
-  auto fetch = [&](int stage) {
-    if (more) {
-      const uint64_t ok = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
+  uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
+  const int fc = lane & 15, fr = lane >> 4;
+  const __nv_bfloat16 *kf = k + 8 * fc, *vf = v + 8 * fc;
+  const uint32_t f_off = fr * 256 + ((fc ^ fr) << 4);
+  auto fetch = [&](int stage, int row) {
+    if (row != -2) {
+      const uint64_t ok = __ballot_sync(0xffffffffu, row >= 0) & 0xffffu;
       counts = (counts & ~(0xffffull << (16 * stage))) | ok << (16 * stage);
       const uint32_t dst = ring + stage * 2 * kPmHalf;
-      const int c = lane & 15;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int r = 2 * i + (lane >> 4), sl = __shfl_sync(0xffffffffu, slot, r);
-        const size_t at = ((size_t)max(sl, 0) * hkv + head) * kD + 8 * c;
-        cp_async16_fill(dst + pm_off(r, c), k + at, sl >= 0);
-        cp_async16_fill(dst + kPmHalf + pm_off(r, c), v + at, sl >= 0);
+        const int r = __shfl_sync(0xffffffffu, row, 2 * i + fr);
+        const size_t at = (size_t)max(r, 0) * kD;
+        const uint32_t to = dst + 512 * i + (f_off ^ ((2 * i & 6) << 4));
+        cp_async16_fill(to, kf + at, r >= 0);
+        cp_async16_fill(to + kPmHalf, vf + at, r >= 0);
       }
     }
     cp_async_commit();
   };
+  {
+    int first[kStages];  // all table entries on their way before the first copies
 #pragma unroll
-  for (int st = 0; st < kStages; ++st) {
-    look_up();
-    fetch(st);
+    for (int st = 0; st < kStages; ++st) first[st] = look_up();
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) fetch(st, first[st]);
   }
 
   const float scale = kPatLog2e * rsqrtf((float)kD);
+  const uint32_t k_off = (lane & 15) * 256 + (((lane >> 4) ^ (lane & 7)) << 4);
+  const uint32_t v_off = ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+  const uint32_t q_smem = smem_u32(sm) + pm_ring(NT);
   Cursor cur = rg.at;
   long long b = rg.b0 + warp;  // the warp's next block to compute
   int stage = 0;
   for (long long seg = rg.b0; seg < rg.b1;) {
     // the part of one item that lies in the range: blocks seg .. seg_end
-    advance(cur, seg, pg, G, kRows, hkv);
-    const int item = (int)((seg - cur.base) / cur.w.blocks);
-    const int h = item / cur.w.chunks, chunk = item % cur.w.chunks;
+    advance(cur, seg, pg, G, chunk_rows, hkv);
+    const int item = (int)(seg - cur.base) / cur.w.blocks;
+    const int h = item / cur.w.chunks, chunk = item - h * cur.w.chunks;
     const long long i0 = cur.base + (long long)item * cur.w.blocks, i1 = i0 + cur.w.blocks;
     const long long seg_end = i1 < rg.b1 ? i1 : rg.b1;
-    const int row0 = chunk * kRows, rows = min(kRows, min(cur.w.fresh, pg.w) * G - row0);
-
-    // query fragments, and the rows that each of the lane's queries sees
-    uint32_t qb[8][NT][2];
-    int sees[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = row0 + 8 * nt + g8, t = cur.w.first + r / G;
-      const bool ok = 8 * nt + g8 < rows && t >= 0 && t < n;
-      const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + ((size_t)(ok ? t : 0) * hq + h * G + r % G) * kD);
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        qb[ks][nt][0] = ok ? qr[8 * ks + t4] : 0u;
-        qb[ks][nt][1] = ok ? qr[8 * ks + 4 + t4] : 0u;
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int x = 8 * nt + 2 * t4 + e;
-        sees[nt][e] = x < rows ? cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G) : 0;
-      }
+    const int row0 = chunk * chunk_rows, rows = min(chunk_rows, min(cur.w.fresh, pg.w) * G - row0);
+    const bool whole = seg == i0 && seg_end == i1;
+    if (describes && seg == i0) {
+      const int id = (cur.s * hkv + h) * chunks + chunk;
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
+      if (by_item)
+        desc[id] = d;
+      else if (!whole)
+        desc[cta] = d;
     }
-    // running state: queries 8 nt + 2 t4 + e; o[mt][nt][j] is dimension
-    // 16 mt + g8 + 8 (j >> 1) of query 8 nt + 2 t4 + (j & 1)
+
+    // query fragments: dimensions 16 ks + 2 t4 + {0, 1} and + 8 of query 8 nt + g8
+    uint32_t qb[NT > 2 ? 1 : 8][NT > 2 ? 1 : NT][2];
+    if constexpr (NT <= 2) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = row0 + 8 * nt + g8, t = cur.w.first + r / G;
+        const bool ok = 8 * nt + g8 < rows && t >= 0 && t < n;
+        const uint32_t* qr = reinterpret_cast<const uint32_t*>(q + ((size_t)(ok ? t : 0) * hq + h * G + r % G) * kD);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          qb[ks][nt][0] = ok ? qr[8 * ks + t4] : 0u;
+          qb[ks][nt][1] = ok ? qr[8 * ks + 4 + t4] : 0u;
+        }
+      }
+    } else {
+      for (int e = tid; e < kRows * 16; e += kPmThreads) {
+        const int x = e >> 4, r = row0 + x, t = cur.w.first + r / G;
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (x < rows && t >= 0 && t < n)
+          y = reinterpret_cast<const uint4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[e & 15];
+        *reinterpret_cast<uint4*>(sm + pm_ring(NT) + pm_off(x, e & 15)) = y;
+      }
+      __syncthreads();
+    }
+    // Running state: raw maximum and the lane's part of the sum of queries
+    // 8 nt + 2 t4 + e; o[mt][nt][j] is dimension 16 mt + g8 + 8 (j >> 1) of
+    // query 8 nt + 2 t4 + (j & 1).
     float m[NT][2], l[NT][2], o[8][NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -335,61 +366,97 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
     }
+    const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
     for (; b < seg_end; b += kPmWarps) {
       cp_async_wait<kStages - 1>();
       __syncwarp();
-      look_up();  // the block that will take this stage
-      const uint32_t kt = ring + stage * 2 * kPmHalf, vt = kt + kPmHalf;
+      const int next = look_up();  // the block that will take this stage
+      const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
       const int base = (int)(b - i0) * kPatBlock;
-      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) >> g8;
-      float c[2][NT][4];
+      constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
+      float c[kChains][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int i = 0; i < kChains; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[0][nt][j] = c[1][nt][j] = 0.f;
+        for (int nt = 0; nt < NT; ++nt) c[i][nt][0] = c[i][nt][1] = c[i][nt][2] = c[i][nt][3] = 0.f;
+      if constexpr (NT <= 2) {
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        uint32_t a[4];
-        pm_ldsm_x4(kt + pm_off(lane & 15, 2 * ks + (lane >> 4)), a);
+        for (int ks = 0; ks < 8; ++ks) {
+          uint32_t a[4];
+          pm_ldsm_x4(kt - k_off + (k_off ^ (ks << 5)), a);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) pm_mma(c[ks & 1][nt], a, qb[ks][nt][0], qb[ks][nt][1]);
+          for (int nt = 0; nt < NT; ++nt) pm_mma(c[ks % kChains][nt], a, qb[ks][nt][0], qb[ks][nt][1]);
+        }
+      } else {
+#pragma unroll
+        for (int kp = 0; kp < 4; ++kp) {
+          uint32_t a[4], a2[4];
+          pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6)), a);
+          pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6 | 32)), a2);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            uint32_t f[4];
+            pm_ldsm_x4(q_smem + pm_off(8 * nt + (lane & 7), 4 * kp + (lane >> 3)), f);
+            pm_mma(c[0][nt], a, f[0], f[1]);
+            pm_mma(c[0][nt], a2, f[2], f[3]);
+          }
+        }
+      }
+      if constexpr (kChains == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[0][0][j] += c[1][0][j];
+      }
+      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
+      if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = g8 + 8 * (j >> 1), sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + (j & 1)) / G);
+            if (!(ok >> r & 1u) || base + r >= sees) c[0][nt][j] = -CUDART_INF_F;
+          }
       }
       uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float p[2][2], alpha[2];  // [row g8, g8 + 8][query]
+        float mn[2], ms[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float x0 = (ok & 1u) && base + g8 < sees[nt][e] ? (c[0][nt][e] + c[1][nt][e]) * scale : -CUDART_INF_F;
-          const float x1 =
-              (ok & 256u) && base + g8 + 8 < sees[nt][e] ? (c[0][nt][2 + e] + c[1][nt][2 + e]) * scale : -CUDART_INF_F;
-          float mx = fmaxf(x0, x1);
+          float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float mn = fmaxf(m[nt][e], mx), ms = mn == -CUDART_INF_F ? 0.f : mn;
-          alpha[e] = ex2_approx(m[nt][e] - ms);
-          p[0][e] = ex2_approx(x0 - ms);
-          p[1][e] = ex2_approx(x1 - ms);
-          l[nt][e] = fmaf(l[nt][e], alpha[e], p[0][e] + p[1][e]);  // the lane's rows only
-          m[nt][e] = mn;
+          mn[e] = fmaxf(m[nt][e], mx);
+          ms[e] = mn[e] == -CUDART_INF_F ? 0.f : mn[e] * scale;
+        }
+        if (__any_sync(0xffffffffu, mn[0] != m[nt][0] || mn[1] != m[nt][1])) {  // rare once the maxima have settled
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float alpha = ex2_approx(fmaf(m[nt][e], scale, -ms[e]));
+            l[nt][e] *= alpha;
+            m[nt][e] = mn[e];
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) {
+              o[mt][nt][e] *= alpha;
+              o[mt][nt][2 + e] *= alpha;
+            }
+          }
         }
 #pragma unroll
-        for (int mt = 0; mt < 8; ++mt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[mt][nt][j] *= alpha[j & 1];
-#pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const uint32_t hi = pack_bf16(p[x][0], p[x][1]);
-          const uint32_t lo = pack_bf16(p[x][0] - __uint_as_float(hi << 16), p[x][1] - __uint_as_float(hi & 0xffff0000u));
+          const float p0 = ex2_approx(fmaf(c[0][nt][2 * x], scale, -ms[0]));
+          const float p1 = ex2_approx(fmaf(c[0][nt][2 * x + 1], scale, -ms[1]));
+          l[nt][0] += p0;
+          l[nt][1] += p1;
+          const uint32_t hi = pack_bf16(p0, p1);
           ph[nt][x] = transpose8x8(hi);
-          pl[nt][x] = transpose8x8(lo);
+          pl[nt][x] = transpose8x8(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
         }
       }
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) {
         uint32_t a[4];
-        pm_ldsm_x4_trans(vt + pm_off((lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), a);
+        pm_ldsm_x4_trans(vt - v_off + (v_off ^ (mt << 5)), a);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           pm_mma(o[mt][nt], a, ph[nt][0], ph[nt][1]);
@@ -397,71 +464,71 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         }
       }
       __syncwarp();
-      fetch(stage);
+      fetch(stage, next);
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-    // the warps' states of this item, merged in shared memory
+    // The warps' states of this item, merged in shared memory, kPass groups of
+    // queries at a time.
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float s = l[nt][e];
         s += __shfl_xor_sync(0xffffffffu, s, 4);
         s += __shfl_xor_sync(0xffffffffu, s, 8);
         s += __shfl_xor_sync(0xffffffffu, s, 16);
-        const int x = 8 * nt + 2 * t4 + e;
-        if (g8 == 0) wml[warp * kRows + x] = make_float2(m[nt][e], s);
-        float* w = wo + (warp * kRows + x) * kPmPitch + g8;
+        if (g8 == 0) wml[warp * kRows + 8 * nt + 2 * t4 + e] = make_float2(m[nt][e] * scale, s);
+      }
+    const int part = 2 * cta + (seg == i0 ? 1 : 0);
 #pragma unroll
-        for (int mt = 0; mt < 8; ++mt) {
-          w[16 * mt] = o[mt][nt][e];
-          w[16 * mt + 8] = o[mt][nt][2 + e];
+    for (int n0 = 0; n0 < NT; n0 += kPass) {
+      if (n0 > 0) __syncthreads();  // the buffer is free again
+#pragma unroll
+      for (int i = 0; i < kPass; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float* w = wo + (warp * 8 * kPass + 8 * i + 2 * t4 + e) * kPmPitch + g8;
+#pragma unroll
+          for (int mt = 0; mt < 8; ++mt) {
+            w[16 * mt] = o[mt][n0 + i][e];
+            w[16 * mt + 8] = o[mt][n0 + i][2 + e];
+          }
+        }
+      __syncthreads();
+      for (int y = warp; y < min(8 * kPass, rows - 8 * n0); y += kPmWarps) {
+        const int x = 8 * n0 + y;
+        float M = -CUDART_INF_F, L = 0.f, wt[kPmWarps];
+#pragma unroll
+        for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
+#pragma unroll
+        for (int w = 0; w < kPmWarps; ++w) {
+          const float2 ml = wml[w * kRows + x];
+          wt[w] = pat_weight(ml.x, M);
+          L = fmaf(ml.y, wt[w], L);
+        }
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kPmWarps; ++w) {
+          const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 * kPass + y) * kPmPitch + 4 * lane);
+          O.x = fmaf(z.x, wt[w], O.x);
+          O.y = fmaf(z.y, wt[w], O.y);
+          O.z = fmaf(z.z, wt[w], O.z);
+          O.w = fmaf(z.w, wt[w], O.w);
+        }
+        const int r = row0 + x, t = cur.w.first + r / G;
+        if (whole) {
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          if (t >= 0 && t < n)
+            *reinterpret_cast<uint2*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
+                make_uint2(pack_bf16(O.x * inv, O.y * inv), pack_bf16(O.z * inv, O.w * inv));
+        } else {
+          *reinterpret_cast<float4*>(part_o + ((size_t)part * kRows + x) * kD + 4 * lane) = O;
+          if (lane == 0) part_ml[part * kRows + x] = make_float2(M, L);
         }
       }
     }
-    __syncthreads();
-    const bool whole = seg == i0 && seg_end == i1;
-    const int part = 2 * cta + (seg == i0 ? 1 : 0);
-    for (int x = warp; x < rows; x += kPmWarps) {
-      float M = -CUDART_INF_F, L = 0.f, wt[kPmWarps];
-#pragma unroll
-      for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
-#pragma unroll
-      for (int w = 0; w < kPmWarps; ++w) {
-        const float2 ml = wml[w * kRows + x];
-        wt[w] = pat_weight(ml.x, M);
-        L = fmaf(ml.y, wt[w], L);
-      }
-      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kPmWarps; ++w) {
-        const float4 y = *reinterpret_cast<const float4*>(wo + (w * kRows + x) * kPmPitch + 4 * lane);
-        O.x = fmaf(y.x, wt[w], O.x);
-        O.y = fmaf(y.y, wt[w], O.y);
-        O.z = fmaf(y.z, wt[w], O.z);
-        O.w = fmaf(y.w, wt[w], O.w);
-      }
-      const int r = row0 + x, t = cur.w.first + r / G;
-      if (whole) {
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        if (t >= 0 && t < n)
-          *reinterpret_cast<uint2*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
-              make_uint2(pack_bf16(O.x * inv, O.y * inv), pack_bf16(O.z * inv, O.w * inv));
-      } else {
-        *reinterpret_cast<float4*>(part_o + ((size_t)part * 16 + x) * kD + 4 * lane) = O;
-        if (lane == 0) part_ml[part * 16 + x] = make_float2(M, L);
-      }
-    }
-    if (tid == 0 && seg == i0) {
-      const int id = (cur.s * hkv + h) * chunks + chunk;
-      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
-      if (by_item)
-        desc[id] = d;
-      else if (!whole)
-        desc[cta] = d;
-    }
     seg = seg_end;
-    if (seg < rg.b1) __syncthreads();  // the merge buffer is free again
+    if (seg < rg.b1) __syncthreads();  // the merge buffer (and the queries) are free again
   }
   cp_async_wait<0>();
 }
@@ -471,8 +538,8 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 // in shared memory while the first partials are on their way.
 template <typename T>
 __global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ PageView pg, T* out, int n, int hq,
-                                                       int hkv, int chunks, int chunk_rows, int by_item,
-                                                       const PartDesc* desc, const float2* part_ml,
+                                                       int hkv, int chunks, int chunk_rows, int part_rows,
+                                                       int by_item, const PartDesc* desc, const float2* part_ml,
                                                        const float* part_o) {
   __shared__ float wts[kPatMaxCtas];
   __shared__ float red[2][16];
@@ -492,8 +559,8 @@ __global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ 
   if (r >= min(w.fresh, pg.w) * G) return;
   const int tid = threadIdx.x, c = tid & (kD - 1), slice = tid / kD, lane = tid & 31, warp = tid >> 5;
   const int parts = d.c1 - d.c0 + 1;
-  auto at = [&](int p) { return (p == 0 ? 2 * d.c0 + 1 : 2 * (d.c0 + p)) * 16 + x; };
-  constexpr int kAtOnce = 10;  // partials of a slice in flight
+  auto at = [&](int p) { return (p == 0 ? 2 * d.c0 + 1 : 2 * (d.c0 + p)) * part_rows + x; };
+  constexpr int kAtOnce = 20;  // partials of a slice in flight
   float y[kAtOnce];
   auto load = [&](int p0) {
 #pragma unroll
@@ -612,11 +679,20 @@ static int paged_ctas() {
   return kPmCtas * sms < kPatMaxCtas ? kPmCtas * sms : kPatMaxCtas;
 }
 
+// Query rows of a CTA's part: groups of eight that share one read of the
+// cache, up to four of them.
+static int paged_part_rows(const PageView& pages, int G) {
+  const int rows = pages.w * G;
+  return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
+}
+
 // Workspace: the error word, the descriptors (16 KB), then two parts of each
-// CTA: (max, sum) of 16 query rows, and their weighted values.
+// CTA: (max, sum) of its query rows, and their weighted values.
 constexpr size_t kPatHead = 256, kPatDescs = kPatMaxCtas * sizeof(PartDesc);
-size_t paged_workspace_bytes(DType, const PageView&, int, int) {
-  return kPatHead + kPatDescs + (size_t)2 * paged_ctas() * 16 * (sizeof(float2) + kD * sizeof(float));
+size_t paged_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
+  if (dt == kF32) return kPatHead;
+  return kPatHead + kPatDescs +
+         (size_t)2 * paged_ctas() * paged_part_rows(pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
 }
 
 cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
@@ -631,13 +707,14 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
                      static_cast<float*>(out), n, hq, hkv, err);
     return e != cudaSuccess ? e : cudaGetLastError();
   }
-  const int ctas = paged_ctas(), chunk_rows = rows <= 8 ? 8 : 16, chunks = (rows + chunk_rows - 1) / chunk_rows;
+  const int ctas = paged_ctas(), part_rows = paged_part_rows(pages, hq / hkv);
+  const int chunks = (rows + part_rows - 1) / part_rows, chunk_rows = (rows + chunks - 1) / chunks;
   const long long items = (long long)pages.n_seqs * hkv * chunks;
   const int by_item = items <= ctas, descs = by_item ? (int)items : ctas;
   uint8_t* at = static_cast<uint8_t*>(ws) + kPatHead;
   PartDesc* desc = reinterpret_cast<PartDesc*>(at);
   float2* part_ml = reinterpret_cast<float2*>(at + kPatDescs);
-  float* part_o = reinterpret_cast<float*>(part_ml + (size_t)2 * ctas * 16);
+  float* part_o = reinterpret_cast<float*>(part_ml + (size_t)2 * ctas * part_rows);
   typedef __nv_bfloat16 B;
   {
     TimingScope ts("paged_attention", st);
@@ -647,18 +724,20 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
       if (e != cudaSuccess) return;
       e = launch_after(k_paged_mma<NT>, dim3(ctas), kPmThreads, pm_smem(NT), st, pages, static_cast<const B*>(q),
                        static_cast<const B*>(k), static_cast<const B*>(v), static_cast<B*>(out), n, hq, hkv, by_item,
-                       chunks, desc, part_ml, part_o, err);
+                       chunks, chunk_rows, desc, part_ml, part_o, err);
     };
-    if (chunk_rows == 8)
+    if (part_rows == 8)
       run(std::integral_constant<int, 1>());
-    else
+    else if (part_rows == 16)
       run(std::integral_constant<int, 2>());
+    else
+      run(std::integral_constant<int, 4>());
     if (e != cudaSuccess) return e;
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
   }
   TimingScope ts("paged_merge", st);
-  e = launch_after(k_paged_merge<B>, dim3(descs, rows < chunk_rows ? rows : chunk_rows), 4 * kD, 0, st, pages,
-                   static_cast<B*>(out), n, hq, hkv, chunks, chunk_rows, by_item, desc, part_ml, part_o);
+  e = launch_after(k_paged_merge<B>, dim3(descs, chunk_rows), 4 * kD, 0, st, pages,
+                   static_cast<B*>(out), n, hq, hkv, chunks, chunk_rows, part_rows, by_item, desc, part_ml, part_o);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
