@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from array import array
 
 import numpy as np
@@ -140,17 +141,14 @@ _sig = {
     "stlite_decode_layers_workspace_size": (_S, [ctypes.POINTER(Shape), ctypes.c_int32,
                                                  ctypes.POINTER(ctypes.c_size_t)]),
     "stlite_rope_init": (_S, [ctypes.c_double, ctypes.POINTER(Rope)]),
-    "stlite_rotate_qk": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(Tokens), _P, _P, _P]),
-    "stlite_paged_append": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Rope), ctypes.POINTER(Tokens),
-                                 ctypes.POINTER(Pages), _P, _P, _P, _P]),
-    "stlite_paged_attention": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Pages), _P, _P, _P, _P, _P,
-                                    ctypes.c_size_t, _P]),
-    "stlite_paged_workspace_size": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Pages),
-                                         ctypes.POINTER(ctypes.c_size_t)]),
-    "stlite_compact_paged": (_S, [ctypes.POINTER(Shape), ctypes.c_int32, ctypes.POINTER(Pages), ctypes.c_int32,
-                                  ctypes.c_int32, _P, _P]),
+    # shape, tokens and pages as packed bytes or addresses: no object for each call
+    "stlite_rotate_qk": (_S, [_P, ctypes.POINTER(Rope), _P, _P, _P, _P]),
+    "stlite_paged_append": (_S, [_P, ctypes.POINTER(Rope), _P, _P, _P, _P, _P, _P]),
+    "stlite_paged_attention": (_S, [_P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "stlite_paged_workspace_size": (_S, [_P, _P, ctypes.POINTER(ctypes.c_size_t)]),
+    "stlite_compact_paged": (_S, [_P, ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, _P, _P]),
     "stlite_compress_layers_paged": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Frames), ctypes.POINTER(Params),
-                                          ctypes.POINTER(Pages), ctypes.c_int32, ctypes.c_int32, _P,
+                                          _P, ctypes.c_int32, ctypes.c_int32, _P,
                                           ctypes.POINTER(ctypes.c_int32), _P, ctypes.c_size_t, _P]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -505,66 +503,86 @@ class PageTable:
 
     def __init__(self, n_pages, page_rows, table, length=None, cu_new=None, max_new=1):
         for t, n in ((table, 2), (length, 1), (cu_new, 1)):
-            if t is not None and (t.dtype != torch.int32 or t.dim() != n or not t.is_contiguous()):
-                raise ValueError("table, length and cu_new are contiguous int32 tensors")
+            if t is not None and (t.dtype != torch.int32 or t.dim() != n or not t.is_contiguous()
+                                  or t.device != table.device):
+                raise ValueError("table, length and cu_new are contiguous int32 tensors of one device")
         n_seqs = table.shape[0]
         if (length is not None and length.shape[0] != n_seqs) or (cu_new is not None and cu_new.shape[0] != n_seqs + 1):
             raise ValueError("length is [S] and cu_new [S + 1] for a table [S][max_pages]")
         self.table, self.length, self.cu_new, self.max_new = table, length, cu_new, int(max_new)
         self.c = Pages(n_seqs, int(n_pages), int(page_rows), table.shape[1], _ptr(table), _ptr(length), _ptr(cu_new))
+        self._address, self._device = ctypes.addressof(self.c), table.get_device()
+        self._pool = (int(n_pages), int(page_rows))
 
 
 def make_pages(n_pages, page_rows, table, length=None, cu_new=None, max_new=1) -> PageTable:
     return PageTable(n_pages, page_rows, table, length, cu_new, max_new)
 
 
-def _check_pools(pages, hkv, dtype, *pools):
-    want = (pages.c.n_pages, pages.c.page_rows, hkv, 128)
-    for p in pools:
-        if p.shape != want or p.dtype != dtype or not p.is_contiguous():
-            raise ValueError("a page pool is a contiguous tensor %s of the cache's type" % (want,))
+_SHAPE = struct.Struct("=6i")            # stlite_shape
+_TOKENS = struct.Struct("=3Q3q2Qf4xQ")   # stlite_tokens
+_CURRENT = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # of a device
 
 
-def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps):
-    """stlite_tokens of q, k, v [T][H][128], each token's heads packed."""
-    n = q.shape[0]
-    strides = []
-    for x in (q, k, v):
-        if x is None:
-            strides.append(0)
-            continue
-        if x.dim() != 3 or x.shape[0] != n or x.shape[2] != 128 or x.dtype != q.dtype:
-            raise ValueError("q, k and v are [T][H][128] of one type")
-        s = x.stride()
-        if s[2] != 1 or (x.shape[1] > 1 and s[1] != 128):
-            raise ValueError("a token's heads are packed")
-        strides.append(s[0] if n > 1 else 0)
-    for w in (q_norm, k_norm):
-        if w is not None and (w.shape != (128,) or w.dtype != q.dtype or not w.is_contiguous()):
-            raise ValueError("a norm's weights are [128] of q's type")
-    axes = 1 if rope.section[0] == 64 else 3
-    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != axes * n:
-        raise ValueError("pos is a contiguous int32 [%sT]" % ("" if axes == 1 else "3]["))
-    return Tokens(q.data_ptr(), k.data_ptr(), _ptr(v), strides[0], strides[1], strides[2], _ptr(q_norm), _ptr(k_norm),
-                  eps, pos.data_ptr())
+def _pool_error(pages, hkv):
+    return ValueError("a page pool is a contiguous tensor %s of the cache's type" % ((*pages._pool, hkv, 128),))
 
 
-def _check_packed(shape, dtype, *outs):
-    for o in outs:
-        if o.shape != shape or o.dtype != dtype or not o.is_contiguous():
-            raise ValueError("an output is a contiguous %s of q's type" % (tuple(shape),))
+def _output_error(shape):
+    return ValueError("an output is a contiguous %s of q's type" % (tuple(shape),))
+
+
+_ELSEWHERE = "the tensors are not on the current CUDA device"
+
+
+def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype) -> bytes:
+    """stlite_tokens of q, k, v [T][H][128] (qs, ks: the shapes of q and k),
+    each token's heads packed."""
+    n, hq, d = qs
+    nk, hkv, dk = ks
+    sq, sk = q.stride(), k.stride()
+    if (d != 128 or dk != 128 or nk != n or k.dtype != dtype or sq[2] != 1 or sk[2] != 1 or (sq[1] != 128 and hq > 1)
+            or (sk[1] != 128 and hkv > 1)):
+        raise ValueError("q and k are [T][H][128] of one type, each token's heads packed")
+    pv = sv0 = 0
+    if v is not None:
+        sv, pv = v.stride(), v.data_ptr()
+        if v.shape != ks or v.dtype != dtype or sv[2] != 1 or (sv[1] != 128 and hkv > 1):
+            raise ValueError("v is as k")
+        sv0 = sv[0] or 1
+    pq = pk = 0
+    if q_norm is not None or k_norm is not None:
+        for w in (q_norm, k_norm):
+            if w is not None and (w.shape != (128,) or w.dtype != dtype or not w.is_contiguous()):
+                raise ValueError("a norm's weights are [128] of q's type")
+            if w is not None and w.get_device() != q.get_device():
+                raise ValueError(_ELSEWHERE)
+        pq, pk = _ptr(q_norm) or 0, _ptr(k_norm) or 0
+    if pos.dtype != torch.int32 or pos.numel() != (n if rope.section[0] == 64 else 3 * n) or not pos.is_contiguous():
+        raise ValueError("pos is a contiguous int32 [T], or [3][T] for three axes")
+    if n == 1:  # no next token: whatever its distance would be
+        return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, 0, 0, 0, pq, pk, eps, pos.data_ptr())
+    # 0 stands for packed, so a broadcast token's goes as 1, which the library refuses
+    return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, sq[0] or 1, sk[0] or 1, sv0, pq, pk, eps, pos.data_ptr())
 
 
 def stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
     """Norm (where weights are given) and rotation of every head of q
     [T][Hq][128] and k [T][Hkv][128] (each may be a slice of one projection's
     output) into q_out and k_out; pos: int32 [T], or [3][T] for three axes."""
-    _check_packed(q.shape, q.dtype, q_out)
-    _check_packed(k.shape, q.dtype, k_out)
-    x = _tokens(q, k, None, pos, rope, q_norm, k_norm, eps)
-    sh = Shape(q.shape[0], q.shape[1], k.shape[1], 128, 1, _DTYPE[q.dtype])
-    _check(_lib.stlite_rotate_qk(sh, rope, x, q_out.data_ptr(), k_out.data_ptr(), _stream(stream)),
-           "stlite_rotate_qk")
+    qs, ks, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    x = _tokens(q, k, None, pos, rope, q_norm, k_norm, eps, qs, ks, dtype)
+    if q_out.shape != qs or q_out.dtype != dtype or not q_out.is_contiguous():
+        raise _output_error(qs)
+    if k_out.shape != ks or k_out.dtype != dtype or not k_out.is_contiguous():
+        raise _output_error(ks)
+    if dev < 0 or not (torch._C._cuda_getDevice() == dev == k.get_device() == pos.get_device() == q_out.get_device()
+                       == k_out.get_device()):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_rotate_qk(_SHAPE.pack(qs[0], qs[1], ks[1], 128, 1, _DTYPE[dtype]), rope, x, q_out.data_ptr(),
+                               k_out.data_ptr(), _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_rotate_qk")
 
 
 def rotate_qk(q, k, pos, rope, q_norm=None, k_norm=None, eps=1e-6, stream=None):
@@ -579,14 +597,24 @@ def stlite_paged_append(q, k, v, pos, rope, pages, q_out, k_pages, v_pages, q_no
                         stream=None):
     """The new tokens' rotated keys and their values into the pages, the
     rotated queries into q_out (see stlite_rotate_qk for q, k, v and pos)."""
-    _check_packed(q.shape, q.dtype, q_out)
-    _check_pools(pages, k.shape[1], q.dtype, k_pages, v_pages)
-    if v.shape != k.shape:
-        raise ValueError("k and v have one shape")
-    x = _tokens(q, k, v, pos, rope, q_norm, k_norm, eps)
-    sh = Shape(q.shape[0], q.shape[1], k.shape[1], 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[q.dtype])
-    _check(_lib.stlite_paged_append(sh, rope, x, pages.c, q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                                    _stream(stream)), "stlite_paged_append")
+    qs, ks, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    x = _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype)
+    if q_out.shape != qs or q_out.dtype != dtype or not q_out.is_contiguous():
+        raise _output_error(qs)
+    hkv = ks[1]
+    want = (*pages._pool, hkv, 128)
+    if (k_pages.shape != want or v_pages.shape != want or k_pages.dtype != dtype or v_pages.dtype != dtype
+            or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
+        raise _pool_error(pages, hkv)
+    if dev < 0 or not (torch._C._cuda_getDevice() == dev == k.get_device() == v.get_device() == pos.get_device()
+                       == q_out.get_device() == k_pages.get_device() == v_pages.get_device() == pages._device):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_paged_append(
+        _SHAPE.pack(qs[0], qs[1], hkv, 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[dtype]), rope, x,
+        pages._address, q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+        _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_paged_append")
 
 
 def _paged_shape(q, k_pages, pages) -> Shape:
@@ -611,12 +639,23 @@ def paged_workspace(q, k_pages, pages):
 def stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream=None):
     """Attention of the new tokens q [T][Hq][128] over their sequences'
     pages into out (q's shape and type)."""
-    sh = _paged_shape(q, k_pages, pages)
-    _check_packed(q.shape, q.dtype, out)
-    _check_pools(pages, sh.n_kv_heads, q.dtype, k_pages, v_pages)
-    _check(_lib.stlite_paged_attention(sh, pages.c, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                                       out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)),
-           "stlite_paged_attention")
+    shape, dtype, dev, pool = q.shape, q.dtype, q.get_device(), k_pages.shape
+    if len(shape) != 3 or shape[2] != 128 or not q.is_contiguous():
+        raise ValueError("q is a contiguous [T][Hq][128]")
+    if out.shape != shape or out.dtype != dtype or not out.is_contiguous():
+        raise _output_error(shape)
+    if (len(pool) != 4 or pool != (*pages._pool, pool[2], 128) or v_pages.shape != pool or k_pages.dtype != dtype
+            or v_pages.dtype != dtype or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
+        raise _pool_error(pages, "Hkv")
+    if dev < 0 or not (torch._C._cuda_getDevice() == dev == k_pages.get_device() == v_pages.get_device()
+                       == out.get_device() == ws.get_device() == pages._device):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_paged_attention(
+        _SHAPE.pack(shape[0], shape[1], pool[2], 128, pages.max_new, _DTYPE[dtype]), pages._address, q.data_ptr(),
+        k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
+        _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_paged_attention")
 
 
 def paged_attention(q, k_pages, v_pages, pages, stream=None):
@@ -626,36 +665,49 @@ def paged_attention(q, k_pages, v_pages, pages, stream=None):
     return out
 
 
-def _paged_layer_table(layers, pages, budget):
-    for k, v, kp, vp, ix in layers:
-        _check_pools(pages, k.shape[1], k.dtype, kp, vp)
-        if k.shape != layers[0][0].shape or v.shape != k.shape or ix.shape != (k.shape[1], budget):
-            raise ValueError("k and v are [N][Hkv][128] and idx [Hkv][budget] in every layer")
-    return _layer_table([(k, k, v, kp, vp, ix) for k, v, kp, vp, ix in layers])
-
-
 def stlite_compact_paged(layers, budget, pages, seq, stream=None):
     """The kept rows of every layer into sequence seq's pages; layers: list
     of (k, v, k_pages, v_pages, idx)."""
-    n, hkv, d = layers[0][0].shape
-    sh = Shape(n, hkv, hkv, d, 1, _DTYPE[layers[0][0].dtype])
-    arr = _paged_layer_table(layers, pages, int(budget))
-    _check(_lib.stlite_compact_paged(sh, int(budget), pages.c, int(seq), len(layers), _address(arr),
-                                     _stream(stream)), "stlite_compact_paged")
+    k0 = layers[0][0]
+    shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
+    n, hkv, d = shape
+    want, kept = (*pages._pool, hkv, d), (hkv, budget)
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
+        raise ValueError(_ELSEWHERE)
+    for k, v, kp, vp, ix in layers:
+        if (k.shape != shape or v.shape != shape or kp.shape != want or vp.shape != want or ix.shape != kept
+                or not k.dtype == v.dtype == kp.dtype == vp.dtype == dtype or ix.dtype != torch.int32
+                or not (k.is_contiguous() and v.is_contiguous() and kp.is_contiguous() and vp.is_contiguous()
+                        and ix.is_contiguous())):
+            raise ValueError("k and v are [N][Hkv][128], pools %s of their type, idx int32 [Hkv][budget], all "
+                             "contiguous" % (want,))
+        if not k.get_device() == kp.get_device() == vp.get_device() == ix.get_device() == dev or (
+                v.get_device() != dev and not v.is_pinned()):
+            raise ValueError(_ELSEWHERE)
+        a = k.data_ptr()
+        flat += (a, a, v.data_ptr(), kp.data_ptr(), vp.data_ptr(), ix.data_ptr())
+    arr = array("Q", flat)
+    st = _lib.stlite_compact_paged(_SHAPE.pack(n, hkv, hkv, d, 1, _DTYPE[dtype]), budget, pages._address, seq,
+                                   len(layers), _address(arr), _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_compact_paged")
 
 
 def stlite_compress_layers_paged(layers, frames, params, pages, seq, ws, stream=None) -> int:
     """stlite_compress_layers with the kept rows in sequence seq's pages;
     layers: list of (q, k, v, k_pages, v_pages, idx_out)."""
     sh = make_shape(layers[0][0], layers[0][1])
+    want, dtype = (*pages._pool, sh.n_kv_heads, 128), layers[0][1].dtype
     for _, _, _, kp, vp, _ in layers:
-        _check_pools(pages, sh.n_kv_heads, layers[0][1].dtype, kp, vp)
+        if not (kp.shape == vp.shape == want and kp.dtype == vp.dtype == dtype and kp.is_contiguous()
+                and vp.is_contiguous()):
+            raise _pool_error(pages, sh.n_kv_heads)
     fs = _frames(frames)
     arr = _layer_table(layers)
     b = ctypes.c_int32(0)
-    _check(_lib.stlite_compress_layers_paged(sh, fs.c, params, pages.c, int(seq), len(layers), _address(arr),
-                                             ctypes.byref(b), _ptr(ws), ws.numel(), _stream(stream)),
-           "stlite_compress_layers_paged")
+    _check(_lib.stlite_compress_layers_paged(ctypes.byref(sh), ctypes.byref(fs.c), ctypes.byref(params),
+                                             pages._address, int(seq), len(layers), _address(arr), ctypes.byref(b),
+                                             _ptr(ws), ws.numel(), _stream(stream)), "stlite_compress_layers_paged")
     return int(b.value)
 
 

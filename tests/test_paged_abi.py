@@ -32,17 +32,18 @@ def good():
 def _pages(st, good, **kw):
     f = dict(n_seqs=4, n_pages=20, page_rows=16, max_pages=5, table=good, len=good, cu_new=None)
     f.update(kw)
-    return st.Pages(*[f[n] for n, _ in st.Pages._fields_])
+    return bytes(st.Pages(*[f[n] for n, _ in st.Pages._fields_]))
 
 
 def _tokens(st, good, **kw):
     f = dict(q=good, k=good, v=good, q_stride=0, k_stride=0, v_stride=0, q_norm=None, k_norm=None, eps=1e-6, pos=good)
     f.update(kw)
-    return st.Tokens(*[f[n] for n, _ in st.Tokens._fields_])
+    return bytes(st.Tokens(*[f[n] for n, _ in st.Tokens._fields_]))
 
 
 def _shape(st, n=4, hq=8, hkv=2, d=128, w=1, dt=0):
-    return st.Shape(n, hq, hkv, d, w, dt)
+    """As packed bytes, which a pointer argument takes as it takes an address."""
+    return bytes(st.Shape(n, hq, hkv, d, w, dt))
 
 
 PAGES = [dict(n_seqs=0), dict(n_pages=0), dict(page_rows=0), dict(max_pages=-1), dict(table=None), dict(table=2),
@@ -81,11 +82,11 @@ def test_lengths_optional_for_compaction_only(st, good):
             setattr(io[0], field, bad)
             assert st._lib.stlite_compact_paged(_shape(st, n=100), 10, pg, 0, 1, io, None) == st.STLITE_EINVAL
     fr, prm = st.FrameSpec([0], [5], [5]), st.make_params(0.9)
-    need = st.stlite_workspace_size(_shape(st, n=100), fr, prm)
+    need = st.stlite_workspace_size(st.Shape(100, 8, 2, 128, 1, 0), fr, prm)
     io = (st.LayerIO * 1)(st.LayerIO(*[good] * 6))
 
     def fused(pages, seq, params, layers, ws_bytes):
-        return st._lib.stlite_compress_layers_paged(_shape(st, n=100), fr.c, params, pages, seq, 1, layers, None, good,
+        return st._lib.stlite_compress_layers_paged(st.Shape(100, 8, 2, 128, 1, 0), fr.c, params, pages, seq, 1, layers, None, good,
                                                     ws_bytes, None)
 
     assert fused(pg, 0, prm, io, need) == st.STLITE_EINVAL  # 90 rows, 80 in the table
@@ -177,6 +178,13 @@ def test_rotation_refused(st, good):
     for base in (0.0, -1.0, math.nan, math.inf):
         assert lib.stlite_rope_init(base, st.Rope()) == inv
     assert lib.stlite_rope_init(1e4, None) == inv
+
+
+def test_packed_arguments_have_the_structs_layout(st):
+    """The binding passes shapes and tokens as packed bytes."""
+    assert st._SHAPE.pack(1, 2, 3, 4, 5, 6) == bytes(st.Shape(1, 2, 3, 4, 5, 6))
+    x = [1 << 40, 2 << 40, 3 << 40, -4, 5, 6, 7 << 40, 8 << 40, 0.25, 9 << 40]
+    assert st._TOKENS.pack(*x) == bytes(st.Tokens(*x))
 
 
 def test_rope_frequencies(st):
