@@ -169,6 +169,40 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// The rows of a warp's blocks, one block after the other: its range's every
+// kPmWarps-th.
+constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
+constexpr int kPmCtas = 2;  // per SM
+struct RowFinder {
+  Cursor at;
+  long long b, end;  // next block; end of the CTA's range
+  int blk, head;     // the last block within its item, and the item's KV head
+
+  // Lane % 16's row of the next block, as a row of 128 elements of the pools
+  // seen as [rows][128]; -1 where it does not count, -2 past the range.
+  __device__ __forceinline__ int next(const PageView& pg, int G, int chunk_rows, int hkv, uint32_t* err) {
+    if (b >= end) return -2;
+    if (blk < 0 || blk + kPmWarps >= at.w.blocks) {
+      advance(at, b, pg, G, chunk_rows, hkv);
+      const int local = (int)(b - at.base), item = local / at.w.blocks;
+      blk = local - item * at.w.blocks;
+      head = item / at.w.chunks;
+    } else {
+      blk += kPmWarps;
+    }
+    b += kPmWarps;
+    const int j = blk * kPatBlock + (threadIdx.x & (kPatBlock - 1));
+    if (j >= at.w.len) return -1;
+    const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
+    const int page = pg.table[(size_t)at.s * pg.max_pages + i];
+    if (page < 0 || page >= pg.n_pages) {
+      record_error(err, kErrInput);
+      return -1;
+    }
+    return (page * pg.page_rows + (j - i * pg.page_rows)) * hkv + head;
+  }
+};
+
 // ---------------------------------------------------------------------- bf16
 // Each warp streams its own blocks (every kPmWarps-th of the range) through its
 // own ring of stages in shared memory: 16 rows of keys and of values by
@@ -183,8 +217,6 @@ __device__ __forceinline__ void cp_async_wait() {
 //   part the weights' rounding would be as large as the result's).
 // NT: groups of eight queries that share one read of the cache: 1 or 2 with
 // their fragments in registers, 4 with them read from shared memory.
-constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
-constexpr int kPmCtas = 2;                          // per SM
 constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
 __host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
@@ -251,33 +283,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (!by_item && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  // Fetching.  look_up: lane % 16's row of the warp's next block, as a row of
-  // 128 elements of the pools seen as [rows][128], or -1 where it does not
-  // count.  fetch: its copies into a stage.
-  Cursor ahead = rg.at;
-  long long fb = rg.b0 + warp;
-  int ahead_blk = -1, ahead_head = 0;
-  auto look_up = [&]() -> int {
-    if (fb >= rg.b1) return -2;  // the range's end
-    if (ahead_blk < 0 || ahead_blk + kPmWarps >= ahead.w.blocks) {
-      advance(ahead, fb, pg, G, chunk_rows, hkv);
-      const int local = (int)(fb - ahead.base), item = local / ahead.w.blocks;
-      ahead_blk = local - item * ahead.w.blocks;
-      ahead_head = item / ahead.w.chunks;
-    } else {
-      ahead_blk += kPmWarps;
-    }
-    fb += kPmWarps;
-    const int j = ahead_blk * kPatBlock + (lane & (kPatBlock - 1));
-    if (j >= ahead.w.len) return -1;
-    const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
-    const int page = pg.table[(size_t)ahead.s * pg.max_pages + i];
-    if (page < 0 || page >= pg.n_pages) {
-      record_error(err, kErrInput);
-      return -1;
-    }
-    return (page * pg.page_rows + (j - i * pg.page_rows)) * hkv + ahead_head;
-  };
+  RowFinder finder = {rg.at, rg.b0 + warp, rg.b1, -1, 0};
   uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
   const int fc = lane & 15, fr = lane >> 4;
   const __nv_bfloat16 *kf = k + 8 * fc, *vf = v + 8 * fc;
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   {
     int first[kStages];  // all table entries on their way before the first copies
 #pragma unroll
-    for (int st = 0; st < kStages; ++st) first[st] = look_up();
+    for (int st = 0; st < kStages; ++st) first[st] = finder.next(pg, G, chunk_rows, hkv, err);
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st, first[st]);
   }
@@ -370,7 +376,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     for (; b < seg_end; b += kPmWarps) {
       cp_async_wait<kStages - 1>();
       __syncwarp();
-      const int next = look_up();  // the block that will take this stage
+      const int next = finder.next(pg, G, chunk_rows, hkv, err);  // the block that will take this stage
       const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
       const int base = (int)(b - i0) * kPatBlock;
       constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
@@ -533,6 +539,244 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   cp_async_wait<0>();
 }
 
+// ---------------------------------------------------------------------- fp32
+// The same split and rings with fp32 products (fmaf).  A block's keys and its
+// values are a slot each, three to a warp.  Scores: lane (r, c), r = 0 .. 7,
+// c = 0 .. 3, holds rows r and r + 8 of the keys at every fourth 16-byte chunk
+// from c on, so that a chunk of a query read from shared memory serves two
+// rows; four lanes' sums are added by shuffles.  Values: a lane owns four
+// dimensions, the probabilities come back through shared memory.  GM: queries
+// of a chunk.  7 queries take 33 % of the FMA pipe at the rate of HBM.
+constexpr int kPfSlots = 3;
+constexpr int kPfHalf = kPatBlock * kD * 4;  // keys, or values, of a block
+constexpr int kPfPass = 4;                   // queries merged at a time
+__host__ __device__ constexpr int pf_ring() { return kPmWarps * kPfSlots * kPfHalf; }
+// the probabilities of a block, and, once an item has ended, the merge buffer
+__host__ __device__ constexpr int pf_shared(int gm) {
+  return gm * kPatBlock * 4 > kPfPass * kPmPitch * 4 ? kPmWarps * gm * kPatBlock * 4 : kPmWarps * kPfPass * kPmPitch * 4;
+}
+__host__ __device__ constexpr int pf_smem(int gm) {
+  return pf_ring() + gm * kD * 4 + pf_shared(gm) + kPmWarps * gm * 8 + (int)sizeof(RangeScratch<kPmThreads>);
+}
+
+// Byte of the 16-byte chunk c of row r: the two rows that eight lanes read at
+// a time in the scores lie in different halves of the banks.
+__device__ __forceinline__ uint32_t pf_off(int r, int c) { return (uint32_t)(r * 512 + ((c ^ ((r & 1) << 2)) << 4)); }
+
+template <int GM>
+__global__ void __launch_bounds__(kPmThreads, kPmCtas)
+    k_paged_fma(const __grid_constant__ PageView pg, const float* q, const float* k, const float* v, float* out, int n,
+                int hq, int hkv, int by_item, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
+                float* part_o, uint32_t* err) {
+  extern __shared__ uint4 pat_smem[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
+  float* qs = reinterpret_cast<float*>(sm + pf_ring());  // [GM][128]
+  float* shared = qs + GM * kD;
+  float2* wml = reinterpret_cast<float2*>(sm + pf_ring() + GM * kD * 4 + pf_shared(GM));  // [warps][GM]
+  RangeScratch<kPmThreads>* scratch = reinterpret_cast<RangeScratch<kPmThreads>*>(wml + kPmWarps * GM);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = hq / hkv, cta = blockIdx.x;
+  uint8_t* ring = sm + warp * kPfSlots * kPfHalf;
+  float* ps = shared + warp * GM * kPatBlock;  // [GM][16]
+  pdl_trigger();
+  pdl_wait();
+  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, err, scratch);
+  const bool describes = tid == kPmThreads - 32;  // the thread that writes the CTA's descriptor
+  if (!by_item && describes) desc[cta].item = -1;
+  if (cta >= rg.ctas) return;
+
+  RowFinder finder = {rg.at, rg.b0 + warp, rg.b1, -1, 0};
+  const int fc = lane;
+  auto fetch = [&](int slot, int row, const float* from) {
+    if (row != -2) {
+      const uint32_t dst = smem_u32(ring) + slot * kPfHalf;
+#pragma unroll
+      for (int r = 0; r < kPatBlock; ++r) {
+        const int x = __shfl_sync(0xffffffffu, row, r);
+        cp_async16_fill(dst + pf_off(r, fc), from + (size_t)max(x, 0) * kD + 4 * fc, x >= 0);
+      }
+    }
+    cp_async_commit();
+  };
+  // keys and values alternate through the slots; the block after the current
+  // one has its keys on the way
+  int now = finder.next(pg, G, chunk_rows, hkv, err), after = finder.next(pg, G, chunk_rows, hkv, err);
+  fetch(0, now, k);
+  fetch(1, now, v);
+  fetch(2, after, k);
+  int slot = 0;
+
+  const float scale = kPatLog2e * rsqrtf((float)kD);
+  const int r8 = lane >> 2, c4 = lane & 3;
+  Cursor cur = rg.at;
+  long long b = rg.b0 + warp;  // the warp's next block to compute
+  for (long long seg = rg.b0; seg < rg.b1;) {
+    // the part of one item that lies in the range: blocks seg .. seg_end
+    advance(cur, seg, pg, G, chunk_rows, hkv);
+    const int item = (int)(seg - cur.base) / cur.w.blocks;
+    const int h = item / cur.w.chunks, chunk = item - h * cur.w.chunks;
+    const long long i0 = cur.base + (long long)item * cur.w.blocks, i1 = i0 + cur.w.blocks;
+    const long long seg_end = i1 < rg.b1 ? i1 : rg.b1;
+    const int row0 = chunk * chunk_rows, rows = min(chunk_rows, min(cur.w.fresh, pg.w) * G - row0);
+    const bool whole = seg == i0 && seg_end == i1;
+    if (describes && seg == i0) {
+      const int id = (cur.s * hkv + h) * chunks + chunk;
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
+      if (by_item)
+        desc[id] = d;
+      else if (!whole)
+        desc[cta] = d;
+    }
+    for (int e = tid; e < GM * (kD / 4); e += kPmThreads) {
+      const int x = e / (kD / 4), r = row0 + x, t = cur.w.first + r / G;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (x < rows && t >= 0 && t < n)
+        y = reinterpret_cast<const float4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[e % (kD / 4)];
+      reinterpret_cast<float4*>(qs)[e] = y;
+    }
+    __syncthreads();
+    float m[GM], l[GM], o[GM][4];  // l: the lane's rows only
+#pragma unroll
+    for (int x = 0; x < GM; ++x) {
+      m[x] = -CUDART_INF_F;
+      l[x] = 0.f;
+      o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+    }
+    const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
+    for (; b < seg_end; b += kPmWarps) {
+      cp_async_wait<kPfSlots - 1>();
+      __syncwarp();
+      const int then = finder.next(pg, G, chunk_rows, hkv, err);
+      const uint32_t ok = __ballot_sync(0xffffffffu, now >= 0) & 0xffffu;
+      const int base = (int)(b - i0) * kPatBlock;
+      float s[GM][2];
+#pragma unroll
+      for (int x = 0; x < GM; ++x) s[x][0] = s[x][1] = 0.f;
+      const uint8_t* kt = ring + slot * kPfHalf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 k0 = *reinterpret_cast<const float4*>(kt + pf_off(r8, 4 * i + c4));
+        const float4 k1 = *reinterpret_cast<const float4*>(kt + pf_off(r8 + 8, 4 * i + c4));
+#pragma unroll
+        for (int x = 0; x < GM; ++x) {
+          const float4 y = *reinterpret_cast<const float4*>(qs + x * kD + 16 * i + 4 * c4);
+          s[x][0] = fmaf(y.x, k0.x, fmaf(y.y, k0.y, fmaf(y.z, k0.z, fmaf(y.w, k0.w, s[x][0]))));
+          s[x][1] = fmaf(y.x, k1.x, fmaf(y.y, k1.y, fmaf(y.z, k1.z, fmaf(y.w, k1.w, s[x][1]))));
+        }
+      }
+      __syncwarp();
+      fetch(slot, after, v);
+      slot = slot + 1 == kPfSlots ? 0 : slot + 1;
+      const bool masked = ok != 0xffffu || base + kPatBlock > all_see;
+#pragma unroll
+      for (int x = 0; x < GM; ++x) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[x][u] += __shfl_xor_sync(0xffffffffu, s[x][u], 1);
+          s[x][u] += __shfl_xor_sync(0xffffffffu, s[x][u], 2);
+        }
+        if (masked) {  // some rows do not count for some queries
+          const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            if (!(ok >> (r8 + 8 * u) & 1u) || base + r8 + 8 * u >= sees) s[x][u] = -CUDART_INF_F;
+        }
+        float mx = fmaxf(s[x][0], s[x][1]);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        const float mn = fmaxf(m[x], mx), ms = mn == -CUDART_INF_F ? 0.f : mn;
+        if (mn != m[x]) {  // the same for the whole warp
+          const float a = exp2f((m[x] - ms) * scale);
+          l[x] *= a;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x][e] *= a;
+          m[x] = mn;
+        }
+        const float p0 = exp2f((s[x][0] - ms) * scale), p1 = exp2f((s[x][1] - ms) * scale);
+        l[x] += p0 + p1;
+        if (c4 == 0) {
+          ps[x * kPatBlock + r8] = p0;
+          ps[x * kPatBlock + r8 + 8] = p1;
+        }
+      }
+      cp_async_wait<kPfSlots - 1>();
+      __syncwarp();
+      const uint8_t* vt = ring + slot * kPfHalf;
+#pragma unroll
+      for (int r0 = 0; r0 < kPatBlock; r0 += 4) {
+        float4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const float4*>(vt + pf_off(r0 + u, lane));
+#pragma unroll
+        for (int x = 0; x < GM; ++x) {
+          const float4 p = *reinterpret_cast<const float4*>(ps + x * kPatBlock + r0);
+          o[x][0] = fmaf(p.w, y[3].x, fmaf(p.z, y[2].x, fmaf(p.y, y[1].x, fmaf(p.x, y[0].x, o[x][0]))));
+          o[x][1] = fmaf(p.w, y[3].y, fmaf(p.z, y[2].y, fmaf(p.y, y[1].y, fmaf(p.x, y[0].y, o[x][1]))));
+          o[x][2] = fmaf(p.w, y[3].z, fmaf(p.z, y[2].z, fmaf(p.y, y[1].z, fmaf(p.x, y[0].z, o[x][2]))));
+          o[x][3] = fmaf(p.w, y[3].w, fmaf(p.z, y[2].w, fmaf(p.y, y[1].w, fmaf(p.x, y[0].w, o[x][3]))));
+        }
+      }
+      __syncwarp();
+      now = after;
+      after = then;
+      fetch(slot, after, k);
+      slot = slot + 1 == kPfSlots ? 0 : slot + 1;
+    }
+    // the warps' states of this item, merged in shared memory
+#pragma unroll
+    for (int x = 0; x < GM; ++x) {
+      float y = l[x];  // four lanes hold the same rows
+      y += __shfl_xor_sync(0xffffffffu, y, 4);
+      y += __shfl_xor_sync(0xffffffffu, y, 8);
+      y += __shfl_xor_sync(0xffffffffu, y, 16);
+      if (lane == 0) wml[warp * GM + x] = make_float2(m[x] * scale, y);
+    }
+    const int part = 2 * cta + (seg == i0 ? 1 : 0);
+#pragma unroll
+    for (int x0 = 0; x0 < GM; x0 += kPfPass) {
+      __syncthreads();  // the probabilities, or the last pass, are done with
+#pragma unroll
+      for (int i = 0; i < kPfPass; ++i)
+        *reinterpret_cast<float4*>(shared + (warp * kPfPass + i) * kPmPitch + 4 * lane) =
+            make_float4(o[x0 + i][0], o[x0 + i][1], o[x0 + i][2], o[x0 + i][3]);
+      __syncthreads();
+      const int x = x0 + warp;  // a query for each warp
+      if (x < rows) {
+        float M = -CUDART_INF_F, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * GM + x].x);
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kPmWarps; ++w) {
+          const float2 ml = wml[w * GM + x];
+          const float a = pat_weight(ml.x, M);
+          L = fmaf(ml.y, a, L);
+          const float4 z = *reinterpret_cast<const float4*>(shared + (w * kPfPass + warp) * kPmPitch + 4 * lane);
+          O.x = fmaf(z.x, a, O.x);
+          O.y = fmaf(z.y, a, O.y);
+          O.z = fmaf(z.z, a, O.z);
+          O.w = fmaf(z.w, a, O.w);
+        }
+        const int r = row0 + x, t = cur.w.first + r / G;
+        if (whole) {
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          if (t >= 0 && t < n)
+            *reinterpret_cast<float4*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
+                make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+        } else {
+          *reinterpret_cast<float4*>(part_o + ((size_t)part * GM + x) * kD + 4 * lane) = O;
+          if (lane == 0) part_ml[part * GM + x] = make_float2(M, L);
+        }
+      }
+    }
+    seg = seg_end;
+    if (seg < rg.b1) __syncthreads();  // the merge buffer and the queries are free again
+  }
+  cp_async_wait<0>();
+}
+
+// --------------------------------------------------------------------- merge
 // out of the items that several CTAs had parts of.  grid (descriptors, rows):
 // four slices of 128 threads, a dimension each; the parts' weights are formed
 // in shared memory while the first partials are on their way.
@@ -615,63 +859,6 @@ __global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ 
   if (t >= 0 && t < n) from_f(L == 0.f ? 0.f : O / L, out + ((size_t)t * hq + h * G + r % G) * kD + c);
 }
 
-// ---------------------------------------------------------------------- fp32
-constexpr int kPfThreads = 256;
-constexpr int kPfWarps = kPfThreads / 32;
-constexpr int kPfRows = 16;  // query rows of a CTA: (new token, query head) pairs of one KV head
-
-// One CTA per (session, KV head, 16 query rows); a warp takes every eighth row
-// of the cache, a lane four dimensions.
-__global__ void __launch_bounds__(kPfThreads) k_paged_fp32(const __grid_constant__ PageView pg, const float* q,
-                                                           const float* k, const float* v, float* out, int n, int hq,
-                                                           int hkv, uint32_t* err) {
-  __shared__ float wo[kPfWarps][kD];
-  __shared__ float2 wml[kPfWarps];
-  pdl_trigger();
-  pdl_wait();
-  const int s = blockIdx.x, h = blockIdx.y, r0 = blockIdx.z * kPfRows, G = hq / hkv;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const SeqWork sw = seq_work(pg, s, pg.len[s], G, kPfRows);
-  if (sw.len != pg.len[s] && threadIdx.x == 0) record_error(err, kErrInput);
-  const float scale = kPatLog2e * rsqrtf((float)kD);
-  for (int rr = r0; rr < min(r0 + kPfRows, min(sw.fresh, pg.w) * G); ++rr) {
-    const int i = rr / G, g = h * G + rr % G, t = sw.first + i;
-    if (t < 0 || t >= n) break;
-    float qf[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -CUDART_INF_F, l = 0.f;
-    for (int e = 0; e < 4; ++e) qf[e] = q[((size_t)t * hq + g) * kD + 4 * lane + e] * scale;
-    const int sees = sw.len - (sw.fresh - 1 - i);
-    for (int j = warp; j < sees; j += kPfWarps) {
-      const int p = j / pg.page_rows, page = pg.table[(size_t)s * pg.max_pages + p];
-      if (page < 0 || page >= pg.n_pages) {
-        if (lane == 0) record_error(err, kErrInput);
-        continue;
-      }
-      const size_t at = (((size_t)page * pg.page_rows + (j - p * pg.page_rows)) * hkv + h) * kD + 4 * lane;
-      float x = 0.f;
-      for (int e = 0; e < 4; ++e) x = fmaf(qf[e], k[at + e], x);
-      x = warp_sum(x);
-      const float mn = fmaxf(m, x), a = pat_weight(m, mn), w = pat_weight(x, mn);
-      l = l * a + w;
-      m = mn;
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], a, w * v[at + e]);
-    }
-    for (int e = 0; e < 4; ++e) wo[warp][4 * lane + e] = o[e];
-    if (lane == 0) wml[warp] = make_float2(m, l);
-    __syncthreads();
-    if (threadIdx.x < kD) {
-      float M = -CUDART_INF_F, L = 0.f, O = 0.f;
-      for (int w = 0; w < kPfWarps; ++w) M = fmaxf(M, wml[w].x);
-      for (int w = 0; w < kPfWarps; ++w) {
-        const float a = pat_weight(wml[w].x, M);
-        L = fmaf(wml[w].y, a, L);
-        O = fmaf(wo[w][threadIdx.x], a, O);
-      }
-      from_f(L == 0.f ? 0.f : O / L, out + ((size_t)t * hq + g) * kD + threadIdx.x);
-    }
-    __syncthreads();
-  }
-}
-
 // -------------------------------------------------------------------- launch
 static int paged_ctas() {
   int dev = 0, sms = 152;
@@ -679,10 +866,10 @@ static int paged_ctas() {
   return kPmCtas * sms < kPatMaxCtas ? kPmCtas * sms : kPatMaxCtas;
 }
 
-// Query rows of a CTA's part: groups of eight that share one read of the
-// cache, up to four of them.
-static int paged_part_rows(const PageView& pages, int G) {
+// Query rows of a CTA's part, which share one read of the cache.
+static int paged_part_rows(DType dt, const PageView& pages, int G) {
   const int rows = pages.w * G;
+  if (dt == kF32) return rows <= 4 ? 4 : (rows <= 8 ? 8 : 16);
   return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
 }
 
@@ -690,54 +877,57 @@ static int paged_part_rows(const PageView& pages, int G) {
 // CTA: (max, sum) of its query rows, and their weighted values.
 constexpr size_t kPatHead = 256, kPatDescs = kPatMaxCtas * sizeof(PartDesc);
 size_t paged_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
-  if (dt == kF32) return kPatHead;
   return kPatHead + kPatDescs +
-         (size_t)2 * paged_ctas() * paged_part_rows(pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
+         (size_t)2 * paged_ctas() * paged_part_rows(dt, pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
 }
 
 cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
                                    void* out, int n, int hq, int hkv, void* ws, cudaStream_t st) {
   uint32_t* err = static_cast<uint32_t*>(ws);
-  const int rows = pages.w * (hq / hkv);
-  cudaError_t e = cudaSuccess;
-  if (dt == kF32) {
-    TimingScope ts("paged_attention", st);
-    e = launch_after(k_paged_fp32, dim3(pages.n_seqs, hkv, (rows + kPfRows - 1) / kPfRows), kPfThreads, 0, st, pages,
-                     static_cast<const float*>(q), static_cast<const float*>(k), static_cast<const float*>(v),
-                     static_cast<float*>(out), n, hq, hkv, err);
-    return e != cudaSuccess ? e : cudaGetLastError();
-  }
-  const int ctas = paged_ctas(), part_rows = paged_part_rows(pages, hq / hkv);
+  const int rows = pages.w * (hq / hkv), part_rows = paged_part_rows(dt, pages, hq / hkv);
   const int chunks = (rows + part_rows - 1) / part_rows, chunk_rows = (rows + chunks - 1) / chunks;
+  const int ctas = paged_ctas();
   const long long items = (long long)pages.n_seqs * hkv * chunks;
   const int by_item = items <= ctas, descs = by_item ? (int)items : ctas;
   uint8_t* at = static_cast<uint8_t*>(ws) + kPatHead;
   PartDesc* desc = reinterpret_cast<PartDesc*>(at);
   float2* part_ml = reinterpret_cast<float2*>(at + kPatDescs);
   float* part_o = reinterpret_cast<float*>(part_ml + (size_t)2 * ctas * part_rows);
-  typedef __nv_bfloat16 B;
-  {
-    TimingScope ts("paged_attention", st);
-    auto run = [&](auto nt) {
-      constexpr int NT = decltype(nt)::value;
-      e = cudaFuncSetAttribute(k_paged_mma<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, pm_smem(NT));
-      if (e != cudaSuccess) return;
-      e = launch_after(k_paged_mma<NT>, dim3(ctas), kPmThreads, pm_smem(NT), st, pages, static_cast<const B*>(q),
-                       static_cast<const B*>(k), static_cast<const B*>(v), static_cast<B*>(out), n, hq, hkv, by_item,
-                       chunks, chunk_rows, desc, part_ml, part_o, err);
-    };
-    if (part_rows == 8)
-      run(std::integral_constant<int, 1>());
-    else if (part_rows == 16)
-      run(std::integral_constant<int, 2>());
-    else
-      run(std::integral_constant<int, 4>());
-    if (e != cudaSuccess) return e;
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  }
-  TimingScope ts("paged_merge", st);
-  e = launch_after(k_paged_merge<B>, dim3(descs, chunk_rows), 4 * kD, 0, st, pages,
-                   static_cast<B*>(out), n, hq, hkv, chunks, chunk_rows, part_rows, by_item, desc, part_ml, part_o);
+  cudaError_t e = cudaSuccess;
+  auto run = [&](auto zero, auto width) {
+    typedef decltype(zero) T;
+    constexpr int kWidth = decltype(width)::value;
+    {
+      TimingScope ts("paged_attention", st);
+      auto go = [&](auto kern, int smem) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return;
+        e = launch_after(kern, dim3(ctas), kPmThreads, smem, st, pages, static_cast<const T*>(q),
+                         static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), n, hq, hkv, by_item,
+                         chunks, chunk_rows, desc, part_ml, part_o, err);
+      };
+      if constexpr (std::is_same<T, float>::value) {
+        auto kern = k_paged_fma<kWidth>;
+        go(kern, pf_smem(kWidth));
+      } else {
+        auto kern = k_paged_mma<kWidth>;
+        go(kern, pm_smem(kWidth));
+      }
+      if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return;
+    }
+    TimingScope ts("paged_merge", st);
+    e = launch_after(k_paged_merge<T>, dim3(descs, chunk_rows), 4 * kD, 0, st, pages, static_cast<T*>(out), n, hq, hkv,
+                     chunks, chunk_rows, part_rows, by_item, desc, part_ml, part_o);
+  };
+  std::integral_constant<int, 1> w1;
+  std::integral_constant<int, 2> w2;
+  std::integral_constant<int, 4> w4;
+  std::integral_constant<int, 8> w8;
+  std::integral_constant<int, 16> w16;
+  if (dt == kF32)
+    part_rows == 4 ? run(float(), w4) : (part_rows == 8 ? run(float(), w8) : run(float(), w16));
+  else
+    part_rows == 8 ? run(__nv_bfloat16(), w1) : (part_rows == 16 ? run(__nv_bfloat16(), w2) : run(__nv_bfloat16(), w4));
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
