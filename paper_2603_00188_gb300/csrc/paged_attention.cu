@@ -6,10 +6,12 @@
 //
 // Work is divided by what the sessions hold when the kernel runs.  An item is
 // (session, KV head, chunk of query rows); its cache is cut into blocks of 16
-// rows, and the blocks of all items, laid end to end, into equal ranges, one
-// per CTA.  A CTA computes the parts of the few items that its range meets: an
-// item that lies inside one range is finished there, the parts of others are
-// merged by a second kernel.
+// rows.  An item counts for its blocks and for kPatItem units before them that
+// stand for its own costs (queries, merge: about 2 us of a CTA); the units of
+// all items, laid end to end, are cut into equal ranges, one per CTA.  A CTA
+// computes the parts of the few items that its range meets: an item whose
+// blocks lie inside one range is finished there, the parts of others are merged
+// by a second kernel.
 #include <type_traits>
 
 #include "kernels.cuh"
@@ -25,12 +27,13 @@ __device__ __forceinline__ void from_f(float x, __nv_bfloat16* y) { *y = __float
 
 // ---------------------------------------------------------------- the split
 constexpr int kPatBlock = 16;  // cached rows of a block
+constexpr int kPatItem = 8;    // units of an item's own costs
 
 // What a session asks for.
 struct SeqWork {
   int first, fresh;  // its packed tokens: first .. first + fresh
   int len;           // cached rows
-  int blocks;        // blocks of one item
+  int blocks;        // blocks of one item; none: its output is zeros
   int chunks;        // items of one KV head
 };
 __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, int G, int chunk_rows) {
@@ -38,61 +41,48 @@ __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, 
   w.first = pg.cu ? pg.cu[s] : s * pg.w;
   w.fresh = pg.cu ? pg.cu[s + 1] - w.first : pg.w;
   w.len = max(0, min(len, pg.max_pages * pg.page_rows));
-  w.blocks = max(1, (w.len + kPatBlock - 1) / kPatBlock);  // an empty session's zeros are one block's work
-  w.chunks = (max(0, min(w.fresh, pg.w)) * G + chunk_rows - 1) / chunk_rows;
+  w.blocks = (w.len + kPatBlock - 1) / kPatBlock;
+  const int rows = max(0, min(w.fresh, pg.w)) * G;
+  w.chunks = rows <= chunk_rows ? (rows > 0 ? 1 : 0) : (rows + chunk_rows - 1) / chunk_rows;
   return w;
 }
 
-// A position in the sequence of all blocks: session s begins at block `base`.
+// A position in the sequence of all units: session s begins at unit `base`.
+// Unit numbers fit an int (the call's checks).
 struct Cursor {
-  long long base;
-  int s;
+  int base, s;
   SeqWork w;
-  __device__ __forceinline__ long long cost(int hkv) const { return (long long)w.blocks * w.chunks * hkv; }
+  __device__ __forceinline__ int cost(int hkv) const { return (kPatItem + w.blocks) * w.chunks * hkv; }
 };
 
-// x / d and x % d; quotients of up to 32-bit numbers, which is what comes, take
-// a tenth of the time of 64-bit ones.
-__device__ __forceinline__ long long div_mod(long long x, int d, int* rem) {
-  if (x < 0x100000000ll) {
-    const uint32_t y = (uint32_t)x / (uint32_t)d;
-    *rem = (int)((uint32_t)x - y * (uint32_t)d);
-    return y;
-  }
-  *rem = (int)(x % d);
-  return x / d;
-}
-
-// A CTA's range of blocks and where it starts.  All blocks are dealt to `ctas`
-// CTAs in ranges of `quota` blocks, the first `extra` one more.
+// A CTA's range of units and where it starts.  All units are dealt to `ctas`
+// CTAs in ranges of `quota`, the first `extra` one more.
 struct Range {
-  long long b0, b1;
-  long long quota;
-  int ctas, extra;
+  int b0, b1;
+  int quota, ctas, extra;
   Cursor at;
-  __device__ __forceinline__ long long start(int c) const { return c * quota + min(c, extra); }
-  __device__ __forceinline__ int cta_of(long long b) const {
-    const long long wide = extra * (quota + 1);
-    int rem;
-    return b < wide ? (int)div_mod(b, (int)(quota + 1), &rem) : extra + (int)div_mod(b - wide, (int)quota, &rem);
+  __device__ __forceinline__ int start(int c) const { return c * quota + min(c, extra); }
+  __device__ __forceinline__ int cta_of(int b) const {
+    const int wide = extra * (quota + 1);
+    return b < wide ? b / (quota + 1) : extra + (b - wide) / quota;
   }
 };
 
-// Threads' block costs are summed over the sessions, and the range's first
-// session found by the thread that holds it.  Whole CTA; min_blocks: the
-// fewest blocks that make a CTA of their own.
+// The costs are summed over the sessions, and the range's first session found
+// by the thread that holds it.  Whole CTA; least: the fewest units that make a
+// CTA's range.
 template <int THREADS>
 struct RangeScratch {
-  long long warp_sum[THREADS / 32];
+  int warp_sum[THREADS / 32];
   Cursor at;
 };
 template <int THREADS>
-__device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int min_blocks, uint32_t* err,
+__device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int least, uint32_t* err,
                             RangeScratch<THREADS>* scratch) {
   constexpr int kWarps = THREADS / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (pg.n_seqs + THREADS - 1) / THREADS, s0 = min(pg.n_seqs, tid * per), s1 = min(pg.n_seqs, s0 + per);
-  long long mine = 0;
+  int mine = 0;
   Cursor c;  // of the thread's last session, and its only one where there are no more than threads
   for (int s = s0; s < s1; ++s) {
     const int asked = pg.len[s];
@@ -100,26 +90,26 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
     mine += c.cost(hkv);
     if (blockIdx.x == 0 && c.w.len != asked) record_error(err, kErrInput);
   }
-  long long incl = mine;
+  int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+    const int x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
   if (lane == 31) scratch->warp_sum[warp] = incl;
   __syncthreads();
-  long long before = 0, total = 0;
+  int before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    const long long x = scratch->warp_sum[w];
+    const int x = scratch->warp_sum[w];
     if (w < warp) before += x;
     total += x;
   }
   Range r;
-  const long long most = (total + min_blocks - 1) / min_blocks;
-  r.ctas = (int)(most < gridDim.x ? most : gridDim.x);
+  r.ctas = min((int)gridDim.x, total / least + (total % least != 0));
   if ((int)blockIdx.x >= r.ctas) return r;  // the same for every thread
-  r.quota = div_mod(total, r.ctas, &r.extra);
+  r.quota = total / r.ctas;
+  r.extra = total - r.quota * r.ctas;
   r.b0 = r.start(blockIdx.x);
   r.b1 = r.start(blockIdx.x + 1);
   incl += before;
@@ -140,8 +130,8 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
   return r;
 }
 
-// Moves on to the session of block b.
-__device__ __forceinline__ void advance(Cursor& c, long long b, const PageView& pg, int G, int chunk_rows, int hkv) {
+// Moves on to the session of unit b.
+__device__ __forceinline__ void advance(Cursor& c, int b, const PageView& pg, int G, int chunk_rows, int hkv) {
   while (b >= c.base + c.cost(hkv)) {
     c.base += c.cost(hkv);
     ++c.s;
@@ -169,29 +159,50 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The rows of a warp's blocks, one block after the other: its range's every
-// kPmWarps-th.
+// An item that a range meets.
+struct Item {
+  int h, chunk;
+  int i0, f0, i1;  // units: its first, its first block's, its end
+};
+__device__ __forceinline__ Item item_at(const Cursor& c, int u) {
+  const int units = kPatItem + c.w.blocks, i = (u - c.base) / units;
+  Item x;
+  x.h = c.w.chunks == 1 ? i : i / c.w.chunks;
+  x.chunk = i - x.h * c.w.chunks;
+  x.i0 = c.base + i * units;
+  x.f0 = x.i0 + kPatItem;
+  x.i1 = x.i0 + units;
+  return x;
+}
+
+// The rows of a warp's blocks, one block after the other.  The block of unit u
+// is warp u % kPmWarps's.
 constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
 constexpr int kPmCtas = 2;  // per SM
+__device__ __forceinline__ int warps_first(int u, int warp) { return u + ((warp - u) & (kPmWarps - 1)); }
 struct RowFinder {
   Cursor at;
-  long long b, end;  // next block; end of the CTA's range
-  int blk, head;     // the last block within its item, and the item's KV head
+  int end;         // of the CTA's range
+  int u, f0, i1;   // the warp's next block, and the first block and the end of the item that it is sought in
+  int head;
 
-  // Lane % 16's row of the next block, as a row of 128 elements of the pools
-  // seen as [rows][128]; -1 where it does not count, -2 past the range.
-  __device__ __forceinline__ int next(const PageView& pg, int G, int chunk_rows, int hkv, uint32_t* err) {
-    if (b >= end) return -2;
-    if (blk < 0 || blk + kPmWarps >= at.w.blocks) {
-      advance(at, b, pg, G, chunk_rows, hkv);
-      const int local = (int)(b - at.base), item = local / at.w.blocks;
-      blk = local - item * at.w.blocks;
-      head = item / at.w.chunks;
-    } else {
-      blk += kPmWarps;
+  __device__ __forceinline__ RowFinder(const Range& r) : at(r.at), end(r.b1), u(r.b0), f0(r.b0), i1(r.b0), head(0) {}
+
+  // Lane % 16's row of the warp's next block, as a row of 128 elements of the
+  // pools seen as [rows][128]; -1 where it does not count, -2 past the range.
+  __device__ __forceinline__ int next(const PageView& pg, int warp, int G, int chunk_rows, int hkv, uint32_t* err) {
+    while (u >= i1) {
+      if (i1 >= end) return -2;
+      advance(at, i1, pg, G, chunk_rows, hkv);
+      const Item x = item_at(at, i1);
+      u = warps_first(max(i1, x.f0), warp);
+      f0 = x.f0;
+      i1 = x.i1;
+      head = x.h;
     }
-    b += kPmWarps;
-    const int j = blk * kPatBlock + (threadIdx.x & (kPatBlock - 1));
+    if (u >= end) return -2;
+    const int j = (u - f0) * kPatBlock + (threadIdx.x & (kPatBlock - 1));
+    u += kPmWarps;
     if (j >= at.w.len) return -1;
     const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
     const int page = pg.table[(size_t)at.s * pg.max_pages + i];
@@ -202,6 +213,16 @@ struct RowFinder {
     return (page * pg.page_rows + (j - i * pg.page_rows)) * hkv + head;
   }
 };
+
+// Query rows row0 .. row0 + rows of a session's KV head, whose first query head
+// is g0, that see nothing.
+template <int THREADS, typename T>
+__device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int g0, int G, int row0, int rows) {
+  for (int e = threadIdx.x; e < rows * kD; e += THREADS) {
+    const int r = row0 + e / kD, t = first + r / G;
+    if (t >= 0 && t < n) from_f(0.f, out + ((size_t)t * hq + g0 + r % G) * kD + e % kD);
+  }
+}
 
 // ---------------------------------------------------------------------- bf16
 // Each warp streams its own blocks (every kPmWarps-th of the range) through its
@@ -283,7 +304,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (!by_item && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  RowFinder finder = {rg.at, rg.b0 + warp, rg.b1, -1, 0};
+  RowFinder finder(rg);
   uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
   const int fc = lane & 15, fr = lane >> 4;
   const __nv_bfloat16 *kf = k + 8 * fc, *vf = v + 8 * fc;
@@ -307,7 +328,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   {
     int first[kStages];  // all table entries on their way before the first copies
 #pragma unroll
-    for (int st = 0; st < kStages; ++st) first[st] = finder.next(pg, G, chunk_rows, hkv, err);
+    for (int st = 0; st < kStages; ++st) first[st] = finder.next(pg, warp, G, chunk_rows, hkv, err);
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st, first[st]);
   }
@@ -317,20 +338,25 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   const uint32_t v_off = ((lane & 7) + 8 * (lane >> 4)) * 256 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
   const uint32_t q_smem = smem_u32(sm) + pm_ring(NT);
   Cursor cur = rg.at;
-  long long b = rg.b0 + warp;  // the warp's next block to compute
   int stage = 0;
-  for (long long seg = rg.b0; seg < rg.b1;) {
-    // the part of one item that lies in the range: blocks seg .. seg_end
+  for (int seg = rg.b0; seg < rg.b1;) {
+    // the part of one item that lies in the range: blocks part0 .. seg_end
     advance(cur, seg, pg, G, chunk_rows, hkv);
-    const int item = (int)(seg - cur.base) / cur.w.blocks;
-    const int h = item / cur.w.chunks, chunk = item - h * cur.w.chunks;
-    const long long i0 = cur.base + (long long)item * cur.w.blocks, i1 = i0 + cur.w.blocks;
-    const long long seg_end = i1 < rg.b1 ? i1 : rg.b1;
+    const Item item = item_at(cur, seg);
+    const int h = item.h, chunk = item.chunk, part0 = max(seg, item.f0), seg_end = min(item.i1, rg.b1);
     const int row0 = chunk * chunk_rows, rows = min(chunk_rows, min(cur.w.fresh, pg.w) * G - row0);
-    const bool whole = seg == i0 && seg_end == i1;
-    if (describes && seg == i0) {
+    const bool owns = part0 == item.f0, whole = owns && seg_end == item.i1;  // has the first block, has them all
+    if (cur.w.blocks == 0 || part0 >= seg_end) {
+      if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
+        if (by_item && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
+        zero_rows<kPmThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
+      }
+      seg = seg_end;
+      continue;
+    }
+    if (describes && owns) {
       const int id = (cur.s * hkv + h) * chunks + chunk;
-      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(item.i1 - 1), 0};
       if (by_item)
         desc[id] = d;
       else if (!whole)
@@ -373,12 +399,12 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
     }
     const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
-    for (; b < seg_end; b += kPmWarps) {
+    for (int u = warps_first(part0, warp); u < seg_end; u += kPmWarps) {
       cp_async_wait<kStages - 1>();
       __syncwarp();
-      const int next = finder.next(pg, G, chunk_rows, hkv, err);  // the block that will take this stage
+      const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
       const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
-      const int base = (int)(b - i0) * kPatBlock;
+      const int base = (u - item.f0) * kPatBlock;
       constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
       float c[kChains][NT][4];
 #pragma unroll
@@ -485,7 +511,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         s += __shfl_xor_sync(0xffffffffu, s, 16);
         if (g8 == 0) wml[warp * kRows + 8 * nt + 2 * t4 + e] = make_float2(m[nt][e] * scale, s);
       }
-    const int part = 2 * cta + (seg == i0 ? 1 : 0);
+    const int part = 2 * cta + (owns ? 1 : 0);
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += kPass) {
       if (n0 > 0) __syncthreads();  // the buffer is free again
@@ -585,7 +611,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (!by_item && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  RowFinder finder = {rg.at, rg.b0 + warp, rg.b1, -1, 0};
+  RowFinder finder(rg);
   const int fc = lane;
   auto fetch = [&](int slot, int row, const float* from) {
     if (row != -2) {
@@ -600,7 +626,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   };
   // keys and values alternate through the slots; the block after the current
   // one has its keys on the way
-  int now = finder.next(pg, G, chunk_rows, hkv, err), after = finder.next(pg, G, chunk_rows, hkv, err);
+  int now = finder.next(pg, warp, G, chunk_rows, hkv, err), after = finder.next(pg, warp, G, chunk_rows, hkv, err);
   fetch(0, now, k);
   fetch(1, now, v);
   fetch(2, after, k);
@@ -609,19 +635,24 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   const float scale = kPatLog2e * rsqrtf((float)kD);
   const int r8 = lane >> 2, c4 = lane & 3;
   Cursor cur = rg.at;
-  long long b = rg.b0 + warp;  // the warp's next block to compute
-  for (long long seg = rg.b0; seg < rg.b1;) {
-    // the part of one item that lies in the range: blocks seg .. seg_end
+  for (int seg = rg.b0; seg < rg.b1;) {
+    // the part of one item that lies in the range: blocks part0 .. seg_end
     advance(cur, seg, pg, G, chunk_rows, hkv);
-    const int item = (int)(seg - cur.base) / cur.w.blocks;
-    const int h = item / cur.w.chunks, chunk = item - h * cur.w.chunks;
-    const long long i0 = cur.base + (long long)item * cur.w.blocks, i1 = i0 + cur.w.blocks;
-    const long long seg_end = i1 < rg.b1 ? i1 : rg.b1;
+    const Item item = item_at(cur, seg);
+    const int h = item.h, chunk = item.chunk, part0 = max(seg, item.f0), seg_end = min(item.i1, rg.b1);
     const int row0 = chunk * chunk_rows, rows = min(chunk_rows, min(cur.w.fresh, pg.w) * G - row0);
-    const bool whole = seg == i0 && seg_end == i1;
-    if (describes && seg == i0) {
+    const bool owns = part0 == item.f0, whole = owns && seg_end == item.i1;  // has the first block, has them all
+    if (cur.w.blocks == 0 || part0 >= seg_end) {
+      if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
+        if (by_item && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
+        zero_rows<kPmThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
+      }
+      seg = seg_end;
+      continue;
+    }
+    if (describes && owns) {
       const int id = (cur.s * hkv + h) * chunks + chunk;
-      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(i1 - 1), 0};
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(item.i1 - 1), 0};
       if (by_item)
         desc[id] = d;
       else if (!whole)
@@ -643,17 +674,17 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
     }
     const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
-    for (; b < seg_end; b += kPmWarps) {
+    for (int u = warps_first(part0, warp); u < seg_end; u += kPmWarps) {
       cp_async_wait<kPfSlots - 1>();
       __syncwarp();
-      const int then = finder.next(pg, G, chunk_rows, hkv, err);
+      const int then = finder.next(pg, warp, G, chunk_rows, hkv, err);
       const uint32_t ok = __ballot_sync(0xffffffffu, now >= 0) & 0xffffu;
-      const int base = (int)(b - i0) * kPatBlock;
+      const int base = (u - item.f0) * kPatBlock;
       float s[GM][2];
 #pragma unroll
       for (int x = 0; x < GM; ++x) s[x][0] = s[x][1] = 0.f;
       const uint8_t* kt = ring + slot * kPfHalf;
-#pragma unroll
+#pragma unroll 2
       for (int i = 0; i < 8; ++i) {
         const float4 k0 = *reinterpret_cast<const float4*>(kt + pf_off(r8, 4 * i + c4));
         const float4 k1 = *reinterpret_cast<const float4*>(kt + pf_off(r8 + 8, 4 * i + c4));
@@ -703,7 +734,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       cp_async_wait<kPfSlots - 1>();
       __syncwarp();
       const uint8_t* vt = ring + slot * kPfHalf;
-#pragma unroll
+#pragma unroll 1
       for (int r0 = 0; r0 < kPatBlock; r0 += 4) {
         float4 y[4];
 #pragma unroll
@@ -732,7 +763,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       y += __shfl_xor_sync(0xffffffffu, y, 16);
       if (lane == 0) wml[warp * GM + x] = make_float2(m[x] * scale, y);
     }
-    const int part = 2 * cta + (seg == i0 ? 1 : 0);
+    const int part = 2 * cta + (owns ? 1 : 0);
 #pragma unroll
     for (int x0 = 0; x0 < GM; x0 += kPfPass) {
       __syncthreads();  // the probabilities, or the last pass, are done with

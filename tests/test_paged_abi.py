@@ -112,8 +112,9 @@ def test_attention_shapes_refused(st, good, kw, code):
 def test_attention_sizes_refused(st, good):
     """Block and item numbers that would pass 32 bits."""
     size = ctypes.c_size_t()
-    for kw, hkv in ((dict(max_pages=1 << 14, page_rows=1 << 14), 8), (dict(n_pages=1 << 24), 8),
-                    (dict(n_seqs=1 << 24, cu_new=good), 8)):
+    for kw, hkv in ((dict(n_seqs=1 << 10, cu_new=good, max_pages=1 << 12, page_rows=1 << 12, n_pages=100), 8),
+                    (dict(n_pages=1 << 24), 8), (dict(n_seqs=1 << 25, cu_new=good), 8),
+                    (dict(n_seqs=1 << 29, max_pages=1, cu_new=good), 8)):
         sh = _shape(st, hkv=hkv)
         assert st._lib.stlite_paged_workspace_size(sh, _pages(st, good, **kw), size) == st.STLITE_EUNSUPPORTED
         assert st._lib.stlite_paged_attention(sh, _pages(st, good, **kw), good, good, good, good, good, 1 << 24,
