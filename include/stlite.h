@@ -508,7 +508,7 @@ STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const st
  * shape: n_tokens = T; window = the most new tokens of a sequence (cu_new NULL:
  *   of each), 1 .. 16 (further tokens of a sequence are left unwritten);
  *   Hq / Hkv <= 16; n_pages * page_rows * Hkv, and n_seqs * Hkv *
- *   ceil(window * (Hq / Hkv) / 16) * (max_pages * page_rows / 16 + 9), below 2^31.
+ *   ceil(window * (Hq / Hkv) / 16) * (max_pages * page_rows / 16 + 13), below 2^31.
  * q, out [T][Hq][d] (shape->dtype), packed; rows behind cu_new[S] are left
  *   alone.  ws: at least stlite_paged_workspace_size bytes, zero-filled before
  *   its first use (its first word is the error word of

@@ -1128,11 +1128,11 @@ stlite_status check_paged_attention(const stlite_shape* shape, const stlite_page
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
   if (shape->window > kPagedMaxNew || shape->n_q_heads / shape->n_kv_heads > kDecMaxG) return STLITE_EUNSUPPORTED;
-  // the kernels number all items' blocks of 16 rows and eight units more, and
+  // the kernels number all items' blocks of 16 rows and twelve units more, and
   // the pools' rows of heads, in int32
   const long long chunks = (shape->window * (shape->n_q_heads / shape->n_kv_heads) + 15) / 16;
   const long long items = pages->n_seqs * chunks * shape->n_kv_heads;  // below 2^31 * 2^4 * 2^12
-  const long long blocks = (long long)pages->max_pages * pages->page_rows / 16 + 9;
+  const long long blocks = (long long)pages->max_pages * pages->page_rows / 16 + 13;
   if (items > 0x7fffffffLL || items * blocks > 0x7fffffffLL) return STLITE_EUNSUPPORTED;
   if ((long long)pages->n_pages * pages->page_rows * shape->n_kv_heads > 0x7fffffffLL) return STLITE_EUNSUPPORTED;
   return STLITE_OK;

@@ -22,12 +22,20 @@ namespace stl {
 constexpr float kPatLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float pat_weight(float a, float m) { return a == -CUDART_INF_F ? 0.f : exp2f(a - m); }
-__device__ __forceinline__ void from_f(float x, float* y) { *y = x; }
-__device__ __forceinline__ void from_f(float x, __nv_bfloat16* y) { *y = __float2bfloat16_rn(x); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store4(float* p, float x, float y, float z, float w) {
+  *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w);
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float z, float w) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x, y), pack_bf16(z, w));
+}
 
 // ---------------------------------------------------------------- the split
 constexpr int kPatBlock = 16;  // cached rows of a block
-constexpr int kPatItem = 8;    // units of an item's own costs
+constexpr int kPatItem = 12;    // units of an item's own costs
 
 // What a session asks for.
 struct SeqWork {
@@ -148,7 +156,7 @@ struct PartDesc {
   int pad;
 };
 
-constexpr int kPatMaxCtas = 1024;  // two parts to a thread of the merge
+constexpr int kPatMaxCtas = 1024;
 
 __device__ __forceinline__ void cp_async16_fill(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
@@ -218,9 +226,9 @@ struct RowFinder {
 // is g0, that see nothing.
 template <int THREADS, typename T>
 __device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int g0, int G, int row0, int rows) {
-  for (int e = threadIdx.x; e < rows * kD; e += THREADS) {
-    const int r = row0 + e / kD, t = first + r / G;
-    if (t >= 0 && t < n) from_f(0.f, out + ((size_t)t * hq + g0 + r % G) * kD + e % kD);
+  for (int e = threadIdx.x; e < rows * (kD / 4); e += THREADS) {
+    const int r = row0 + e / (kD / 4), t = first + r / G;
+    if (t >= 0 && t < n) store4(out + ((size_t)t * hq + g0 + r % G) * kD + 4 * (e % (kD / 4)), 0.f, 0.f, 0.f, 0.f);
   }
 }
 
@@ -246,7 +254,7 @@ __host__ __device__ constexpr int pm_queries(int nt) { return nt > 2 ? 8 * nt * 
 __host__ __device__ constexpr int pm_pass(int nt) { return nt > 2 ? 2 : nt; }  // groups merged at a time
 __host__ __device__ constexpr int pm_smem(int nt) {
   return pm_ring(nt) + pm_queries(nt) + kPmWarps * 8 * (pm_pass(nt) * kPmPitch * 4 + nt * 8) +
-         (int)sizeof(RangeScratch<kPmThreads>);
+         (int)sizeof(RangeScratch<kPmThreads>) + 8 * nt * 4;
 }
 
 __device__ __forceinline__ void pm_ldsm_x4(uint32_t addr, uint32_t (&a)[4]) {
@@ -274,10 +282,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 // Byte of the 16-byte chunk c of row r of a half stage, swizzled so that eight
 // rows' chunks lie in eight different bank groups.
@@ -294,6 +298,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   float* wo = reinterpret_cast<float*>(sm + pm_ring(NT) + pm_queries(NT));
   float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * 8 * kPass * kPmPitch);
   RangeScratch<kPmThreads>* scratch = reinterpret_cast<RangeScratch<kPmThreads>*>(wml + kPmWarps * kRows);
+  float* inv = reinterpret_cast<float*>(scratch + 1);  // [kRows] 1 / sum
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
   const int G = hq / hkv, cta = blockIdx.x;
   const uint32_t ring = smem_u32(sm) + warp * kStages * 2 * kPmHalf;
@@ -511,7 +516,19 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         s += __shfl_xor_sync(0xffffffffu, s, 16);
         if (g8 == 0) wml[warp * kRows + 8 * nt + 2 * t4 + e] = make_float2(m[nt][e] * scale, s);
       }
+    __syncthreads();
     const int part = 2 * cta + (owns ? 1 : 0);
+    if (tid < rows) {  // each query's maximum and sum over the warps
+      float M = -CUDART_INF_F, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + tid].x);
+#pragma unroll
+      for (int w = 0; w < kPmWarps; ++w) L = fmaf(wml[w * kRows + tid].y, pat_weight(wml[w * kRows + tid].x, M), L);
+      if (whole)
+        inv[tid] = L == 0.f ? 0.f : 1.f / L;
+      else
+        part_ml[part * kRows + tid] = make_float2(M, L);
+    }
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += kPass) {
       if (n0 > 0) __syncthreads();  // the buffer is free again
@@ -519,43 +536,38 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       for (int i = 0; i < kPass; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float* w = wo + (warp * 8 * kPass + 8 * i + 2 * t4 + e) * kPmPitch + g8;
+          const int x = 8 * i + 2 * t4 + e;
+          float M = -CUDART_INF_F;
+#pragma unroll
+          for (int y = 0; y < kPmWarps; ++y) M = fmaxf(M, wml[y * kRows + 8 * n0 + x].x);
+          const float a = pat_weight(m[n0 + i][e] * scale, M);
+          float* w = wo + (warp * 8 * kPass + x) * kPmPitch + g8;
 #pragma unroll
           for (int mt = 0; mt < 8; ++mt) {
-            w[16 * mt] = o[mt][n0 + i][e];
-            w[16 * mt + 8] = o[mt][n0 + i][2 + e];
+            w[16 * mt] = o[mt][n0 + i][e] * a;
+            w[16 * mt + 8] = o[mt][n0 + i][2 + e] * a;
           }
         }
       __syncthreads();
+#pragma unroll 2
       for (int y = warp; y < min(8 * kPass, rows - 8 * n0); y += kPmWarps) {
         const int x = 8 * n0 + y;
-        float M = -CUDART_INF_F, L = 0.f, wt[kPmWarps];
-#pragma unroll
-        for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
-#pragma unroll
-        for (int w = 0; w < kPmWarps; ++w) {
-          const float2 ml = wml[w * kRows + x];
-          wt[w] = pat_weight(ml.x, M);
-          L = fmaf(ml.y, wt[w], L);
-        }
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kPmWarps; ++w) {
           const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 * kPass + y) * kPmPitch + 4 * lane);
-          O.x = fmaf(z.x, wt[w], O.x);
-          O.y = fmaf(z.y, wt[w], O.y);
-          O.z = fmaf(z.z, wt[w], O.z);
-          O.w = fmaf(z.w, wt[w], O.w);
+          O.x += z.x;
+          O.y += z.y;
+          O.z += z.z;
+          O.w += z.w;
         }
-        const int r = row0 + x, t = cur.w.first + r / G;
         if (whole) {
-          const float inv = L == 0.f ? 0.f : 1.f / L;
+          const int r = row0 + x, t = cur.w.first + r / G;
+          const float f = inv[x];
           if (t >= 0 && t < n)
-            *reinterpret_cast<uint2*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
-                make_uint2(pack_bf16(O.x * inv, O.y * inv), pack_bf16(O.z * inv, O.w * inv));
+            store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * f, O.y * f, O.z * f, O.w * f);
         } else {
-          *reinterpret_cast<float4*>(part_o + ((size_t)part * kRows + x) * kD + 4 * lane) = O;
-          if (lane == 0) part_ml[part * kRows + x] = make_float2(M, L);
+          store4(part_o + ((size_t)part * kRows + x) * kD + 4 * lane, O.x, O.y, O.z, O.w);
         }
       }
     }
@@ -793,8 +805,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         if (whole) {
           const float inv = L == 0.f ? 0.f : 1.f / L;
           if (t >= 0 && t < n)
-            *reinterpret_cast<float4*>(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane) =
-                make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+            store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * inv, O.y * inv, O.z * inv, O.w * inv);
         } else {
           *reinterpret_cast<float4*>(part_o + ((size_t)part * GM + x) * kD + 4 * lane) = O;
           if (lane == 0) part_ml[part * GM + x] = make_float2(M, L);
@@ -809,85 +820,97 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 
 // --------------------------------------------------------------------- merge
 // out of the items that several CTAs had parts of.  grid (descriptors, rows):
-// four slices of 128 threads, a dimension each; the parts' weights are formed
-// in shared memory while the first partials are on their way.
+// four warps take a quarter of the parts each, a lane four dimensions; the
+// parts' weights are formed in shared memory while the first partials are on
+// their way.  (Twenty in flight at a time: 76 parts, one session on the whole
+// GPU, in one latency; with 512 threads, a dimension each, the launch of 900
+// such CTAs took 2 us longer.)
+constexpr int kMrgThreads = 128, kMrgSlices = kMrgThreads / 32, kMrgAtOnce = 20;
 template <typename T>
-__global__ void __launch_bounds__(4 * kD) k_paged_merge(const __grid_constant__ PageView pg, T* out, int n, int hq,
-                                                       int hkv, int chunks, int chunk_rows, int part_rows,
-                                                       int by_item, const PartDesc* desc, const float2* part_ml,
-                                                       const float* part_o) {
+__global__ void __launch_bounds__(kMrgThreads) k_paged_merge(const __grid_constant__ PageView pg, T* out, int n,
+                                                             int hq, int hkv, int chunks, int chunk_rows,
+                                                             int part_rows, int by_item, const PartDesc* desc,
+                                                             const float2* part_ml, const float* part_o) {
   __shared__ float wts[kPatMaxCtas];
-  __shared__ float red[2][16];
-  __shared__ float acc[3][kD];
+  __shared__ float red[2][kMrgSlices];
+  __shared__ float4 acc[kMrgSlices - 1][32];
   pdl_trigger();
   pdl_wait();
-  if (by_item) {  // items of sessions with fewer rows have no entry
-    const int s = blockIdx.x / (hkv * chunks);
-    const SeqWork w = seq_work(pg, s, 0, hq / hkv, chunk_rows);
-    if ((int)blockIdx.x % chunks >= w.chunks) return;
-  }
   const PartDesc d = desc[blockIdx.x];
+  const int G = hq / hkv;
+  if (by_item) {  // items of sessions with fewer rows have no entry
+    const int per = hkv * chunks, s = blockIdx.x / per;
+    if ((int)(blockIdx.x - s * per) % chunks >= seq_work(pg, s, 0, G, chunk_rows).chunks) return;
+  }
   if (d.item < 0) return;
-  const int G = hq / hkv, chunk = d.item % chunks, h = d.item / chunks % hkv, s = d.item / chunks / hkv;
-  const SeqWork w = seq_work(pg, s, 0, G, chunk_rows);
-  const int x = blockIdx.y, r = chunk * chunk_rows + x;
-  if (r >= min(w.fresh, pg.w) * G) return;
-  const int tid = threadIdx.x, c = tid & (kD - 1), slice = tid / kD, lane = tid & 31, warp = tid >> 5;
-  const int parts = d.c1 - d.c0 + 1;
+  const int hs = d.item / chunks, chunk = d.item - hs * chunks, s = hs / hkv, h = hs - s * hkv;
+  const int x = blockIdx.y, r = chunk * chunk_rows + x, parts = d.c1 - d.c0 + 1;
+  const int tid = threadIdx.x, slice = tid >> 5, lane = tid & 31;
   auto at = [&](int p) { return (p == 0 ? 2 * d.c0 + 1 : 2 * (d.c0 + p)) * part_rows + x; };
-  constexpr int kAtOnce = 20;  // partials of a slice in flight
-  float y[kAtOnce];
+  float4 y[kMrgAtOnce];
   auto load = [&](int p0) {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int p = p0 + slice + 4 * u;
-      y[u] = p < parts ? part_o[(size_t)at(p) * kD + c] : 0.f;
+    for (int u = 0; u < kMrgAtOnce; ++u) {
+      const int p = p0 + slice + kMrgSlices * u;
+      if (p < parts) y[u] = reinterpret_cast<const float4*>(part_o + (size_t)at(p) * kD)[lane];
     }
   };
   load(0);
-  float2 ml[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int p = tid + 4 * kD * i;
-    ml[i] = p < parts ? part_ml[at(p)] : make_float2(-CUDART_INF_F, 0.f);
-  }
-  float M = fmaxf(ml[0].x, ml[1].x);
+  const float2 none = make_float2(-CUDART_INF_F, 0.f);
+  const float2 ml0 = tid < parts ? part_ml[at(tid)] : none;
+  const SeqWork w = seq_work(pg, s, 0, G, chunk_rows);
+  float M = ml0.x;
+  for (int p = tid + kMrgThreads; p < parts; p += kMrgThreads) M = fmaxf(M, part_ml[at(p)].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  if (lane == 0) red[0][warp] = M;
+  if (lane == 0) red[0][slice] = M;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 16; ++i) M = fmaxf(M, red[0][i]);
+  for (int i = 0; i < kMrgSlices; ++i) M = fmaxf(M, red[0][i]);
   float L = 0.f;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float a = pat_weight(ml[i].x, M);
-    wts[tid + 4 * kD * i] = a;
-    L = fmaf(ml[i].y, a, L);
+  for (int p = tid; p < parts; p += kMrgThreads) {
+    const float2 ml = p == tid ? ml0 : part_ml[at(p)];
+    const float a = pat_weight(ml.x, M);
+    wts[p] = a;
+    L = fmaf(ml.y, a, L);
   }
   L = warp_sum(L);
-  if (lane == 0) red[1][warp] = L;
+  if (lane == 0) red[1][slice] = L;
   __syncthreads();
   L = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) L += red[1][i];
-  float O = 0.f;
+  for (int i = 0; i < kMrgSlices; ++i) L += red[1][i];
+  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int p0 = 0;;) {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int p = p0 + slice + 4 * u;
-      if (p < parts) O = fmaf(y[u], wts[p], O);
+    for (int u = 0; u < kMrgAtOnce; ++u) {
+      const int p = p0 + slice + kMrgSlices * u;
+      if (p < parts) {
+        const float a = wts[p];
+        O.x = fmaf(y[u].x, a, O.x);
+        O.y = fmaf(y[u].y, a, O.y);
+        O.z = fmaf(y[u].z, a, O.z);
+        O.w = fmaf(y[u].w, a, O.w);
+      }
     }
-    p0 += 4 * kAtOnce;
+    p0 += kMrgSlices * kMrgAtOnce;
     if (p0 >= parts) break;
     load(p0);
   }
-  if (slice > 0) acc[slice - 1][c] = O;
+  if (slice > 0) acc[slice - 1][lane] = O;
   __syncthreads();
   if (slice > 0) return;
-  O = (O + acc[0][c]) + (acc[1][c] + acc[2][c]);
+#pragma unroll
+  for (int i = 0; i < kMrgSlices - 1; ++i) {
+    O.x += acc[i][lane].x;
+    O.y += acc[i][lane].y;
+    O.z += acc[i][lane].z;
+    O.w += acc[i][lane].w;
+  }
   const int t = w.first + r / G;
-  if (t >= 0 && t < n) from_f(L == 0.f ? 0.f : O / L, out + ((size_t)t * hq + h * G + r % G) * kD + c);
+  if (r >= min(w.fresh, pg.w) * G || t < 0 || t >= n) return;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * inv, O.y * inv, O.z * inv, O.w * inv);
 }
 
 // -------------------------------------------------------------------- launch
@@ -947,7 +970,7 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
       if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return;
     }
     TimingScope ts("paged_merge", st);
-    e = launch_after(k_paged_merge<T>, dim3(descs, chunk_rows), 4 * kD, 0, st, pages, static_cast<T*>(out), n, hq, hkv,
+    e = launch_after(k_paged_merge<T>, dim3(descs, chunk_rows), kMrgThreads, 0, st, pages, static_cast<T*>(out), n, hq, hkv,
                      chunks, chunk_rows, part_rows, by_item, desc, part_ml, part_o);
   };
   std::integral_constant<int, 1> w1;
