@@ -1095,6 +1095,8 @@ stlite_status token_view(const stlite_shape* s, const stlite_rope* rope, const s
                          TokenView* v) {
   stlite_status st = check_rope(rope);
   if (st != STLITE_OK) return st;
+  // the kernel numbers the tokens' heads in int32
+  if ((long long)s->n_tokens * (s->n_q_heads + 2 * s->n_kv_heads) > 0x7fffffc0LL) return STLITE_EUNSUPPORTED;
   if (!x || !x->q || !x->k || (need_v && !x->v) || !x->pos) return STLITE_EINVAL;
   if (!aligned16(x->q) || !aligned16(x->k) || (need_v && !aligned16(x->v)) || !aligned16(x->q_norm) ||
       !aligned16(x->k_norm) || !aligned4(x->pos))

@@ -1,5 +1,7 @@
 // Paged caches: new tokens' heads normed, rotated and written (packed, or keys
 // and values into pages), and the compaction's rows moved into pages.
+#include <type_traits>
+
 #include "kernels.cuh"
 
 namespace stl {
@@ -13,41 +15,60 @@ namespace stl {
 // upper 32 bits are the angle within the turn to 2^-33 of one, exact for any
 // position, where fp32 angles lose a bit with every doubling of the position.
 //
-// Eight lanes hold a head, each eight pairs (two 16-byte vectors of bf16); a
-// warp holds four heads of one token at a time and walks the token's heads
-// with its sines and cosines in registers.
+// Eight lanes hold a head, each eight pairs (two 16-byte vectors of bf16), so
+// that a warp holds four heads.  A warp takes up to NB such groups of a token's
+// heads, all loaded before anything else, and meanwhile forms the token's 64
+// sines and cosines, two to a lane, exchanged through shared memory.  The bytes
+// moved bound it.
+constexpr int kRotThreads = 128, kRotWarps = kRotThreads / 32;
+constexpr int kRotHeads = 4;   // heads of a group
 
-constexpr int kRotThreads = 256;
-constexpr int kRotHeads = 4;   // heads of a warp at a time
-constexpr int kRotPairs = 8;   // pairs of a lane
-
-__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&f)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight consecutive elements as they are in memory.
+template <typename T>
+struct Vec8;
+template <>
+struct Vec8<__nv_bfloat16> {
+  uint4 u;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = u; }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
   }
-}
-__device__ __forceinline__ void load_vec(const float* p, float (&f)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void store_vec(__nv_bfloat16* p, const float (&f)[8]) {
-  uint32_t w[4];
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    u = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store_vec(float* p, const float (&f)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
+};
+template <>
+struct Vec8<float> {
+  float4 x, y;
+  __device__ __forceinline__ void load(const float* p) {
+    x = reinterpret_cast<const float4*>(p)[0];
+    y = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<float4*>(p)[0] = x;
+    reinterpret_cast<float4*>(p)[1] = y;
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+    f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    x = make_float4(f[0], f[1], f[2], f[3]);
+    y = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
 
 // Slot (page * page_rows + row of the page) of row r of sequence s, or -1.
 __device__ __forceinline__ int page_slot(const PageView& pg, int s, int r) {
@@ -56,39 +77,55 @@ __device__ __forceinline__ int page_slot(const PageView& pg, int s, int r) {
   return page >= 0 && page < pg.n_pages ? page * pg.page_rows + (r - i * pg.page_rows) : -1;
 }
 
-// Sequence of packed new token t, or -1 for padding behind the last one.
+// Sequence of packed new token t, or -1 for padding behind the last one.  A
+// whole warp calls it: 32 entries of cu are compared at a time.
 __device__ __forceinline__ int find_seq(const PageView& pg, int t) {
   if (!pg.cu) {
     const int s = t / pg.w;
     return s < pg.n_seqs ? s : -1;
   }
-  if (t >= pg.cu[pg.n_seqs]) return -1;
-  int lo = 0, hi = pg.n_seqs;  // cu[lo] <= t < cu[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pg.cu[mid] <= t)
-      lo = mid;
-    else
-      hi = mid;
+  const int lane = threadIdx.x & 31, end = pg.cu[pg.n_seqs];
+  int lo = 0, count = pg.n_seqs;  // cu[lo] <= t, and the sequence is one of the `count` from lo on
+  while (count > 1) {
+    const int step = (count + 31) / 32, i = lane * step;
+    const uint32_t le = __ballot_sync(0xffffffffu, i < count && pg.cu[lo + i] <= t);
+    const int k = le ? 31 - __clz(le) : 0;
+    lo += k * step;
+    count = min(step, count - k * step);
   }
-  return lo;
+  return t < end ? lo : -1;
 }
 
 // One warp per unit: segment `u % segs` of the head groups of token u / segs.
-template <typename T, bool IL, bool PAGED>
+template <typename T, int NB, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ TokenView x,
                                                         const __grid_constant__ RopeView rope,
                                                         const __grid_constant__ PageView pg, T* q_out, T* k_out,
                                                         T* v_out, int groups, int segs) {
   __shared__ uint64_t turn[kD / 2];
+  // [warp][four of a lane's eight pairs][lane][pair], so that eight lanes' vectors are adjacent
+  __shared__ float4 cs[kRotWarps][2][8], sn[kRotWarps][2][8];
   if (threadIdx.x < kD / 2) turn[threadIdx.x] = rope.turn[threadIdx.x];
   __syncthreads();
   pdl_trigger();
   pdl_wait();
-  const long long u = (long long)blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5);
-  const int t = (int)(u / segs), seg = (int)(u % segs);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, c = lane & 7;
+  const int u = blockIdx.x * kRotWarps + warp, t = u / segs, seg = u - t * segs;
   if (t >= x.n) return;
-  const int lane = threadIdx.x & 31, sub = lane >> 3, c = lane & 7;
+  const int total = x.hq + (PAGED ? 2 : 1) * x.hkv;
+  const int g0 = groups * seg / segs, g1 = groups * (seg + 1) / segs;
+  const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
+  Vec8<T> va[NB], vb[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int head = kRotHeads * (g0 + i) + sub;
+    if (g0 + i >= g1 || head >= total) continue;
+    const T* src = static_cast<const T*>(x.q) + t * x.q_stride + head * kD;
+    if (head >= x.hq) src = static_cast<const T*>(x.k) + t * x.k_stride + (head - x.hq) * kD;
+    if (PAGED && head >= x.hq + x.hkv) src = static_cast<const T*>(x.v) + t * x.v_stride + (head - x.hq - x.hkv) * kD;
+    va[i].load(src + off0);
+    vb[i].load(src + off1);
+  }
   int slot = -1;
   if (PAGED) {
     const int s = find_seq(pg, t);
@@ -96,78 +133,75 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
     const int next = pg.cu ? pg.cu[s + 1] : (s + 1) * pg.w;
     slot = page_slot(pg, s, pg.len[s] - (next - t));
   }
-  float cs[kRotPairs], sn[kRotPairs];
-  {
-    const bool axes = rope.end0 < kD / 2;
-    const int p0 = x.pos[t], p1 = axes ? x.pos[x.n + t] : 0, p2 = axes ? x.pos[2 * (size_t)x.n + t] : 0;
 #pragma unroll
-    for (int i = 0; i < kRotPairs; ++i) {
-      const int pair = kRotPairs * c + i;
-      const int p = pair < rope.end0 ? p0 : (pair < rope.end1 ? p1 : p2);
-      const uint64_t a = (uint64_t)(int64_t)p * turn[pair];
-      sincospif((float)(int32_t)(a >> 32) * 0x1p-31f, &sn[i], &cs[i]);
-    }
+  for (int e = 0; e < 2; ++e) {
+    const int pair = lane + 32 * e, axis = pair < rope.end0 ? 0 : (pair < rope.end1 ? 1 : 2);
+    const uint64_t angle = (uint64_t)(int64_t)x.pos[(size_t)axis * x.n + t] * turn[pair];
+    const int at = (pair & 4) * 8 + (pair >> 3) * 4 + (pair & 3);
+    sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, reinterpret_cast<float*>(sn[warp]) + at,
+              reinterpret_cast<float*>(cs[warp]) + at);
   }
-  const int total = x.hq + (PAGED ? 2 : 1) * x.hkv;
-  const int g0 = (int)((long long)groups * seg / segs), g1 = (int)((long long)groups * (seg + 1) / segs);
-  const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
-  for (int g = g0; g < g1; ++g) {
-    const int head = kRotHeads * g + sub;
-    const bool is_q = head < x.hq, is_k = !is_q && head < x.hq + x.hkv;
-    const T *src = nullptr, *norm = nullptr;
-    T* dst = nullptr;
-    if (is_q) {
-      src = static_cast<const T*>(x.q) + t * x.q_stride + head * kD;
-      norm = static_cast<const T*>(x.q_norm);
-      dst = q_out + ((size_t)t * x.hq + head) * kD;
-    } else if (head < total) {
-      const int h = head - x.hq - (is_k ? 0 : x.hkv);
-      src = (is_k ? static_cast<const T*>(x.k) + t * x.k_stride : static_cast<const T*>(x.v) + t * x.v_stride) + h * kD;
-      norm = is_k ? static_cast<const T*>(x.k_norm) : nullptr;
-      if (!PAGED)
-        dst = k_out + ((size_t)t * x.hkv + h) * kD;
-      else if (slot >= 0)
-        dst = (is_k ? k_out : v_out) + ((size_t)slot * x.hkv + h) * kD;
-    }
-    float a[8], b[8];  // the lane's elements: pair i is (a[i], b[i]), or interleaved within a, then b
-    if (src) {
-      load_vec(src + off0, a);
-      load_vec(src + off1, b);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int head = kRotHeads * (g0 + i) + sub;
+    const bool live = g0 + i < g1 && head < total, is_q = head < x.hq, is_v = PAGED && head >= x.hq + x.hkv;
+    if (g0 + i >= g1) break;  // the same for the whole warp
+    float a[8], b[8];  // the lane's elements: pair j is (a[j], b[j]), or interleaved within a, then b
+    if (live) {
+      va[i].get(a);
+      vb[i].get(b);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
+      for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.f;
     }
     if (x.q_norm || x.k_norm) {
       float ss = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+      for (int j = 0; j < 8; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      const T* norm = static_cast<const T*>(is_v ? nullptr : (is_q ? x.q_norm : x.k_norm));
       if (norm) {
         const float r = rsqrtf(ss * (1.f / kD) + x.eps);
+        Vec8<T> n0, n1;
         float wa[8], wb[8];
-        load_vec(norm + off0, wa);
-        load_vec(norm + off1, wb);
+        n0.load(norm + off0);
+        n1.load(norm + off1);
+        n0.get(wa);
+        n1.get(wb);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          a[i] = a[i] * r * wa[i];
-          b[i] = b[i] * r * wb[i];
+        for (int j = 0; j < 8; ++j) {
+          a[j] = a[j] * r * wa[j];
+          b[j] = b[j] * r * wb[j];
         }
       }
     }
-    if (is_q || is_k) {
+    if (!is_v) {
 #pragma unroll
-      for (int i = 0; i < kRotPairs; ++i) {
-        float& p = IL ? (i < 4 ? a[2 * i] : b[2 * i - 8]) : a[i];
-        float& q = IL ? (i < 4 ? a[2 * i + 1] : b[2 * i - 7]) : b[i];
-        const float y0 = p * cs[i] - q * sn[i], y1 = q * cs[i] + p * sn[i];
-        p = y0;
-        q = y1;
+      for (int g = 0; g < 2; ++g) {
+        const float4 c4 = cs[warp][g][c], s4 = sn[warp][g][c];
+        const float cv[4] = {c4.x, c4.y, c4.z, c4.w}, sv[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float& p = IL ? (g == 0 ? a[2 * j] : b[2 * j]) : a[4 * g + j];
+          float& q = IL ? (g == 0 ? a[2 * j + 1] : b[2 * j + 1]) : b[4 * g + j];
+          const float y0 = p * cv[j] - q * sv[j], y1 = q * cv[j] + p * sv[j];
+          p = y0;
+          q = y1;
+        }
       }
+      va[i].set(a);
+      vb[i].set(b);
     }
-    if (dst) {
-      store_vec(dst + off0, a);
-      store_vec(dst + off1, b);
+    T* dst = q_out + ((size_t)t * x.hq + head) * kD;
+    if (!is_q) {
+      const int h = head - x.hq - (is_v ? x.hkv : 0);
+      dst = (is_v ? v_out : k_out) + ((size_t)(PAGED ? slot : t) * x.hkv + h) * kD;
+    }
+    if (live && (is_q || !PAGED || slot >= 0)) {
+      va[i].store(dst + off0);
+      vb[i].store(dst + off1);
     }
   }
 }
@@ -175,25 +209,40 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
 cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, const PageView* pages, void* q_out,
                           void* k_out, void* v_out, cudaStream_t st) {
   const int groups = (x.hq + (pages ? 2 : 1) * x.hkv + kRotHeads - 1) / kRotHeads;
-  // enough warps for the GPU's SMs where there are few tokens
-  long long segs = (152 * 16 + x.n - 1) / x.n;
+  // groups of a warp: all of a token's that fit its registers, fewer where
+  // there are few tokens for the GPU's SMs
+  const int most = dt == kBF16 ? 8 : 4;
+  long long segs = (152 * 32 + x.n - 1) / x.n;
+  if (segs < (groups + most - 1) / most) segs = (groups + most - 1) / most;
   if (segs > groups) segs = groups;
-  const long long warps = (long long)x.n * segs, per = kRotThreads / 32;
-  const dim3 grid((unsigned)((warps + per - 1) / per));
+  const int each = (int)((groups + segs - 1) / segs);
+  const dim3 grid((unsigned)((x.n * segs + kRotWarps - 1) / kRotWarps));
   const PageView pg = pages ? *pages : PageView{};
   TimingScope ts(pages ? "paged_append" : "rotate_qk", st);
   cudaError_t e = cudaSuccess;
-  auto run = [&](auto zero) {
+  auto run = [&](auto zero, auto nb) {
     typedef decltype(zero) T;
+    constexpr int NB = decltype(nb)::value;
     T *qo = static_cast<T*>(q_out), *ko = static_cast<T*>(k_out), *vo = static_cast<T*>(v_out);
-    auto kern = rope.interleaved ? (pages ? k_rotate<T, true, true> : k_rotate<T, true, false>)
-                                 : (pages ? k_rotate<T, false, true> : k_rotate<T, false, false>);
+    auto kern = rope.interleaved ? (pages ? k_rotate<T, NB, true, true> : k_rotate<T, NB, true, false>)
+                                 : (pages ? k_rotate<T, NB, false, true> : k_rotate<T, NB, false, false>);
     e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, groups, (int)segs);
   };
+  auto pick = [&](auto zero) {
+    typedef decltype(zero) T;
+    if (each <= 1)
+      run(zero, std::integral_constant<int, 1>());
+    else if (each <= 2)
+      run(zero, std::integral_constant<int, 2>());
+    else if (each <= 4)
+      run(zero, std::integral_constant<int, 4>());
+    else if constexpr (sizeof(T) == 2)
+      run(zero, std::integral_constant<int, 8>());
+  };
   if (dt == kBF16)
-    run(__nv_bfloat16());
+    pick(__nv_bfloat16());
   else
-    run(float());
+    pick(float());
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
