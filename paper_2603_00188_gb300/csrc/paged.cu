@@ -77,23 +77,28 @@ __device__ __forceinline__ int page_slot(const PageView& pg, int s, int r) {
   return page >= 0 && page < pg.n_pages ? page * pg.page_rows + (r - i * pg.page_rows) : -1;
 }
 
-// Sequence of packed new token t, or -1 for padding behind the last one.  A
-// whole warp calls it: 32 entries of cu are compared at a time.
-__device__ __forceinline__ int find_seq(const PageView& pg, int t) {
+// The slot of packed new token t, which is not padding, or -1.  A whole warp
+// calls it; 32 sequences are compared at a time, so that up to 32 take two
+// memory latencies: their cu and len, then the table.
+__device__ __forceinline__ int token_slot(const PageView& pg, int t) {
   if (!pg.cu) {
     const int s = t / pg.w;
-    return s < pg.n_seqs ? s : -1;
+    return s < pg.n_seqs ? page_slot(pg, s, pg.len[s] - ((s + 1) * pg.w - t)) : -1;
   }
-  const int lane = threadIdx.x & 31, end = pg.cu[pg.n_seqs];
+  const int lane = threadIdx.x & 31;
   int lo = 0, count = pg.n_seqs;  // cu[lo] <= t, and the sequence is one of the `count` from lo on
-  while (count > 1) {
+  while (count > 32) {
     const int step = (count + 31) / 32, i = lane * step;
     const uint32_t le = __ballot_sync(0xffffffffu, i < count && pg.cu[lo + i] <= t);
     const int k = le ? 31 - __clz(le) : 0;
     lo += k * step;
     count = min(step, count - k * step);
   }
-  return t < end ? lo : -1;
+  const int mine = lo + min(lane, count - 1), first = pg.cu[mine], next = pg.cu[mine + 1], len = pg.len[mine];
+  const uint32_t le = __ballot_sync(0xffffffffu, lane < count && first <= t);
+  const int k = le ? 31 - __clz(le) : 0;
+  const int row = __shfl_sync(0xffffffffu, len, k) - (__shfl_sync(0xffffffffu, next, k) - t);
+  return page_slot(pg, lo + k, row);
 }
 
 // One warp per unit: segment `u % segs` of the head groups of token u / segs.
@@ -115,6 +120,7 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
   const int total = x.hq + (PAGED ? 2 : 1) * x.hkv;
   const int g0 = groups * seg / segs, g1 = groups * (seg + 1) / segs;
   const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
+  const int end = PAGED && pg.cu ? pg.cu[pg.n_seqs] : x.n;
   Vec8<T> va[NB], vb[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
@@ -126,13 +132,6 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
     va[i].load(src + off0);
     vb[i].load(src + off1);
   }
-  int slot = -1;
-  if (PAGED) {
-    const int s = find_seq(pg, t);
-    if (s < 0) return;
-    const int next = pg.cu ? pg.cu[s + 1] : (s + 1) * pg.w;
-    slot = page_slot(pg, s, pg.len[s] - (next - t));
-  }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int pair = lane + 32 * e, axis = pair < rope.end0 ? 0 : (pair < rope.end1 ? 1 : 2);
@@ -141,6 +140,9 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
     sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, reinterpret_cast<float*>(sn[warp]) + at,
               reinterpret_cast<float*>(cs[warp]) + at);
   }
+  if (t >= end) return;  // padding behind the last sequence
+  int slot = -1;
+  if (PAGED && kRotHeads * g1 > x.hq) slot = token_slot(pg, t);  // keys or values among the segment's heads
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
@@ -211,7 +213,7 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
   const int groups = (x.hq + (pages ? 2 : 1) * x.hkv + kRotHeads - 1) / kRotHeads;
   // groups of a warp: all of a token's that fit its registers, fewer where
   // there are few tokens for the GPU's SMs
-  const int most = dt == kBF16 ? 8 : 4;
+  constexpr int most = 3;
   long long segs = (152 * 32 + x.n - 1) / x.n;
   if (segs < (groups + most - 1) / most) segs = (groups + most - 1) / most;
   if (segs > groups) segs = groups;
@@ -229,15 +231,12 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
     e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, groups, (int)segs);
   };
   auto pick = [&](auto zero) {
-    typedef decltype(zero) T;
     if (each <= 1)
       run(zero, std::integral_constant<int, 1>());
     else if (each <= 2)
       run(zero, std::integral_constant<int, 2>());
-    else if (each <= 4)
-      run(zero, std::integral_constant<int, 4>());
-    else if constexpr (sizeof(T) == 2)
-      run(zero, std::integral_constant<int, 8>());
+    else
+      run(zero, std::integral_constant<int, most>());
   };
   if (dt == kBF16)
     pick(__nv_bfloat16());

@@ -147,6 +147,31 @@ def test_append_matches(st, page, dtype, hq, hkv, norm, fused):
     assert torch.equal(vp.cpu(), want_v)
 
 
+@pytest.mark.parametrize("seqs", [32, 33, 200, 1100])
+def test_append_finds_every_sequence(st, seqs):
+    """Each token's sequence among many, several of them without new tokens, the last ones too."""
+    r = random.Random(seqs)
+    new = [r.choice([0, 0, 1, 2, 5]) for _ in range(seqs - 2)] + [0, 0]
+    rows = [m + r.randint(0, 20) for m in new]
+    cu = [sum(new[:i]) for i in range(seqs + 1)]
+    g = _gen(seqs)
+    q, k, v = _randn(g, cu[-1] + 2, 1, 128), _randn(g, cu[-1] + 2, 1, 128), _randn(g, cu[-1] + 2, 1, 128)
+    table, pages = _table(rows, 4, seqs)
+    kp, vp = (torch.full((pages, 4, 1, 128), 7, dtype=BF, device="cuda") for _ in range(2))
+    pg = st.make_pages(pages, 4, table.cuda(), _ints(rows), _ints(cu))
+    pos = torch.arange(cu[-1] + 2, dtype=I32, device="cuda")
+    qo = torch.full_like(q, 5)
+    st.stlite_paged_append(q, k, v, pos, st.make_rope(), pg, qo, kp, vp)
+    wq, wk = st.rotate_qk(q, k, pos, st.make_rope())
+    want_k, want_v = torch.full_like(kp, 7), torch.full_like(vp, 7)
+    at = [(int(table[s, (rows[s] - m + i) // 4]), (rows[s] - m + i) % 4, cu[s] + i)
+          for s, m in enumerate(new) for i in range(m)]
+    p, o, t = (torch.tensor(x, device="cuda") for x in zip(*at))
+    want_k[p, o], want_v[p, o] = wk[t], v[t]
+    assert torch.equal(kp, want_k) and torch.equal(vp, want_v)
+    assert torch.equal(qo[:cu[-1]], wq[:cu[-1]]) and (qo[cu[-1]:] == 5).all()
+
+
 def test_append_one_each_and_in_place(st):
     """Without cu_new: `max_new` tokens of each sequence, q rotated in place."""
     g = _gen(4)
