@@ -476,8 +476,8 @@ typedef struct {
  *   out = y rotated by its token's position   (see stlite_rope)
  * in fp32, rounded once.  q_out [T][Hq][d], k_out [T][Hkv][d], packed.
  * q_out may be x->q, and k_out x->k, where those are packed; other overlap of
- * inputs and outputs is not allowed.  shape->window is not used (any valid
- * value). */
+ * inputs and outputs is not allowed.  shape->window is not used (any value
+ * >= 1). */
 STLITE_API stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
                                           void* q_out, void* k_out, void* stream);
 
@@ -490,7 +490,7 @@ STLITE_API stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlit
  * not written (its q_out is).  Rows that two sequences share are not to be
  * written by both.  q_out may be x->q where that is packed.
  * shape: n_tokens = T; window = tokens of each sequence where cu_new is NULL
- *   (otherwise not used). */
+ *   (any number >= 1; otherwise not used). */
 STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope,
                                              const stlite_tokens* x, const stlite_pages* pages, void* q_out,
                                              void* k_pages, void* v_pages, void* stream);
@@ -526,7 +526,8 @@ STLITE_API stlite_status stlite_paged_workspace_size(const stlite_shape* shape, 
  * `seq` becomes k[idx[h][r]][h], r < budget.  layers: HOST array; each
  * entry's k and v are the layer's cache [N][Hkv][d] (v may be page-locked host
  * memory), k_out and v_out its page POOLS, idx_out (read) its device int32
- * [Hkv][budget]; q is not used.  A row whose index lies outside [0, N), or
+ * [Hkv][budget], which need not be more than 4-byte aligned (a layer's part of
+ * all layers' indices); q is not used.  A row whose index lies outside [0, N), or
  * whose page is not one, is left unwritten.  pages->len is the caller's to
  * set. */
 STLITE_API stlite_status stlite_compact_paged(const stlite_shape* shape, int32_t budget, const stlite_pages* pages,

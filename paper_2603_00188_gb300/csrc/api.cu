@@ -1025,6 +1025,15 @@ stlite_status check_pages(const stlite_pages* pg, bool need_len) {
   return STLITE_OK;
 }
 
+// The shape of calls whose window is a number of tokens, not of an observation
+// window's queries: any number.
+stlite_status check_token_shape(const stlite_shape* shape) {
+  if (!shape || shape->window < 1) return STLITE_EINVAL;
+  stlite_shape s = *shape;
+  s.window = 1;
+  return check_shape(&s);
+}
+
 // Without cu_new every sequence has w new tokens.
 stlite_status check_new(const stlite_shape* s, const stlite_pages* pg) {
   if (!pg->cu_new && (long long)pg->n_seqs * s->window != s->n_tokens) return STLITE_EINVAL;
@@ -1155,7 +1164,7 @@ stlite_status stlite_rope_init(double base, stlite_rope* rope) {
 
 stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
                                void* q_out, void* k_out, void* stream) {
-  stlite_status s = check_shape(shape);
+  stlite_status s = check_token_shape(shape);
   if (s != STLITE_OK) return s;
   TokenView v;
   if ((s = token_view(shape, rope, x, false, &v)) != STLITE_OK) return s;
@@ -1169,7 +1178,7 @@ stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rop
 stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
                                   const stlite_pages* pages, void* q_out, void* k_pages, void* v_pages,
                                   void* stream) {
-  stlite_status s = check_shape(shape);
+  stlite_status s = check_token_shape(shape);
   if (s != STLITE_OK) return s;
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
@@ -1217,7 +1226,7 @@ stlite_status stlite_compact_paged(const stlite_shape* shape, int32_t budget, co
   for (int l = 0; l < n_layers; ++l) {
     const stlite_layer_io& x = layers[l];
     if (!x.k || !x.v || !x.k_out || !x.v_out || !x.idx_out) return STLITE_EINVAL;
-    if (!aligned16(x.k) || !aligned16(x.v) || !aligned16(x.k_out) || !aligned16(x.v_out) || !aligned16(x.idx_out))
+    if (!aligned16(x.k) || !aligned16(x.v) || !aligned16(x.k_out) || !aligned16(x.v_out) || !aligned4(x.idx_out))
       return STLITE_EINVAL;
   }
   const PageView pg = page_view(pages, 1);

@@ -77,7 +77,7 @@ def test_lengths_optional_for_compaction_only(st, good):
                                        (10, 0, 0, io), (10, 0, 1, None)):
         assert st._lib.stlite_compact_paged(_shape(st, n=100), budget, pg, seq, layers, table, None) == st.STLITE_EINVAL
     for field in ("k", "v", "k_out", "v_out", "idx_out"):
-        for bad in (None, good + 8):
+        for bad in (None, good + (2 if field == "idx_out" else 8)):
             io = (st.LayerIO * 1)(st.LayerIO(*[good] * 6))
             setattr(io[0], field, bad)
             assert st._lib.stlite_compact_paged(_shape(st, n=100), 10, pg, 0, 1, io, None) == st.STLITE_EINVAL
@@ -166,7 +166,11 @@ def test_rotation_refused(st, good):
     both(st.make_rope(), _tokens(st, good), inv, q_out=good + 8)
     both(st.make_rope(), _tokens(st, good), inv, k_out=None)
     both(st.make_rope(), _tokens(st, good), inv, shape=_shape(st, n=0))
+    both(st.make_rope(), _tokens(st, good), inv, shape=_shape(st, w=0))
     both(st.make_rope(), _tokens(st, good), st.STLITE_EUNSUPPORTED, shape=_shape(st, d=64))
+    # more heads of tokens than fit an int32
+    both(st.make_rope(), _tokens(st, good), st.STLITE_EUNSUPPORTED, shape=_shape(st, n=200000, hq=40000, hkv=2000,
+                                                                                  w=50000))
     # an output that is its input has the output's packing
     both(st.make_rope(), _tokens(st, good, q_stride=8 * 128 + 8), inv, q_out=good)
     assert lib.stlite_rotate_qk(sh, st.make_rope(), _tokens(st, good, k=good + 4096, k_stride=264), good, good + 4096,
@@ -219,6 +223,13 @@ def test_binding_checks_tensors(st):
         with pytest.raises(ValueError):
             st.stlite_paged_append(**a)
 
+    append()  # everything fits, but the tensors are on the host
+    with pytest.raises(ValueError):
+        st.stlite_rotate_qk(x, kv, pos, rope, x.clone(), kv.clone())
+    with pytest.raises(ValueError):
+        st.stlite_paged_attention(x, pool, pool, pages, x.clone(), ln)
+    with pytest.raises(ValueError):
+        st.stlite_compact_paged([(kv, kv, pool, pool, torch.zeros((2, 2), dtype=i32))], 2, pages, 0)
     append(k_pages=pool[:5])
     append(v_pages=pool.float())
     append(k_pages=pool.transpose(0, 1).contiguous().transpose(0, 1))

@@ -190,6 +190,25 @@ def test_append_one_each_and_in_place(st):
     assert int(kp.ne(0).any(-1).any(-1).sum()) == 6
 
 
+def test_append_many_each(st):
+    """A long chunk of every prompt without cu_new, more tokens each than an observation window may have."""
+    g = _gen(6)
+    rows, w = [700, 601, 999], 600
+    table, pages = _table(rows, 24, 2)
+    q, k, v = _randn(g, 3 * w, 3, 128), _randn(g, 3 * w, 1, 128), _randn(g, 3 * w, 1, 128)
+    pos = torch.arange(3 * w, dtype=I32, device="cuda")
+    kp, vp = (torch.zeros((pages, 24, 1, 128), dtype=BF, device="cuda") for _ in range(2))
+    qo = torch.empty_like(q)
+    pg = st.make_pages(pages, 24, table.cuda(), _ints(rows), max_new=w)
+    st.stlite_paged_append(q, k, v, pos, st.make_rope(), pg, qo, kp, vp)
+    wq, wk = st.rotate_qk(q, k, pos, st.make_rope())
+    assert torch.equal(qo, wq)
+    for s, n in enumerate(rows):
+        assert torch.equal(ref.rows_of(kp, table[s], n)[-w:], wk[s * w:s * w + w])
+        assert torch.equal(ref.rows_of(vp, table[s], n)[-w:], v[s * w:s * w + w])
+        assert not ref.rows_of(vp, table[s], n)[:-w].any()
+
+
 def test_append_leaves_bad_rows(st):
     """Rows outside a sequence's pages, and pages outside the pool, are not written; q is rotated all the same."""
     g = _gen(5)
@@ -209,17 +228,19 @@ def test_append_leaves_bad_rows(st):
 
 @pytest.mark.parametrize("n,budget,hkv,page,dtype,layers", [(50, 1, 1, 16, BF, 1), (300, 77, 4, 16, BF, 3),
                                                             (300, 300, 3, 7, F32, 2), (2000, 513, 2, 64, BF, 34),
-                                                            (129, 64, 8, 1, F32, 1)])
+                                                            (129, 64, 8, 1, F32, 1), (90, 33, 1, 16, BF, 5)])
 def test_compact_paged_matches_dense(st, n, budget, hkv, page, dtype, layers):
     g = _gen(n)
     rows = [20, budget, 5]
     table, pages = _table(rows, page, 2)
     io, dense = [], []
-    for _ in range(layers):
+    all_idx = torch.empty((layers, hkv, budget), dtype=I32, device="cuda")  # a layer's part on any 4-byte boundary
+    for l in range(layers):
         k, v = _randn(g, n, hkv, 128, dtype=dtype), _randn(g, n, hkv, 128, dtype=dtype)
         idx = torch.stack([torch.randperm(n, generator=g)[:budget].sort().values for _ in range(hkv)]).to(I32).cuda()
         kp, vp = (torch.full((pages, page, hkv, 128), 2, dtype=dtype, device="cuda") for _ in range(2))
-        io.append((k, v, kp, vp, idx))
+        all_idx[l] = idx
+        io.append((k, v, kp, vp, all_idx[l]))
         ko, vo = torch.empty((budget, hkv, 128), dtype=dtype, device="cuda"), torch.empty((budget, hkv, 128), dtype=dtype, device="cuda")
         q = torch.zeros((1, hkv, 128), dtype=dtype, device="cuda")
         st.stlite_compact(q, k, v, budget, idx, ko, vo)
