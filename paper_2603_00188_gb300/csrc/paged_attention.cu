@@ -578,28 +578,59 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 }
 
 // ---------------------------------------------------------------------- fp32
-// The same split and rings with fp32 products (fmaf).  A block's keys and its
-// values are a slot each, three to a warp.  Scores: lane (r, c), r = 0 .. 7,
-// c = 0 .. 3, holds rows r and r + 8 of the keys at every fourth 16-byte chunk
-// from c on, so that a chunk of a query read from shared memory serves two
-// rows; four lanes' sums are added by shuffles.  Values: a lane owns four
-// dimensions, the probabilities come back through shared memory.  GM: queries
-// of a chunk.  7 queries take 33 % of the FMA pipe at the rate of HBM.
+// The same split and rings with fp32 products, two to an instruction
+// (fma.rn.f32x2).  A block's keys and its values are a slot each, three to a
+// warp.  Shared-memory reads bound the products, so a lane holds four rows of
+// the keys against each chunk of a query that it reads:
+//   scores: lane (r, c), r = 0 .. 3, c = 0 .. 7, sums rows r, r + 4, r + 8 and
+//     r + 12 over every eighth 16-byte chunk from c on; the eight lanes' sums of
+//     eight queries are added in 28 shuffles that leave lane c with query c's;
+//   softmax: each lane its own query;
+//   values: a lane owns four dimensions of every query, the probabilities come
+//     back through shared memory.
+// GM: queries of a chunk (4, or one or two times eight).
 constexpr int kPfSlots = 3;
 constexpr int kPfHalf = kPatBlock * kD * 4;  // keys, or values, of a block
 constexpr int kPfPass = 4;                   // queries merged at a time
 __host__ __device__ constexpr int pf_ring() { return kPmWarps * kPfSlots * kPfHalf; }
-// the probabilities of a block, and, once an item has ended, the merge buffer
+// a warp's floats: probabilities of a block [gm][16] and rescaling factors [gm]
+__host__ __device__ constexpr int pf_probs(int gm) { return gm * (kPatBlock + 1); }
+// these, and, once an item has ended, the merge buffer
 __host__ __device__ constexpr int pf_shared(int gm) {
-  return gm * kPatBlock * 4 > kPfPass * kPmPitch * 4 ? kPmWarps * gm * kPatBlock * 4 : kPmWarps * kPfPass * kPmPitch * 4;
+  return kPmWarps * 4 * (pf_probs(gm) > kPfPass * kPmPitch ? pf_probs(gm) : kPfPass * kPmPitch);
 }
 __host__ __device__ constexpr int pf_smem(int gm) {
   return pf_ring() + gm * kD * 4 + pf_shared(gm) + kPmWarps * gm * 8 + (int)sizeof(RangeScratch<kPmThreads>);
 }
 
-// Byte of the 16-byte chunk c of row r: the two rows that eight lanes read at
-// a time in the scores lie in different halves of the banks.
-__device__ __forceinline__ uint32_t pf_off(int r, int c) { return (uint32_t)(r * 512 + ((c ^ ((r & 1) << 2)) << 4)); }
+// The sums over eight neighbouring lanes of s[row][query]: lane c of them is
+// left with query c % Q's, rows 0 .. 3 for Q = 8, rows 2 (c / 4) + 0, 1 for Q = 4.
+__device__ __forceinline__ void lane_sums(const float (&s)[4][8], int c, float (&out)[4]) {
+  float a[4][4], b[4][2];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      a[j][x] = (c & 4 ? s[j][x + 4] : s[j][x]) + __shfl_xor_sync(0xffffffffu, c & 4 ? s[j][x] : s[j][x + 4], 4);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      b[j][x] = (c & 2 ? a[j][x + 2] : a[j][x]) + __shfl_xor_sync(0xffffffffu, c & 2 ? a[j][x] : a[j][x + 2], 2);
+    out[j] = (c & 1 ? b[j][1] : b[j][0]) + __shfl_xor_sync(0xffffffffu, c & 1 ? b[j][0] : b[j][1], 1);
+  }
+}
+__device__ __forceinline__ void lane_sums(const float (&s)[4][4], int c, float (&out)[2]) {
+  float a[2][4], b[2][2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      a[j][x] = (c & 4 ? s[j + 2][x] : s[j][x]) + __shfl_xor_sync(0xffffffffu, c & 4 ? s[j][x] : s[j + 2][x], 4);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      b[j][x] = (c & 2 ? a[j][x + 2] : a[j][x]) + __shfl_xor_sync(0xffffffffu, c & 2 ? a[j][x] : a[j][x + 2], 2);
+    out[j] = (c & 1 ? b[j][1] : b[j][0]) + __shfl_xor_sync(0xffffffffu, c & 1 ? b[j][0] : b[j][1], 1);
+  }
+}
 
 template <int GM>
 __global__ void __launch_bounds__(kPmThreads, kPmCtas)
@@ -615,7 +646,8 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = hq / hkv, cta = blockIdx.x;
   uint8_t* ring = sm + warp * kPfSlots * kPfHalf;
-  float* ps = shared + warp * GM * kPatBlock;  // [GM][16]
+  float* ps = shared + warp * pf_probs(GM);  // [GM][16]
+  float* rescale = ps + GM * kPatBlock;      // [GM]
   pdl_trigger();
   pdl_wait();
   const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, err, scratch);
@@ -624,14 +656,13 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (cta >= rg.ctas) return;
 
   RowFinder finder(rg);
-  const int fc = lane;
   auto fetch = [&](int slot, int row, const float* from) {
     if (row != -2) {
       const uint32_t dst = smem_u32(ring) + slot * kPfHalf;
 #pragma unroll
       for (int r = 0; r < kPatBlock; ++r) {
         const int x = __shfl_sync(0xffffffffu, row, r);
-        cp_async16_fill(dst + pf_off(r, fc), from + (size_t)max(x, 0) * kD + 4 * fc, x >= 0);
+        cp_async16_fill(dst + 512 * r + 16 * lane, from + (size_t)max(x, 0) * kD + 4 * lane, x >= 0);
       }
     }
     cp_async_commit();
@@ -645,7 +676,9 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   int slot = 0;
 
   const float scale = kPatLog2e * rsqrtf((float)kD);
-  const int r8 = lane >> 2, c4 = lane & 3;
+  constexpr int Q = GM < 8 ? GM : 8, kSets = GM / Q, kLaneRows = Q == 8 ? 4 : 2;
+  const int r4 = lane >> 3, c8 = lane & 7, mine = c8 & (Q - 1);  // the lane's query of each set
+  const int lane_row = r4 + (Q == 8 ? 0 : 8 * (c8 >> 2));        // its rows: lane_row, + 4, ...
   Cursor cur = rg.at;
   for (int seg = rg.b0; seg < rg.b1;) {
     // the part of one item that lies in the range: blocks part0 .. seg_end
@@ -678,13 +711,14 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       reinterpret_cast<float4*>(qs)[e] = y;
     }
     __syncthreads();
-    float m[GM], l[GM], o[GM][4];  // l: the lane's rows only
+    float m[kSets], l[kSets], o[GM][4];  // raw maximum and the lane's part of the sum of its queries
 #pragma unroll
-    for (int x = 0; x < GM; ++x) {
-      m[x] = -CUDART_INF_F;
-      l[x] = 0.f;
-      o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+    for (int u = 0; u < kSets; ++u) {
+      m[u] = -CUDART_INF_F;
+      l[u] = 0.f;
     }
+#pragma unroll
+    for (int x = 0; x < GM; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
     const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
     for (int u = warps_first(part0, warp); u < seg_end; u += kPmWarps) {
       cp_async_wait<kPfSlots - 1>();
@@ -692,72 +726,96 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       const int then = finder.next(pg, warp, G, chunk_rows, hkv, err);
       const uint32_t ok = __ballot_sync(0xffffffffu, now >= 0) & 0xffffu;
       const int base = (u - item.f0) * kPatBlock;
-      float s[GM][2];
+      const uint8_t* kt = ring + slot * kPfHalf + 512 * r4 + 16 * c8;
+      float s[kSets][kLaneRows];
 #pragma unroll
-      for (int x = 0; x < GM; ++x) s[x][0] = s[x][1] = 0.f;
-      const uint8_t* kt = ring + slot * kPfHalf;
-#pragma unroll 2
-      for (int i = 0; i < 8; ++i) {
-        const float4 k0 = *reinterpret_cast<const float4*>(kt + pf_off(r8, 4 * i + c4));
-        const float4 k1 = *reinterpret_cast<const float4*>(kt + pf_off(r8 + 8, 4 * i + c4));
+      for (int y = 0; y < kSets; ++y) {
+        float lo[4][Q], hi[4][Q];  // even and odd dimensions
 #pragma unroll
-        for (int x = 0; x < GM; ++x) {
-          const float4 y = *reinterpret_cast<const float4*>(qs + x * kD + 16 * i + 4 * c4);
-          s[x][0] = fmaf(y.x, k0.x, fmaf(y.y, k0.y, fmaf(y.z, k0.z, fmaf(y.w, k0.w, s[x][0]))));
-          s[x][1] = fmaf(y.x, k1.x, fmaf(y.y, k1.y, fmaf(y.z, k1.z, fmaf(y.w, k1.w, s[x][1]))));
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < Q; ++x) lo[j][x] = hi[j][x] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float4 kk[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4*>(kt + 2048 * j + 128 * i);
+#pragma unroll
+          for (int x = 0; x < Q; ++x) {
+            const float4 z = *reinterpret_cast<const float4*>(qs + (Q * y + x) * kD + 32 * i + 4 * c8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              fma2(kk[j].x, kk[j].y, z.x, z.y, lo[j][x], hi[j][x], lo[j][x], hi[j][x]);
+              fma2(kk[j].z, kk[j].w, z.z, z.w, lo[j][x], hi[j][x], lo[j][x], hi[j][x]);
+            }
+          }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < Q; ++x) lo[j][x] += hi[j][x];
+        lane_sums(lo, c8, s[y]);
       }
       __syncwarp();
       fetch(slot, after, v);
       slot = slot + 1 == kPfSlots ? 0 : slot + 1;
-      const bool masked = ok != 0xffffu || base + kPatBlock > all_see;
+      if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
 #pragma unroll
-      for (int x = 0; x < GM; ++x) {
+        for (int y = 0; y < kSets; ++y) {
+          const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + Q * y + mine) / G);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          s[x][u] += __shfl_xor_sync(0xffffffffu, s[x][u], 1);
-          s[x][u] += __shfl_xor_sync(0xffffffffu, s[x][u], 2);
-        }
-        if (masked) {  // some rows do not count for some queries
-          const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            if (!(ok >> (r8 + 8 * u) & 1u) || base + r8 + 8 * u >= sees) s[x][u] = -CUDART_INF_F;
-        }
-        float mx = fmaxf(s[x][0], s[x][1]);
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        const float mn = fmaxf(m[x], mx), ms = mn == -CUDART_INF_F ? 0.f : mn;
-        if (mn != m[x]) {  // the same for the whole warp
-          const float a = exp2f((m[x] - ms) * scale);
-          l[x] *= a;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[x][e] *= a;
-          m[x] = mn;
-        }
-        const float p0 = exp2f((s[x][0] - ms) * scale), p1 = exp2f((s[x][1] - ms) * scale);
-        l[x] += p0 + p1;
-        if (c4 == 0) {
-          ps[x * kPatBlock + r8] = p0;
-          ps[x * kPatBlock + r8 + 8] = p1;
+          for (int j = 0; j < kLaneRows; ++j)
+            if (!(ok >> (lane_row + 4 * j) & 1u) || base + lane_row + 4 * j >= sees) s[y][j] = -CUDART_INF_F;
         }
       }
+      bool moved = false;
+#pragma unroll
+      for (int y = 0; y < kSets; ++y) {
+        float mx = s[y][0];
+#pragma unroll
+        for (int j = 1; j < kLaneRows; ++j) mx = fmaxf(mx, s[y][j]);
+        if (Q == 4) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        const float mn = fmaxf(m[y], mx), ms = mn == -CUDART_INF_F ? 0.f : mn;
+        const float a = exp2f((m[y] - ms) * scale);  // 1 where the maximum stays
+        moved |= mn != m[y];
+        m[y] = mn;
+        l[y] *= a;
+        if (lane < Q) rescale[Q * y + mine] = a;
+#pragma unroll
+        for (int j = 0; j < kLaneRows; ++j) {
+          const float e = exp2f((s[y][j] - ms) * scale);
+          l[y] += e;
+          ps[(Q * y + mine) * kPatBlock + lane_row + 4 * j] = e;
+        }
+      }
+      moved = __any_sync(0xffffffffu, moved);
       cp_async_wait<kPfSlots - 1>();
       __syncwarp();
-      const uint8_t* vt = ring + slot * kPfHalf;
-#pragma unroll 1
+      if (moved) {  // rare once the maxima have settled
+#pragma unroll
+        for (int x = 0; x < GM; ++x) {
+          const float a = rescale[x];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x][e] *= a;
+        }
+      }
+      const uint8_t* vt = ring + slot * kPfHalf + 16 * lane;
+#pragma unroll 2
       for (int r0 = 0; r0 < kPatBlock; r0 += 4) {
         float4 y[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const float4*>(vt + pf_off(r0 + u, lane));
+        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(vt + 512 * (r0 + j));
 #pragma unroll
         for (int x = 0; x < GM; ++x) {
-          const float4 p = *reinterpret_cast<const float4*>(ps + x * kPatBlock + r0);
-          o[x][0] = fmaf(p.w, y[3].x, fmaf(p.z, y[2].x, fmaf(p.y, y[1].x, fmaf(p.x, y[0].x, o[x][0]))));
-          o[x][1] = fmaf(p.w, y[3].y, fmaf(p.z, y[2].y, fmaf(p.y, y[1].y, fmaf(p.x, y[0].y, o[x][1]))));
-          o[x][2] = fmaf(p.w, y[3].z, fmaf(p.z, y[2].z, fmaf(p.y, y[1].z, fmaf(p.x, y[0].z, o[x][2]))));
-          o[x][3] = fmaf(p.w, y[3].w, fmaf(p.z, y[2].w, fmaf(p.y, y[1].w, fmaf(p.x, y[0].w, o[x][3]))));
+          const float4 p4 = *reinterpret_cast<const float4*>(ps + x * kPatBlock + r0);
+          const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            fma2(p[j], p[j], y[j].x, y[j].y, o[x][0], o[x][1], o[x][0], o[x][1]);
+            fma2(p[j], p[j], y[j].z, y[j].w, o[x][2], o[x][3], o[x][2], o[x][3]);
+          }
         }
       }
       __syncwarp();
@@ -768,12 +826,12 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     }
     // the warps' states of this item, merged in shared memory
 #pragma unroll
-    for (int x = 0; x < GM; ++x) {
-      float y = l[x];  // four lanes hold the same rows
-      y += __shfl_xor_sync(0xffffffffu, y, 4);
-      y += __shfl_xor_sync(0xffffffffu, y, 8);
-      y += __shfl_xor_sync(0xffffffffu, y, 16);
-      if (lane == 0) wml[warp * GM + x] = make_float2(m[x] * scale, y);
+    for (int y = 0; y < kSets; ++y) {
+      float sum = l[y];
+      if (Q == 4) sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+      if (lane < Q) wml[warp * GM + Q * y + mine] = make_float2(m[y] * scale, sum);
     }
     const int part = 2 * cta + (owns ? 1 : 0);
 #pragma unroll
