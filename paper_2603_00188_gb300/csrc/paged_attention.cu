@@ -245,7 +245,7 @@ __device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int 
 //   movmatrix and taken as P = hi + lo, two bf16 parts (16 bits of it: with one
 //   part the weights' rounding would be as large as the result's).
 // NT: groups of eight queries that share one read of the cache: 1 or 2 with
-// their fragments in registers, 4 with them read from shared memory.
+// their fragments in registers, 3 or 4 with them read from shared memory.
 constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
 __host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 #pragma unroll
       for (int i = 0; i < kPass; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 2 && n0 + i < NT; ++e) {
           const int x = 8 * i + 2 * t4 + e;
           float M = -CUDART_INF_F;
 #pragma unroll
@@ -980,9 +980,10 @@ static int paged_ctas() {
 
 // Query rows of a CTA's part, which share one read of the cache.
 static int paged_part_rows(DType dt, const PageView& pages, int G) {
-  const int rows = pages.w * G;
-  if (dt == kF32) return rows <= 4 ? 4 : (rows <= 8 ? 8 : 16);
-  return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
+  const int rows = pages.w * G, most = dt == kF32 ? 16 : 32;
+  const int chunks = (rows + most - 1) / most, each = (rows + chunks - 1) / chunks;
+  if (dt == kF32) return each <= 4 ? 4 : (each <= 8 ? 8 : 16);
+  return (each + 7) / 8 * 8;
 }
 
 // Workspace: the error word, the descriptors (16 KB), then two parts of each
@@ -997,7 +998,7 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
                                    void* out, int n, int hq, int hkv, void* ws, cudaStream_t st) {
   uint32_t* err = static_cast<uint32_t*>(ws);
   const int rows = pages.w * (hq / hkv), part_rows = paged_part_rows(dt, pages, hq / hkv);
-  const int chunks = (rows + part_rows - 1) / part_rows, chunk_rows = (rows + chunks - 1) / chunks;
+  const int most = dt == kF32 ? 16 : 32, chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks;
   const int ctas = paged_ctas();
   const long long items = (long long)pages.n_seqs * hkv * chunks;
   const int by_item = items <= ctas, descs = by_item ? (int)items : ctas;
@@ -1033,13 +1034,15 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
   };
   std::integral_constant<int, 1> w1;
   std::integral_constant<int, 2> w2;
+  std::integral_constant<int, 3> w3;
   std::integral_constant<int, 4> w4;
   std::integral_constant<int, 8> w8;
   std::integral_constant<int, 16> w16;
   if (dt == kF32)
     part_rows == 4 ? run(float(), w4) : (part_rows == 8 ? run(float(), w8) : run(float(), w16));
   else
-    part_rows == 8 ? run(__nv_bfloat16(), w1) : (part_rows == 16 ? run(__nv_bfloat16(), w2) : run(__nv_bfloat16(), w4));
+    part_rows <= 16 ? (part_rows == 8 ? run(__nv_bfloat16(), w1) : run(__nv_bfloat16(), w2))
+                    : (part_rows == 24 ? run(__nv_bfloat16(), w3) : run(__nv_bfloat16(), w4));
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
