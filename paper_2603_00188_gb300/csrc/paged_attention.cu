@@ -37,6 +37,10 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float
 constexpr int kPatBlock = 16;  // cached rows of a block
 constexpr int kPatItem = 12;    // units of an item's own costs
 
+// Whether any item can be split, and whether what is left for the second
+// kernel is described by CTA or by item.
+enum SplitMode { kWholeItems = 0, kDescByCta = 1, kDescByItem = 2 };
+
 // What a session asks for.
 struct SeqWork {
   int first, fresh;  // its packed tokens: first .. first + fresh
@@ -76,26 +80,60 @@ struct Range {
   }
 };
 
+// Moves on to the session of unit b.
+__device__ __forceinline__ void advance(Cursor& c, int b, const PageView& pg, int G, int chunk_rows, int hkv) {
+  while (b >= c.base + c.cost(hkv)) {
+    c.base += c.cost(hkv);
+    ++c.s;
+    c.w = seq_work(pg, c.s, pg.len[c.s], G, chunk_rows);
+  }
+}
+
+// An item that a range meets.
+struct Item {
+  int h, chunk;
+  int i0, f0, i1;  // units: its first, its first block's, its end
+};
+__device__ __forceinline__ Item item_at(const Cursor& c, int u) {
+  const int units = kPatItem + c.w.blocks, i = (u - c.base) / units;
+  Item x;
+  x.h = c.w.chunks == 1 ? i : i / c.w.chunks;
+  x.chunk = i - x.h * c.w.chunks;
+  x.i0 = c.base + i * units;
+  x.f0 = x.i0 + kPatItem;
+  x.i1 = x.i0 + units;
+  return x;
+}
+
 // The costs are summed over the sessions, and the range's first session found
 // by the thread that holds it.  Whole CTA; least: the fewest units that make a
-// CTA's range.
+// CTA's range.  split: the units that splitting an item costs beside its parts
+// (writing them, a second part in the CTA, the merge).  Where CTAs with whole
+// items, each the CTA's where its first unit falls, are sure to take no longer
+// than the even ranges and this, the range's ends move on to the next item's
+// start: 64 sessions of 2,000 rows on 304 CTAs take 45 us so and 53 split; 8 of
+// 256 rows 7.8 and 8.2; 8 of 500 rows, a tenth of the CTAs, 11.2 and 9.0.
 template <int THREADS>
 struct RangeScratch {
-  int warp_sum[THREADS / 32];
+  int warp_sum[THREADS / 32], warp_most[THREADS / 32], warp_least[THREADS / 32];
   Cursor at;
 };
 template <int THREADS>
-__device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int least, uint32_t* err,
+__device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int least, int split, uint32_t* err,
                             RangeScratch<THREADS>* scratch) {
   constexpr int kWarps = THREADS / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (pg.n_seqs + THREADS - 1) / THREADS, s0 = min(pg.n_seqs, tid * per), s1 = min(pg.n_seqs, s0 + per);
-  int mine = 0;
+  int mine = 0, longest = 0, shortest = 0x7fffffff;
   Cursor c;  // of the thread's last session, and its only one where there are no more than threads
   for (int s = s0; s < s1; ++s) {
     const int asked = pg.len[s];
     c.w = seq_work(pg, s, asked, G, chunk_rows);
     mine += c.cost(hkv);
+    if (c.w.chunks > 0) {
+      longest = max(longest, kPatItem + c.w.blocks);
+      shortest = min(shortest, kPatItem + c.w.blocks);
+    }
     if (blockIdx.x == 0 && c.w.len != asked) record_error(err, kErrInput);
   }
   int incl = mine;
@@ -104,7 +142,13 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
     const int x = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += x;
   }
-  if (lane == 31) scratch->warp_sum[warp] = incl;
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  shortest = __reduce_min_sync(0xffffffffu, shortest);
+  if (lane == 31) {
+    scratch->warp_sum[warp] = incl;
+    scratch->warp_most[warp] = longest;
+    scratch->warp_least[warp] = shortest;
+  }
   __syncthreads();
   int before = 0, total = 0;
 #pragma unroll
@@ -112,6 +156,8 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
     const int x = scratch->warp_sum[w];
     if (w < warp) before += x;
     total += x;
+    longest = max(longest, scratch->warp_most[w]);
+    shortest = min(shortest, scratch->warp_least[w]);
   }
   Range r;
   r.ctas = min((int)gridDim.x, total / least + (total % least != 0));
@@ -135,16 +181,16 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
   }
   __syncthreads();
   r.at = scratch->at;
-  return r;
-}
-
-// Moves on to the session of unit b.
-__device__ __forceinline__ void advance(Cursor& c, int b, const PageView& pg, int G, int chunk_rows, int hkv) {
-  while (b >= c.base + c.cost(hkv)) {
-    c.base += c.cost(hkv);
-    ++c.s;
-    c.w = seq_work(pg, c.s, pg.len[c.s], G, chunk_rows);
+  // a range of `most` units holds at most most / shortest (rounded up) items' starts
+  const int most = r.quota + (r.extra > 0);
+  if (min(most + longest, (most / shortest + (most % shortest != 0)) * longest) - r.quota <= split) {
+    c = r.at;
+    advance(c, r.b1 - 1, pg, G, chunk_rows, hkv);
+    const Item first = item_at(r.at, r.b0);
+    if (first.i0 < r.b0) r.b0 = first.i1;
+    r.b1 = item_at(c, r.b1 - 1).i1;
   }
+  return r;
 }
 
 // Which part of which item is left for the second kernel: `desc` has an entry
@@ -165,22 +211,6 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-// An item that a range meets.
-struct Item {
-  int h, chunk;
-  int i0, f0, i1;  // units: its first, its first block's, its end
-};
-__device__ __forceinline__ Item item_at(const Cursor& c, int u) {
-  const int units = kPatItem + c.w.blocks, i = (u - c.base) / units;
-  Item x;
-  x.h = c.w.chunks == 1 ? i : i / c.w.chunks;
-  x.chunk = i - x.h * c.w.chunks;
-  x.i0 = c.base + i * units;
-  x.f0 = x.i0 + kPatItem;
-  x.i1 = x.i0 + units;
-  return x;
 }
 
 // The rows of a warp's blocks, one block after the other.  The block of unit u
@@ -290,7 +320,7 @@ __device__ __forceinline__ uint32_t pm_off(int r, int c) { return (uint32_t)(r *
 template <int NT>
 __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     k_paged_mma(const __grid_constant__ PageView pg, const __nv_bfloat16* q, const __nv_bfloat16* k,
-                const __nv_bfloat16* v, __nv_bfloat16* out, int n, int hq, int hkv, int by_item, int chunks,
+                const __nv_bfloat16* v, __nv_bfloat16* out, int n, int hq, int hkv, int mode, int split, int chunks,
                 int chunk_rows, PartDesc* desc, float2* part_ml, float* part_o, uint32_t* err) {
   constexpr int kStages = pm_stages(NT), kRows = 8 * NT, kPass = pm_pass(NT);
   extern __shared__ uint4 pat_smem[];
@@ -304,9 +334,9 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   const uint32_t ring = smem_u32(sm) + warp * kStages * 2 * kPmHalf;
   pdl_trigger();
   pdl_wait();
-  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, err, scratch);
+  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, split, err, scratch);
   const bool describes = tid == kPmThreads - 32;  // the thread that writes the CTA's descriptor
-  if (!by_item && describes) desc[cta].item = -1;
+  if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
   RowFinder finder(rg);
@@ -353,16 +383,16 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     const bool owns = part0 == item.f0, whole = owns && seg_end == item.i1;  // has the first block, has them all
     if (cur.w.blocks == 0 || part0 >= seg_end) {
       if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
-        if (by_item && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
+        if (mode == kDescByItem && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
         zero_rows<kPmThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
       }
       seg = seg_end;
       continue;
     }
-    if (describes && owns) {
+    if (describes && owns && mode != kWholeItems) {
       const int id = (cur.s * hkv + h) * chunks + chunk;
       const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(item.i1 - 1), 0};
-      if (by_item)
+      if (mode == kDescByItem)
         desc[id] = d;
       else if (!whole)
         desc[cta] = d;
@@ -635,7 +665,7 @@ __device__ __forceinline__ void lane_sums(const float (&s)[4][4], int c, float (
 template <int GM>
 __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     k_paged_fma(const __grid_constant__ PageView pg, const float* q, const float* k, const float* v, float* out, int n,
-                int hq, int hkv, int by_item, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
+                int hq, int hkv, int mode, int split, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
                 float* part_o, uint32_t* err) {
   extern __shared__ uint4 pat_smem[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
@@ -650,9 +680,9 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   float* rescale = ps + GM * kPatBlock;      // [GM]
   pdl_trigger();
   pdl_wait();
-  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, err, scratch);
+  const Range rg = find_range<kPmThreads>(pg, G, chunk_rows, hkv, kPmWarps, split, err, scratch);
   const bool describes = tid == kPmThreads - 32;  // the thread that writes the CTA's descriptor
-  if (!by_item && describes) desc[cta].item = -1;
+  if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
   RowFinder finder(rg);
@@ -689,16 +719,16 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     const bool owns = part0 == item.f0, whole = owns && seg_end == item.i1;  // has the first block, has them all
     if (cur.w.blocks == 0 || part0 >= seg_end) {
       if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
-        if (by_item && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
+        if (mode == kDescByItem && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
         zero_rows<kPmThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
       }
       seg = seg_end;
       continue;
     }
-    if (describes && owns) {
+    if (describes && owns && mode != kWholeItems) {
       const int id = (cur.s * hkv + h) * chunks + chunk;
       const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(item.i1 - 1), 0};
-      if (by_item)
+      if (mode == kDescByItem)
         desc[id] = d;
       else if (!whole)
         desc[cta] = d;
@@ -1001,7 +1031,16 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
   const int most = dt == kF32 ? 16 : 32, chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks;
   const int ctas = paged_ctas();
   const long long items = (long long)pages.n_seqs * hkv * chunks;
-  const int by_item = items <= ctas, descs = by_item ? (int)items : ctas;
+  // What a split costs, in units: 24 where a unit is a block of up to 16 bf16
+  // queries, 14 where its products take longer (more queries, fp32).
+  int split = dt == kBF16 && part_rows <= 16 ? 24 : 14;
+  // Sessions that cannot be longer than a split and a little are never split,
+  // which saves the second launch (one session of 256 rows: 7.0 us, split 6.9,
+  // and 2 us less on the host; 64 sessions 8.4 and 14.8).
+  const long long longest = kPatItem + ((long long)pages.max_pages * pages.page_rows + kPatBlock - 1) / kPatBlock;
+  const int mode = longest <= split + kPmWarps ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
+  if (mode == kWholeItems) split = 1 << 30;
+  const int descs = items <= ctas ? (int)items : ctas;
   uint8_t* at = static_cast<uint8_t*>(ws) + kPatHead;
   PartDesc* desc = reinterpret_cast<PartDesc*>(at);
   float2* part_ml = reinterpret_cast<float2*>(at + kPatDescs);
@@ -1016,7 +1055,7 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return;
         e = launch_after(kern, dim3(ctas), kPmThreads, smem, st, pages, static_cast<const T*>(q),
-                         static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), n, hq, hkv, by_item,
+                         static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), n, hq, hkv, mode, split,
                          chunks, chunk_rows, desc, part_ml, part_o, err);
       };
       if constexpr (std::is_same<T, float>::value) {
@@ -1026,11 +1065,11 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
         auto kern = k_paged_mma<kWidth>;
         go(kern, pm_smem(kWidth));
       }
-      if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return;
+      if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || mode == kWholeItems) return;
     }
     TimingScope ts("paged_merge", st);
     e = launch_after(k_paged_merge<T>, dim3(descs, chunk_rows), kMrgThreads, 0, st, pages, static_cast<T*>(out), n, hq, hkv,
-                     chunks, chunk_rows, part_rows, by_item, desc, part_ml, part_o);
+                     chunks, chunk_rows, part_rows, mode == kDescByItem, desc, part_ml, part_o);
   };
   std::integral_constant<int, 1> w1;
   std::integral_constant<int, 2> w2;
