@@ -35,7 +35,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float
 
 // ---------------------------------------------------------------- the split
 constexpr int kPatBlock = 16;  // cached rows of a block
-constexpr int kPatItem = 12;    // units of an item's own costs
+constexpr int kPatItem = 12;   // units of an item's own costs
 
 // Whether any item can be split, and whether what is left for the second
 // kernel is described by CTA or by item.
@@ -48,15 +48,19 @@ struct SeqWork {
   int blocks;        // blocks of one item; none: its output is zeros
   int chunks;        // items of one KV head
 };
-__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, int G, int chunk_rows) {
+__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int first, int fresh, int len, int G, int chunk_rows) {
   SeqWork w;
-  w.first = pg.cu ? pg.cu[s] : s * pg.w;
-  w.fresh = pg.cu ? pg.cu[s + 1] - w.first : pg.w;
+  w.first = first;
+  w.fresh = fresh;
   w.len = max(0, min(len, pg.max_pages * pg.page_rows));
   w.blocks = (w.len + kPatBlock - 1) / kPatBlock;
-  const int rows = max(0, min(w.fresh, pg.w)) * G;
+  const int rows = max(0, min(fresh, pg.w)) * G;
   w.chunks = rows <= chunk_rows ? (rows > 0 ? 1 : 0) : (rows + chunk_rows - 1) / chunk_rows;
   return w;
+}
+__device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, int G, int chunk_rows) {
+  const int first = pg.cu ? pg.cu[s] : s * pg.w;
+  return seq_work(pg, first, pg.cu ? pg.cu[s + 1] - first : pg.w, len, G, chunk_rows);
 }
 
 // A position in the sequence of all units: session s begins at unit `base`.
@@ -121,20 +125,28 @@ struct RangeScratch {
 template <int THREADS>
 __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, int least, int split, uint32_t* err,
                             RangeScratch<THREADS>* scratch) {
-  constexpr int kWarps = THREADS / 32;
+  constexpr int kWarps = THREADS / 32, kAtOnce = 4;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (pg.n_seqs + THREADS - 1) / THREADS, s0 = min(pg.n_seqs, tid * per), s1 = min(pg.n_seqs, s0 + per);
   int mine = 0, longest = 0, shortest = 0x7fffffff;
   Cursor c;  // of the thread's last session, and its only one where there are no more than threads
-  for (int s = s0; s < s1; ++s) {
-    const int asked = pg.len[s];
-    c.w = seq_work(pg, s, asked, G, chunk_rows);
-    mine += c.cost(hkv);
-    if (c.w.chunks > 0) {
-      longest = max(longest, kPatItem + c.w.blocks);
-      shortest = min(shortest, kPatItem + c.w.blocks);
+  for (int s = s0; s < s1; s += kAtOnce) {
+    int asked[kAtOnce], first[kAtOnce + 1];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) asked[i] = s + i < s1 ? pg.len[s + i] : 0;
+#pragma unroll
+    for (int i = 0; i <= kAtOnce; ++i) first[i] = pg.cu ? pg.cu[min(s + i, s1)] : (s + i) * pg.w;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (s + i >= s1) break;
+      c.w = seq_work(pg, first[i], first[i + 1] - first[i], asked[i], G, chunk_rows);
+      mine += c.cost(hkv);
+      if (c.w.chunks > 0) {
+        longest = max(longest, kPatItem + c.w.blocks);
+        shortest = min(shortest, kPatItem + c.w.blocks);
+      }
+      if (blockIdx.x == 0 && c.w.len != asked[i]) record_error(err, kErrInput);
     }
-    if (blockIdx.x == 0 && c.w.len != asked) record_error(err, kErrInput);
   }
   int incl = mine;
 #pragma unroll
@@ -183,7 +195,8 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
   r.at = scratch->at;
   // a range of `most` units holds at most most / shortest (rounded up) items' starts
   const int most = r.quota + (r.extra > 0);
-  if (min(most + longest, (most / shortest + (most % shortest != 0)) * longest) - r.quota <= split) {
+  const long long whole = min((long long)most + longest, (long long)(most / shortest + (most % shortest != 0)) * longest);
+  if (whole - r.quota <= split) {
     c = r.at;
     advance(c, r.b1 - 1, pg, G, chunk_rows, hkv);
     const Item first = item_at(r.at, r.b0);
@@ -313,6 +326,11 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
+// Whether either of two bf16 is an infinity or a NaN.
+__device__ __forceinline__ bool has_odd_bf16(uint32_t x) {
+  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+
 // Byte of the 16-byte chunk c of row r of a half stage, swizzled so that eight
 // rows' chunks lie in eight different bank groups.
 __device__ __forceinline__ uint32_t pm_off(int r, int c) { return (uint32_t)(r * 256 + ((c ^ (r & 7)) << 4)); }
@@ -439,6 +457,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       __syncwarp();
       const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
       const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
+      uint8_t* stage_ptr = sm + (warp * kStages + stage) * 2 * kPmHalf;
       const int base = (u - item.f0) * kPatBlock;
       constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
       float c[kChains][NT][4];
@@ -474,7 +493,22 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         for (int j = 0; j < 4; ++j) c[0][0][j] += c[1][0][j];
       }
       const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
+      uint32_t apart = 0;  // rows whose values are added apart from the others
       if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
+        if (cur.w.fresh > 1) {
+          // Rows that only the newer tokens see: a weight of 0 times a value
+          // that is no number would reach the older ones.
+          const uint32_t rows_apart = ok & ~((1u << max(0, min(kPatBlock, all_see - base))) - 1u);
+          bool odd = false;
+          if (rows_apart >> (lane & 15) & 1u) {
+#pragma unroll 4
+            for (int i = 0; i < 8; ++i) {
+              const uint4 y = *reinterpret_cast<const uint4*>(stage_ptr + kPmHalf + pm_off(lane & 15, 8 * (lane >> 4) + i));
+              odd |= has_odd_bf16(y.x) || has_odd_bf16(y.y) || has_odd_bf16(y.z) || has_odd_bf16(y.w);
+            }
+          }
+          if (__any_sync(0xffffffffu, odd)) apart = rows_apart;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -509,16 +543,51 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
             }
           }
         }
+        float p[2][2];  // [row g8, g8 + 8][query]
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            p[x][e] = ex2_approx(fmaf(c[0][nt][2 * x + e], scale, -ms[e]));
+            l[nt][e] += p[x][e];
+          }
+        if (apart != 0u) {
+          for (uint32_t left = apart; left != 0u; left &= left - 1u) {
+            const int r = __ffs(left) - 1, from = (r & 7) * 4 + t4;
+            float w[2];
+            bool seen[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float y0 = __shfl_sync(0xffffffffu, p[0][e], from), y1 = __shfl_sync(0xffffffffu, p[1][e], from);
+              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G);
+              w[e] = r < 8 ? y0 : y1;
+              seen[e] = base + r < sees;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int dim = 8 * i + g8;
+              const float y = __bfloat162float(
+                  *reinterpret_cast<const __nv_bfloat16*>(stage_ptr + kPmHalf + pm_off(r, i) + 2 * (dim & 7)));
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (seen[e]) o[i >> 1][nt][2 * (i & 1) + e] = fmaf(w[e], y, o[i >> 1][nt][2 * (i & 1) + e]);
+            }
+          }
+        }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const float p0 = ex2_approx(fmaf(c[0][nt][2 * x], scale, -ms[0]));
-          const float p1 = ex2_approx(fmaf(c[0][nt][2 * x + 1], scale, -ms[1]));
-          l[nt][0] += p0;
-          l[nt][1] += p1;
-          const uint32_t hi = pack_bf16(p0, p1);
+          const uint32_t hi = pack_bf16(p[x][0], p[x][1]);
           ph[nt][x] = transpose8x8(hi);
-          pl[nt][x] = transpose8x8(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+          pl[nt][x] =
+              transpose8x8(pack_bf16(p[x][0] - __uint_as_float(hi << 16), p[x][1] - __uint_as_float(hi & 0xffff0000u)));
         }
+      }
+      if (apart != 0u) {  // added: they count no more
+        __syncwarp();
+        if (apart >> (lane & 15) & 1u)
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(stage_ptr + kPmHalf + pm_off(lane & 15, 8 * (lane >> 4) + i)) = make_uint4(0, 0, 0, 0);
+        __syncwarp();
       }
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) {
@@ -831,7 +900,33 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
           for (int e = 0; e < 4; ++e) o[x][e] *= a;
         }
       }
-      const uint8_t* vt = ring + slot * kPfHalf + 16 * lane;
+      uint8_t* vt = ring + slot * kPfHalf + 16 * lane;
+      if (cur.w.fresh > 1 && base + kPatBlock > all_see) {
+        // Rows that only the newer tokens see: a weight of 0 times a value that
+        // is no number would reach the older ones.  If there is one, these
+        // rows are added here and count no more.
+        const uint32_t rows_apart = ok & ~((1u << max(0, all_see - base)) - 1u);
+        bool odd = false;
+        for (uint32_t left = rows_apart; left != 0u; left &= left - 1u) {
+          const float4 y = *reinterpret_cast<const float4*>(vt + 512 * (__ffs(left) - 1));
+          odd |= !(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w));
+        }
+        if (__any_sync(0xffffffffu, odd))
+          for (uint32_t left = rows_apart; left != 0u; left &= left - 1u) {
+            const int r = __ffs(left) - 1;
+            const float4 y = *reinterpret_cast<const float4*>(vt + 512 * r);
+            *reinterpret_cast<float4*>(vt + 512 * r) = make_float4(0.f, 0.f, 0.f, 0.f);  // the lane's own dimensions
+#pragma unroll
+            for (int x = 0; x < GM; ++x) {
+              const float w = ps[x * kPatBlock + r];
+              if (base + r >= cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G)) continue;
+              o[x][0] = fmaf(w, y.x, o[x][0]);
+              o[x][1] = fmaf(w, y.y, o[x][1]);
+              o[x][2] = fmaf(w, y.z, o[x][2]);
+              o[x][3] = fmaf(w, y.w, o[x][3]);
+            }
+          }
+      }
 #pragma unroll 2
       for (int r0 = 0; r0 < kPatBlock; r0 += 4) {
         float4 y[4];

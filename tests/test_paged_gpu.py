@@ -343,7 +343,7 @@ def test_attention_matches(st, dtype, hq, hkv, page, rows, new):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rows,new,w", [([300, 12, 0, 5000, 31], [2, 0, 3, 5, 1], 5), ([40, 700], [0, 16], 16),
-                                        ([64, 64, 64], [4, 1, 6], 3), ([200], [0], 2), ([9] * 300, [1] * 300, 1)])
+                                        ([64, 64, 64], [4, 1, 6], 3), ([200], [0], 2), ([9] * 300, [1] * 300, 1), ([5, 20] * 600, [0, 1] * 600, 2)])
 def test_attention_ragged(st, dtype, rows, new, w):
     """cu_new: any number of new tokens; those past w of a sequence are left alone."""
     cu = [sum(new[:i]) for i in range(len(new) + 1)]
@@ -392,6 +392,28 @@ def test_attention_extreme_scores(st, dtype):
         p = torch.softmax(kk[:, g // 4] @ q[1, g].cpu().double() / 128 ** 0.5, 0)
         want = p @ vv[:, g // 4]
         assert ((out[1, g].cpu().double() - want).abs() <= 0.01 * (p @ vv[:, g // 4].abs())).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hq,hkv,new", [(4, 2, 3), (6, 2, 5), (7, 1, 3), (12, 2, 5), (16, 1, 8)])
+@pytest.mark.parametrize("length", [5, 18, 400, 2003])
+def test_attention_no_numbers_in_masked_rows(st, dtype, hq, hkv, new, length):
+    """A newer token's key and value may hold anything: the older tokens do not see them.  The newest does."""
+    rows, cu = [length, 40], [0, new, 2 * new]
+    q, kp, vp, pg, table = _attention_case(st, rows, cu, 16, hq, hkv, dtype, length + new)
+    clean, _ = _attend(st, q, kp, vp, pg)
+    for j, x in ((length - 1, float("nan")), (length - 2, float("inf"))):
+        at = int(table[0, j // 16]), j % 16
+        vp[at][0, 5] = x
+        kp[at][hkv - 1, 7] = x
+    out, _ = _attend(st, q, kp, vp, pg)
+    older, spoilt = [i for i in range(2 * new) if i not in (new - 1, new - 2)], out[new - 1]
+    r, b = ref.attention(q, kp, vp, table, rows, cu)
+    assert not r[older].isnan().any()
+    ref.within(out[older], r[older], b[older])
+    assert (out[older].float() - clean[older].float()).abs().max() <= 2 ** -6 * clean.float().abs().max()
+    assert spoilt[:, 5].float().isnan()[: hq // hkv].all()  # the newest token sees the NaN of its own value
+    assert out[new - 2, 0, 5].float().isinf() or out[new - 2, 0, 5].float().isnan()
 
 
 def test_attention_bad_pages_and_lengths(st):
