@@ -517,48 +517,57 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
             if (!(ok >> r & 1u) || base + r >= sees) c[0][nt][j] = -CUDART_INF_F;
           }
       }
-      uint32_t ph[NT][2], pl[NT][2];
+      float ms[NT][2];  // the new maxima, scaled
+      bool moved = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float mn[2], ms[2];
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          mn[e] = fmaxf(m[nt][e], mx);
-          ms[e] = mn[e] == -CUDART_INF_F ? 0.f : mn[e] * scale;
+          mx = fmaxf(m[nt][e], mx);
+          ms[nt][e] = mx == -CUDART_INF_F ? 0.f : mx * scale;
+          moved |= mx != m[nt][e];
         }
-        if (__any_sync(0xffffffffu, mn[0] != m[nt][0] || mn[1] != m[nt][1])) {  // rare once the maxima have settled
+      if (__any_sync(0xffffffffu, moved)) {  // rare once the maxima have settled
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float alpha = ex2_approx(fmaf(m[nt][e], scale, -ms[e]));
+            const float mx = max3(m[nt][e], c[0][nt][e], c[0][nt][2 + e]);
+            float all = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 8));
+            all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 16));
+            const float alpha = ex2_approx(fmaf(m[nt][e], scale, -ms[nt][e]));
             l[nt][e] *= alpha;
-            m[nt][e] = mn[e];
+            m[nt][e] = all;
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) {
               o[mt][nt][e] *= alpha;
               o[mt][nt][2 + e] *= alpha;
             }
           }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // scores become probabilities
+          c[0][nt][j] = ex2_approx(fmaf(c[0][nt][j], scale, -ms[nt][j & 1]));
+          l[nt][j & 1] += c[0][nt][j];
         }
-        float p[2][2];  // [row g8, g8 + 8][query]
+      if (apart != 0u) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            p[x][e] = ex2_approx(fmaf(c[0][nt][2 * x + e], scale, -ms[e]));
-            l[nt][e] += p[x][e];
-          }
-        if (apart != 0u) {
+        for (int nt = 0; nt < NT; ++nt)
           for (uint32_t left = apart; left != 0u; left &= left - 1u) {
             const int r = __ffs(left) - 1, from = (r & 7) * 4 + t4;
             float w[2];
             bool seen[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float y0 = __shfl_sync(0xffffffffu, p[0][e], from), y1 = __shfl_sync(0xffffffffu, p[1][e], from);
+              const float y0 = __shfl_sync(0xffffffffu, c[0][nt][e], from);
+              const float y1 = __shfl_sync(0xffffffffu, c[0][nt][2 + e], from);
               const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G);
               w[e] = r < 8 ? y0 : y1;
               seen[e] = base + r < sees;
@@ -573,22 +582,22 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
                 if (seen[e]) o[i >> 1][nt][2 * (i & 1) + e] = fmaf(w[e], y, o[i >> 1][nt][2 * (i & 1) + e]);
             }
           }
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint32_t hi = pack_bf16(p[x][0], p[x][1]);
-          ph[nt][x] = transpose8x8(hi);
-          pl[nt][x] =
-              transpose8x8(pack_bf16(p[x][0] - __uint_as_float(hi << 16), p[x][1] - __uint_as_float(hi & 0xffff0000u)));
-        }
-      }
-      if (apart != 0u) {  // added: they count no more
-        __syncwarp();
+        __syncwarp();  // added: they count no more
         if (apart >> (lane & 15) & 1u)
           for (int i = 0; i < 8; ++i)
             *reinterpret_cast<uint4*>(stage_ptr + kPmHalf + pm_off(lane & 15, 8 * (lane >> 4) + i)) = make_uint4(0, 0, 0, 0);
         __syncwarp();
       }
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const float p0 = c[0][nt][2 * x], p1 = c[0][nt][2 * x + 1];
+          const uint32_t hi = pack_bf16(p0, p1);
+          ph[nt][x] = transpose8x8(hi);
+          pl[nt][x] = transpose8x8(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+        }
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) {
         uint32_t a[4];
