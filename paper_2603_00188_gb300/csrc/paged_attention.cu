@@ -6,8 +6,8 @@
 //
 // Work is divided by what the sessions hold when the kernel runs.  An item is
 // (session, KV head, chunk of query rows); its cache is cut into blocks of 16
-// rows.  An item counts for its blocks and for kPatItem units before them that
-// stand for its own costs (queries, merge: about 2 us of a CTA); the units of
+// rows.  An item counts for its blocks and for some units before them that stand
+// for its own costs (queries, merge: 1 to 2 us of a CTA); the units of
 // all items, laid end to end, are cut into equal ranges, one per CTA.  A CTA
 // computes the parts of the few items that its range meets: an item whose
 // blocks lie inside one range is finished there, the parts of others are merged
@@ -35,7 +35,6 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float
 
 // ---------------------------------------------------------------- the split
 constexpr int kPatBlock = 16;  // cached rows of a block
-constexpr int kPatItem = 12;   // units of an item's own costs
 
 // Whether any item can be split, and whether what is left for the second
 // kernel is described by CTA or by item.
@@ -46,6 +45,7 @@ struct SeqWork {
   int first, fresh;  // its packed tokens: first .. first + fresh
   int len;           // cached rows
   int blocks;        // blocks of one item; none: its output is zeros
+  int units;         // what the item counts for: these after pg.item_units
   int chunks;        // items of one KV head
 };
 __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int first, int fresh, int len, int G, int chunk_rows) {
@@ -54,6 +54,7 @@ __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int first, int f
   w.fresh = fresh;
   w.len = max(0, min(len, pg.max_pages * pg.page_rows));
   w.blocks = (w.len + kPatBlock - 1) / kPatBlock;
+  w.units = pg.item_units + w.blocks;
   const int rows = max(0, min(fresh, pg.w)) * G;
   w.chunks = rows <= chunk_rows ? (rows > 0 ? 1 : 0) : (rows + chunk_rows - 1) / chunk_rows;
   return w;
@@ -68,7 +69,7 @@ __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int s, int len, 
 struct Cursor {
   int base, s;
   SeqWork w;
-  __device__ __forceinline__ int cost(int hkv) const { return (kPatItem + w.blocks) * w.chunks * hkv; }
+  __device__ __forceinline__ int cost(int hkv) const { return w.units * w.chunks * hkv; }
 };
 
 // A CTA's range of units and where it starts.  All units are dealt to `ctas`
@@ -99,13 +100,13 @@ struct Item {
   int i0, f0, i1;  // units: its first, its first block's, its end
 };
 __device__ __forceinline__ Item item_at(const Cursor& c, int u) {
-  const int units = kPatItem + c.w.blocks, i = (u - c.base) / units;
+  const int units = c.w.units, i = (u - c.base) / units;
   Item x;
   x.h = c.w.chunks == 1 ? i : i / c.w.chunks;
   x.chunk = i - x.h * c.w.chunks;
   x.i0 = c.base + i * units;
-  x.f0 = x.i0 + kPatItem;
   x.i1 = x.i0 + units;
+  x.f0 = x.i1 - c.w.blocks;
   return x;
 }
 
@@ -142,8 +143,8 @@ __device__ Range find_range(const PageView& pg, int G, int chunk_rows, int hkv, 
       c.w = seq_work(pg, first[i], first[i + 1] - first[i], asked[i], G, chunk_rows);
       mine += c.cost(hkv);
       if (c.w.chunks > 0) {
-        longest = max(longest, kPatItem + c.w.blocks);
-        shortest = min(shortest, kPatItem + c.w.blocks);
+        longest = max(longest, c.w.units);
+        shortest = min(shortest, c.w.units);
       }
       if (blockIdx.x == 0 && c.w.len != asked[i]) record_error(err, kErrInput);
     }
@@ -1012,17 +1013,19 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 
 // --------------------------------------------------------------------- merge
 // out of the items that several CTAs had parts of.  grid (descriptors, rows):
-// four warps take a quarter of the parts each, a lane four dimensions; the
-// parts' weights are formed in shared memory while the first partials are on
-// their way.  (Twenty in flight at a time: 76 parts, one session on the whole
-// GPU, in one latency; with 512 threads, a dimension each, the launch of 900
-// such CTAs took 2 us longer.)
-constexpr int kMrgThreads = 128, kMrgSlices = kMrgThreads / 32, kMrgAtOnce = 20;
-template <typename T>
+// each warp takes its share of the parts, a lane four dimensions; the parts'
+// weights are formed in shared memory while the first partials are on their
+// way, ten to a warp.  Eight warps take the 76 parts of one session on the whole
+// GPU in one latency (10.3 us for 10,757 rows; four warps 12.1, four with twenty
+// at once 11.4); where there are many CTAs the parts are few, and four warps
+// launch faster (32 sessions: 150 us, eight warps 153).
+constexpr int kMrgAtOnce = 10;
+template <typename T, int kMrgThreads>
 __global__ void __launch_bounds__(kMrgThreads) k_paged_merge(const __grid_constant__ PageView pg, T* out, int n,
                                                              int hq, int hkv, int chunks, int chunk_rows,
                                                              int part_rows, int by_item, const PartDesc* desc,
                                                              const float2* part_ml, const float* part_o) {
+  constexpr int kMrgSlices = kMrgThreads / 32;
   __shared__ float wts[kPatMaxCtas];
   __shared__ float red[2][kMrgSlices];
   __shared__ float4 acc[kMrgSlices - 1][32];
@@ -1128,21 +1131,26 @@ size_t paged_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
          (size_t)2 * paged_ctas() * paged_part_rows(dt, pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
 }
 
-cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
+cudaError_t launch_paged_attention(DType dt, const PageView& view, const void* q, const void* k, const void* v,
                                    void* out, int n, int hq, int hkv, void* ws, cudaStream_t st) {
+  PageView pages = view;
   uint32_t* err = static_cast<uint32_t*>(ws);
   const int rows = pages.w * (hq / hkv), part_rows = paged_part_rows(dt, pages, hq / hkv);
   const int most = dt == kF32 ? 16 : 32, chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks;
   const int ctas = paged_ctas();
   const long long items = (long long)pages.n_seqs * hkv * chunks;
-  // What a split costs, in units: 24 where a unit is a block of up to 16 bf16
-  // queries, 14 where its products take longer (more queries, fp32).
-  int split = dt == kBF16 && part_rows <= 16 ? 24 : 14;
+  // An item's own costs, and what a split costs, in units: a block of up to 16
+  // bf16 queries takes 0.2 us of a CTA's, one of more queries or of fp32 0.4.
+  // (12 for the first: one session of 10,757 rows 0.6 us slower; 6 for the
+  // others: five drafted tokens of eight sessions 1.8 us slower.)
+  const bool light = dt == kBF16 && part_rows <= 16;
+  pages.item_units = light ? 6 : 12;
+  int split = light ? 24 : 14;
   // Sessions that cannot be longer than a split and a little are never split,
   // which saves the second launch (one session of 256 rows: 7.0 us, split 6.9,
   // and 2 us less on the host; 64 sessions 8.4 and 14.8).
-  const long long longest = kPatItem + ((long long)pages.max_pages * pages.page_rows + kPatBlock - 1) / kPatBlock;
-  const int mode = longest <= split + kPmWarps ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
+  const long long longest = ((long long)pages.max_pages * pages.page_rows + kPatBlock - 1) / kPatBlock;
+  const int mode = longest <= (light ? 16 : 6) ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
   if (mode == kWholeItems) split = 1 << 30;
   const int descs = items <= ctas ? (int)items : ctas;
   uint8_t* at = static_cast<uint8_t*>(ws) + kPatHead;
@@ -1172,8 +1180,11 @@ cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* 
       if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || mode == kWholeItems) return;
     }
     TimingScope ts("paged_merge", st);
-    e = launch_after(k_paged_merge<T>, dim3(descs, chunk_rows), kMrgThreads, 0, st, pages, static_cast<T*>(out), n, hq, hkv,
-                     chunks, chunk_rows, part_rows, mode == kDescByItem, desc, part_ml, part_o);
+    const dim3 grid(descs, chunk_rows);
+    const bool few = descs * chunk_rows <= 304;
+    auto kern = few ? k_paged_merge<T, 256> : k_paged_merge<T, 128>;
+    e = launch_after(kern, grid, few ? 256 : 128, 0, st, pages, static_cast<T*>(out), n, hq, hkv, chunks, chunk_rows,
+                     part_rows, mode == kDescByItem, desc, part_ml, part_o);
   };
   std::integral_constant<int, 1> w1;
   std::integral_constant<int, 2> w2;
