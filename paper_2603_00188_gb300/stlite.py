@@ -668,19 +668,22 @@ def paged_attention(q, k_pages, v_pages, pages, stream=None):
 def stlite_compact_paged(layers, budget, pages, seq, stream=None):
     """The kept rows of every layer into sequence seq's pages; layers: list
     of (k, v, k_pages, v_pages, idx)."""
-    k0 = layers[0][0]
+    k0, v0, kp0, vp0, ix0 = layers[0]
     shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
     n, hkv, d = shape
-    want, kept = (*pages._pool, hkv, d), (hkv, budget)
+    want = (*pages._pool, hkv, d)
+    if (v0.shape != shape or kp0.shape != want or vp0.shape != want or ix0.shape != (hkv, budget)
+            or not v0.dtype == kp0.dtype == vp0.dtype == dtype or ix0.dtype != torch.int32):
+        raise ValueError("k and v are [N][Hkv][128], pools %s of their type and idx int32 [Hkv][budget]" % (want,))
     if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
         raise ValueError(_ELSEWHERE)
+    # the layers are alike: each tensor is as large as the first layer's
+    rows, pool, index = k0.nbytes, kp0.nbytes, ix0.nbytes
     for k, v, kp, vp, ix in layers:
-        if (k.shape != shape or v.shape != shape or kp.shape != want or vp.shape != want or ix.shape != kept
-                or not k.dtype == v.dtype == kp.dtype == vp.dtype == dtype or ix.dtype != torch.int32
-                or not (k.is_contiguous() and v.is_contiguous() and kp.is_contiguous() and vp.is_contiguous()
-                        and ix.is_contiguous())):
-            raise ValueError("k and v are [N][Hkv][128], pools %s of their type, idx int32 [Hkv][budget], all "
-                             "contiguous" % (want,))
+        if not (k.nbytes == rows == v.nbytes and kp.nbytes == pool == vp.nbytes and ix.nbytes == index
+                and k.is_contiguous() and v.is_contiguous() and kp.is_contiguous() and vp.is_contiguous()
+                and ix.is_contiguous()):
+            raise ValueError("every layer's tensors are contiguous and as the first layer's")
         if not k.get_device() == kp.get_device() == vp.get_device() == ix.get_device() == dev or (
                 v.get_device() != dev and not v.is_pinned()):
             raise ValueError(_ELSEWHERE)

@@ -258,6 +258,26 @@ def test_compact_paged_matches_dense(st, n, budget, hkv, page, dtype, layers):
             assert torch.equal(pool, written)
 
 
+def test_compact_paged_refuses_unlike_layers(st):
+    def layer(n=20, hkv=2, pages=4, dtype=BF, budget=5):
+        k = torch.zeros((n, hkv, 128), dtype=dtype, device="cuda")
+        kp = torch.zeros((pages, 8, hkv, 128), dtype=dtype, device="cuda")
+        return k, k.clone(), kp, kp.clone(), torch.zeros((hkv, budget), dtype=I32, device="cuda")
+
+    pg = st.make_pages(4, 8, torch.zeros((1, 2), dtype=I32, device="cuda"))
+    st.stlite_compact_paged([layer(), layer()], 5, pg, 0)
+    good = layer()
+    bad = [layer(n=19), layer(pages=3), layer(budget=4), layer(hkv=1), (good[0].cpu(), *good[1:]),
+           (good[0], good[1].cpu(), *good[2:]), (*good[:4], good[4].cpu()),
+           (good[0].transpose(0, 1).contiguous().transpose(0, 1), *good[1:])]
+    for other in bad:
+        for io in ([layer(), other], [other, layer()]):
+            with pytest.raises((ValueError, st.StliteError)):
+                st.stlite_compact_paged(io, 5, pg, 0)
+    with pytest.raises(st.StliteError):
+        st.stlite_compact_paged([layer(n=20, budget=17)], 17, pg, 0)  # the sequence's table has 16 rows
+
+
 def test_compact_paged_leaves_bad_rows_and_reads_host_values(st):
     g = _gen(1)
     k = _randn(g, 40, 2, 128)
