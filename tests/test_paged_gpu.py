@@ -382,6 +382,21 @@ def test_attention_ragged(st, dtype, rows, new, w):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("seqs,most,hq,hkv,w,page", [(330, 60, 4, 4, 1, 16), (700, 35, 2, 2, 2, 7), (250, 300, 8, 8, 1, 64),
+                                                     (1300, 16, 14, 1, 1, 16), (64, 900, 8, 4, 1, 32)])
+def test_attention_many_short(st, dtype, seqs, most, hq, hkv, w, page):
+    """So many sessions that items are not split, or are a warp's each; idle ones and ones without a token among them."""
+    r = random.Random(seqs)
+    rows = [r.choice([0, 1, r.randint(1, most), r.randint(1, most), most]) for _ in range(seqs)]
+    new = [r.randint(0, w) if w > 1 else 1 for _ in range(seqs)]
+    cu = [sum(new[:i]) for i in range(seqs + 1)]
+    q, kp, vp, pg, table = _attention_case(st, rows, cu, page, hq, hkv, dtype, seqs, w)
+    out, ws = _attend(st, q, kp, vp, pg)
+    _check(out, q, kp, vp, table, rows, cu, w)
+    assert st.stlite_device_status(ws) == st.STLITE_OK
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_long_and_last_rows_count(st, dtype):
     """Long caches of several sequences; large values in the first and the last row alone."""
     rows, hq, hkv = [20011, 7003, 1], 8, 2
