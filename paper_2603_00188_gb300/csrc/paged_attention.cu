@@ -438,13 +438,17 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
         }
       }
     } else {
-      for (int e = tid; e < kRows * 16; e += kPmThreads) {
-        const int x = e >> 4, r = row0 + x, t = cur.w.first + r / G;
-        uint4 y = make_uint4(0, 0, 0, 0);
+      uint4 y[NT];  // a thread's chunks of the chunk's queries, loaded together
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int x = 8 * i + (tid >> 4), r = row0 + x, t = cur.w.first + r / G;
+        y[i] = make_uint4(0, 0, 0, 0);
         if (x < rows && t >= 0 && t < n)
-          y = reinterpret_cast<const uint4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[e & 15];
-        *reinterpret_cast<uint4*>(sm + pm_ring(NT) + pm_off(x, e & 15)) = y;
+          y[i] = reinterpret_cast<const uint4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[tid & 15];
       }
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        *reinterpret_cast<uint4*>(sm + pm_ring(NT) + pm_off(8 * i + (tid >> 4), tid & 15)) = y[i];
       __syncthreads();
     }
     // Running state: raw maximum and the lane's part of the sum of queries
@@ -821,12 +825,17 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       else if (!whole)
         desc[cta] = d;
     }
-    for (int e = tid; e < GM * (kD / 4); e += kPmThreads) {
-      const int x = e / (kD / 4), r = row0 + x, t = cur.w.first + r / G;
-      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (x < rows && t >= 0 && t < n)
-        y = reinterpret_cast<const float4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[e % (kD / 4)];
-      reinterpret_cast<float4*>(qs)[e] = y;
+    {
+      float4 y[GM / 4];
+#pragma unroll
+      for (int i = 0; i < GM / 4; ++i) {
+        const int x = 4 * i + warp, r = row0 + x, t = cur.w.first + r / G;
+        y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (x < rows && t >= 0 && t < n)
+          y[i] = reinterpret_cast<const float4*>(q + ((size_t)t * hq + h * G + r % G) * kD)[lane];
+      }
+#pragma unroll
+      for (int i = 0; i < GM / 4; ++i) reinterpret_cast<float4*>(qs + (4 * i + warp) * kD)[lane] = y[i];
     }
     __syncthreads();
     float m[kSets], l[kSets], o[GM][4];  // raw maximum and the lane's part of the sum of its queries
