@@ -312,6 +312,46 @@ def test_compress_into_pages_equals_dense(st, make):
     assert st.stlite_device_status(ws) == st.STLITE_OK
 
 
+def test_compress_into_pages_captured(st):
+    """The fused pass into two sequences' pages, 34 layers, captured and replayed on new contents."""
+    wl = synth.scaled("traj50", 2, beta=0.2)
+    q, k, v = to_device(wl)
+    prm, b, hkv = st.make_params(wl.beta), st.stlite_budget(k.shape[0], wl.beta), k.shape[1]
+    table, pages = _table([b, b], 16, 4)
+    pg = st.make_pages(pages, 16, table.cuda())
+    layers = 34
+    ks, vs = (torch.stack([x] * layers) for x in (k, v))
+    kp, vp = (torch.zeros((layers, pages, 16, hkv, 128), dtype=BF, device="cuda") for _ in range(2))
+    idx = torch.empty((layers, hkv, (b + 3) // 4 * 4), dtype=I32, device="cuda")  # every layer's on 16 bytes
+    io = [(q, ks[l], vs[l], kp[l], vp[l], idx[l]) for l in range(layers)]
+    ws = torch.zeros(layers * st.stlite_workspace_size(st.make_shape(q, k), wl.frames, prm), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def both(stream):
+        for seq in (0, 1):
+            st.stlite_compress_layers_paged(io, wl.frames, prm, pg, seq, ws, stream)
+
+    both(side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        both(side)
+    for l in range(layers):
+        ks[l].copy_(k.roll(l, 0))
+        vs[l].copy_(v.roll(l, 0))
+    kp.zero_()
+    vp.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for l in (0, 1, 31, 32, 33):
+        ko, vo, _ = st.compress_layer(q, ks[l], vs[l], wl.frames, beta=wl.beta)
+        for seq in (0, 1):
+            assert torch.equal(ref.rows_of(kp[l], table[seq], b), ko)
+            assert torch.equal(ref.rows_of(vp[l], table[seq], b), vo)
+    assert st.stlite_device_status(ws) == st.STLITE_OK
+
+
 # ----------------------------------------------------------------- attention
 
 def _attention_case(st, rows, cu, page, hq, hkv, dtype, seed, w=None, scale=1.0, garbage=float("nan")):
