@@ -231,6 +231,9 @@ __device__ __forceinline__ void cp_async_wait() {
 // is warp u % kPmWarps's.
 constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
 constexpr int kPmCtas = 2;  // per SM
+// Whether kPmCtas CTAs of so much dynamic shared memory share an SM's 228 KB
+// (1 KB of it each is reserved).
+__host__ __device__ constexpr bool fits_sm(int smem) { return kPmCtas * ((smem + 127) / 128 * 128 + 1024) <= 228 * 1024; }
 __device__ __forceinline__ int warps_first(int u, int warp) { return u + ((warp - u) & (kPmWarps - 1)); }
 struct RowFinder {
   Cursor at;
@@ -294,7 +297,7 @@ __device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int 
 // 152 us (6.4 TB/s with start and merge; the copies without the products take
 // the same time, so HBM bounds it; four warps and two CTAs per SM 155 where
 // eight and one take 160); one session of 10,757 rows 10.3 us, all latency.  16
-// sessions of 25,000 rows: 6.3 TB/s with 7 or 14 queries, 5.8 with 21, 5.2 with
+// sessions of 25,000 rows: 6.3 TB/s with 7 or 14 queries, 6.0 with 21, 5.3 with
 // 28, bound by the products' latency at two warps per scheduler.
 constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
@@ -302,10 +305,14 @@ __host__ __device__ constexpr int pm_stages(int nt) { return nt == 1 ? 3 : 2; }
 __host__ __device__ constexpr int pm_ring(int nt) { return kPmWarps * pm_stages(nt) * 2 * kPmHalf; }
 __host__ __device__ constexpr int pm_queries(int nt) { return nt > 2 ? 8 * nt * kD * 2 : 0; }
 __host__ __device__ constexpr int pm_pass(int nt) { return nt > 2 ? 2 : nt; }  // groups merged at a time
-__host__ __device__ constexpr int pm_smem(int nt) {
-  return pm_ring(nt) + pm_queries(nt) + kPmWarps * 8 * (pm_pass(nt) * kPmPitch * 4 + nt * 8) +
-         (int)sizeof(RangeScratch<kPmThreads>) + 8 * nt * 4;
+__host__ __device__ constexpr int pm_factors(int nt) {
+  return 8 * nt * 4 * (1 + kPmWarps) > (int)sizeof(RangeScratch<kPmThreads>) ? 8 * nt * 4 * (1 + kPmWarps)
+                                                                            : (int)sizeof(RangeScratch<kPmThreads>);
 }
+__host__ __device__ constexpr int pm_smem(int nt) {
+  return pm_ring(nt) + pm_queries(nt) + kPmWarps * 8 * (pm_pass(nt) * kPmPitch * 4 + nt * 8) + pm_factors(nt);
+}
+static_assert(fits_sm(pm_smem(1)) && fits_sm(pm_smem(2)) && fits_sm(pm_smem(3)) && fits_sm(pm_smem(4)), "kPmCtas per SM");
 
 __device__ __forceinline__ void pm_ldsm_x4(uint32_t addr, uint32_t (&a)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -353,7 +360,10 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   float* wo = reinterpret_cast<float*>(sm + pm_ring(NT) + pm_queries(NT));
   float2* wml = reinterpret_cast<float2*>(wo + kPmWarps * 8 * kPass * kPmPitch);
   RangeScratch<kPmThreads>* scratch = reinterpret_cast<RangeScratch<kPmThreads>*>(wml + kPmWarps * kRows);
-  float* inv = reinterpret_cast<float*>(scratch + 1);  // [kRows] 1 / sum
+  // once an item has ended (the range was found long before): 1 / sum of each
+  // query, and the warps' factors
+  float* inv = reinterpret_cast<float*>(scratch);  // [kRows]
+  float* factor = inv + kRows;                     // [warps][kRows]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
   const int G = hq / hkv, cta = blockIdx.x;
   const uint32_t ring = smem_u32(sm) + warp * kStages * 2 * kPmHalf;
@@ -637,17 +647,25 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
       }
     __syncthreads();
     const int part = 2 * cta + (owns ? 1 : 0);
-    if (tid < rows) {  // each query's maximum and sum over the warps
-      float M = -CUDART_INF_F, L = 0.f;
+    // a thread for each warp's query: its factor, and, from the first warp's
+    // thread, the query's maximum and sum over the warps
+    for (int e = tid; e < kPmWarps * kRows; e += kPmThreads) {
+      const int x = e % kRows;
+      float M = -CUDART_INF_F;
 #pragma unroll
-      for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + tid].x);
+      for (int w = 0; w < kPmWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
+      factor[e] = pat_weight(wml[e].x, M);
+      if (e < rows) {
+        float L = 0.f;
 #pragma unroll
-      for (int w = 0; w < kPmWarps; ++w) L = fmaf(wml[w * kRows + tid].y, pat_weight(wml[w * kRows + tid].x, M), L);
-      if (whole)
-        inv[tid] = L == 0.f ? 0.f : 1.f / L;
-      else
-        part_ml[part * kRows + tid] = make_float2(M, L);
+        for (int w = 0; w < kPmWarps; ++w) L = fmaf(wml[w * kRows + x].y, pat_weight(wml[w * kRows + x].x, M), L);
+        if (whole)
+          inv[x] = L == 0.f ? 0.f : 1.f / L;
+        else
+          part_ml[part * kRows + x] = make_float2(M, L);
+      }
     }
+    __syncthreads();
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += kPass) {
       if (n0 > 0) __syncthreads();  // the buffer is free again
@@ -656,10 +674,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 #pragma unroll
         for (int e = 0; e < 2 && n0 + i < NT; ++e) {
           const int x = 8 * i + 2 * t4 + e;
-          float M = -CUDART_INF_F;
-#pragma unroll
-          for (int y = 0; y < kPmWarps; ++y) M = fmaxf(M, wml[y * kRows + 8 * n0 + x].x);
-          const float a = pat_weight(m[n0 + i][e] * scale, M);
+          const float a = factor[warp * kRows + 8 * n0 + x];
           float* w = wo + (warp * 8 * kPass + x) * kPmPitch + g8;
 #pragma unroll
           for (int mt = 0; mt < 8; ++mt) {
@@ -724,6 +739,7 @@ __host__ __device__ constexpr int pf_shared(int gm) {
 __host__ __device__ constexpr int pf_smem(int gm) {
   return pf_ring() + gm * kD * 4 + pf_shared(gm) + kPmWarps * gm * 8 + (int)sizeof(RangeScratch<kPmThreads>);
 }
+static_assert(fits_sm(pf_smem(4)) && fits_sm(pf_smem(8)) && fits_sm(pf_smem(16)), "kPmCtas per SM");
 
 // The sums over eight neighbouring lanes of s[row][query]: lane c of them is
 // left with query c % Q's, rows 0 .. 3 for Q = 8, rows 2 (c / 4) + 0, 1 for Q = 4.
