@@ -104,12 +104,12 @@ __device__ __forceinline__ int token_slot(const PageView& pg, int t) {
   return page_slot(pg, lo + k, row);
 }
 
-// One warp per unit: segment `u % segs` of the head groups of token u / segs.
+// One warp per unit: segment `u % segs`, of `each` head groups, of token u / segs.
 template <typename T, int NB, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ TokenView x,
                                                         const __grid_constant__ RopeView rope,
                                                         const __grid_constant__ PageView pg, T* q_out, T* k_out,
-                                                        T* v_out, int groups, int segs) {
+                                                        T* v_out, int groups, int each, int segs) {
   __shared__ uint64_t turn[kD / 2];
   // [warp][four of a lane's eight pairs][lane][pair], so that eight lanes' vectors are adjacent
   __shared__ float4 cs[kRotWarps][2][8], sn[kRotWarps][2][8];
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
   const int u = blockIdx.x * kRotWarps + warp, t = u / segs, seg = u - t * segs;
   if (t >= x.n) return;
   const int total = x.hq + (PAGED ? 2 : 1) * x.hkv;
-  const int g0 = groups * seg / segs, g1 = groups * (seg + 1) / segs;
+  const int g0 = seg * each, g1 = min(g0 + each, groups);
   const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
   const int end = PAGED && pg.cu ? pg.cu[pg.n_seqs] : x.n;
   Vec8<T> va[NB], vb[NB];
@@ -221,6 +221,7 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
   if (segs < (groups + most - 1) / most) segs = (groups + most - 1) / most;
   if (segs > groups) segs = groups;
   const int each = (int)((groups + segs - 1) / segs);
+  segs = (groups + each - 1) / each;
   const dim3 grid((unsigned)((x.n * segs + kRotWarps - 1) / kRotWarps));
   const PageView pg = pages ? *pages : PageView{};
   TimingScope ts(pages ? "paged_append" : "rotate_qk", st);
@@ -231,7 +232,7 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
     T *qo = static_cast<T*>(q_out), *ko = static_cast<T*>(k_out), *vo = static_cast<T*>(v_out);
     auto kern = rope.interleaved ? (pages ? k_rotate<T, NB, true, true> : k_rotate<T, NB, true, false>)
                                  : (pages ? k_rotate<T, NB, false, true> : k_rotate<T, NB, false, false>);
-    e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, groups, (int)segs);
+    e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, groups, each, (int)segs);
   };
   auto pick = [&](auto zero) {
     if (each <= 1)
@@ -252,7 +253,7 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
 // k_gather with the kept rows going to a sequence's pages: a thread moves one
 // 16-byte chunk of a key and of a value, CPR of them to a head's row, so that
 // consecutive threads write consecutive chunks.  The bytes moved bound it: at
-// 28 layers of 10,720 rows it copies at 0.94 of the rate of a plain copy (194
+// 28 layers of 10,720 rows it copies at 0.98 of the rate of a plain copy (186
 // us; four chunks to a thread, all loads first, 208; the same in a loop over a
 // grid of eight CTAs per SM 234: such threads all read, then all write).
 template <int CPR>

@@ -92,6 +92,34 @@ def test_rotate_at_far_positions(st):
             ref.within(got, r, b)
 
 
+@pytest.mark.parametrize("section", [(0, 64, 0), (0, 0, 64), (1, 62, 1), (63, 0, 1), (32, 32, 0)])
+def test_rotate_sections(st, section):
+    """Any division of the pairs among the axes, empty ones too."""
+    g = _gen(11)
+    q, k = _randn(g, 9, 3, 128), _randn(g, 9, 1, 128)
+    pos = torch.randint(-50, 5000, (3, 9), generator=g, dtype=I32)
+    for interleaved in (False, True):
+        qo, ko = st.rotate_qk(q, k, pos.cuda(), st.make_rope(1e4, section, interleaved))
+        for got, src in ((qo, q), (ko, k)):
+            r, b = ref.rotate(src, pos, ref.default_freq(1e4), section, interleaved)
+            ref.within(got, r, b)
+
+
+def test_rotate_very_many_heads(st):
+    """One token of more heads than the square of a 16-bit number's groups: the same as as many tokens of one head."""
+    hq, hkv = 100 * 4096, 4096
+    q, k = (torch.randn((1, h, 128), generator=torch.Generator("cuda").manual_seed(h), device="cuda").to(BF) for h in (hq, hkv))
+    pos = _ints([4321])
+    qo, ko = st.rotate_qk(q, k, pos, st.make_rope())
+    for src, got in ((q, qo), (k, ko)):
+        x = src[0, ::1024, None].contiguous()
+        want, _ = st.rotate_qk(x, x, pos.repeat(x.shape[0]), st.make_rope())
+        assert torch.equal(got[0, ::1024, None], want)
+    part = slice(hq - 3000, hq)  # whole, at the far end
+    x = q[0, part, None].contiguous()
+    assert torch.equal(qo[0, part, None], st.rotate_qk(x, x, pos.repeat(3000), st.make_rope())[0])
+
+
 def test_rotate_in_place_and_extremes(st):
     g = _gen(8)
     q, k = _randn(g, 50, 12, 128), _randn(g, 50, 2, 128)
