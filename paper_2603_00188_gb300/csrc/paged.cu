@@ -19,10 +19,10 @@ namespace stl {
 // that a warp holds four heads.  A warp takes up to NB such groups of a token's
 // heads, all loaded before anything else, and meanwhile forms the token's 64
 // sines and cosines, two to a lane, exchanged through shared memory.  The bytes
-// moved bound it: 8,576 tokens of 28 + 4 bf16 heads take 22.6 us (6.2 TB/s, 0.92
+// moved bound it: 8,576 tokens of 28 + 4 bf16 heads take 22.3 us (6.3 TB/s, 0.93
 // of a plain copy's rate; groups of a loop without loading ahead 27.1, eight
 // groups ahead 22.8, a CTA to 32 heads with shared sines 29.8), 8,616 tokens
-// with 4 value heads into pages 26.8 (eight groups 34.0, four 29.2).
+// with 4 value heads into pages 26.0 (eight groups 34.0, four 27.2, two 28.0).
 constexpr int kRotThreads = 128, kRotWarps = kRotThreads / 32;
 constexpr int kRotHeads = 4;   // heads of a group
 
@@ -104,12 +104,13 @@ __device__ __forceinline__ int token_slot(const PageView& pg, int t) {
   return page_slot(pg, lo + k, row);
 }
 
-// One warp per unit: segment `u % segs`, of `each` head groups, of token u / segs.
+// One warp per unit: segment `u % segs` of the head groups of token u / segs, `base` of them or, in the first
+// `extra` segments, one more.
 template <typename T, int NB, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ TokenView x,
                                                         const __grid_constant__ RopeView rope,
                                                         const __grid_constant__ PageView pg, T* q_out, T* k_out,
-                                                        T* v_out, int groups, int each, int segs) {
+                                                        T* v_out, int base, int extra, int segs) {
   __shared__ uint64_t turn[kD / 2];
   // [warp][four of a lane's eight pairs][lane][pair], so that eight lanes' vectors are adjacent
   __shared__ float4 cs[kRotWarps][2][8], sn[kRotWarps][2][8];
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
   const int u = blockIdx.x * kRotWarps + warp, t = u / segs, seg = u - t * segs;
   if (t >= x.n) return;
   const int total = x.hq + (PAGED ? 2 : 1) * x.hkv;
-  const int g0 = seg * each, g1 = min(g0 + each, groups);
+  const int g0 = seg * base + min(seg, extra), g1 = g0 + base + (seg < extra);
   const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
   const int end = PAGED && pg.cu ? pg.cu[pg.n_seqs] : x.n;
   Vec8<T> va[NB], vb[NB];
@@ -214,14 +215,12 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
 cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, const PageView* pages, void* q_out,
                           void* k_out, void* v_out, cudaStream_t st) {
   const int groups = (x.hq + (pages ? 2 : 1) * x.hkv + kRotHeads - 1) / kRotHeads;
-  // groups of a warp: three, fewer where there are few tokens for the GPU's SMs
-  // (1,152 fp32 tokens: 7.4 us; at 16 warps per SM instead of 32 7.7)
+  // groups of a warp: three, fewer where there are few tokens: 32 warps for each SM
   constexpr int most = 3;
   long long segs = (152 * 32 + x.n - 1) / x.n;
   if (segs < (groups + most - 1) / most) segs = (groups + most - 1) / most;
   if (segs > groups) segs = groups;
-  const int each = (int)((groups + segs - 1) / segs);
-  segs = (groups + each - 1) / each;
+  const int base = (int)(groups / segs), extra = (int)(groups % segs), each = base + (extra > 0);
   const dim3 grid((unsigned)((x.n * segs + kRotWarps - 1) / kRotWarps));
   const PageView pg = pages ? *pages : PageView{};
   TimingScope ts(pages ? "paged_append" : "rotate_qk", st);
@@ -232,7 +231,7 @@ cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, co
     T *qo = static_cast<T*>(q_out), *ko = static_cast<T*>(k_out), *vo = static_cast<T*>(v_out);
     auto kern = rope.interleaved ? (pages ? k_rotate<T, NB, true, true> : k_rotate<T, NB, true, false>)
                                  : (pages ? k_rotate<T, NB, false, true> : k_rotate<T, NB, false, false>);
-    e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, groups, each, (int)segs);
+    e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, base, extra, (int)segs);
   };
   auto pick = [&](auto zero) {
     if (each <= 1)
