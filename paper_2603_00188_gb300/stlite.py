@@ -639,20 +639,21 @@ def paged_workspace(q, k_pages, pages):
 def stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream=None):
     """Attention of the new tokens q [T][Hq][128] over their sequences'
     pages into out (q's shape and type)."""
-    shape, dtype, dev, pool = q.shape, q.dtype, q.get_device(), k_pages.shape
-    if len(shape) != 3 or shape[2] != 128 or not q.is_contiguous():
+    (n, hq, d), dtype, dev = q.shape, q.dtype, q.get_device()
+    if d != 128 or not q.is_contiguous():
         raise ValueError("q is a contiguous [T][Hq][128]")
-    if out.shape != shape or out.dtype != dtype or not out.is_contiguous():
-        raise _output_error(shape)
-    if (len(pool) != 4 or pool != (*pages._pool, pool[2], 128) or v_pages.shape != pool or k_pages.dtype != dtype
-            or v_pages.dtype != dtype or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
+    if out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
+        raise _output_error(q.shape)
+    p, r, hkv, d = k_pages.shape
+    if ((p, r) != pages._pool or d != 128 or k_pages.dtype != dtype or v_pages.dtype != dtype
+            or v_pages.nbytes != k_pages.nbytes or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
         raise _pool_error(pages, "Hkv")
     if dev < 0 or not (torch._C._cuda_getDevice() == dev == k_pages.get_device() == v_pages.get_device()
                        == out.get_device() == ws.get_device() == pages._device):
         raise ValueError(_ELSEWHERE)
     st = _lib.stlite_paged_attention(
-        _SHAPE.pack(shape[0], shape[1], pool[2], 128, pages.max_new, _DTYPE[dtype]), pages._address, q.data_ptr(),
-        k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
+        _SHAPE.pack(n, hq, hkv, 128, pages.max_new, _DTYPE[dtype]), pages._address, q.data_ptr(), k_pages.data_ptr(),
+        v_pages.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.nbytes,
         _CURRENT(dev) if stream is None else stream.cuda_stream)
     if st != STLITE_OK:
         raise StliteError(st, "stlite_paged_attention")
