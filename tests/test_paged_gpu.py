@@ -420,7 +420,7 @@ def _check(out, q, kp, vp, table, rows, cu, w=None, **kw):
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("hq,hkv,page", [(28, 4, 16), (12, 2, 64), (16, 1, 7), (3, 3, 1), (40, 8, 24), (9, 1, 100)])
 @pytest.mark.parametrize("rows,new", [([1], 1), ([257], 1), ([1000, 3, 0, 64, 65, 15, 16, 17], 1),
-                                      ([5, 2, 300], 4), ([129, 40], 8)])
+                                      ([5, 2, 300], 4), ([129, 40], 8), ([33, 300], 16)])
 def test_attention_matches(st, dtype, hq, hkv, page, rows, new):
     cu = [new * i for i in range(len(rows) + 1)]
     q, kp, vp, pg, table = _attention_case(st, rows, cu, page, hq, hkv, dtype, sum(rows) + page)
