@@ -591,6 +591,21 @@ def test_attention_repeats_its_bits(st):
         assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,hkv,new", [([9000, 40], 2, 1), ([300] * 200, 2, 1), ([700, 0, 5000], 1, 5)])
+def test_attention_workspace_of_others(st, dtype, rows, hkv, new):
+    """Behind the error word a workspace may hold anything: other calls on the stream share it."""
+    cu = [new * i for i in range(len(rows) + 1)]
+    q, kp, vp, pg, _ = _attention_case(st, rows, cu, 16, 7 * hkv, hkv, dtype, hkv + new)
+    want, ws = _attend(st, q, kp, vp, pg)
+    for fill in (0xff, 0x01, 0x7f):
+        ws[256:] = fill
+        out = torch.full_like(q, 11)
+        st.stlite_paged_attention(q, kp, vp, pg, out, ws)
+        assert torch.equal(out, want)
+    assert st.stlite_device_status(ws) == st.STLITE_OK
+
+
 def test_attention_on_a_side_stream_and_in_graphs(st):
     """A call on a stream of its own; one capture replayed as the cache grows; two captures sharing a workspace."""
     rows = [40, 700]
