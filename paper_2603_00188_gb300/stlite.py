@@ -5,6 +5,13 @@ Every function here has the name of the C entry point it calls (declared in
 on the current torch stream.  No computation happens in Python: if the
 library is not built this module raises at import time.
 
+A function's ``stream`` is the torch stream to run on in place of the current
+one.  The entry points take it as the library does: ordering it behind the
+streams that fill the tensors, and keeping their memory until it is done, is
+the caller's.  The helpers that allocate (``compress_layer``,
+``decode_attention``, ``rotate_qk`` and the like) do both; reading their
+results on another stream still waits for ``stream``.
+
     from paper_2603_00188_gb300 import stlite
     k_out, v_out, idx = stlite.compress_layer(q, k, v, frames, beta=0.2)
 """
@@ -176,6 +183,20 @@ def _stream(stream):
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
+
+
+def _lend(stream, *tensors):
+    """What a helper that allocates does before its call on a `stream` that is
+    not the current one: `stream` waits for what the current one holds so far
+    (the tensors' contents, a workspace's zeros, an earlier user of an
+    output's memory), and the device tensors' memory is not given out again
+    before `stream` has used it."""
+    if stream is None or stream == torch.cuda.current_stream():
+        return
+    stream.wait_stream(torch.cuda.current_stream())
+    for t in tensors:
+        if t is not None and t.is_cuda:
+            t.record_stream(stream)
 
 
 _DTYPE = {torch.bfloat16: STLITE_BF16, torch.float32: STLITE_F32}
@@ -419,6 +440,7 @@ def decode_attention(q, k, v, stream=None):
     sh = make_shape(q, k)
     ws = torch.zeros(stlite_decode_workspace_size(sh), dtype=torch.uint8, device=k.device)
     out = torch.empty(q.shape, dtype=torch.float32, device=k.device)
+    _lend(stream, q, k, v, out, ws)
     stlite_decode_attention(q, k, v, out, ws, stream)
     return out
 
@@ -452,6 +474,7 @@ def prompt_score(q_prompt, k, base=STLITE_PROMPT_MEAN, stream=None):
     sh = prompt_shape(q_prompt, k)
     ws = torch.zeros(stlite_prompt_workspace_size(sh, q_prompt.shape[0]), dtype=torch.uint8, device=k.device)
     a = torch.empty((sh.n_kv_heads, sh.n_tokens), dtype=torch.float32, device=k.device)
+    _lend(stream, q_prompt, k, a, ws)
     stlite_prompt_score(q_prompt, k, base, a, ws, stream)
     return a, ws
 
@@ -478,6 +501,7 @@ def decode_attention_layers(qs, ks, vs, stream=None):
     sh = make_shape(qs[0], ks[0])
     ws = torch.zeros(stlite_decode_layers_workspace_size(sh, len(qs)), dtype=torch.uint8, device=ks[0].device)
     outs = [torch.empty(q.shape, dtype=torch.float32, device=ks[0].device) for q in qs]
+    _lend(stream, *qs, *ks, *vs, *outs, ws)
     stlite_decode_attention_layers(list(zip(qs, ks, vs, outs)), ws, stream)
     return outs, ws
 
@@ -589,6 +613,7 @@ def rotate_qk(q, k, pos, rope, q_norm=None, k_norm=None, eps=1e-6, stream=None):
     """Allocates the outputs and runs stlite_rotate_qk."""
     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _lend(stream, q, k, pos, q_norm, k_norm, q_out, k_out)
     stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm, k_norm, eps, stream)
     return q_out, k_out
 
@@ -661,8 +686,9 @@ def stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream=None):
 
 def paged_attention(q, k_pages, v_pages, pages, stream=None):
     """Allocates the output and the workspace and runs stlite_paged_attention."""
-    out = torch.empty_like(q)
-    stlite_paged_attention(q, k_pages, v_pages, pages, out, paged_workspace(q, k_pages, pages), stream)
+    out, ws = torch.empty_like(q), paged_workspace(q, k_pages, pages)
+    _lend(stream, q, k_pages, v_pages, pages.table, pages.length, pages.cu_new, out, ws)
+    stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream)
     return out
 
 
@@ -770,5 +796,6 @@ def compress_layer(q, k, v, frames, beta=0.2, k_override=0, alpha=1.0, tsg_enabl
     k_out = torch.empty((b, sh.n_kv_heads, sh.head_dim), dtype=k.dtype, device=k.device)
     v_out = torch.empty_like(k_out)
     idx = torch.empty((sh.n_kv_heads, b), dtype=torch.int32, device=k.device)
+    _lend(stream, q, k, v, ws, k_out, v_out, idx)
     stlite_compress_layer(q, k, v, fs, params, k_out, v_out, idx, ws, stream)
     return k_out, v_out, idx
