@@ -490,7 +490,9 @@ STLITE_API stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlit
  * not written (its q_out is).  Rows that two sequences share are not to be
  * written by both.  q_out may be x->q where that is packed.
  * shape: n_tokens = T; window = tokens of each sequence where cu_new is NULL
- *   (any number >= 1; otherwise not used). */
+ *   (any number >= 1; otherwise not used).  T = 0 (a step without a token,
+ *   cu_new given): x, q_out and the pools are not looked at and nothing is
+ *   enqueued. */
 STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope,
                                              const stlite_tokens* x, const stlite_pages* pages, void* q_out,
                                              void* k_pages, void* v_pages, void* stream);
@@ -510,7 +512,7 @@ STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const st
  *   Hq / Hkv <= 16; n_pages * page_rows * Hkv, and n_seqs * Hkv *
  *   ceil(window * (Hq / Hkv) / 16) * (max_pages * page_rows / 16 + 13), below 2^31.
  * q, out [T][Hq][d] (shape->dtype), packed; rows behind cu_new[S] are left
- *   alone.  ws: at least stlite_paged_workspace_size bytes, zero-filled before
+ *   alone.  T = 0: as for stlite_paged_append.  ws: at least stlite_paged_workspace_size bytes, zero-filled before
  *   its first use (its first word is the error word of
  *   stlite_device_status).  The work is divided over the GPU by the lengths as
  *   they are when the kernels run, so one capture serves growing caches. */

@@ -1025,13 +1025,21 @@ stlite_status check_pages(const stlite_pages* pg, bool need_len) {
   return STLITE_OK;
 }
 
-// The shape of calls whose window is a number of tokens, not of an observation
+// check_shape for a serving step's packed tokens, of which there may be none.
+stlite_status check_step_shape(const stlite_shape* shape) {
+  if (!shape || shape->n_tokens < 0) return STLITE_EINVAL;
+  stlite_shape s = *shape;
+  if (s.n_tokens == 0) s.n_tokens = 1;
+  return check_shape(&s);
+}
+
+// The same for calls whose window is a number of tokens, not of an observation
 // window's queries: any number.
 stlite_status check_token_shape(const stlite_shape* shape) {
   if (!shape || shape->window < 1) return STLITE_EINVAL;
   stlite_shape s = *shape;
   s.window = 1;
-  return check_shape(&s);
+  return check_step_shape(&s);
 }
 
 // Without cu_new every sequence has w new tokens.
@@ -1135,7 +1143,7 @@ bool in_place_ok(const void* in, long long stride, int heads, const void* out) {
 }
 
 stlite_status check_paged_attention(const stlite_shape* shape, const stlite_pages* pages) {
-  stlite_status s = check_shape(shape);
+  stlite_status s = check_step_shape(shape);
   if (s != STLITE_OK) return s;
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
@@ -1167,6 +1175,7 @@ stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rop
                                void* q_out, void* k_out, void* stream) {
   stlite_status s = check_token_shape(shape);
   if (s != STLITE_OK) return s;
+  if (shape->n_tokens == 0) return STLITE_EINVAL;  // a prompt has tokens
   TokenView v;
   if ((s = token_view(shape, rope, x, false, &v)) != STLITE_OK) return s;
   if (!q_out || !k_out || !aligned16(q_out) || !aligned16(k_out)) return STLITE_EINVAL;
@@ -1183,6 +1192,8 @@ stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* 
   if (s != STLITE_OK) return s;
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
+  if ((s = check_rope(rope)) != STLITE_OK) return s;
+  if (shape->n_tokens == 0) return STLITE_OK;
   TokenView v;
   if ((s = token_view(shape, rope, x, true, &v)) != STLITE_OK) return s;
   if (!q_out || !k_pages || !v_pages || !aligned16(q_out) || !aligned16(k_pages) || !aligned16(v_pages))
@@ -1205,7 +1216,7 @@ stlite_status stlite_paged_attention(const stlite_shape* shape, const stlite_pag
                                      const void* k_pages, const void* v_pages, void* out, void* ws, size_t ws_bytes,
                                      void* stream) {
   const stlite_status s = check_paged_attention(shape, pages);
-  if (s != STLITE_OK) return s;
+  if (s != STLITE_OK || shape->n_tokens == 0) return s;
   if (!q || !k_pages || !v_pages || !out || !ws) return STLITE_EINVAL;
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(ws))
     return STLITE_EINVAL;

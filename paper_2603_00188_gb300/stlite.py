@@ -593,7 +593,8 @@ def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype) -> bytes:
 def stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
     """Norm (where weights are given) and rotation of every head of q
     [T][Hq][128] and k [T][Hkv][128] (each may be a slice of one projection's
-    output) into q_out and k_out; pos: int32 [T], or [3][T] for three axes."""
+    output) into q_out and k_out; pos: int32 [T], or [3][T] for three axes.
+    T = 0 does nothing."""
     qs, ks, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
     x = _tokens(q, k, None, pos, rope, q_norm, k_norm, eps, qs, ks, dtype)
     if q_out.shape != qs or q_out.dtype != dtype or not q_out.is_contiguous():
@@ -603,6 +604,8 @@ def stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm=None, k_norm=None, ep
     if dev < 0 or not (torch._C._cuda_getDevice() == dev == k.get_device() == pos.get_device() == q_out.get_device()
                        == k_out.get_device()):
         raise ValueError(_ELSEWHERE)
+    if qs[0] == 0:
+        return
     st = _lib.stlite_rotate_qk(_SHAPE.pack(qs[0], qs[1], ks[1], 128, 1, _DTYPE[dtype]), rope, x, q_out.data_ptr(),
                                k_out.data_ptr(), _CURRENT(dev) if stream is None else stream.cuda_stream)
     if st != STLITE_OK:
