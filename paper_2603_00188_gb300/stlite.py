@@ -582,7 +582,9 @@ def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype) -> bytes:
             if w is not None and w.get_device() != q.get_device():
                 raise ValueError(_ELSEWHERE)
         pq, pk = _ptr(q_norm) or 0, _ptr(k_norm) or 0
-    if pos.dtype != torch.int32 or pos.numel() != (n if rope.section[0] == 64 else 3 * n) or not pos.is_contiguous():
+    one = rope.section[0] == 64
+    if (pos.dtype != torch.int32 or pos.numel() != (n if one else 3 * n) or not pos.is_contiguous()
+            or not (one or pos.dim() == 1 or pos.shape[0] == 3)):
         raise ValueError("pos is a contiguous int32 [T], or [3][T] for three axes")
     if n == 1:  # no next token: whatever its distance would be
         return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, 0, 0, 0, pq, pk, eps, pos.data_ptr())

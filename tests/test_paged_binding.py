@@ -1,0 +1,46 @@
+"""Tensors of the right size and the wrong shape, type or device, which the
+binding of the paged calls refuses before the library sees an address."""
+import pytest
+import torch
+
+from test_paged_abi import st  # noqa: F401  (fixture)
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+DEVICE = "on the current CUDA device"
+
+
+@pytest.fixture
+def anywhere(st, monkeypatch):
+    """The library's calls, which never come; a CPU tensor gets as far as the check of the devices."""
+    for name in ("stlite_paged_append", "stlite_rotate_qk", "stlite_paged_attention", "stlite_compact_paged",
+                 "stlite_compress_layers_paged"):
+        monkeypatch.setattr(st._lib, name, None)
+
+
+def _refused(call, *args, match=None, **kw):
+    with pytest.raises(ValueError, match=match):
+        call(*args, **kw)
+
+
+def test_positions_by_axis(st, anywhere):
+    """Positions of three axes are [3][T] (or as many numbers in one row), not [T][3]."""
+    q, k = torch.zeros((5, 4, 128), dtype=BF), torch.zeros((5, 2, 128), dtype=BF)
+    three, one = st.make_rope(section=(16, 24, 24)), st.make_rope()
+
+    def rotate(pos, rope, match):
+        _refused(st.stlite_rotate_qk, q, k, pos, rope, q.clone(), k.clone(), match=match)
+
+    for shape in ((5, 3), (5, 1, 3), (15, 1), (1, 15), (1, 5, 3)):
+        rotate(torch.zeros(shape, dtype=I32), three, "pos is")
+    for shape in ((3, 5), (15,), (3, 5, 1), (3, 1, 5)):
+        rotate(torch.zeros(shape, dtype=I32), three, DEVICE)
+    for shape in ((5,), (1, 5), (5, 1)):  # one order of five numbers
+        rotate(torch.zeros(shape, dtype=I32), one, DEVICE)
+    for pos in (torch.zeros((3, 5), dtype=I32), torch.zeros(4, dtype=I32)):
+        rotate(pos, one, "pos is")
+    table = torch.zeros((1, 3), dtype=I32)
+    pool = torch.zeros((6, 4, 2, 128), dtype=BF)
+    pages = st.make_pages(6, 4, table, torch.zeros(1, dtype=I32), max_new=5)
+    for shape, match in (((5, 3), "pos is"), ((3, 5), DEVICE)):
+        _refused(st.stlite_paged_append, q, k, k.clone(), torch.zeros(shape, dtype=I32), three, pages, q.clone(), pool,
+                 pool.clone(), match=match)
