@@ -674,9 +674,9 @@ def stlite_paged_attention(q, k_pages, v_pages, pages, out, ws, stream=None):
         raise ValueError("q is a contiguous [T][Hq][128]")
     if out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
         raise _output_error(q.shape)
-    p, r, hkv, d = k_pages.shape
+    p, r, hkv, d = pool = k_pages.shape
     if ((p, r) != pages._pool or d != 128 or k_pages.dtype != dtype or v_pages.dtype != dtype
-            or v_pages.nbytes != k_pages.nbytes or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
+            or v_pages.shape != pool or not (k_pages.is_contiguous() and v_pages.is_contiguous())):
         raise _pool_error(pages, "Hkv")
     if dev < 0 or not (torch._C._cuda_getDevice() == dev == k_pages.get_device() == v_pages.get_device()
                        == out.get_device() == ws.get_device() == pages._device):

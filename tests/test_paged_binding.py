@@ -44,3 +44,19 @@ def test_positions_by_axis(st, anywhere):
     for shape, match in (((5, 3), "pos is"), ((3, 5), DEVICE)):
         _refused(st.stlite_paged_append, q, k, k.clone(), torch.zeros(shape, dtype=I32), three, pages, q.clone(), pool,
                  pool.clone(), match=match)
+
+
+def test_value_pool_has_the_key_pools_shape(st, anywhere):
+    q = torch.zeros((2, 4, 128), dtype=BF)
+    k = torch.zeros((6, 4, 2, 128), dtype=BF)
+    pages = st.make_pages(6, 4, torch.zeros((2, 3), dtype=I32), torch.zeros(2, dtype=I32))
+    ws = torch.zeros(64, dtype=torch.uint8)
+
+    def attend(v, match):
+        _refused(st.stlite_paged_attention, q, k, v, pages, q.clone(), ws, match=match)
+
+    attend(k.clone(), DEVICE)
+    for shape in ((6, 2, 4, 128), (4, 6, 2, 128), (6, 4, 1, 256), (48, 128), (6, 4, 2, 64)):
+        attend(torch.zeros(shape, dtype=BF), "page pool")
+    for dtype in (torch.float16, torch.int16, F32):
+        attend(torch.zeros(k.shape, dtype=dtype), "page pool")
