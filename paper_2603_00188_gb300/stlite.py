@@ -700,27 +700,24 @@ def paged_attention(q, k_pages, v_pages, pages, stream=None):
 def stlite_compact_paged(layers, budget, pages, seq, stream=None):
     """The kept rows of every layer into sequence seq's pages; layers: list
     of (k, v, k_pages, v_pages, idx)."""
-    k0, v0, kp0, vp0, ix0 = layers[0]
+    k0 = layers[0][0]
     shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
     n, hkv, d = shape
-    want = (*pages._pool, hkv, d)
-    if (v0.shape != shape or kp0.shape != want or vp0.shape != want or ix0.shape != (hkv, budget)
-            or not v0.dtype == kp0.dtype == vp0.dtype == dtype or ix0.dtype != torch.int32):
-        raise ValueError("k and v are [N][Hkv][128], pools %s of their type and idx int32 [Hkv][budget]" % (want,))
-    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
-        raise ValueError(_ELSEWHERE)
-    # the layers are alike: each tensor is as large as the first layer's
-    rows, pool, index = k0.nbytes, kp0.nbytes, ix0.nbytes
+    want, index = (*pages._pool, hkv, d), (hkv, budget)
     for k, v, kp, vp, ix in layers:
-        if not (k.nbytes == rows == v.nbytes and kp.nbytes == pool == vp.nbytes and ix.nbytes == index
+        if not (k.shape == shape == v.shape and kp.shape == want == vp.shape and ix.shape == index
+                and k.dtype == dtype == v.dtype and kp.dtype == dtype == vp.dtype and ix.dtype == torch.int32
                 and k.is_contiguous() and v.is_contiguous() and kp.is_contiguous() and vp.is_contiguous()
                 and ix.is_contiguous()):
-            raise ValueError("every layer's tensors are contiguous and as the first layer's")
+            raise ValueError("every layer's k and v are [N][Hkv][128], pools %s of their type and idx int32 "
+                             "[Hkv][budget], contiguous" % (want,))
         if not k.get_device() == kp.get_device() == vp.get_device() == ix.get_device() == dev or (
                 v.get_device() != dev and not v.is_pinned()):
             raise ValueError(_ELSEWHERE)
         a = k.data_ptr()
         flat += (a, a, v.data_ptr(), kp.data_ptr(), vp.data_ptr(), ix.data_ptr())
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
+        raise ValueError(_ELSEWHERE)
     arr = array("Q", flat)
     st = _lib.stlite_compact_paged(_SHAPE.pack(n, hkv, hkv, d, 1, _DTYPE[dtype]), budget, pages._address, seq,
                                    len(layers), _address(arr), _CURRENT(dev) if stream is None else stream.cuda_stream)

@@ -60,3 +60,27 @@ def test_value_pool_has_the_key_pools_shape(st, anywhere):
         attend(torch.zeros(shape, dtype=BF), "page pool")
     for dtype in (torch.float16, torch.int16, F32):
         attend(torch.zeros(k.shape, dtype=dtype), "page pool")
+
+
+def _compaction_layer(n=20, hkv=2, budget=6):
+    k, pool = torch.zeros((n, hkv, 128), dtype=BF), torch.zeros((5, 4, hkv, 128), dtype=BF)
+    return dict(k=k, v=k.clone(), k_pages=pool, v_pages=pool.clone(), idx=torch.zeros((hkv, budget), dtype=I32))
+
+
+# as many bytes as the first layer's, and something else
+UNLIKE = [("k", torch.zeros((40, 1, 128), dtype=BF)), ("k", torch.zeros((2, 20, 128), dtype=BF)),
+          ("v", torch.zeros((10, 2, 128), dtype=F32)), ("v", torch.zeros((20, 2, 128), dtype=torch.float16)),
+          ("k", torch.zeros((20, 2, 128), dtype=torch.int16)), ("k_pages", torch.zeros((5, 2, 4, 128), dtype=BF)),
+          ("v_pages", torch.zeros((4, 5, 2, 128), dtype=BF)), ("v_pages", torch.zeros((5, 4, 2, 64), dtype=F32)),
+          ("idx", torch.zeros((2, 3), dtype=torch.int64)), ("idx", torch.zeros((2, 6), dtype=F32)),
+          ("idx", torch.zeros((6, 2), dtype=I32)), ("idx", torch.zeros(12, dtype=I32))]
+
+
+@pytest.mark.parametrize("name,other", UNLIKE, ids=lambda x: x if isinstance(x, str) else "%s %s" % (tuple(x.shape), x.dtype))
+def test_compaction_layers_are_alike(st, anywhere, name, other):
+    pages = st.make_pages(5, 4, torch.zeros((1, 3), dtype=I32))
+    good = _compaction_layer()
+    _refused(st.stlite_compact_paged, [tuple(good.values())] * 2, 6, pages, 0, match=DEVICE)
+    bad = tuple({**good, name: other}.values())
+    for layers in ([tuple(good.values()), bad], [bad, tuple(good.values())], [tuple(good.values())] * 3 + [bad]):
+        _refused(st.stlite_compact_paged, layers, 6, pages, 0, match="every layer|idx")
