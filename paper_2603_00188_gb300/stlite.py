@@ -728,12 +728,25 @@ def stlite_compact_paged(layers, budget, pages, seq, stream=None):
 def stlite_compress_layers_paged(layers, frames, params, pages, seq, ws, stream=None) -> int:
     """stlite_compress_layers with the kept rows in sequence seq's pages;
     layers: list of (q, k, v, k_pages, v_pages, idx_out)."""
-    sh = make_shape(layers[0][0], layers[0][1])
-    want, dtype = (*pages._pool, sh.n_kv_heads, 128), layers[0][1].dtype
-    for _, _, _, kp, vp, _ in layers:
-        if not (kp.shape == vp.shape == want and kp.dtype == vp.dtype == dtype and kp.is_contiguous()
+    q0, k0 = layers[0][:2]
+    sh = make_shape(q0, k0)
+    qs, shape, dtype, dev = q0.shape, k0.shape, k0.dtype, k0.get_device()
+    want = (*pages._pool, sh.n_kv_heads, 128)
+    kept = sh.n_kv_heads * stlite_budget(sh.n_tokens, params.beta, params.k_override)
+    for q, k, v, kp, vp, ix in layers:
+        if not (kp.shape == want == vp.shape and kp.dtype == dtype == vp.dtype and kp.is_contiguous()
                 and vp.is_contiguous()):
             raise _pool_error(pages, sh.n_kv_heads)
+        if not (q.shape == qs and k.shape == shape == v.shape and q.dtype == dtype == k.dtype and v.dtype == dtype
+                and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("every layer's q is [w][Hq][128] and its k and v [N][Hkv][128], of one type, contiguous")
+        if ix.dtype != torch.int32 or ix.numel() < kept or not ix.is_contiguous():
+            raise ValueError("every layer's idx_out is contiguous int32 with room for [Hkv][B]")
+        if not q.get_device() == k.get_device() == kp.get_device() == vp.get_device() == ix.get_device() == dev or (
+                v.get_device() != dev and not v.is_pinned()):
+            raise ValueError(_ELSEWHERE)
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device == ws.get_device():
+        raise ValueError(_ELSEWHERE)
     fs = _frames(frames)
     arr = _layer_table(layers)
     b = ctypes.c_int32(0)

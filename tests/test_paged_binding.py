@@ -84,3 +84,48 @@ def test_compaction_layers_are_alike(st, anywhere, name, other):
     bad = tuple({**good, name: other}.values())
     for layers in ([tuple(good.values()), bad], [bad, tuple(good.values())], [tuple(good.values())] * 3 + [bad]):
         _refused(st.stlite_compact_paged, layers, 6, pages, 0, match="every layer|idx")
+
+
+FRAMES = ([0], [4], [4])
+FUSED = [("q", torch.zeros((1, 8, 128), dtype=BF)), ("q", torch.zeros((2, 2, 128), dtype=F32)),
+         ("k", torch.zeros((40, 1, 128), dtype=BF)), ("v", torch.zeros((19, 2, 128), dtype=BF)),
+         ("v", torch.zeros((40, 1, 128), dtype=BF)), ("v", torch.zeros((20, 2, 128), dtype=torch.float16)),
+         ("v", torch.zeros((20, 2, 64), dtype=F32)), ("k", torch.zeros((2, 20, 128), dtype=BF).transpose(0, 1)),
+         ("idx", torch.zeros((2, 4), dtype=I32)), ("idx", torch.zeros((2, 5), dtype=torch.int64)),
+         ("idx", torch.zeros((5, 2), dtype=I32).t()), ("k_pages", torch.zeros((5, 2, 4, 128), dtype=BF))]
+
+
+@pytest.mark.parametrize("name,other", FUSED, ids=lambda x: x if isinstance(x, str) else "%s %s" % (tuple(x.shape), x.dtype))
+def test_fused_pass_into_pages_checks_every_layer(st, anywhere, name, other):
+    """Five rows of 20 are kept: idx_out has room for [2][5]."""
+    pages, prm = st.make_pages(5, 4, torch.zeros((1, 3), dtype=I32)), st.make_params(0.25)
+    good = dict(q=torch.zeros((2, 4, 128), dtype=BF), **_compaction_layer(budget=5))
+    ws = torch.zeros(64, dtype=torch.uint8)
+
+    def fused(layers, match):
+        _refused(st.stlite_compress_layers_paged, layers, FRAMES, prm, pages, 0, ws, match=match)
+
+    fused([tuple(good.values())] * 2, DEVICE)
+    fused([tuple({**good, "idx": torch.zeros((2, 8), dtype=I32)}.values())], DEVICE)  # room to spare
+    bad = tuple({**good, name: other}.values())
+    for layers in ([tuple(good.values()), bad], [tuple(good.values())] * 3 + [bad]):
+        fused(layers, "every layer|page pool")
+
+
+@pytest.mark.gpu
+def test_fused_pass_into_pages_wants_one_device(st):
+    """A tensor on the host among the others on the device (values may be page-locked there)."""
+    prm, b = st.make_params(0.25), 5
+    good = {n: t.cuda() for n, t in dict(q=torch.zeros((2, 4, 128), dtype=BF), **_compaction_layer(budget=8)).items()}
+    table = torch.tensor([[0, 3, 1]], dtype=I32)
+    pages = st.make_pages(5, 4, table.cuda())
+    ws = st.workspace(st.make_shape(good["q"], good["k"]), FRAMES, prm)
+    call = st.stlite_compress_layers_paged
+    assert call([tuple(good.values())], FRAMES, prm, pages, 0, ws) == b
+    assert call([tuple({**good, "v": good["v"].cpu().pin_memory()}.values())], FRAMES, prm, pages, 0, ws) == b
+    for name in good:
+        bad = tuple({**good, name: good[name].cpu()}.values())
+        _refused(call, [bad], FRAMES, prm, pages, 0, ws, match=DEVICE)
+    _refused(call, [tuple(good.values())], FRAMES, prm, st.make_pages(5, 4, table), 0, ws, match=DEVICE)
+    _refused(call, [tuple(good.values())], FRAMES, prm, pages, 0, ws.cpu(), match=DEVICE)
+    assert st.stlite_device_status(ws) == st.STLITE_OK
