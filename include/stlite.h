@@ -457,8 +457,9 @@ STLITE_API stlite_status stlite_rope_init(double base, stlite_rope* rope);
 /* T = shape->n_tokens packed tokens as the projections leave them (device):
  * q [T][Hq][d], k and v [T][Hkv][d], each token's heads packed and tokens
  * *_stride elements apart (0: packed; otherwise a multiple of 16 bytes, at
- * least the heads' extent), so that the three may be slices of one
- * projection's output. */
+ * least the heads' extent, at most 2^40), so that the three may be slices of
+ * one projection's output.  Hkv <= 4096, Hq / Hkv <= 512 and
+ * T * (Hq + 2 Hkv) <= 2^31 - 64. */
 typedef struct {
   const void* q;
   const void* k;
@@ -509,12 +510,12 @@ STLITE_API stlite_status stlite_paged_append(const stlite_shape* shape, const st
  * the workspace error word.
  * shape: n_tokens = T; window = the most new tokens of a sequence (cu_new NULL:
  *   of each), 1 .. 16 (further tokens of a sequence are left unwritten);
- *   Hq / Hkv <= 16; n_pages * page_rows * Hkv, and n_seqs * Hkv *
+ *   Hq / Hkv <= 16; Hkv <= 4096; n_pages * page_rows * Hkv, and n_seqs * Hkv *
  *   ceil(window * (Hq / Hkv) / 16) * (max_pages * page_rows / 16 + 13), below 2^31.
  * q, out [T][Hq][d] (shape->dtype), packed; rows behind cu_new[S] are left
- *   alone.  T = 0: as for stlite_paged_append.  ws: at least stlite_paged_workspace_size bytes, zero-filled before
- *   its first use (its first word is the error word of
- *   stlite_device_status).  The work is divided over the GPU by the lengths as
+ *   alone.  T = 0: as for stlite_paged_append.  ws: at least
+ *   stlite_paged_workspace_size bytes, zero-filled before its first use (its
+ *   first word is the error word of stlite_device_status).  The work is divided over the GPU by the lengths as
  *   they are when the kernels run, so one capture serves growing caches. */
 STLITE_API stlite_status stlite_paged_attention(const stlite_shape* shape, const stlite_pages* pages, const void* q,
                                                 const void* k_pages, const void* v_pages, void* out, void* ws,

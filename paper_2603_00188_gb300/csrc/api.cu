@@ -1025,21 +1025,18 @@ stlite_status check_pages(const stlite_pages* pg, bool need_len) {
   return STLITE_OK;
 }
 
-// check_shape for a serving step's packed tokens, of which there may be none.
-stlite_status check_step_shape(const stlite_shape* shape) {
-  if (!shape || shape->n_tokens < 0) return STLITE_EINVAL;
-  stlite_shape s = *shape;
-  if (s.n_tokens == 0) s.n_tokens = 1;
-  return check_shape(&s);
-}
-
-// The same for calls whose window is a number of tokens, not of an observation
-// window's queries: any number.
-stlite_status check_token_shape(const stlite_shape* shape) {
-  if (!shape || shape->window < 1) return STLITE_EINVAL;
-  stlite_shape s = *shape;
-  s.window = 1;
-  return check_step_shape(&s);
+// The shape of a serving step's packed tokens, of which there may be none.
+// Their number has none of the selection's bounds (check_shape), and window,
+// a number of tokens here, none of an observation window's.
+stlite_status check_step_shape(const stlite_shape* s) {
+  if (!s || s->n_tokens < 0 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->window < 1 || s->head_dim < 1)
+    return STLITE_EINVAL;
+  if (s->n_q_heads % s->n_kv_heads != 0) return STLITE_EINVAL;
+  if (s->dtype != STLITE_BF16 && s->dtype != STLITE_F32) return STLITE_EINVAL;
+  if (s->head_dim != STLITE_HEAD_DIM) return STLITE_EUNSUPPORTED;
+  // the kernels number the elements of a token's heads in int32
+  if (s->n_kv_heads > 4096 || s->n_q_heads / s->n_kv_heads > 512) return STLITE_EUNSUPPORTED;
+  return STLITE_OK;
 }
 
 // Without cu_new every sequence has w new tokens.
@@ -1114,7 +1111,7 @@ stlite_status token_view(const stlite_shape* s, const stlite_rope* rope, const s
   stlite_status st = check_rope(rope);
   if (st != STLITE_OK) return st;
   // the kernel numbers the tokens' heads in int32
-  if ((long long)s->n_tokens * (s->n_q_heads + 2 * s->n_kv_heads) > 0x7fffffc0LL) return STLITE_EUNSUPPORTED;
+  if ((long long)s->n_tokens * (s->n_q_heads + 2LL * s->n_kv_heads) > 0x7fffffc0LL) return STLITE_EUNSUPPORTED;
   if (!x || !x->q || !x->k || (need_v && !x->v) || !x->pos) return STLITE_EINVAL;
   if (!aligned16(x->q) || !aligned16(x->k) || (need_v && !aligned16(x->v)) || !aligned16(x->q_norm) ||
       !aligned16(x->k_norm) || !aligned4(x->pos))
@@ -1173,7 +1170,7 @@ stlite_status stlite_rope_init(double base, stlite_rope* rope) {
 
 stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
                                void* q_out, void* k_out, void* stream) {
-  stlite_status s = check_token_shape(shape);
+  stlite_status s = check_step_shape(shape);
   if (s != STLITE_OK) return s;
   if (shape->n_tokens == 0) return STLITE_EINVAL;  // a prompt has tokens
   TokenView v;
@@ -1188,7 +1185,7 @@ stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlite_rope* rop
 stlite_status stlite_paged_append(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
                                   const stlite_pages* pages, void* q_out, void* k_pages, void* v_pages,
                                   void* stream) {
-  stlite_status s = check_token_shape(shape);
+  stlite_status s = check_step_shape(shape);
   if (s != STLITE_OK) return s;
   if ((s = check_pages(pages, true)) != STLITE_OK) return s;
   if ((s = check_new(shape, pages)) != STLITE_OK) return s;
