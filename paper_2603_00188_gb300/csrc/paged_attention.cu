@@ -241,7 +241,13 @@ struct RowFinder {
   int u, f0, i1;   // the warp's next block, and the first block and the end of the item that it is sought in
   int head;
 
-  __device__ __forceinline__ RowFinder(const Range& r) : at(r.at), end(r.b1), u(r.b0), f0(r.b0), i1(r.b0), head(0) {}
+  __device__ __forceinline__ RowFinder(const Range& r) : end(r.b1), head(0) { start(r.at, r.b0); }
+
+  // The next block is the first at or after unit `from`, of c's session or a later one.
+  __device__ __forceinline__ void start(const Cursor& c, int from) {
+    at = c;
+    u = f0 = i1 = from;
+  }
 
   // Lane % 16's row of the warp's next block, as a row of 128 elements of the
   // pools seen as [rows][128]; -1 where it does not count, -2 past the range.
@@ -291,13 +297,18 @@ __device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int 
 //   O^T (128 dims x 8 queries) += V^T P^T, P transposed in registers by
 //   movmatrix and taken as P = hi + lo, two bf16 parts (16 bits of it: with one
 //   part the weights' rounding would be as large as the result's).
+// A value that is an infinity or a NaN does not go through these products: a
+// weight of 0 (a row that only newer tokens see), a part lo of 0 or one of the
+// other sign would make a NaN of it.  A warp whose sums are not finite at an
+// item's end takes its blocks again and adds such rows apart, by fp32 products
+// of the whole weight, to the queries that see them.
 // NT: groups of eight queries that share one read of the cache: 1 or 2 with
 // their fragments in registers, 3 or 4 with them read from shared memory.
-// Measured: 32 sessions of 1,000 to 53,600 rows, 7 queries to a KV head, 147 to
-// 152 us (6.4 TB/s with start and merge; the copies without the products take
-// the same time, so HBM bounds it; four warps and two CTAs per SM 155 where
-// eight and one take 160); one session of 10,757 rows 10.3 us, all latency.  16
-// sessions of 25,000 rows: 6.3 TB/s with 7 or 14 queries, 6.0 with 21, 5.3 with
+// Measured: 32 sessions of 1,000 to 53,600 rows, 7 queries to a KV head, 146 to
+// 153 us (6.2 to 6.5 TB/s with start and merge; the copies without the products
+// take the same time, so HBM bounds it; four warps and two CTAs per SM 155 where
+// eight and one take 160); one session of 10,757 rows 10.2 us, all latency.  16
+// sessions of 25,000 rows: 6.4 TB/s with 7 or 14 queries, 6.1 with 21, 5.2 with
 // 28, bound by the products' latency at two warps per scheduler.
 constexpr int kPmHalf = kPatBlock * kD * 2;         // keys, or values, of a block
 constexpr int kPmPitch = kD + 4;                    // floats from row to row of the merge buffer
@@ -395,13 +406,14 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     }
     cp_async_commit();
   };
-  {
+  auto fill = [&]() {
     int first[kStages];  // all table entries on their way before the first copies
 #pragma unroll
     for (int st = 0; st < kStages; ++st) first[st] = finder.next(pg, warp, G, chunk_rows, hkv, err);
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st, first[st]);
-  }
+  };
+  fill();
 
   const float scale = kPatLog2e * rsqrtf((float)kD);
   const uint32_t k_off = (lane & 15) * 256 + (((lane >> 4) ^ (lane & 7)) << 4);
@@ -465,173 +477,187 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
     // 8 nt + 2 t4 + e; o[mt][nt][j] is dimension 16 mt + g8 + 8 (j >> 1) of
     // query 8 nt + 2 t4 + (j & 1).
     float m[NT][2], l[NT][2], o[8][NT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -CUDART_INF_F;
-      l[nt][0] = l[nt][1] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
-    }
     const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
-    for (int u = warps_first(part0, warp); u < seg_end; u += kPmWarps) {
-      cp_async_wait<kStages - 1>();
-      __syncwarp();
-      const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
-      const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
-      uint8_t* stage_ptr = sm + (warp * kStages + stage) * 2 * kPmHalf;
-      const int base = (u - item.f0) * kPatBlock;
-      constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
-      float c[kChains][NT][4];
+    // The warp's blocks of the part; look: for values that are no numbers.
+    auto take = [&](auto look) {
 #pragma unroll
-      for (int i = 0; i < kChains; ++i)
+      for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = -CUDART_INF_F;
+        l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) c[i][nt][0] = c[i][nt][1] = c[i][nt][2] = c[i][nt][3] = 0.f;
-      if constexpr (NT <= 2) {
+        for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
+      }
+      for (int u = warps_first(part0, warp); u < seg_end; u += kPmWarps) {
+        cp_async_wait<kStages - 1>();
+        __syncwarp();
+        const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
+        const uint32_t kt = ring + stage * 2 * kPmHalf + k_off, vt = ring + stage * 2 * kPmHalf + kPmHalf + v_off;
+        const int base = (u - item.f0) * kPatBlock;
+        constexpr int kChains = NT == 1 ? 2 : 1;  // independent accumulations
+        float c[kChains][NT][4];
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          uint32_t a[4];
-          pm_ldsm_x4(kt - k_off + (k_off ^ (ks << 5)), a);
+        for (int i = 0; i < kChains; ++i)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) pm_mma(c[ks % kChains][nt], a, qb[ks][nt][0], qb[ks][nt][1]);
-        }
-      } else {
+          for (int nt = 0; nt < NT; ++nt) c[i][nt][0] = c[i][nt][1] = c[i][nt][2] = c[i][nt][3] = 0.f;
+        if constexpr (NT <= 2) {
 #pragma unroll
-        for (int kp = 0; kp < 4; ++kp) {
-          uint32_t a[4], a2[4];
-          pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6)), a);
-          pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6 | 32)), a2);
+          for (int ks = 0; ks < 8; ++ks) {
+            uint32_t a[4];
+            pm_ldsm_x4(kt - k_off + (k_off ^ (ks << 5)), a);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t f[4];
-            pm_ldsm_x4(q_smem + pm_off(8 * nt + (lane & 7), 4 * kp + (lane >> 3)), f);
-            pm_mma(c[0][nt], a, f[0], f[1]);
-            pm_mma(c[0][nt], a2, f[2], f[3]);
+            for (int nt = 0; nt < NT; ++nt) pm_mma(c[ks % kChains][nt], a, qb[ks][nt][0], qb[ks][nt][1]);
           }
-        }
-      }
-      if constexpr (kChains == 2) {
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[0][0][j] += c[1][0][j];
-      }
-      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
-      uint32_t apart = 0;  // rows whose values are added apart from the others
-      if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
-        if (cur.w.fresh > 1) {
-          // Rows that only the newer tokens see: a weight of 0 times a value
-          // that is no number would reach the older ones.
-          const uint32_t rows_apart = ok & ~((1u << max(0, min(kPatBlock, all_see - base))) - 1u);
-          bool odd = false;
-          if (rows_apart >> (lane & 15) & 1u) {
-#pragma unroll 4
-            for (int i = 0; i < 8; ++i) {
-              const uint4 y = *reinterpret_cast<const uint4*>(stage_ptr + kPmHalf + pm_off(lane & 15, 8 * (lane >> 4) + i));
-              odd |= has_odd_bf16(y.x) || has_odd_bf16(y.y) || has_odd_bf16(y.z) || has_odd_bf16(y.w);
+          for (int kp = 0; kp < 4; ++kp) {
+            uint32_t a[4], a2[4];
+            pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6)), a);
+            pm_ldsm_x4(kt - k_off + (k_off ^ (kp << 6 | 32)), a2);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              uint32_t f[4];
+              pm_ldsm_x4(q_smem + pm_off(8 * nt + (lane & 7), 4 * kp + (lane >> 3)), f);
+              pm_mma(c[0][nt], a, f[0], f[1]);
+              pm_mma(c[0][nt], a2, f[2], f[3]);
             }
           }
-          if (__any_sync(0xffffffffu, odd)) apart = rows_apart;
         }
+        if constexpr (kChains == 2) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = g8 + 8 * (j >> 1), sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + (j & 1)) / G);
-            if (!(ok >> r & 1u) || base + r >= sees) c[0][nt][j] = -CUDART_INF_F;
-          }
-      }
-      float ms[NT][2];  // the new maxima, scaled
-      bool moved = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          mx = fmaxf(m[nt][e], mx);
-          ms[nt][e] = mx == -CUDART_INF_F ? 0.f : mx * scale;
-          moved |= mx != m[nt][e];
+          for (int j = 0; j < 4; ++j) c[0][0][j] += c[1][0][j];
         }
-      if (__any_sync(0xffffffffu, moved)) {  // rare once the maxima have settled
+        const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
+        if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int r = g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
+              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+              if (!(ok >> r & 1u) || base + r >= sees) c[0][nt][j] = -CUDART_INF_F;
+            }
+        }
+        float ms[NT][2];  // the new maxima, scaled
+        bool moved = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float mx = max3(m[nt][e], c[0][nt][e], c[0][nt][2 + e]);
-            float all = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 8));
-            all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 16));
-            const float alpha = ex2_approx(fmaf(m[nt][e], scale, -ms[nt][e]));
-            l[nt][e] *= alpha;
-            m[nt][e] = all;
-#pragma unroll
-            for (int mt = 0; mt < 8; ++mt) {
-              o[mt][nt][e] *= alpha;
-              o[mt][nt][2 + e] *= alpha;
-            }
+            float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+            mx = fmaxf(m[nt][e], mx);
+            ms[nt][e] = mx == -CUDART_INF_F ? 0.f : mx * scale;
+            moved |= mx != m[nt][e];
           }
-      }
+        if (__any_sync(0xffffffffu, moved)) {  // rare once the maxima have settled
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {  // scores become probabilities
-          c[0][nt][j] = ex2_approx(fmaf(c[0][nt][j], scale, -ms[nt][j & 1]));
-          l[nt][j & 1] += c[0][nt][j];
-        }
-      if (apart != 0u) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          for (uint32_t left = apart; left != 0u; left &= left - 1u) {
-            const int r = __ffs(left) - 1, from = (r & 7) * 4 + t4;
-            float w[2];
-            bool seen[2];
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float y0 = __shfl_sync(0xffffffffu, c[0][nt][e], from);
-              const float y1 = __shfl_sync(0xffffffffu, c[0][nt][2 + e], from);
-              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G);
-              w[e] = r < 8 ? y0 : y1;
-              seen[e] = base + r < sees;
+              const float mx = max3(m[nt][e], c[0][nt][e], c[0][nt][2 + e]);
+              float all = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+              all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 8));
+              all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, 16));
+              const float alpha = ex2_approx(fmaf(m[nt][e], scale, -ms[nt][e]));
+              l[nt][e] *= alpha;
+              m[nt][e] = all;
+#pragma unroll
+              for (int mt = 0; mt < 8; ++mt) {
+                o[mt][nt][e] *= alpha;
+                o[mt][nt][2 + e] *= alpha;
+              }
             }
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int dim = 8 * i + g8;
-              const float y = __bfloat162float(
-                  *reinterpret_cast<const __nv_bfloat16*>(stage_ptr + kPmHalf + pm_off(r, i) + 2 * (dim & 7)));
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (seen[e]) o[i >> 1][nt][2 * (i & 1) + e] = fmaf(w[e], y, o[i >> 1][nt][2 * (i & 1) + e]);
+          for (int j = 0; j < 4; ++j) {  // scores become probabilities
+            c[0][nt][j] = ex2_approx(fmaf(c[0][nt][j], scale, -ms[nt][j & 1]));
+            l[nt][j & 1] += c[0][nt][j];
+          }
+        if constexpr (decltype(look)::value) {
+          uint8_t* values = sm + (warp * kStages + stage) * 2 * kPmHalf + kPmHalf;
+          bool odd = false;
+          if (ok >> (lane & 15) & 1u) {
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+              const uint4 y = *reinterpret_cast<const uint4*>(values + pm_off(lane & 15, 8 * (lane >> 4) + i));
+              odd |= has_odd_bf16(y.x) || has_odd_bf16(y.y) || has_odd_bf16(y.z) || has_odd_bf16(y.w);
             }
           }
-        __syncwarp();  // added: they count no more
-        if (apart >> (lane & 15) & 1u)
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(stage_ptr + kPmHalf + pm_off(lane & 15, 8 * (lane >> 4) + i)) = make_uint4(0, 0, 0, 0);
+          const uint32_t halves = __ballot_sync(0xffffffffu, odd), apart = (halves | halves >> 16) & 0xffffu;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            for (uint32_t left = apart; left != 0u; left &= left - 1u) {
+              const int r = __ffs(left) - 1, from = (r & 7) * 4 + t4;
+              float w[2];
+              bool seen[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float y0 = __shfl_sync(0xffffffffu, c[0][nt][e], from);
+                const float y1 = __shfl_sync(0xffffffffu, c[0][nt][2 + e], from);
+                const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G);
+                w[e] = r < 8 ? y0 : y1;
+                seen[e] = base + r < sees;
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int dim = 8 * i + g8;
+                const float y = __bfloat162float(
+                    *reinterpret_cast<const __nv_bfloat16*>(values + pm_off(r, i) + 2 * (dim & 7)));
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (seen[e]) o[i >> 1][nt][2 * (i & 1) + e] = fmaf(w[e], y, o[i >> 1][nt][2 * (i & 1) + e]);
+              }
+            }
+          __syncwarp();  // added: they count no more
+          if (apart >> (lane & 15) & 1u)
+            for (int i = 0; i < 8; ++i)
+              *reinterpret_cast<uint4*>(values + pm_off(lane & 15, 8 * (lane >> 4) + i)) = make_uint4(0, 0, 0, 0);
+          __syncwarp();
+        }
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float p0 = c[0][nt][2 * x], p1 = c[0][nt][2 * x + 1];
+            const uint32_t hi = pack_bf16(p0, p1);
+            ph[nt][x] = transpose8x8(hi);
+            pl[nt][x] = transpose8x8(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
+          }
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) {
+          uint32_t a[4];
+          pm_ldsm_x4_trans(vt - v_off + (v_off ^ (mt << 5)), a);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            pm_mma(o[mt][nt], a, ph[nt][0], ph[nt][1]);
+            pm_mma(o[mt][nt], a, pl[nt][0], pl[nt][1]);
+          }
+        }
         __syncwarp();
+        fetch(stage, next);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
       }
-      uint32_t ph[NT][2], pl[NT][2];
+    };
+    take(std::false_type());
+    float none = 0.f;  // or a NaN, where a sum is not finite
+#pragma unroll
+    for (int mt = 0; mt < 8; ++mt)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float p0 = c[0][nt][2 * x], p1 = c[0][nt][2 * x + 1];
-          const uint32_t hi = pack_bf16(p0, p1);
-          ph[nt][x] = transpose8x8(hi);
-          pl[nt][x] = transpose8x8(pack_bf16(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)));
-        }
-#pragma unroll
-      for (int mt = 0; mt < 8; ++mt) {
-        uint32_t a[4];
-        pm_ldsm_x4_trans(vt - v_off + (v_off ^ (mt << 5)), a);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          pm_mma(o[mt][nt], a, ph[nt][0], ph[nt][1]);
-          pm_mma(o[mt][nt], a, pl[nt][0], pl[nt][1]);
-        }
-      }
+        for (int j = 0; j < 4; ++j) none = fmaf(o[mt][nt][j], 0.f, none);
+    if (__any_sync(0xffffffffu, none != 0.f)) {
+      cp_async_wait<0>();  // no copy is on its way to the stages
       __syncwarp();
-      fetch(stage, next);
-      stage = stage + 1 == kStages ? 0 : stage + 1;
+      finder.start(cur, part0);
+      fill();
+      stage = 0;
+      take(std::true_type());
     }
     // The warps' states of this item, merged in shared memory, kPass groups of
     // queries at a time.
