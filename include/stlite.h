@@ -488,8 +488,10 @@ STLITE_API stlite_status stlite_rotate_qk(const stlite_shape* shape, const stlit
  * new ones of sequence s becomes row len[s] - n_s + i.  Tokens behind
  * cu_new[S] are padding: they and their rows of q_out are left alone.  A row
  * that lies outside its sequence's pages or names a page outside the pool is
- * not written (its q_out is).  Rows that two sequences share are not to be
- * written by both.  q_out may be x->q where that is packed.
+ * not written (its q_out is); the call has no error word, but
+ * stlite_paged_attention over the same pages records a bad page and a length
+ * past the table (not a length below the new tokens: an idle session's).  Rows
+ * that two sequences share are not to be written by both.  q_out may be x->q where that is packed.
  * shape: n_tokens = T; window = tokens of each sequence where cu_new is NULL
  *   (any number >= 1; otherwise not used).  T = 0 (a step without a token,
  *   cu_new given): x, q_out and the pools are not looked at and nothing is

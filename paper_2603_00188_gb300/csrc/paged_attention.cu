@@ -7,8 +7,8 @@
 // Work is divided by what the sessions hold when the kernel runs.  An item is
 // (session, KV head, chunk of query rows); its cache is cut into blocks of 16
 // rows.  An item counts for its blocks and for some units before them that stand
-// for its own costs (queries, merge: 1 to 2 us of a CTA); the units of
-// all items, laid end to end, are cut into equal ranges, one per CTA.  A CTA
+// for its own costs (queries, merge: launch_paged_attention gives their number);
+// the units of all items, laid end to end, are cut into equal ranges, one per CTA.  A CTA
 // computes the parts of the few items that its range meets: an item whose
 // blocks lie inside one range is finished there, the parts of others are merged
 // by a second kernel.
@@ -291,12 +291,15 @@ __device__ __forceinline__ void zero_rows(T* out, int first, int n, int hq, int 
 // asynchronous 16-byte copies (any page size: a lane looks up its row's page
 // one block ahead; rows that do not count are filled with zeros and masked).
 // No warp waits for another until an item ends.  Both products run on the
-// warp's tensor cores (m16n8k16, fp32 accumulation), as a session's new tokens
-// make a few query rows, below the smallest tile of tcgen05:
+// warp's tensor cores (m16n8k16, fp32 accumulation):
 //   S (16 rows x 8 queries) = K Q^T,
 //   O^T (128 dims x 8 queries) += V^T P^T, P transposed in registers by
 //   movmatrix and taken as P = hi + lo, two bf16 parts (16 bits of it: with one
 //   part the weights' rounding would be as large as the result's).
+// That way the products of up to 21 query rows take less time than the bytes
+// (rates below), and a warp passes from one product to the next in registers.
+// From 28 rows on the products bound it; tcgen05 tiles with the cached rows, then
+// the dimensions, as M and the queries as N would be the form for those.
 // A value that is an infinity or a NaN does not go through these products: a
 // weight of 0 (a row that only newer tokens see), a part lo of 0 or one of the
 // other sign would make a NaN of it.  A warp whose sums are not finite at an
@@ -749,9 +752,10 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
 //   values: a lane owns four dimensions of every query, the probabilities come
 //     back through shared memory.
 // GM: queries of a chunk (4, or one or two times eight).
-// Measured: 8 sessions of 25,000 rows, 7 queries to a KV head, 132 to 137 us (6.3
-// TB/s; with two rows to a lane and every lane's exponentials of all queries
-// 178), 14 queries 200 (30 TFLOP/s).
+// Measured: 8 sessions of 25,000 rows, 7 queries to a KV head, 128 to 137 us (6.0
+// to 6.4 TB/s; with two rows to a lane and every lane's exponentials of all queries
+// 178), 14 queries 196 (30 TFLOP/s), bound by the reads of the products from
+// shared memory; k_paged_fma<16> also spills (255 registers, 120 bytes).
 constexpr int kPfSlots = 3;
 constexpr int kPfHalf = kPatBlock * kD * 4;  // keys, or values, of a block
 constexpr int kPfPass = 4;                   // queries merged at a time
@@ -1241,7 +1245,7 @@ cudaError_t launch_paged_attention(DType dt, const PageView& view, const void* q
     }
     TimingScope ts("paged_merge", st);
     const dim3 grid(descs, chunk_rows);
-    const bool few = descs * chunk_rows <= 304;
+    const bool few = descs * chunk_rows <= 304;  // two CTAs for each of the chip's SMs
     auto kern = few ? k_paged_merge<T, 256> : k_paged_merge<T, 128>;
     e = launch_after(kern, grid, few ? 256 : 128, 0, st, pages, static_cast<T*>(out), n, hq, hkv, chunks, chunk_rows,
                      part_rows, mode == kDescByItem, desc, part_ml, part_o);
