@@ -62,6 +62,9 @@ def test_no_token_through_the_binding(st, dtype, axes):
     assert st.paged_attention(qo, kp, vp, pages).shape == q.shape
     assert (kp == 3).all() and (vp == 3).all() and st.stlite_device_status(ws) == st.STLITE_OK
     side = torch.cuda.Stream()
+    assert st.rotate_qk(q, k, pos, rope, stream=side)[1].shape == k.shape
+    assert st.paged_attention(qo, kp, vp, pages, stream=side).shape == q.shape
+    side.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):  # an empty step among others
         kp.add_(1)
