@@ -548,12 +548,137 @@ STLITE_API stlite_status stlite_compress_layers_paged(const stlite_shape* shape,
                                                       int32_t seq, int32_t n_layers, const stlite_layer_io* layers,
                                                       int32_t* budget_out, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- pages in 4 bits --------------------------------------------------------
+ * A paged cache whose rows take 72 bytes for 128 elements: a layer's pools are
+ *     k, v              codes,  uint8 [n_pages][Hkv][page_rows][64]
+ *     k_scale, v_scale  scales, uint8 [n_pages][Hkv][page_rows][8]
+ * (a head's rows of a page lie together).  Element 2 i of a row is the low half
+ * of byte i, element 2 i + 1 the high half: an e2m1 code (sign, then 0, 0.5, 1,
+ * 1.5, 2, 3, 4 or 6).  Each 16 elements have a scale, an e4m3 number, and each
+ * KV head may have a factor:
+ *     element = code * scale * factor.
+ * Rows are put in so: top = the largest magnitude of the group / (6 factor),
+ * scale = top within 2^-9 .. 448, rounded to e4m3, code = element / (scale *
+ * factor), rounded to e2m1 (each to nearest, ties to even, in fp32).  So zeros
+ * stay zeros, magnitudes beyond 2688 factors become that, and groups whose
+ * largest is below 0.012 factors lose precision: a factor near the head's usual
+ * magnitude keeps them within.  A group that holds an infinity or a NaN gets a
+ * scale of 0x7f, a NaN, with codes of 0.
+ * Tables, lengths and cu_new are those of stlite_pages; so are the checks of
+ * every entry. */
+typedef struct {
+  void* k;               /* 16-byte aligned */
+  void* v;               /* 16-byte aligned */
+  void* k_scale;         /* 8-byte aligned */
+  void* v_scale;         /* 8-byte aligned */
+  const float* k_factor; /* device [Hkv], each finite and > 0, or NULL: 1 */
+  const float* v_factor; /* the same for values */
+} stlite_q4_pools;
+
+/* stlite_paged_append into 4-bit pages: keys are put in as they leave the
+ * rotation, in fp32, values as they are; q_out as there.  Everything else as
+ * for stlite_paged_append. */
+STLITE_API stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope,
+                                                const stlite_tokens* x, const stlite_pages* pages, void* q_out,
+                                                const stlite_q4_pools* pools, void* stream);
+
+/* stlite_paged_attention over 4-bit pages: the same result for the elements'
+ * values above.  bf16 queries: weights are rounded to 11 bits.  A row that a
+ * token sees and whose key has a NaN scale makes the token's head's output NaN;
+ * one whose value has makes its 16 elements NaN.  Rows that a token does not see
+ * take no part, whatever they hold.
+ * q, out [T][Hq][d] (shape->dtype), packed.  shape, ws, T = 0 and errors as for
+ * stlite_paged_attention; ws: at least stlite_paged_q4_workspace_size bytes. */
+STLITE_API stlite_status stlite_paged_attention_q4(const stlite_shape* shape, const stlite_pages* pages, const void* q,
+                                                   const stlite_q4_pools* pools, void* out, void* ws, size_t ws_bytes,
+                                                   void* stream);
+
+/* Workspace bytes of stlite_paged_attention_q4. */
+STLITE_API stlite_status stlite_paged_q4_workspace_size(const stlite_shape* shape, const stlite_pages* pages,
+                                                        size_t* bytes);
+
+/* One layer's tensors for the calls below.
+ * stlite_compact_paged_q4: k and v are the layer's cache [N][Hkv][d] (v may be
+ *   page-locked host memory), idx its indices [Hkv][budget] (read; 4-byte
+ *   aligned); q is not used.
+ * stlite_compress_layers_paged_q4: as for stlite_layer_io, idx is written.
+ * stlite_paged_fetch_q4: k and v are written; q and idx are not used. */
+typedef struct {
+  const void* q;
+  void* k;
+  void* v;
+  int32_t* idx;
+  stlite_q4_pools pools;
+} stlite_q4_layer;
+
+/* stlite_compact_paged into 4-bit pages: row r of head h of sequence `seq`
+ * becomes k[idx[h][r]][h], r < budget, and the same for v.  layers: HOST array.
+ * Everything else as for stlite_compact_paged. */
+STLITE_API stlite_status stlite_compact_paged_q4(const stlite_shape* shape, int32_t budget, const stlite_pages* pages,
+                                                 int32_t seq, int32_t n_layers, const stlite_q4_layer* layers,
+                                                 void* stream);
+
+/* stlite_compress_layers_paged with the kept rows going to 4-bit pages. */
+STLITE_API stlite_status stlite_compress_layers_paged_q4(const stlite_shape* shape, const stlite_frames* frames,
+                                                         const stlite_params* params, const stlite_pages* pages,
+                                                         int32_t seq, int32_t n_layers, const stlite_q4_layer* layers,
+                                                         int32_t* budget_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows out of 4-bit pages, as values, for n_layers layers: k and v [T][Hkv][d]
+ * (shape->dtype, packed) receive, for token i of the n_s of sequence s, row
+ * len[s] - n_s + i, the row that stlite_paged_append_q4 would write for it.
+ * n_s = len[s] takes whole sessions, as the dense caches that
+ * stlite_compress_layer takes.  A value is formed in fp32 and rounded once.
+ * shape: n_tokens = T, window as for stlite_paged_append, n_q_heads any
+ *   multiple of Hkv; T * Hkv <= 2^31 - 64.  layers: HOST array.
+ * Tokens behind cu_new[S], and those whose row lies outside its sequence's pages
+ * or names a page outside the pool, are left unwritten.  T = 0: as for
+ * stlite_paged_append. */
+STLITE_API stlite_status stlite_paged_fetch_q4(const stlite_shape* shape, const stlite_pages* pages, int32_t n_layers,
+                                               const stlite_q4_layer* layers, void* stream);
+
+/* ---- a step's page tables -----------------------------------------------------
+ * Gives pages to the sessions that grow and takes them from those that shrink
+ * or end, on the GPU, before a step's append (and attention): pages->table, len
+ * and cu_new, which those calls read, are WRITTEN here.
+ * Session s has len[s] rows before the call (out of 0 .. max_pages * page_rows:
+ * taken as the nearest of these).
+ *   1. keep[s] of them stay (NULL: all; above len[s]: all; below 0: none): fewer
+ *      where drafted tokens were refused, none where the session has ended.  The
+ *      table entries of pages that hold none of the rows that stay,
+ *      ceil(keep / page_rows) .. ceil(len / page_rows), go on top of the free
+ *      pages, session by session, in their order.
+ *   2. fresh[s] >= 0 new tokens (below 0: none) are asked for.  Sessions are
+ *      served in their order.  One that needs pages is served while all that
+ *      were asked for up to it, itself included, are at most the free ones; one
+ *      that needs none is served whatever others ask for.  Of these, one with
+ *      tokens is served while theirs, up to it, are at most n_tokens.  A session
+ *      that would pass max_pages * page_rows asks for nothing and is not served.
+ *      A session that is not served gets no new token and keeps the rows that
+ *      stay.  Its pages are taken from the top of the free ones, one after the
+ *      other, to the next entries of the table; entries behind a session's
+ *      pages are left as they were.
+ *   3. len[s] = rows that stay + new tokens, cu_new[S + 1] the sums of the new
+ *      tokens, *n_free the pages that are left.  slot[i], i < n_tokens: page *
+ *      page_rows + row of the page of packed new token i, -1 for those behind
+ *      cu_new[S] and where the table names a page outside the pool.
+ * pages: all fields as above, cu_new given.  keep, fresh: device [S].
+ * free_pages: device [n_pages], its first *n_free entries (0 .. n_pages) pages
+ * that no session holds; entries past *n_free are room.  n_free: device.
+ * n_tokens >= 0: places of the step (shape->n_tokens of its calls).  slot:
+ * device [n_tokens], or NULL.  All arrays int32, 4-byte aligned, none
+ * overlapping another.  Entries are moved as they are: a page that is named
+ * twice stays so. */
+STLITE_API stlite_status stlite_pages_step(const stlite_pages* pages, const int32_t* keep, const int32_t* fresh,
+                                           int32_t* free_pages, int32_t* n_free, int32_t n_tokens, int32_t* slot,
+                                           void* stream);
+
 /* Reads and clears the workspace's device error word (synchronises `stream`).
  * *status receives STLITE_OK, STLITE_ETIMEOUT if a kernel's bounded wait ran
  * out since the last read, STLITE_ECUDA if a kernel found its launch
  * configuration unusable (it then returned without touching its outputs), or
- * STLITE_EINVAL if stlite_paged_attention met a page or a length outside its
- * bounds.
+ * STLITE_EINVAL if stlite_paged_attention or stlite_paged_attention_q4 met a
+ * page or a length outside its bounds.
  * ws = NULL reads the error word of stlite_score_noalloc's fixed scratch on
  * the current device instead. */
 STLITE_API stlite_status stlite_device_status(void* ws, void* stream, stlite_status* status);

@@ -425,11 +425,17 @@ void select_variants(SelectArgs& a, const stlite_params* params, const Problem& 
   a.a_norm_max = params->abase_norm == STLITE_ABASE_MAX ? 1 : 0;
 }
 
+Q4View q4_view(const stlite_q4_pools& p) {
+  return {static_cast<uint8_t*>(p.k), static_cast<uint8_t*>(p.v), static_cast<uint8_t*>(p.k_scale),
+          static_cast<uint8_t*>(p.v_scale), p.k_factor, p.v_factor};
+}
+
 // Pages and sequence that the kept rows of a call go to, in place of dense
 // outputs, and every layer's budget.
 struct PagedRows {
   PageView pages;
   int seq, budget;
+  const stlite_q4_layer* q4;  // every layer's 4-bit pools, or null: stlite_layer_io's
 };
 
 // Algorithm 1 for a batch of layers (steps 1-5), every stage one launch.
@@ -440,8 +446,9 @@ struct PagedRows {
 // CSS's inverse norms but not Phi, so with the tensor-core CSS its second
 // kernel (Phi from the dots) goes last on the second stream, after an event
 // that marks the dots done: TSG starts as soon as the dots are written.
+// first: the batch's first layer of the call's.
 stlite_status compress_batch(const Ctx& c, const stlite_params* params, const LayerPtrs& io,
-                             const PagedRows* to = nullptr) {
+                             const PagedRows* to = nullptr, int first = 0) {
   const bool tsg = params->tsg_enable && c.ft.n_frames >= 2;
   const bool window = params->base_scorer == STLITE_BASE_WINDOW;
   Strided<float> a_base = c.view<float>(c.plan.a_base);
@@ -492,6 +499,16 @@ stlite_status compress_batch(const Ctx& c, const stlite_params* params, const La
   a.write_stages = 0;  // rho, gate and S stay on chip: only the indices leave
   for (int l = 0; l < c.p.L; ++l) a.idx[l] = io.idx[l];
   if ((e = launch_select(c.p, c.ft, a, c.st)) != cudaSuccess) return STLITE_ECUDA;
+  if (to && to->q4) {
+    Q4Layers rows = {};
+    for (int l = 0; l < c.p.L; ++l) {
+      rows.k[l] = io.k[l];
+      rows.v[l] = io.v[l];
+      rows.idx[l] = io.idx[l];
+      rows.pools[l] = q4_view(to->q4[first + l].pools);
+    }
+    return cuda_status(launch_gather_q4(c.p, rows, to->budget, to->pages, to->seq, c.st));
+  }
   return cuda_status(to ? launch_gather_paged(c.p, io, to->pages, to->seq, c.st) : launch_gather(c.p, io, c.st));
 }
 
@@ -685,7 +702,7 @@ stlite_status compress_layers_impl(const stlite_shape* shape, const stlite_frame
       io.idx[l] = x.idx_out;
       io.budget[l] = to ? to->budget : budgets[l0 + l];
     }
-    if ((s = compress_batch(cb, params, io, to)) != STLITE_OK) return s;
+    if ((s = compress_batch(cb, params, io, to, l0)) != STLITE_OK) return s;
   }
   return STLITE_OK;
 }
@@ -1269,10 +1286,179 @@ stlite_status stlite_compress_layers_paged(const stlite_shape* shape, const stli
   if (seq < 0 || seq >= pages->n_seqs) return STLITE_EINVAL;
   const int32_t budget = stlite_budget(shape->n_tokens, params->beta, params->k_override);
   if (budget < 1 || budget > (long long)pages->max_pages * pages->page_rows) return STLITE_EINVAL;
-  const PagedRows to = {page_view(pages, 1), seq, budget};
+  const PagedRows to = {page_view(pages, 1), seq, budget, nullptr};
   s = compress_layers_impl(shape, frames, params, n_layers, layers, nullptr, ws, ws_bytes, stream, true, &to);
   if (s == STLITE_OK && budget_out) *budget_out = budget;
   return s;
+}
+
+// ---- pages in 4 bits ----------------------------------------------------------
+namespace {
+
+stlite_status check_q4_pools(const stlite_q4_pools* p) {
+  if (!p || !p->k || !p->v || !p->k_scale || !p->v_scale) return STLITE_EINVAL;
+  if (!aligned16(p->k) || !aligned16(p->v) || ((uintptr_t)p->k_scale & 7u) || ((uintptr_t)p->v_scale & 7u) ||
+      !aligned4(p->k_factor) || !aligned4(p->v_factor))
+    return STLITE_EINVAL;
+  return STLITE_OK;
+}
+
+// Every layer's rows and pools; idx: the call takes indices.
+stlite_status check_q4_layers(int n_layers, const stlite_q4_layer* layers, bool idx) {
+  if (n_layers < 1 || !layers) return STLITE_EINVAL;
+  for (int l = 0; l < n_layers; ++l) {
+    const stlite_q4_layer& x = layers[l];
+    if (!x.k || !x.v || !aligned16(x.k) || !aligned16(x.v)) return STLITE_EINVAL;
+    if (idx && (!x.idx || !aligned4(x.idx))) return STLITE_EINVAL;
+    const stlite_status s = check_q4_pools(&x.pools);
+    if (s != STLITE_OK) return s;
+  }
+  return STLITE_OK;
+}
+
+Q4Layers q4_layers(const stlite_q4_layer* layers, int L) {
+  Q4Layers io = {};
+  for (int l = 0; l < L; ++l) {
+    io.k[l] = layers[l].k;
+    io.v[l] = layers[l].v;
+    io.idx[l] = layers[l].idx;
+    io.pools[l] = q4_view(layers[l].pools);
+  }
+  return io;
+}
+
+}  // namespace
+
+stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope, const stlite_tokens* x,
+                                     const stlite_pages* pages, void* q_out, const stlite_q4_pools* pools,
+                                     void* stream) {
+  stlite_status s = check_step_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, true)) != STLITE_OK) return s;
+  if ((s = check_new(shape, pages)) != STLITE_OK) return s;
+  if ((s = check_rope(rope)) != STLITE_OK) return s;
+  if (shape->n_tokens == 0) return STLITE_OK;
+  TokenView v;
+  if ((s = token_view(shape, rope, x, true, &v)) != STLITE_OK) return s;
+  if (!q_out || !aligned16(q_out)) return STLITE_EINVAL;
+  if ((s = check_q4_pools(pools)) != STLITE_OK) return s;
+  if (!in_place_ok(x->q, v.q_stride, v.hq, q_out)) return STLITE_EINVAL;
+  return cuda_status(launch_append_q4(to_dtype(shape), v, rope_view(rope), page_view(pages, shape->window),
+                                      q4_view(*pools), q_out, static_cast<cudaStream_t>(stream)));
+}
+
+stlite_status stlite_paged_q4_workspace_size(const stlite_shape* shape, const stlite_pages* pages, size_t* bytes) {
+  if (!bytes) return STLITE_EINVAL;
+  const stlite_status s = check_paged_attention(shape, pages);
+  if (s != STLITE_OK) return s;
+  *bytes = paged_q4_workspace_bytes(to_dtype(shape), page_view(pages, shape->window), shape->n_q_heads,
+                                    shape->n_kv_heads);
+  return STLITE_OK;
+}
+
+stlite_status stlite_paged_attention_q4(const stlite_shape* shape, const stlite_pages* pages, const void* q,
+                                        const stlite_q4_pools* pools, void* out, void* ws, size_t ws_bytes,
+                                        void* stream) {
+  stlite_status s = check_paged_attention(shape, pages);
+  if (s != STLITE_OK || shape->n_tokens == 0) return s;
+  if (!q || !out || !ws || !aligned16(q) || !aligned16(out) || !aligned16(ws)) return STLITE_EINVAL;
+  if ((s = check_q4_pools(pools)) != STLITE_OK) return s;
+  const PageView pg = page_view(pages, shape->window);
+  const DType dt = to_dtype(shape);
+  if (ws_bytes < paged_q4_workspace_bytes(dt, pg, shape->n_q_heads, shape->n_kv_heads)) return STLITE_EWORKSPACE;
+  return cuda_status(launch_paged_attention_q4(dt, pg, q, q4_view(*pools), out, shape->n_tokens, shape->n_q_heads,
+                                               shape->n_kv_heads, ws, static_cast<cudaStream_t>(stream)));
+}
+
+stlite_status stlite_compact_paged_q4(const stlite_shape* shape, int32_t budget, const stlite_pages* pages,
+                                      int32_t seq, int32_t n_layers, const stlite_q4_layer* layers, void* stream) {
+  stlite_status s = check_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, false)) != STLITE_OK) return s;
+  if (seq < 0 || seq >= pages->n_seqs) return STLITE_EINVAL;
+  if (budget < 1 || budget > shape->n_tokens || budget > (long long)pages->max_pages * pages->page_rows)
+    return STLITE_EINVAL;
+  if ((s = check_q4_layers(n_layers, layers, true)) != STLITE_OK) return s;
+  const PageView pg = page_view(pages, 1);
+  for (int l0 = 0; l0 < n_layers; l0 += kMaxLayers) {
+    const int L = n_layers - l0 < kMaxLayers ? n_layers - l0 : kMaxLayers;
+    s = cuda_status(launch_gather_q4(to_problem(shape, L), q4_layers(layers + l0, L), budget, pg, seq,
+                                     static_cast<cudaStream_t>(stream)));
+    if (s != STLITE_OK) return s;
+  }
+  return STLITE_OK;
+}
+
+stlite_status stlite_compress_layers_paged_q4(const stlite_shape* shape, const stlite_frames* frames,
+                                              const stlite_params* params, const stlite_pages* pages, int32_t seq,
+                                              int32_t n_layers, const stlite_q4_layer* layers, int32_t* budget_out,
+                                              void* ws, size_t ws_bytes, void* stream) {
+  if (!shape) return STLITE_EINVAL;
+  stlite_status s = check_params(params);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, false)) != STLITE_OK) return s;
+  if (seq < 0 || seq >= pages->n_seqs) return STLITE_EINVAL;
+  const int32_t budget = stlite_budget(shape->n_tokens, params->beta, params->k_override);
+  if (budget < 1 || budget > (long long)pages->max_pages * pages->page_rows) return STLITE_EINVAL;
+  if ((s = check_q4_layers(n_layers, layers, true)) != STLITE_OK) return s;
+  // the pass's own checks see each layer's rows in place of dense outputs
+  std::vector<stlite_layer_io> io;
+  try {
+    io.resize(n_layers);
+  } catch (...) {  // no exception leaves a C entry
+    return STLITE_EUNSUPPORTED;
+  }
+  for (int l = 0; l < n_layers; ++l)
+    io[l] = {layers[l].q, layers[l].k, layers[l].v, layers[l].pools.k, layers[l].pools.v, layers[l].idx};
+  const PagedRows to = {page_view(pages, 1), seq, budget, layers};
+  s = compress_layers_impl(shape, frames, params, n_layers, io.data(), nullptr, ws, ws_bytes, stream, true, &to);
+  if (s == STLITE_OK && budget_out) *budget_out = budget;
+  return s;
+}
+
+stlite_status stlite_paged_fetch_q4(const stlite_shape* shape, const stlite_pages* pages, int32_t n_layers,
+                                    const stlite_q4_layer* layers, void* stream) {
+  stlite_status s = check_step_shape(shape);
+  if (s != STLITE_OK) return s;
+  if ((s = check_pages(pages, true)) != STLITE_OK) return s;
+  if ((s = check_new(shape, pages)) != STLITE_OK) return s;
+  if ((long long)shape->n_tokens * shape->n_kv_heads > 0x7fffffc0LL) return STLITE_EUNSUPPORTED;
+  if (n_layers < 1) return STLITE_EINVAL;
+  if (shape->n_tokens == 0) return STLITE_OK;
+  if ((s = check_q4_layers(n_layers, layers, false)) != STLITE_OK) return s;
+  const PageView pg = page_view(pages, shape->window);
+  for (int l0 = 0; l0 < n_layers; l0 += kMaxLayers) {
+    const int L = n_layers - l0 < kMaxLayers ? n_layers - l0 : kMaxLayers;
+    s = cuda_status(launch_fetch_q4(to_dtype(shape), q4_layers(layers + l0, L), L, shape->n_tokens, shape->n_kv_heads,
+                                    pg, static_cast<cudaStream_t>(stream)));
+    if (s != STLITE_OK) return s;
+  }
+  return STLITE_OK;
+}
+
+stlite_status stlite_pages_step(const stlite_pages* pages, const int32_t* keep, const int32_t* fresh,
+                                int32_t* free_pages, int32_t* n_free, int32_t n_tokens, int32_t* slot, void* stream) {
+  const stlite_status s = check_pages(pages, true);
+  if (s != STLITE_OK) return s;
+  if (!pages->cu_new || !fresh || !free_pages || !n_free || n_tokens < 0) return STLITE_EINVAL;
+  if (!aligned4(keep) || !aligned4(fresh) || !aligned4(free_pages) || !aligned4(n_free) || !aligned4(slot))
+    return STLITE_EINVAL;
+  StepView v;
+  // the step is the one call that writes them
+  v.table = const_cast<int32_t*>(pages->table);
+  v.len = const_cast<int32_t*>(pages->len);
+  v.cu = const_cast<int32_t*>(pages->cu_new);
+  v.keep = keep;
+  v.fresh = fresh;
+  v.free_pages = free_pages;
+  v.n_free = n_free;
+  v.slot = slot;
+  v.n_seqs = pages->n_seqs;
+  v.n_pages = pages->n_pages;
+  v.page_rows = pages->page_rows;
+  v.max_pages = pages->max_pages;
+  v.n_tokens = n_tokens;
+  return cuda_status(launch_pages_step(v, static_cast<cudaStream_t>(stream)));
 }
 
 stlite_status stlite_device_status(void* ws, void* stream, stlite_status* status) {

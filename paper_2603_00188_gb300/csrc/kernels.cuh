@@ -311,4 +311,43 @@ size_t paged_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv);
 cudaError_t launch_paged_attention(DType dt, const PageView& pages, const void* q, const void* k, const void* v,
                                    void* out, int n, int hq, int hkv, void* ws, cudaStream_t st);
 
+// ---- pages in 4 bits ---------------------------------------------------------
+// A layer's pools: codes [n_pages][hkv][page_rows][64], scales [..][8], and a
+// factor for each KV head (null: 1).
+struct Q4View {
+  uint8_t *k, *v, *k_scale, *v_scale;
+  const float *k_factor, *v_factor;
+};
+// Layers of one launch: the dense rows k, v (read by the compaction, written by
+// the fetch) and the pools.
+struct Q4Layers {
+  const void* k[kMaxLayers];
+  const void* v[kMaxLayers];
+  const int32_t* idx[kMaxLayers];
+  Q4View pools[kMaxLayers];
+};
+// launch_rotate with keys and values going to 4-bit pages.
+cudaError_t launch_append_q4(DType dt, const TokenView& x, const RopeView& rope, const PageView& pages,
+                             const Q4View& pools, void* q_out, cudaStream_t st);
+// Rows idx[h][r] of every layer to row r of sequence seq's 4-bit pages.
+cudaError_t launch_gather_q4(const Problem& p, const Q4Layers& io, int budget, const PageView& pages, int seq,
+                             cudaStream_t st);
+// The rows of n packed new tokens (see PageView::cu) to k, v [n][hkv][128].
+cudaError_t launch_fetch_q4(DType dt, const Q4Layers& io, int layers, int n, int hkv, const PageView& pages,
+                            cudaStream_t st);
+// launch_paged_attention over 4-bit pages.
+size_t paged_q4_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv);
+cudaError_t launch_paged_attention_q4(DType dt, const PageView& pages, const void* q, const Q4View& pools, void* out,
+                                      int n, int hq, int hkv, void* ws, cudaStream_t st);
+
+// ---- page tables ---------------------------------------------------------------
+// A step's pages: see stlite_pages_step.
+struct StepView {
+  int32_t *table, *len, *cu;
+  const int32_t *keep, *fresh;
+  int32_t *free_pages, *n_free, *slot;
+  int n_seqs, n_pages, page_rows, max_pages, n_tokens;
+};
+cudaError_t launch_pages_step(const StepView& s, cudaStream_t st);
+
 }  // namespace stl

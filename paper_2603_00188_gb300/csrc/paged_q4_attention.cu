@@ -1,0 +1,536 @@
+// Attention of a serving step's new tokens over paged caches in 4 bits:
+//   out[t][g] = sum_j softmax_j(q_{t,g} . K_j / sqrt(d)) V_j,
+//   K = code * scale * factor (q4.cuh), and V the same,
+// over the rows that paged_attention.cu says, divided among CTAs as there
+// (paged_split.cuh).
+//
+// Each warp streams its own blocks of 16 rows through its own ring in shared
+// memory and decodes them in registers, as operands of its tensor cores'
+// m16n8k16 products of fp16 with fp32 sums:
+//   S (16 rows x 8 queries) = K Q^T: a lane takes 32 neighbouring elements of a
+//     row (one 16-byte read; four codes a step, the sum's order is free),
+//   O^T (128 dims x 8 queries) += V^T P^T: a lane takes one group of 16 elements
+//     of each of four rows, whose codes it pairs by rows (the sum runs over
+//     them) before they are decoded.
+// code * scale is exact in fp16. What is rounded: queries, scaled by a power of
+// two so that the largest element of each is in [1, 2), to fp16, which holds
+// bf16 ones exactly down to 2^-17 of the largest and loses less than 2^-25 of
+// it below; and weights, to fp16's 11 bits (2^-12, an eighth of the bf16
+// result's own rounding).  fp32 queries and their weights are taken as hi + lo,
+// two parts of 11 bits, which is twice the products.
+//
+// Weights are 2^(x - m) with m moved only when a score exceeds it by more than
+// 2^4, at most 2^14 (fp16 goes to 2^16): no maximum is formed for blocks that do
+// not exceed it.
+#include <type_traits>
+
+#include "paged_split.cuh"
+#include "q4.cuh"
+
+namespace stl {
+
+constexpr int kQaCtas = 2;    // per SM
+constexpr int kQaStages = 4;  // of a warp's ring
+constexpr int kQaCodes = kPatBlock * kQ4Row, kQaScales = kPatBlock * kQ4Scales;  // of keys, or of values, of a block
+constexpr int kQaStage = 2 * (kQaCodes + kQaScales);
+constexpr int kQaPitch = kD + 4;      // floats from row to row of the merge buffer
+constexpr float kQaLift = 10.f;       // weights are 2^(x - m), m their reference less this
+constexpr float kQaSlack = 4.f;       // how far a score may exceed the reference
+// Warps of a CTA: eight where 128 registers hold a warp's state.
+__host__ __device__ constexpr int qa_warps(int nt) { return nt == 1 ? 8 : 4; }
+// Bytes of shared memory for queries; none where they are in registers.
+__host__ __device__ constexpr int qa_queries(int nt, int parts) { return 8 * nt * parts > 16 ? 8 * nt * parts * kD * 2 : 0; }
+__host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
+__host__ __device__ constexpr int qa_factors(int nt) {
+  return 8 * nt * 4 * (1 + qa_warps(nt)) > (int)sizeof(RangeScratch<256>) ? 8 * nt * 4 * (1 + qa_warps(nt))
+                                                                          : (int)sizeof(RangeScratch<256>);
+}
+__host__ __device__ constexpr int qa_smem(int nt, int parts) {
+  return qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (kQaPitch * 4 + nt * 8) + qa_factors(nt);
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+// The 8 x 8 matrix of 16-bit values held two to a lane, transposed.
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void cp_async8_fill(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
+}
+
+// Four neighbouring elements of a query.
+__device__ __forceinline__ float4 load_query4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load_query4(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+
+// Byte of the 16-byte chunk c of value row r in its block: eight rows' first
+// chunks, which a read takes together, lie in different banks.
+__device__ __forceinline__ uint32_t qa_value_off(int r, int c) {
+  return (uint32_t)((r >> 1) * 128 + ((((r & 1) * 4 + c) ^ (((r >> 1) & 3) << 1)) << 4));
+}
+
+// NT: groups of eight queries that share one read of the cache.
+template <typename T, int NT>
+__global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
+    k_paged_q4(const __grid_constant__ PageView pg, const __grid_constant__ Q4View pools, const T* q, T* out, int n,
+               int hq, int hkv, int mode, int split, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
+               float* part_o, uint32_t* err) {
+  constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;  // of a query's elements and of a weight
+  constexpr int kRows = 8 * NT, kWarps = qa_warps(NT), kThreads = 32 * kWarps;
+  constexpr bool kRegs = qa_queries(NT, kParts) == 0;  // queries in registers, else in shared memory
+  extern __shared__ uint4 pat_smem[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
+  uint2* qs = reinterpret_cast<uint2*>(sm + qa_ring(NT));  // [part][NT][step][lane]
+  float* wo = reinterpret_cast<float*>(sm + qa_ring(NT) + qa_queries(NT, kParts));
+  float2* wml = reinterpret_cast<float2*>(wo + kWarps * 8 * kQaPitch);
+  RangeScratch<kThreads>* scratch = reinterpret_cast<RangeScratch<kThreads>*>(wml + kWarps * kRows);
+  // once an item has ended (the range was found long before): 1 / sum of each
+  // query, and the warps' factors
+  float* inv = reinterpret_cast<float*>(scratch);  // [kRows]
+  float* factor = inv + kRows;                     // [warps][kRows]
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
+  const int G = hq / hkv, cta = blockIdx.x;
+  uint8_t* stages = sm + warp * kQaStages * kQaStage;
+  const uint32_t ring = smem_u32(stages);
+  pdl_trigger();
+  pdl_wait();
+  const Range rg = find_range<kThreads>(pg, G, chunk_rows, hkv, kWarps, split, err, scratch);
+  const bool describes = tid == kThreads - 32;  // the thread that writes the CTA's descriptor
+  if (mode == kDescByCta && describes) desc[cta].item = -1;
+  if (cta >= rg.ctas) return;
+
+  RowFinder<kWarps, true> finder(rg);
+  uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
+  // a stage: keys' codes, values' codes, keys' scales, values' scales
+  auto fetch = [&](int stage, int row) {
+    if (row != -2) {
+      const uint64_t ok = __ballot_sync(0xffffffffu, row >= 0) & 0xffffu;
+      counts = (counts & ~(0xffffull << (16 * stage))) | ok << (16 * stage);
+      const uint32_t dst = ring + stage * kQaStage;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = __shfl_sync(0xffffffffu, row, g8 + 8 * i);
+        const size_t at = (size_t)max(r, 0) * kQ4Row + 16 * t4;
+        cp_async16_fill(dst + (g8 + 8 * i) * kQ4Row + 16 * t4, pools.k + at, r >= 0);
+        cp_async16_fill(dst + kQaCodes + qa_value_off(g8 + 8 * i, t4), pools.v + at, r >= 0);
+      }
+      // lane % 16's row is the lane's own: keys' scales by the first 16 lanes, values' by the others
+      cp_async8_fill(dst + 2 * kQaCodes + 8 * lane, (lane < 16 ? pools.k_scale : pools.v_scale) + (size_t)max(row, 0) * kQ4Scales,
+                     row >= 0);
+    }
+    cp_async_commit();
+  };
+  {
+    int first[kQaStages];  // all table entries on their way before the first copies
+#pragma unroll
+    for (int st = 0; st < kQaStages; ++st) first[st] = finder.next(pg, warp, G, chunk_rows, hkv, err);
+#pragma unroll
+    for (int st = 0; st < kQaStages; ++st) fetch(st, first[st]);
+  }
+
+  Cursor cur = rg.at;
+  int stage = 0;
+  for (int seg = rg.b0; seg < rg.b1;) {
+    // the part of one item that lies in the range: blocks part0 .. seg_end
+    advance(cur, seg, pg, G, chunk_rows, hkv);
+    const Item item = item_at(cur, seg);
+    const int h = item.h, chunk = item.chunk, part0 = max(seg, item.f0), seg_end = min(item.i1, rg.b1);
+    const int row0 = chunk * chunk_rows, rows = min(chunk_rows, min(cur.w.fresh, pg.w) * G - row0);
+    const bool owns = part0 == item.f0, whole = owns && seg_end == item.i1;  // has the first block, has them all
+    if (cur.w.blocks == 0 || part0 >= seg_end) {
+      if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
+        if (mode == kDescByItem && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
+        zero_rows<kThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
+      }
+      seg = seg_end;
+      continue;
+    }
+    if (describes && owns && mode != kWholeItems) {
+      const int id = (cur.s * hkv + h) * chunks + chunk;
+      const PartDesc d = {whole ? -1 : id, cta, whole ? cta : rg.cta_of(item.i1 - 1), 0};
+      if (mode == kDescByItem)
+        desc[id] = d;
+      else if (!whole)
+        desc[cta] = d;
+    }
+
+    // Queries: step ks takes elements 32 t4 + 4 ks .. + 3 of query 8 nt + g8.
+    // sc: what the sums of queries 8 nt + 2 t4 + e are multiplied by.
+    uint2 qr[kRegs ? kParts : 1][kRegs ? NT : 1][kRegs ? 8 : 1];
+    float sc[NT][2];
+    const float base_scale = kPatLog2e * rsqrtf((float)kD) * (pools.k_factor ? pools.k_factor[h] : 1.f);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + 8 * nt + g8, t = cur.w.first + r / G;
+      const bool ok = 8 * nt + g8 < rows && t >= 0 && t < n;
+      const T* from = q + ((size_t)(ok ? t : 0) * hq + h * G + r % G) * kD + 32 * t4;
+      float4 y[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        y[ks] = ok ? load_query4(from + 4 * ks) : make_float4(0.f, 0.f, 0.f, 0.f);
+        top = max(max(top, __float_as_uint(y[ks].x) & 0x7fffffffu), max(__float_as_uint(y[ks].y) & 0x7fffffffu, __float_as_uint(y[ks].z) & 0x7fffffffu));
+        top = max(top, __float_as_uint(y[ks].w) & 0x7fffffffu);
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int ex = min((int)(top >> 23), 253);
+      float mul = __uint_as_float((uint32_t)(254 - ex) << 23);  // 2^-exponent
+      const float back = base_scale / mul;
+      if (top >= 0x7f800000u) mul = CUDART_NAN_F;  // not all are numbers: nor are its scores
+#pragma unroll
+      for (int e = 0; e < 2; ++e) sc[nt][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e));
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        const float4 z = make_float4(y[ks].x * mul, y[ks].y * mul, y[ks].z * mul, y[ks].w * mul);
+        const uint2 hi = make_uint2(pack_f16(z.x, z.y), pack_f16(z.z, z.w));
+        uint2 lo = make_uint2(0u, 0u);
+        if (kParts == 2) {
+          const float2 a = unpack_f16(hi.x), b = unpack_f16(hi.y);
+          lo = make_uint2(pack_f16(z.x - a.x, z.y - a.y), pack_f16(z.z - b.x, z.w - b.y));
+        }
+        if constexpr (kRegs) {
+          qr[0][nt][ks] = hi;
+          if (kParts == 2) qr[kParts - 1][nt][ks] = lo;
+        } else if (warp == 0) {
+          qs[(nt * 8 + ks) * 32 + lane] = hi;
+          if (kParts == 2) qs[((NT + nt) * 8 + ks) * 32 + lane] = lo;
+        }
+      }
+    }
+    if constexpr (!kRegs) __syncthreads();
+
+    // Running state: reference and the lane's part of the sum of queries
+    // 8 nt + 2 t4 + e; o[mt][nt][j] is dimension 16 g8 + 2 mt + (j >> 1) of
+    // query 8 nt + 2 t4 + (j & 1).
+    float m[NT][2], l[NT][2], o[8][NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -1e30f;
+      l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
+    }
+    const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
+    for (int u = warps_first<kWarps>(part0, warp); u < seg_end; u += kWarps) {
+      cp_async_wait<kQaStages - 1>();
+      __syncwarp();
+      const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
+      const uint8_t* at = stages + stage * kQaStage;
+      const uint8_t* scales = at + 2 * kQaCodes;
+      const int base = (u - item.f0) * kPatBlock;
+      float c[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+      {
+        const uint4 w0 = *reinterpret_cast<const uint4*>(at + g8 * kQ4Row + 16 * t4);
+        const uint4 w1 = *reinterpret_cast<const uint4*>(at + (g8 + 8) * kQ4Row + 16 * t4);
+        const uint32_t s0 = q4_scales(*reinterpret_cast<const uint16_t*>(scales + g8 * kQ4Scales + 2 * t4));
+        const uint32_t s1 = q4_scales(*reinterpret_cast<const uint16_t*>(scales + (g8 + 8) * kQ4Scales + 2 * t4));
+        const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t f0 = __byte_perm(s0, 0, i < 2 ? 0x1010 : 0x3232), f1 = __byte_perm(s1, 0, i < 2 ? 0x1010 : 0x3232);
+          uint32_t p0[4], p1[4];
+          q4_codes(x0[i], p0);
+          q4_codes(x1[i], p1);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t a[4] = {mul_f16x2(p0[2 * j], f0), mul_f16x2(p1[2 * j], f1), mul_f16x2(p0[2 * j + 1], f0),
+                                   mul_f16x2(p1[2 * j + 1], f1)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int part = 0; part < kParts; ++part) {
+                uint2 b;
+                if constexpr (kRegs)
+                  b = qr[part][nt][2 * i + j];
+                else
+                  b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
+                mma_f16(c[nt], a, b.x, b.y);
+              }
+          }
+        }
+      }
+      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
+      if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
+            const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+            // times a factor above zero
+            if (!(ok >> r & 1u) || base + r >= sees) c[nt][j] = -CUDART_INF_F;
+          }
+      }
+      // Scores over their references, in powers of two.  A product and a difference,
+      // each rounded: fused, a huge score would exceed itself.
+      float d[NT][4];
+      bool moved = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          c[nt][j] = __fmul_rn(c[nt][j], sc[nt][j & 1]);
+          d[nt][j] = __fsub_rn(c[nt][j], m[nt][j & 1]);
+          moved |= d[nt][j] > kQaLift + kQaSlack;
+        }
+      if (__any_sync(0xffffffffu, moved)) {  // rare once the references have settled
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float mx = fmaxf(c[nt][e], c[nt][2 + e]) - kQaLift;
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+            mx = fmaxf(m[nt][e], mx);
+            const float alpha = ex2_approx(m[nt][e] - mx);
+            m[nt][e] = mx;
+            l[nt][e] *= alpha;
+            d[nt][e] = c[nt][e] - mx;
+            d[nt][2 + e] = c[nt][2 + e] - mx;
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) {
+              o[mt][nt][e] *= alpha;
+              o[mt][nt][2 + e] *= alpha;
+            }
+          }
+      }
+      uint32_t p[kParts][NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // scores become weights
+          c[nt][j] = ex2_approx(d[nt][j]);
+          l[nt][j & 1] += c[nt][j];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t hi = pack_f16(c[nt][2 * x], c[nt][2 * x + 1]);
+          p[0][nt][x] = turn8x8(hi);
+          if (kParts == 2) {
+            const float2 z = unpack_f16(hi);
+            p[kParts - 1][nt][x] = turn8x8(pack_f16(c[nt][2 * x] - z.x, c[nt][2 * x + 1] - z.y));
+          }
+        }
+      }
+      {
+        const uint8_t* vs = scales + kQaScales + g8;
+        uint32_t b[2];  // scales of rows 2 t4, 2 t4 + 1, and of those + 8
+#pragma unroll
+        for (int i = 0; i < 2; ++i) b[i] = vs[(2 * t4 + 8 * i) * kQ4Scales] | vs[(2 * t4 + 8 * i + 1) * kQ4Scales] << 8;
+        // A scale that is no number makes its group's results so for the tokens
+        // that see its row; a weight of 0 would carry it to the others too.
+        const bool odd = (((b[0] & 0x7f7fu) + 0x0101u) | ((b[1] & 0x7f7fu) + 0x0101u)) & 0x8080u;
+        if (__any_sync(0xffffffffu, odd)) {
+          uint32_t which = 0;  // rows, of the lane's four
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
+              which |= 1u << (2 * t4 + 8 * (i >> 1) + (i & 1));
+              b[i >> 1] &= ~(0xffu << (8 * (i & 1)));
+            }
+          which |= __shfl_xor_sync(0xffffffffu, which, 1);
+          which |= __shfl_xor_sync(0xffffffffu, which, 2);
+          which &= ok;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base;  // of the block's rows
+              if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
+#pragma unroll
+                for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
+            }
+        }
+        const uint32_t f0 = q4_scales(b[0]), f1 = q4_scales(b[1]);
+        const uint8_t* vt = at + kQaCodes + 8 * (g8 & 1);
+        uint2 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = *reinterpret_cast<const uint2*>(vt + qa_value_off(2 * t4 + 8 * (i >> 1) + (i & 1), g8 >> 1));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          // bytes of two rows' codes of one dimension: even dimensions, odd ones
+          const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
+                         r3 = i ? w[3].y : w[3].x;
+          uint32_t even0[4], odd0[4], even1[4], odd1[4];
+          q4_codes((r0 & 0x0f0f0f0fu) | (r1 << 4 & 0xf0f0f0f0u), even0);
+          q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
+          q4_codes((r2 & 0x0f0f0f0fu) | (r3 << 4 & 0xf0f0f0f0u), even1);
+          q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t a[4] = {mul_f16x2(even0[j], f0), mul_f16x2(odd0[j], f0), mul_f16x2(even1[j], f1),
+                                   mul_f16x2(odd1[j], f1)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+          }
+        }
+      }
+      __syncwarp();
+      fetch(stage, next);
+      stage = stage + 1 == kQaStages ? 0 : stage + 1;
+    }
+    // The warps' states of this item, merged in shared memory, eight queries at
+    // a time.
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float s = l[nt][e];
+        s += __shfl_xor_sync(0xffffffffu, s, 4);
+        s += __shfl_xor_sync(0xffffffffu, s, 8);
+        s += __shfl_xor_sync(0xffffffffu, s, 16);
+        if (g8 == 0) wml[warp * kRows + 8 * nt + 2 * t4 + e] = make_float2(m[nt][e], s);
+      }
+    __syncthreads();
+    const int part = 2 * cta + (owns ? 1 : 0);
+    const float vf = pools.v_factor ? pools.v_factor[h] : 1.f;
+    // a thread for each warp's query: its factor, and, from the first warp's
+    // thread, the query's maximum and sum over the warps
+    for (int e = tid; e < kWarps * kRows; e += kThreads) {
+      const int x = e % kRows;
+      float M = -CUDART_INF_F;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
+      factor[e] = pat_weight(wml[e].x, M) * vf;
+      if (e < rows) {
+        float L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) L = fmaf(wml[w * kRows + x].y, pat_weight(wml[w * kRows + x].x, M), L);
+        if (whole)
+          inv[x] = L == 0.f ? 0.f : 1.f / L;
+        else
+          part_ml[part * kRows + x] = make_float2(M, L);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n0 = 0; n0 < NT; ++n0) {
+      if (n0 > 0) __syncthreads();  // the buffer is free again
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int x = 2 * t4 + e;
+        const float a = factor[warp * kRows + 8 * n0 + x];
+        float* w = wo + (warp * 8 + x) * kQaPitch + 16 * g8;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          store4(w + 4 * k, o[2 * k][n0][e] * a, o[2 * k][n0][2 + e] * a, o[2 * k + 1][n0][e] * a, o[2 * k + 1][n0][2 + e] * a);
+      }
+      __syncthreads();
+      for (int y = warp; y < min(8, rows - 8 * n0); y += kWarps) {
+        const int x = 8 * n0 + y;
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 + y) * kQaPitch + 4 * lane);
+          O.x += z.x;
+          O.y += z.y;
+          O.z += z.z;
+          O.w += z.w;
+        }
+        if (whole) {
+          const int r = row0 + x, t = cur.w.first + r / G;
+          const float f = inv[x];
+          if (t >= 0 && t < n)
+            store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * f, O.y * f, O.z * f, O.w * f);
+        } else {
+          store4(part_o + ((size_t)part * kRows + x) * kD + 4 * lane, O.x, O.y, O.z, O.w);
+        }
+      }
+    }
+    seg = seg_end;
+    if (seg < rg.b1) __syncthreads();  // the merge buffer (and the queries) are free again
+  }
+  cp_async_wait<0>();
+}
+
+// -------------------------------------------------------------------- launch
+static int q4_ctas() {
+  int dev = 0, sms = 152;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return kQaCtas * sms < kPatMaxCtas ? kQaCtas * sms : kPatMaxCtas;
+}
+
+// Query rows of a CTA's part, which share one read of the cache: at most 32, or
+// 16 of fp32 (two parts of each).
+static int q4_most_rows(DType dt) { return dt == kF32 ? 16 : 32; }
+static int q4_part_rows(DType dt, const PageView& pages, int G) {
+  const int rows = pages.w * G, most = q4_most_rows(dt), chunks = (rows + most - 1) / most;
+  return ((rows + chunks - 1) / chunks + 7) / 8 * 8;
+}
+
+// Workspace: as paged_workspace_bytes says.
+constexpr size_t kQaHead = 256, kQaDescs = kPatMaxCtas * sizeof(PartDesc);
+size_t paged_q4_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
+  return kQaHead + kQaDescs +
+         (size_t)2 * q4_ctas() * q4_part_rows(dt, pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
+}
+
+cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void* q, const Q4View& pools, void* out,
+                                      int n, int hq, int hkv, void* ws, cudaStream_t st) {
+  PageView pages = view;
+  uint32_t* err = static_cast<uint32_t*>(ws);
+  const int rows = pages.w * (hq / hkv), part_rows = q4_part_rows(dt, pages, hq / hkv), most = q4_most_rows(dt);
+  const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas();
+  const long long items = (long long)pages.n_seqs * hkv * chunks;
+  pages.item_units = 12;
+  int split = 48;
+  const long long longest = ((long long)pages.max_pages * pages.page_rows + kPatBlock - 1) / kPatBlock;
+  const int mode = longest <= 32 ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
+  if (mode == kWholeItems) split = 1 << 30;
+  const int descs = items <= ctas ? (int)items : ctas;
+  uint8_t* at = static_cast<uint8_t*>(ws) + kQaHead;
+  PartDesc* desc = reinterpret_cast<PartDesc*>(at);
+  float2* part_ml = reinterpret_cast<float2*>(at + kQaDescs);
+  float* part_o = reinterpret_cast<float*>(part_ml + (size_t)2 * ctas * part_rows);
+  cudaError_t e = cudaSuccess;
+  auto run = [&](auto zero, auto width) {
+    typedef decltype(zero) T;
+    constexpr int NT = decltype(width)::value, kParts = std::is_same<T, float>::value ? 2 : 1;
+    static_assert(fits_sm(qa_smem(NT, kParts), kQaCtas), "kQaCtas per SM");
+    TimingScope ts("paged_attention_q4", st);
+    auto kern = k_paged_q4<T, NT>;
+    const int smem = qa_smem(NT, kParts);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return;
+    e = launch_after(kern, dim3(ctas), 32 * qa_warps(NT), smem, st, pages, pools, static_cast<const T*>(q),
+                     static_cast<T*>(out), n, hq, hkv, mode, split, chunks, chunk_rows, desc, part_ml, part_o, err);
+  };
+  if (dt == kF32)
+    part_rows == 8 ? run(float(), std::integral_constant<int, 1>()) : run(float(), std::integral_constant<int, 2>());
+  else if (part_rows <= 16)
+    part_rows == 8 ? run(__nv_bfloat16(), std::integral_constant<int, 1>())
+                   : run(__nv_bfloat16(), std::integral_constant<int, 2>());
+  else
+    part_rows == 24 ? run(__nv_bfloat16(), std::integral_constant<int, 3>())
+                    : run(__nv_bfloat16(), std::integral_constant<int, 4>());
+  if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
+  if (mode == kWholeItems) return cudaSuccess;
+  e = launch_paged_merge(dt, pages, out, n, hq, hkv, chunks, chunk_rows, part_rows, mode == kDescByItem, descs, desc,
+                         part_ml, part_o, st);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace stl

@@ -1,0 +1,153 @@
+// Page tables, lengths and places of a serving step.
+#include "kernels.cuh"
+
+namespace stl {
+
+// All of a step in one launch of one cluster.  Each CTA sums over all sessions
+// for itself, kStepThreads of them at a time, a thread a session; the entries
+// to move are then dealt out flat, to all threads of the cluster, which find
+// an entry's session among the sums in shared memory.  Two waits of the whole
+// cluster separate what reads the state before from what changes it: pages that
+// go back are on the free list before any is taken, and lengths are written
+// when no CTA reads the old ones.  Latency bounds it: lengths, table, free list.
+constexpr int kStepThreads = 512, kStepCtas = 8;
+
+__device__ __forceinline__ void cluster_wait_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The sum of x over the threads up to this one; *total: over all.  Whole CTA.
+__device__ __forceinline__ long long scan(long long x, long long* warp_sums, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kStepThreads / 32; ++w) {
+    const long long y = warp_sums[w];
+    if (w < warp) before += y;
+    all += y;
+  }
+  __syncthreads();
+  *total = all;
+  return x + before;
+}
+
+// The last of the kStepThreads sessions whose entries begin at or before j.
+__device__ __forceinline__ int session_of(const int* start, int j) {
+  int lo = 0;
+#pragma unroll
+  for (int step = kStepThreads / 2; step > 0; step >>= 1)
+    if (start[lo + step] <= j) lo += step;
+  return lo;
+}
+
+__global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads)
+    k_pages_step(const __grid_constant__ StepView s) {
+  __shared__ int start[kStepThreads], tok_start[kStepThreads], kept_of[kStepThreads], keep_of[kStepThreads];
+  __shared__ long long warp_sums[kStepThreads / 32];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, rank = blockIdx.x, flat = rank * kStepThreads + tid, all = kStepCtas * kStepThreads;
+  const int rows_max = s.max_pages * s.page_rows, pr = s.page_rows;
+  const int n0 = max(0, min(*s.n_free, s.n_pages));
+  int have = 0, keep = 0, fresh = 0, held = 0, kept = 0;
+  auto load = [&](int s0) {
+    have = keep = fresh = 0;
+    const int i = s0 + tid;
+    if (i < s.n_seqs) {
+      have = max(0, min(s.len[i], rows_max));
+      keep = s.keep ? max(0, min(s.keep[i], have)) : have;
+      fresh = max(0, s.fresh[i]);
+    }
+    held = have / pr + (have % pr != 0);
+    kept = keep / pr + (keep % pr != 0);
+  };
+  // pages past the rows that stay go on top of the free ones
+  long long back = 0, total;
+  for (int s0 = 0; s0 < s.n_seqs; s0 += kStepThreads) {
+    load(s0);
+    const int mine = held - kept;
+    const long long incl = scan(mine, warp_sums, &total);
+    start[tid] = (int)incl - mine;
+    kept_of[tid] = kept;
+    __syncthreads();
+    for (int j = flat; j < total; j += all) {
+      const int b = session_of(start, j);
+      const long long to = n0 + back + j;
+      if (to < s.n_pages)
+        s.free_pages[to] = s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]];
+    }
+    back += total;
+    if (s0 + kStepThreads < s.n_seqs) __syncthreads();
+  }
+  cluster_wait_all();
+  const int n_free = (int)min((long long)s.n_pages, n0 + back);
+
+  // who is served, and what it gets
+  long long asked_pages = 0, asked_tokens = 0;
+  int taken = 0, given = 0;  // pages and tokens of the sessions before
+  int new_len = 0;
+  if (rank == 0 && tid == 0) s.cu[0] = 0;
+  for (int s0 = 0; s0 < s.n_seqs; s0 += kStepThreads) {
+    if (s.n_seqs > kStepThreads) load(s0);
+    const bool fits = fresh <= rows_max - keep;
+    const int rows = fits ? keep + fresh : keep, want = rows / pr + (rows % pr != 0) - kept;
+    long long incl = asked_pages + scan(want, warp_sums, &total);
+    asked_pages += total;
+    const bool may = fits && (want == 0 || incl <= n_free);
+    incl = asked_tokens + scan(may ? fresh : 0, warp_sums, &total);
+    asked_tokens += total;
+    const bool served = may && (fresh == 0 || incl <= s.n_tokens);
+    const int pages = served ? want : 0, got = served ? fresh : 0;
+    // both sums are below 2^31: pages of the pool, places of the step
+    incl = scan((long long)pages << 32 | got, warp_sums, &total);
+    const int my_pages = (int)(incl >> 32) - pages, my_tokens = (int)(incl & 0xffffffffu) - got;
+    start[tid] = my_pages;
+    tok_start[tid] = my_tokens;
+    kept_of[tid] = kept;
+    keep_of[tid] = keep;
+    new_len = keep + got;
+    if (rank == 0 && s0 + tid < s.n_seqs) s.cu[s0 + tid + 1] = given + my_tokens + got;
+    __syncthreads();
+    const int n_pages = (int)(total >> 32), n_tok = (int)(total & 0xffffffffu), top = n_free - 1 - taken;
+    for (int j = flat; j < n_pages; j += all) {
+      const int b = session_of(start, j);
+      s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]] = s.free_pages[top - j];
+    }
+    if (s.slot)
+      for (int j = flat; j < n_tok; j += all) {
+        const int b = session_of(tok_start, j), row = keep_of[b] + j - tok_start[b], i = row / pr;
+        const int page = i < kept_of[b] ? s.table[(size_t)(s0 + b) * s.max_pages + i]
+                                        : s.free_pages[top - (start[b] + i - kept_of[b])];
+        s.slot[given + j] = page >= 0 && page < s.n_pages ? page * pr + (row - i * pr) : -1;
+      }
+    taken += n_pages;
+    given += n_tok;
+    if (s0 + kStepThreads < s.n_seqs) __syncthreads();
+  }
+  if (s.slot)
+    for (int j = given + flat; j < s.n_tokens; j += all) s.slot[j] = -1;
+  cluster_wait_all();
+  if (rank > 0) return;
+  if (tid == 0) *s.n_free = n_free - taken;
+  const int last = (s.n_seqs - 1) / kStepThreads * kStepThreads;  // the sessions that the threads still hold
+  for (int i = tid; i < last; i += kStepThreads) {
+    const int was = max(0, min(s.len[i], rows_max)), stays = s.keep ? max(0, min(s.keep[i], was)) : was;
+    s.len[i] = stays + (s.cu[i + 1] - s.cu[i]);
+  }
+  if (last + tid < s.n_seqs) s.len[last + tid] = new_len;
+}
+
+cudaError_t launch_pages_step(const StepView& s, cudaStream_t st) {
+  TimingScope ts("pages_step", st);
+  const cudaError_t e = launch_after(k_pages_step, dim3(kStepCtas), kStepThreads, 0, st, s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace stl

@@ -1,0 +1,92 @@
+// Rows of 128 elements in 4 bits: 64 bytes of codes (e2m1, element 2 i in the
+// low half of byte i) and 8 scales (e4m3), one to 16 elements; an element is
+// code * scale * factor, the factor its KV head's.
+//
+// A code has two significant bits and a scale four, so that code * scale has at
+// most six and lies within 2^-10 .. 2688: exact in fp16 (and in bf16).  What is
+// decoded below is that product; the factor goes to the scores or the result.
+#pragma once
+
+#include "kernels.cuh"
+
+namespace stl {
+
+constexpr int kQ4Row = kD / 2;         // bytes of a row's codes
+constexpr int kQ4Group = 16;           // elements of a scale
+constexpr int kQ4Scales = kD / kQ4Group;
+constexpr uint32_t kQ4NaN = 0x7f;      // the scale of a group that holds an infinity or a NaN
+
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// The two e4m3 scales of the low 16 bits, as fp16.
+__device__ __forceinline__ uint32_t q4_scales(uint32_t two) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((unsigned short)two));
+  return d;
+}
+// The eight codes of a word as four pairs of fp16, each byte a pair.
+__device__ __forceinline__ void q4_codes(uint32_t word, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(word));
+}
+
+// How a group is put into 4 bits: its scale is the largest magnitude over six
+// times the factor, rounded to e4m3, at least the smallest (a group of zeros
+// divides by something) and at most the largest.  top: the bits of the largest
+// magnitude; integer order puts infinities and NaN above every number.
+struct Q4Scale {
+  uint32_t byte;
+  float r, r_lo;  // 1 / (scale * factor) rounded down, and what that cut off
+};
+__device__ __forceinline__ Q4Scale q4_scale(uint32_t top, float factor) {
+  const float want = fminf(fmaxf(__uint_as_float(top) / (6.f * factor), 0x1p-9f), 448.f);
+  unsigned short two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(want));
+  const uint32_t half = q4_scales(two);
+  const float t = __low2float(*reinterpret_cast<const __half2*>(&half)) * factor;
+  Q4Scale s;
+  s.byte = top >= 0x7f800000u ? kQ4NaN : two & 0xffu;
+  s.r = __frcp_rd(t);  // downwards: both parts have t's sign, and a zero keeps its own below
+  s.r_lo = fmaf(-s.r, t, 1.f) * s.r;
+  return s;
+}
+// Eight elements' codes.  x / t is rounded to fp32 and then to a code; with the
+// reciprocal's two parts a quotient that fp32 holds (a border between two codes,
+// where bf16 elements often lie) comes out exact, for two operations instead of
+// a division.
+__device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& s) {
+  uint32_t b[4], w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = fmaf(x[2 * i], s.r, x[2 * i] * s.r_lo), hi = fmaf(x[2 * i + 1], s.r, x[2 * i + 1] * s.r_lo);
+    asm("{\n\t.reg .b8 a;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %1, %2;\n\t"
+        "cvt.u32.u8 %0, a;\n\t}"
+        : "=r"(b[i])
+        : "f"(hi), "f"(lo));
+  }
+  w = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+  return s.byte == kQ4NaN ? 0u : w;
+}
+__device__ __forceinline__ uint32_t q4_top(const float (&x)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  return top;
+}
+
+// Row r of head h in page `page` of pools [n_pages][hkv][page_rows].
+__device__ __forceinline__ size_t q4_row(const PageView& pg, int page, int r, int h, int hkv) {
+  return ((size_t)page * hkv + h) * pg.page_rows + r;
+}
+
+}  // namespace stl

@@ -43,7 +43,9 @@ EXPORTED = ("stlite_budget", "stlite_workspace_size", "stlite_score", "stlite_ga
             "stlite_decode_attention_layers", "stlite_decode_layers_workspace_size",
             "stlite_selftest_wait_timeout", "stlite_rope_init", "stlite_rotate_qk", "stlite_paged_append",
             "stlite_paged_attention", "stlite_paged_workspace_size", "stlite_compact_paged",
-            "stlite_compress_layers_paged")
+            "stlite_compress_layers_paged", "stlite_paged_append_q4", "stlite_paged_attention_q4",
+            "stlite_paged_q4_workspace_size", "stlite_compact_paged_q4", "stlite_compress_layers_paged_q4",
+            "stlite_paged_fetch_q4", "stlite_pages_step")
 
 
 class Shape(ctypes.Structure):
@@ -93,6 +95,16 @@ class Tokens(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_norm", ctypes.c_void_p),
                 ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float), ("pos", ctypes.c_void_p)]
+
+
+class Q4PoolsC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("k_factor", ctypes.c_void_p), ("v_factor", ctypes.c_void_p)]
+
+
+class Q4Layer(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("idx", ctypes.c_void_p),
+                ("pools", Q4PoolsC)]
 
 
 class KernelTime(ctypes.Structure):
@@ -157,6 +169,15 @@ _sig = {
     "stlite_compress_layers_paged": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Frames), ctypes.POINTER(Params),
                                           _P, ctypes.c_int32, ctypes.c_int32, _P,
                                           ctypes.POINTER(ctypes.c_int32), _P, ctypes.c_size_t, _P]),
+    "stlite_paged_append_q4": (_S, [_P, ctypes.POINTER(Rope), _P, _P, _P, _P, _P]),
+    "stlite_paged_attention_q4": (_S, [_P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "stlite_paged_q4_workspace_size": (_S, [_P, _P, ctypes.POINTER(ctypes.c_size_t)]),
+    "stlite_compact_paged_q4": (_S, [_P, ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, _P, _P]),
+    "stlite_compress_layers_paged_q4": (_S, [ctypes.POINTER(Shape), ctypes.POINTER(Frames), ctypes.POINTER(Params),
+                                             _P, ctypes.c_int32, ctypes.c_int32, _P,
+                                             ctypes.POINTER(ctypes.c_int32), _P, ctypes.c_size_t, _P]),
+    "stlite_paged_fetch_q4": (_S, [_P, _P, ctypes.c_int32, _P, _P]),
+    "stlite_pages_step": (_S, [_P, _P, _P, _P, _P, ctypes.c_int32, _P, _P]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -754,6 +775,232 @@ def stlite_compress_layers_paged(layers, frames, params, pages, seq, ws, stream=
                                              pages._address, int(seq), len(layers), _address(arr), ctypes.byref(b),
                                              _ptr(ws), ws.numel(), _stream(stream)), "stlite_compress_layers_paged")
     return int(b.value)
+
+
+# ---------------------------------------------------------- pages in 4 bits
+
+class Q4Pools:
+    """stlite_q4_pools of one layer's device tensors (kept alive with it): codes
+    k, v uint8 [n_pages][Hkv][page_rows][64], scales k_scale, v_scale
+    (torch.float8_e4m3fn or uint8) [n_pages][Hkv][page_rows][8], factors float32
+    [Hkv] or None."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_factor=None, v_factor=None):
+        if k.dim() != 4 or k.shape[3] != 64:
+            raise ValueError("codes are [n_pages][Hkv][page_rows][64]")
+        p, hkv, r, _ = k.shape
+        for t, shape, types in ((k, k.shape, (torch.uint8,)), (v, k.shape, (torch.uint8,)),
+                                (k_scale, (p, hkv, r, 8), (torch.float8_e4m3fn, torch.uint8)),
+                                (v_scale, (p, hkv, r, 8), (torch.float8_e4m3fn, torch.uint8)),
+                                (k_factor, (hkv,), (torch.float32,)), (v_factor, (hkv,), (torch.float32,))):
+            if t is not None and (t.shape != shape or t.dtype not in types or not t.is_contiguous()
+                                  or t.device != k.device):
+                raise ValueError("codes are uint8 [n_pages][Hkv][page_rows][64], scales e4m3 [n_pages][Hkv][page_rows]"
+                                 "[8] and factors float32 [Hkv], contiguous, of one device")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_factor, self.v_factor = k, v, k_scale, v_scale, k_factor, v_factor
+        self.c = Q4PoolsC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_factor), _ptr(v_factor))
+        self.hkv, self._pool, self._device = hkv, (p, r), k.get_device()
+        self._address, self._words = ctypes.addressof(self.c), tuple(getattr(self.c, n) or 0 for n, _ in self.c._fields_)
+
+
+def make_q4_pools(n_pages, page_rows, hkv, k_factor=None, v_factor=None, device="cuda") -> Q4Pools:
+    """Allocates zero-filled pools of one layer."""
+    shape = (int(n_pages), int(hkv), int(page_rows))
+    k, v = (torch.zeros(shape + (64,), dtype=torch.uint8, device=device) for _ in range(2))
+    ks, vs = (torch.zeros(shape + (8,), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    return Q4Pools(k, v, ks, vs, k_factor, v_factor)
+
+
+def _q4_error():
+    return ValueError("every layer's pools are Q4Pools of the pages' numbers and of k's heads")
+
+
+def stlite_paged_append_q4(q, k, v, pos, rope, pages, q_out, pools, q_norm=None, k_norm=None, eps=1e-6, stream=None):
+    """stlite_paged_append into a layer's 4-bit pages (Q4Pools)."""
+    qs, ks, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    x = _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype)
+    if q_out.shape != qs or q_out.dtype != dtype or not q_out.is_contiguous():
+        raise _output_error(qs)
+    hkv = ks[1]
+    if pools._pool != pages._pool or pools.hkv != hkv:
+        raise _q4_error()
+    if dev < 0 or not (torch._C._cuda_getDevice() == dev == k.get_device() == v.get_device() == pos.get_device()
+                       == q_out.get_device() == pools._device == pages._device):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_paged_append_q4(
+        _SHAPE.pack(qs[0], qs[1], hkv, 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[dtype]), rope, x,
+        pages._address, q_out.data_ptr(), pools._address, _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_paged_append_q4")
+
+
+def stlite_paged_q4_workspace_size(shape: Shape, pages: PageTable) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.stlite_paged_q4_workspace_size(ctypes.byref(shape), ctypes.byref(pages.c), ctypes.byref(out)),
+           "stlite_paged_q4_workspace_size")
+    return int(out.value)
+
+
+def paged_q4_workspace(q, pools, pages):
+    """Zero-filled workspace tensor of stlite_paged_attention_q4."""
+    if q.dim() != 3 or q.shape[2] != 128 or not q.is_contiguous():
+        raise ValueError("q is a contiguous [T][Hq][128]")
+    shape = Shape(q.shape[0], q.shape[1], pools.hkv, 128, pages.max_new, _DTYPE[q.dtype])
+    return torch.zeros(stlite_paged_q4_workspace_size(shape, pages), dtype=torch.uint8, device=q.device)
+
+
+def stlite_paged_attention_q4(q, pools, pages, out, ws, stream=None):
+    """stlite_paged_attention over a layer's 4-bit pages (Q4Pools)."""
+    (n, hq, d), dtype, dev = q.shape, q.dtype, q.get_device()
+    if d != 128 or not q.is_contiguous():
+        raise ValueError("q is a contiguous [T][Hq][128]")
+    if out.shape != q.shape or out.dtype != dtype or not out.is_contiguous():
+        raise _output_error(q.shape)
+    if pools._pool != pages._pool:
+        raise _q4_error()
+    if dev < 0 or not (torch._C._cuda_getDevice() == dev == out.get_device() == ws.get_device() == pools._device
+                       == pages._device):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_paged_attention_q4(
+        _SHAPE.pack(n, hq, pools.hkv, 128, pages.max_new, _DTYPE[dtype]), pages._address, q.data_ptr(), pools._address,
+        out.data_ptr(), ws.data_ptr(), ws.nbytes, _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_paged_attention_q4")
+
+
+def paged_attention_q4(q, pools, pages, stream=None):
+    """Allocates the output and the workspace and runs stlite_paged_attention_q4."""
+    out, ws = torch.empty_like(q), paged_q4_workspace(q, pools, pages)
+    _lend(stream, q, pools.k, pools.v, pools.k_scale, pools.v_scale, pools.k_factor, pools.v_factor, pages.table,
+          pages.length, pages.cu_new, out, ws)
+    stlite_paged_attention_q4(q, pools, pages, out, ws, stream)
+    return out
+
+
+def stlite_compact_paged_q4(layers, budget, pages, seq, stream=None):
+    """The kept rows of every layer into sequence seq's 4-bit pages; layers:
+    list of (k, v, pools, idx)."""
+    k0 = layers[0][0]
+    shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
+    n, hkv, d = shape
+    want, index = pages._pool, (hkv, budget)
+    for k, v, pools, ix in layers:
+        if pools._pool != want or pools.hkv != hkv:
+            raise _q4_error()
+        if not (k.shape == shape == v.shape and ix.shape == index and k.dtype == dtype == v.dtype
+                and ix.dtype == torch.int32 and k.is_contiguous() and v.is_contiguous() and ix.is_contiguous()):
+            raise ValueError("every layer's k and v are [N][Hkv][128] of one type and idx int32 [Hkv][budget], "
+                             "contiguous")
+        if not k.get_device() == pools._device == ix.get_device() == dev or (v.get_device() != dev
+                                                                             and not v.is_pinned()):
+            raise ValueError(_ELSEWHERE)
+        flat += (0, k.data_ptr(), v.data_ptr(), ix.data_ptr(), *pools._words)
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
+        raise ValueError(_ELSEWHERE)
+    arr = array("Q", flat)
+    st = _lib.stlite_compact_paged_q4(_SHAPE.pack(n, hkv, hkv, d, 1, _DTYPE[dtype]), budget, pages._address, seq,
+                                      len(layers), _address(arr),
+                                      _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_compact_paged_q4")
+
+
+def stlite_compress_layers_paged_q4(layers, frames, params, pages, seq, ws, stream=None) -> int:
+    """stlite_compress_layers with the kept rows in sequence seq's 4-bit
+    pages; layers: list of (q, k, v, pools, idx_out)."""
+    q0, k0 = layers[0][:2]
+    sh = make_shape(q0, k0)
+    qs, shape, dtype, dev, flat = q0.shape, k0.shape, k0.dtype, k0.get_device(), []
+    kept = sh.n_kv_heads * stlite_budget(sh.n_tokens, params.beta, params.k_override)
+    for q, k, v, pools, ix in layers:
+        if pools._pool != pages._pool or pools.hkv != sh.n_kv_heads:
+            raise _q4_error()
+        if not (q.shape == qs and k.shape == shape == v.shape and q.dtype == dtype == k.dtype and v.dtype == dtype
+                and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("every layer's q is [w][Hq][128] and its k and v [N][Hkv][128], of one type, contiguous")
+        if ix.dtype != torch.int32 or ix.numel() < kept or not ix.is_contiguous():
+            raise ValueError("every layer's idx_out is contiguous int32 with room for [Hkv][B]")
+        if not q.get_device() == k.get_device() == pools._device == ix.get_device() == dev or (
+                v.get_device() != dev and not v.is_pinned()):
+            raise ValueError(_ELSEWHERE)
+        flat += (q.data_ptr(), k.data_ptr(), v.data_ptr(), ix.data_ptr(), *pools._words)
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device == ws.get_device():
+        raise ValueError(_ELSEWHERE)
+    fs = _frames(frames)
+    arr = array("Q", flat)
+    b = ctypes.c_int32(0)
+    _check(_lib.stlite_compress_layers_paged_q4(ctypes.byref(sh), ctypes.byref(fs.c), ctypes.byref(params),
+                                                pages._address, int(seq), len(layers), _address(arr), ctypes.byref(b),
+                                                _ptr(ws), ws.numel(), _stream(stream)),
+           "stlite_compress_layers_paged_q4")
+    return int(b.value)
+
+
+def stlite_paged_fetch_q4(layers, pages, stream=None):
+    """Rows out of every layer's 4-bit pages, as values: the last cu_new[s + 1]
+    - cu_new[s] (or max_new) rows of each sequence; layers: list of (pools, k_out,
+    v_out), outputs [T][Hkv][128]."""
+    k0 = layers[0][1]
+    shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
+    n, hkv, d = shape
+    want = pages._pool
+    for pools, k, v in layers:
+        if pools._pool != want or pools.hkv != hkv:
+            raise _q4_error()
+        if not (d == 128 and k.shape == shape == v.shape and k.dtype == dtype == v.dtype and k.is_contiguous()
+                and v.is_contiguous()):
+            raise ValueError("every layer's outputs are contiguous [T][Hkv][128] of one type")
+        if not k.get_device() == v.get_device() == pools._device == dev:
+            raise ValueError(_ELSEWHERE)
+        flat += (0, k.data_ptr(), v.data_ptr(), 0, *pools._words)
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
+        raise ValueError(_ELSEWHERE)
+    arr = array("Q", flat)
+    st = _lib.stlite_paged_fetch_q4(
+        _SHAPE.pack(n, hkv, hkv, 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[dtype]), pages._address,
+        len(layers), _address(arr), _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_paged_fetch_q4")
+
+
+def paged_fetch_q4(pools, pages, n, dtype=torch.bfloat16, stream=None):
+    """Allocates the outputs and runs stlite_paged_fetch_q4 on one layer for
+    the n packed tokens of pages; rows that it leaves out are zeros."""
+    k, v = (torch.zeros((n, pools.hkv, 128), dtype=dtype, device=pools.k.device) for _ in range(2))
+    _lend(stream, pools.k, pools.v, pools.k_scale, pools.v_scale, pools.k_factor, pools.v_factor, pages.table,
+          pages.length, pages.cu_new, k, v)
+    stlite_paged_fetch_q4([(pools, k, v)], pages, stream)
+    return k, v
+
+
+# ------------------------------------------------------- a step's page tables
+
+def stlite_pages_step(pages, keep, fresh, free_pages, n_free, slot, stream=None):
+    """Gives pages to the sessions that grow and takes them from those that
+    shrink or end: updates pages.table, length and cu_new, free_pages [n_pages]
+    and n_free [1].  keep [S] (or None: all): rows that stay; fresh [S]: new
+    tokens asked for; slot: int32 [n_tokens], the place of every new token, or
+    the number of places.  All int32."""
+    dev, S, i32 = pages._device, pages.c.n_seqs, torch.int32
+    if pages.length is None or pages.cu_new is None:
+        raise ValueError("a step's pages have length and cu_new")
+    places = slot if isinstance(slot, int) else slot.shape[0] if slot.dim() == 1 else -1
+    if (fresh.dtype != i32 or fresh.shape != (S,) or not fresh.is_contiguous() or free_pages.dtype != i32
+            or free_pages.shape != pages._pool[:1] or not free_pages.is_contiguous() or n_free.dtype != i32
+            or n_free.numel() != 1 or (keep is not None and (keep.dtype != i32 or keep.shape != (S,)
+                                                             or not keep.is_contiguous()))
+            or places < 0 or (slot is not places and (slot.dtype != i32 or not slot.is_contiguous()))):
+        raise ValueError("keep and fresh are [S], free_pages [n_pages], n_free [1] and slot [n_tokens], contiguous int32")
+    if dev < 0 or not torch._C._cuda_getDevice() == dev == fresh.get_device() == free_pages.get_device() == (
+            n_free.get_device()) or (keep is not None and keep.get_device() != dev) or (
+            slot is not places and slot.get_device() != dev):
+        raise ValueError(_ELSEWHERE)
+    st = _lib.stlite_pages_step(pages._address, None if keep is None else keep.data_ptr(), fresh.data_ptr(),
+                                free_pages.data_ptr(), n_free.data_ptr(), places,
+                                None if slot is places or places == 0 else slot.data_ptr(),
+                                _CURRENT(dev) if stream is None else stream.cuda_stream)
+    if st != STLITE_OK:
+        raise StliteError(st, "stlite_pages_step")
 
 
 def stlite_selftest_wait_timeout(ws, limit_ns: int, stream=None):
