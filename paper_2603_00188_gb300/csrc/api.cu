@@ -1073,7 +1073,7 @@ PageView page_view(const stlite_pages* pg, int w) {
   v.max_pages = pg->max_pages;
   v.w = w;
   v.page_shift = -1;
-  v.item_units = 0;
+  v.item_units = v.block_shift = 0;
   for (int i = 0; i < 31; ++i)
     if (pg->page_rows == 1 << i) v.page_shift = i;
   return v;

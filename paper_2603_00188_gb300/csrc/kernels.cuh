@@ -279,7 +279,7 @@ struct PageView {
   const int32_t* cu;   // [n_seqs + 1], or null: w new tokens per sequence
   int n_seqs, n_pages, page_rows, max_pages, w;
   int page_shift;      // log2(page_rows), or -1 where that is no whole number
-  int item_units;      // of the attention's split of work (launch_paged_attention sets it)
+  int item_units, block_shift;  // of the attention's split of work (its launchers set them)
 };
 // Rotation by position: pair i turns by turn[i] * 2^-64 of a turn per
 // position (what exceeds a turn falls off the top of 64 bits) on axis 0, 1 or

@@ -11,6 +11,7 @@ namespace stl {
 
 constexpr int kPmWarps = 4, kPmThreads = 32 * kPmWarps;
 constexpr int kPmCtas = 2;  // per SM
+constexpr int kPatBlock = 16, kPatBlockShift = 4;  // cached rows of a block
 
 // ---------------------------------------------------------------------- bf16
 // Each warp streams its own blocks (every kPmWarps-th of the range) through its
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  RowFinder<kPmWarps, false> finder(rg);
+  RowFinder<kPmWarps, kPatBlock> finder(rg);
   uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
   const int fc = lane & 15, fr = lane >> 4;
   const __nv_bfloat16 *kf = k + 8 * fc, *vf = v + 8 * fc;
@@ -551,7 +552,7 @@ __global__ void __launch_bounds__(kPmThreads, kPmCtas)
   if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  RowFinder<kPmWarps, false> finder(rg);
+  RowFinder<kPmWarps, kPatBlock> finder(rg);
   auto fetch = [&](int slot, int row, const float* from) {
     if (row != -2) {
       const uint32_t dst = smem_u32(ring) + slot * kPfHalf;
@@ -952,6 +953,7 @@ cudaError_t launch_paged_attention(DType dt, const PageView& view, const void* q
   // others: five drafted tokens of eight sessions 1.8 us slower.)
   const bool light = dt == kBF16 && part_rows <= 16;
   pages.item_units = light ? 6 : 12;
+  pages.block_shift = kPatBlockShift;
   int split = light ? 24 : 14;
   // Sessions that cannot be longer than a split and a little are never split,
   // which saves the second launch (one session of 256 rows: 7.0 us, split 6.9,

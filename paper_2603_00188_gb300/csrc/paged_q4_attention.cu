@@ -4,7 +4,7 @@
 // over the rows that paged_attention.cu says, divided among CTAs as there
 // (paged_split.cuh).
 //
-// Each warp streams its own blocks of 16 rows through its own ring in shared
+// Each warp streams its own blocks of 32 rows through its own ring in shared
 // memory and decodes them in registers, as operands of its tensor cores'
 // m16n8k16 products of fp16 with fp32 sums:
 //   S (16 rows x 8 queries) = K Q^T: a lane takes 32 neighbouring elements of a
@@ -29,17 +29,18 @@
 
 namespace stl {
 
-constexpr int kQaCtas = 2;    // per SM
-constexpr int kQaStages = 4;  // of a warp's ring
-constexpr int kQaCodes = kPatBlock * kQ4Row, kQaScales = kPatBlock * kQ4Scales;  // of keys, or of values, of a block
+constexpr int kQaBlock = 32, kQaBlockShift = 5;  // cached rows of a block
+constexpr int kQaStages = 2;  // of a warp's ring
+constexpr int kQaCodes = kQaBlock * kQ4Row, kQaScales = kQaBlock * kQ4Scales;  // of keys, or of values, of a block
 constexpr int kQaStage = 2 * (kQaCodes + kQaScales);
 constexpr int kQaPitch = kD + 4;      // floats from row to row of the merge buffer
 constexpr float kQaLift = 10.f;       // weights are 2^(x - m), m their reference less this
 constexpr float kQaSlack = 4.f;       // how far a score may exceed the reference
-// Warps of a CTA: eight where 128 registers hold a warp's state.
-__host__ __device__ constexpr int qa_warps(int nt) { return nt == 1 ? 8 : 4; }
+// Warps of a CTA: eight where 128 registers hold a warp's state; and CTAs per SM.
+__host__ __device__ constexpr int qa_warps(int nt) { return 4; }
+__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt == 1 ? (parts == 1 ? 4 : 3) : (nt == 2 ? 3 : 2); }
 // Bytes of shared memory for queries; none where they are in registers.
-__host__ __device__ constexpr int qa_queries(int nt, int parts) { return 8 * nt * parts > 16 ? 8 * nt * parts * kD * 2 : 0; }
+__host__ __device__ constexpr int qa_queries(int nt, int parts) { return nt * parts > 1 ? 8 * nt * parts * kD * 2 : 0; }
 __host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
 __host__ __device__ constexpr int qa_factors(int nt) {
   return 8 * nt * 4 * (1 + qa_warps(nt)) > (int)sizeof(RangeScratch<256>) ? 8 * nt * 4 * (1 + qa_warps(nt))
@@ -50,11 +51,15 @@ __host__ __device__ constexpr int qa_smem(int nt, int parts) {
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t mul_half2(uint32_t x, __half2 y) {
+  const __half2 z = __hmul2(as_half2(x), y);
+  return *reinterpret_cast<const uint32_t*>(&z);
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -69,6 +74,34 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
 }
 __device__ __forceinline__ void cp_async8_fill(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
+}
+
+// Reads of a ring's stage: after the wait for its copies and before the next copies to it.
+template <int OFFSET>
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 x;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4 + %5];"
+               : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+               : "r"(at), "n"(OFFSET));
+  return x;
+}
+template <int OFFSET>
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 x;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2 + %3];" : "=r"(x.x), "=r"(x.y) : "r"(at), "n"(OFFSET));
+  return x;
+}
+template <int OFFSET>
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.b32 %0, [%1 + %2];" : "=r"(x) : "r"(at), "n"(OFFSET));
+  return x;
+}
+template <int OFFSET>
+__device__ __forceinline__ uint32_t lds16(uint32_t at) {
+  uint16_t x;
+  asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(x) : "r"(at), "n"(OFFSET));
+  return x;
 }
 
 // Four neighbouring elements of a query.
@@ -87,7 +120,7 @@ __device__ __forceinline__ uint32_t qa_value_off(int r, int c) {
 
 // NT: groups of eight queries that share one read of the cache.
 template <typename T, int NT>
-__global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
+__global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T, float>::value ? 2 : 1))
     k_paged_q4(const __grid_constant__ PageView pg, const __grid_constant__ Q4View pools, const T* q, T* out, int n,
                int hq, int hkv, int mode, int split, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
                float* part_o, uint32_t* err) {
@@ -106,8 +139,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
   float* factor = inv + kRows;                     // [warps][kRows]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
   const int G = hq / hkv, cta = blockIdx.x;
-  uint8_t* stages = sm + warp * kQaStages * kQaStage;
-  const uint32_t ring = smem_u32(stages);
+  const uint32_t pick = (g8 & 3) | (4 + (g8 & 3)) << 4;  // the lane's group's byte of two words
+  const uint32_t ring = smem_u32(sm) + warp * kQaStages * kQaStage;
   pdl_trigger();
   pdl_wait();
   const Range rg = find_range<kThreads>(pg, G, chunk_rows, hkv, kWarps, split, err, scratch);
@@ -115,37 +148,97 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
   if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
-  RowFinder<kWarps, true> finder(rg);
-  uint64_t counts = 0;  // 16 bits per stage: which rows of its block count
-  // a stage: keys' codes, values' codes, keys' scales, values' scales
-  auto fetch = [&](int stage, int row) {
-    if (row != -2) {
-      const uint64_t ok = __ballot_sync(0xffffffffu, row >= 0) & 0xffffu;
-      counts = (counts & ~(0xffffull << (16 * stage))) | ok << (16 * stage);
-      const uint32_t dst = ring + stage * kQaStage;
+  // The warp's blocks, one after the other.  A block's table entries are asked for
+  // while another block is worked on, and looked at when it is to be copied.
+  struct {
+    Cursor at;
+    int u, f0, i1;  // the next block, and the first block and the end of the item that it is sought in
+    const int32_t* entries;
+    int head_row;   // of the item's head: its first row in a page
+  } find;
+  auto start = [&](const Cursor& c, int from) {
+    find.at = c;
+    find.u = find.f0 = find.i1 = from;
+  };
+  struct Entry {
+    int page, row;  // the lane's row of the block: the page, and the row in it and the head; -1: no row of the session
+  };
+  auto look_up = [&](Entry& e) {  // false past the range
+    while (find.u >= find.i1) {
+      if (find.i1 >= rg.b1) return false;
+      advance(find.at, find.i1, pg, G, chunk_rows, hkv);
+      const Item x = item_at(find.at, find.i1);
+      find.u = warps_first<kWarps>(max(find.i1, x.f0), warp);
+      find.f0 = x.f0;
+      find.i1 = x.i1;
+      find.entries = pg.table + (size_t)find.at.s * pg.max_pages;
+      find.head_row = x.h * pg.page_rows;
+    }
+    if (find.u >= rg.b1) return false;
+    const int j = (find.u - find.f0) * kQaBlock + lane;
+    find.u += kWarps;
+    const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
+    e.row = find.head_row + j - i * pg.page_rows;
+    if (j < find.at.w.len)
+      e.page = find.entries[i];
+    else
+      e.row = -1;
+    return true;
+  };
+  // A stage: keys' codes, values' codes, keys' scales, values' scales.  Of a row
+  // that does not count only the scales are written, zeros: whatever codes lie in
+  // its place are numbers.
+  uint32_t ok = 0, ok_next = 0;  // rows that count of the block at hand, and of the one after it
+  // where the lane reads in a stage: keys' codes and scales, values' even and odd rows and scales
+  const uint32_t k_at = ring + 16 * lane, ks_at = ring + 2 * kQaCodes + kQ4Scales * g8 + 2 * t4;
+  const uint32_t v_at = ring + kQaCodes + qa_value_off(2 * t4, g8 >> 1) + 8 * (g8 & 1);
+  const uint32_t v_odd = ring + kQaCodes + qa_value_off(2 * t4 + 1, g8 >> 1) + 8 * (g8 & 1);
+  const uint32_t vs_at = ring + 2 * kQaCodes + kQaScales + 2 * kQ4Scales * t4 + (g8 & 4);
+  const uint8_t *k_from = pools.k + 16 * t4, *v_from = pools.v + 16 * t4;
+  const uint32_t v_to = kQaCodes + qa_value_off(g8, t4);
+  const int page_all = hkv * pg.page_rows;  // rows of all heads
+  // Known to be 64 and 8, addresses become two shifted additions each on the
+  // pipe that the conversions fill; as numbers they are one multiplication.
+  uint32_t code_bytes, scale_bytes;
+  asm volatile("mov.u32 %0, 64;\n\tmov.u32 %1, 8;" : "=r"(code_bytes), "=r"(scale_bytes));
+  auto fetch = [&](uint32_t dst, bool any, const Entry& e) {
+    ok = ok_next;
+    ok_next = 0;
+    if (any) {
+      const bool good = e.row >= 0 && (uint32_t)e.page < (uint32_t)pg.n_pages;
+      if (e.row >= 0 && !good) record_error(err, kErrInput);
+      const int row = good ? e.page * page_all + e.row : -1;
+      ok_next = __ballot_sync(0xffffffffu, good);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kQaBlock / 8; ++i) {
         const int r = __shfl_sync(0xffffffffu, row, g8 + 8 * i);
-        const size_t at = (size_t)max(r, 0) * kQ4Row + 16 * t4;
-        cp_async16_fill(dst + (g8 + 8 * i) * kQ4Row + 16 * t4, pools.k + at, r >= 0);
-        cp_async16_fill(dst + kQaCodes + qa_value_off(g8 + 8 * i, t4), pools.v + at, r >= 0);
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ge.s32 p, %4, 0;\n\t"
+            "@p cp.async.cg.shared.global [%0], [%1], 16;\n\t"
+            "@p cp.async.cg.shared.global [%2], [%3], 16;\n\t}" ::"r"(dst + 512 * i + 16 * lane),
+            "l"(k_from + (uint64_t)(uint32_t)r * code_bytes), "r"(dst + 512 * i + v_to),
+            "l"(v_from + (uint64_t)(uint32_t)r * code_bytes), "r"(r)
+            : "memory");
       }
-      // lane % 16's row is the lane's own: keys' scales by the first 16 lanes, values' by the others
-      cp_async8_fill(dst + 2 * kQaCodes + 8 * lane, (lane < 16 ? pools.k_scale : pools.v_scale) + (size_t)max(row, 0) * kQ4Scales,
-                     row >= 0);
+      const uint64_t at = (uint64_t)(uint32_t)max(row, 0) * scale_bytes;
+      cp_async8_fill(dst + 2 * kQaCodes + 8 * lane, pools.k_scale + at, row >= 0);
+      cp_async8_fill(dst + 2 * kQaCodes + kQaScales + 8 * lane, pools.v_scale + at, row >= 0);
     }
     cp_async_commit();
   };
-  {
-    int first[kQaStages];  // all table entries on their way before the first copies
+  auto fill = [&]() {
+    Entry first[kQaStages];  // all table entries on their way before the first copies
+    bool any[kQaStages];
 #pragma unroll
-    for (int st = 0; st < kQaStages; ++st) first[st] = finder.next(pg, warp, G, chunk_rows, hkv, err);
+    for (int st = 0; st < kQaStages; ++st) any[st] = look_up(first[st]);
 #pragma unroll
-    for (int st = 0; st < kQaStages; ++st) fetch(st, first[st]);
-  }
+    for (int st = 0; st < kQaStages; ++st) fetch(ring + st * kQaStage, any[st], first[st]);
+  };
+  start(rg.at, rg.b0);
+  fill();
 
   Cursor cur = rg.at;
-  int stage = 0;
+  int stage = 0;  // bytes to the stage at hand
   for (int seg = rg.b0; seg < rg.b1;) {
     // the part of one item that lies in the range: blocks part0 .. seg_end
     advance(cur, seg, pg, G, chunk_rows, hkv);
@@ -220,6 +313,12 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
     // 8 nt + 2 t4 + e; o[mt][nt][j] is dimension 16 g8 + 2 mt + (j >> 1) of
     // query 8 nt + 2 t4 + (j & 1).
     float m[NT][2], l[NT][2], o[8][NT][4];
+    const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
+    // The warp's blocks of the part.  A value's scale that is no number makes its
+    // group's results so for the tokens that see its row, and a weight of 0 would
+    // carry it to the others too: a warp whose sums are not numbers at the part's
+    // end takes its blocks again and looks for them.
+    for (bool look = false;; look = true) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       m[nt][0] = m[nt][1] = -1e30f;
@@ -227,33 +326,35 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
     }
-    const int all_see = cur.w.len - (cur.w.fresh - 1 - row0 / G);  // rows that every query sees
     for (int u = warps_first<kWarps>(part0, warp); u < seg_end; u += kWarps) {
       cp_async_wait<kQaStages - 1>();
       __syncwarp();
-      const int next = finder.next(pg, warp, G, chunk_rows, hkv, err);  // the block that will take this stage
-      const uint8_t* at = stages + stage * kQaStage;
-      const uint8_t* scales = at + 2 * kQaCodes;
-      const int base = (u - item.f0) * kPatBlock;
-      float c[NT][4];
+      Entry next;  // of the block that will take this stage
+      const bool any = look_up(next);
+      const int base = (u - item.f0) * kQaBlock;
+      float c[2][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) c[y][nt][0] = c[y][nt][1] = c[y][nt][2] = c[y][nt][3] = 0.f;
       {
-        const uint4 w0 = *reinterpret_cast<const uint4*>(at + g8 * kQ4Row + 16 * t4);
-        const uint4 w1 = *reinterpret_cast<const uint4*>(at + (g8 + 8) * kQ4Row + 16 * t4);
-        const uint32_t s0 = q4_scales(*reinterpret_cast<const uint16_t*>(scales + g8 * kQ4Scales + 2 * t4));
-        const uint32_t s1 = q4_scales(*reinterpret_cast<const uint16_t*>(scales + (g8 + 8) * kQ4Scales + 2 * t4));
-        const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+        const uint32_t kt = k_at + stage, st = ks_at + stage;
+        // rows g8, g8 + 8, g8 + 16 and g8 + 24
+        const uint4 w[4] = {lds128<0>(kt), lds128<8 * kQ4Row>(kt), lds128<16 * kQ4Row>(kt), lds128<24 * kQ4Row>(kt)};
+        const __half2 s[4] = {as_half2(q4_scales(lds16<0>(st))), as_half2(q4_scales(lds16<8 * kQ4Scales>(st))),
+                              as_half2(q4_scales(lds16<16 * kQ4Scales>(st))), as_half2(q4_scales(lds16<24 * kQ4Scales>(st)))};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t f0 = __byte_perm(s0, 0, i < 2 ? 0x1010 : 0x3232), f1 = __byte_perm(s1, 0, i < 2 ? 0x1010 : 0x3232);
-          uint32_t p0[4], p1[4];
-          q4_codes(x0[i], p0);
-          q4_codes(x1[i], p1);
+          uint32_t p[4][4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t a[4] = {mul_f16x2(p0[2 * j], f0), mul_f16x2(p1[2 * j], f1), mul_f16x2(p0[2 * j + 1], f0),
-                                   mul_f16x2(p1[2 * j + 1], f1)};
+          for (int x = 0; x < 4; ++x) {
+            q4_codes(i == 0 ? w[x].x : (i == 1 ? w[x].y : (i == 2 ? w[x].z : w[x].w)), p[x]);
+            const __half2 f = i < 2 ? __low2half2(s[x]) : __high2half2(s[x]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[x][j] = mul_half2(p[x][j], f);
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -263,41 +364,51 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
                   b = qr[part][nt][2 * i + j];
                 else
                   b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
-                mma_f16(c[nt], a, b.x, b.y);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {  // two sums that do not wait for one another
+                  const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
+                  mma_f16(c[y][nt], a, b.x, b.y);
+                }
               }
-          }
         }
       }
-      const uint32_t ok = (uint32_t)(counts >> (16 * stage)) & 0xffffu;
-      if (ok != 0xffffu || base + kPatBlock > all_see) {  // some rows do not count for some queries
+      if (ok != 0xffffffffu || base + kQaBlock > all_see) {  // some rows do not count for some queries
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
-            const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
-            // times a factor above zero
-            if (!(ok >> r & 1u) || base + r >= sees) c[nt][j] = -CUDART_INF_F;
-          }
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int r = 16 * y + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
+              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+              // times a factor above zero
+              if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
+            }
       }
       // Scores over their references, in powers of two.  A product and a difference,
       // each rounded: fused, a huge score would exceed itself.
-      float d[NT][4];
-      bool moved = false;
+      float d[2][NT][4];
+      float most = -CUDART_INF_F;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          c[nt][j] = __fmul_rn(c[nt][j], sc[nt][j & 1]);
-          d[nt][j] = __fsub_rn(c[nt][j], m[nt][j & 1]);
-          moved |= d[nt][j] > kQaLift + kQaSlack;
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            c[y][nt][j] = __fmul_rn(c[y][nt][j], sc[nt][j & 1]);
+            d[y][nt][j] = __fsub_rn(c[y][nt][j], m[nt][j & 1]);
+          }
+          most = max3(max3(most, d[y][nt][0], d[y][nt][1]), d[y][nt][2], d[y][nt][3]);
         }
-      if (__any_sync(0xffffffffu, moved)) {  // rare once the references have settled
+      if (__any_sync(0xffffffffu, most > kQaLift + kQaSlack)) {  // rare once the references have settled
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(c[nt][e], c[nt][2 + e]) - kQaLift;
+            float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
+#pragma unroll
+            for (int y = 1; y < 2; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
+            mx -= kQaLift;
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -305,8 +416,11 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
             const float alpha = ex2_approx(m[nt][e] - mx);
             m[nt][e] = mx;
             l[nt][e] *= alpha;
-            d[nt][e] = c[nt][e] - mx;
-            d[nt][2 + e] = c[nt][2 + e] - mx;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              d[y][nt][e] = __fsub_rn(c[y][nt][e], mx);
+              d[y][nt][2 + e] = __fsub_rn(c[y][nt][2 + e], mx);
+            }
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) {
               o[mt][nt][e] *= alpha;
@@ -314,34 +428,34 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
             }
           }
       }
-      uint32_t p[kParts][NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int y = 0; y < 2; ++y) {
+        uint32_t p[kParts][NT][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {  // scores become weights
-          c[nt][j] = ex2_approx(d[nt][j]);
-          l[nt][j & 1] += c[nt][j];
-        }
+        for (int nt = 0; nt < NT; ++nt) {
+          float z[4];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint32_t hi = pack_f16(c[nt][2 * x], c[nt][2 * x + 1]);
-          p[0][nt][x] = turn8x8(hi);
-          if (kParts == 2) {
-            const float2 z = unpack_f16(hi);
-            p[kParts - 1][nt][x] = turn8x8(pack_f16(c[nt][2 * x] - z.x, c[nt][2 * x + 1] - z.y));
+          for (int j = 0; j < 4; ++j) {  // scores become weights
+            z[j] = ex2_approx(d[y][nt][j]);
+            l[nt][j & 1] += z[j];
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
+            p[0][nt][x] = turn8x8(hi);
+            if (kParts == 2) {
+              const float2 t = unpack_f16(hi);
+              p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
+            }
           }
         }
-      }
-      {
-        const uint8_t* vs = scales + kQaScales + g8;
-        uint32_t b[2];  // scales of rows 2 t4, 2 t4 + 1, and of those + 8
-#pragma unroll
-        for (int i = 0; i < 2; ++i) b[i] = vs[(2 * t4 + 8 * i) * kQ4Scales] | vs[(2 * t4 + 8 * i + 1) * kQ4Scales] << 8;
-        // A scale that is no number makes its group's results so for the tokens
-        // that see its row; a weight of 0 would carry it to the others too.
-        const bool odd = (((b[0] & 0x7f7fu) + 0x0101u) | ((b[1] & 0x7f7fu) + 0x0101u)) & 0x8080u;
-        if (__any_sync(0xffffffffu, odd)) {
-          uint32_t which = 0;  // rows, of the lane's four
+        const uint32_t vt = v_at + stage + 16 * kQ4Row * y, vo = v_odd + stage + 16 * kQ4Row * y;
+        const uint32_t st = vs_at + stage + 16 * kQ4Scales * y;
+        // scales of rows 2 t4, 2 t4 + 1 of the tile, and of those + 8
+        uint32_t b[2] = {__byte_perm(lds32<0>(st), lds32<kQ4Scales>(st), pick),
+                         __byte_perm(lds32<8 * kQ4Scales>(st), lds32<9 * kQ4Scales>(st), pick)};
+        if (look) {
+          uint32_t which = 0;  // rows of the tile, of the lane's four
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
@@ -350,23 +464,19 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
             }
           which |= __shfl_xor_sync(0xffffffffu, which, 1);
           which |= __shfl_xor_sync(0xffffffffu, which, 2);
-          which &= ok;
+          which &= ok >> (16 * y);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base;  // of the block's rows
+              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * y;  // of the tile's rows
               if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
 #pragma unroll
                 for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
             }
         }
-        const uint32_t f0 = q4_scales(b[0]), f1 = q4_scales(b[1]);
-        const uint8_t* vt = at + kQaCodes + 8 * (g8 & 1);
-        uint2 w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[i] = *reinterpret_cast<const uint2*>(vt + qa_value_off(2 * t4 + 8 * (i >> 1) + (i & 1), g8 >> 1));
+        const __half2 f0 = as_half2(q4_scales(b[0])), f1 = as_half2(q4_scales(b[1]));
+        const uint2 w[4] = {lds64<0>(vt), lds64<0>(vo), lds64<8 * kQ4Row>(vt), lds64<8 * kQ4Row>(vo)};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           // bytes of two rows' codes of one dimension: even dimensions, odd ones
@@ -379,8 +489,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
           q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t a[4] = {mul_f16x2(even0[j], f0), mul_f16x2(odd0[j], f0), mul_f16x2(even1[j], f1),
-                                   mul_f16x2(odd1[j], f1)};
+            const uint32_t a[4] = {mul_half2(even0[j], f0), mul_half2(odd0[j], f0), mul_half2(even1[j], f1),
+                                   mul_half2(odd1[j], f1)};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -389,8 +499,22 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
         }
       }
       __syncwarp();
-      fetch(stage, next);
-      stage = stage + 1 == kQaStages ? 0 : stage + 1;
+      fetch(ring + stage, any, next);
+      stage = kQaStage - stage;
+    }
+    float none = 0.f;  // or a NaN, where a sum is one
+#pragma unroll
+    for (int mt = 0; mt < 8; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) none = fmaf(o[mt][nt][j], 0.f, none);
+    if (look || !__any_sync(0xffffffffu, none != 0.f)) break;
+    cp_async_wait<0>();  // no copy is on its way to the stages
+    __syncwarp();
+    start(cur, part0);
+    stage = 0;
+    fill();
     }
     // The warps' states of this item, merged in shared memory, eight queries at
     // a time.
@@ -467,10 +591,11 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), kQaCtas)
 }
 
 // -------------------------------------------------------------------- launch
-static int q4_ctas() {
+static int q4_ctas(DType dt, int part_rows) {
   int dev = 0, sms = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return kQaCtas * sms < kPatMaxCtas ? kQaCtas * sms : kPatMaxCtas;
+  const int ctas = qa_ctas(part_rows / 8, dt == kF32 ? 2 : 1) * sms;
+  return ctas < kPatMaxCtas ? ctas : kPatMaxCtas;
 }
 
 // Query rows of a CTA's part, which share one read of the cache: at most 32, or
@@ -484,8 +609,8 @@ static int q4_part_rows(DType dt, const PageView& pages, int G) {
 // Workspace: as paged_workspace_bytes says.
 constexpr size_t kQaHead = 256, kQaDescs = kPatMaxCtas * sizeof(PartDesc);
 size_t paged_q4_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
-  return kQaHead + kQaDescs +
-         (size_t)2 * q4_ctas() * q4_part_rows(dt, pages, hq / hkv) * (sizeof(float2) + kD * sizeof(float));
+  const int rows = q4_part_rows(dt, pages, hq / hkv);
+  return kQaHead + kQaDescs + (size_t)2 * q4_ctas(dt, rows) * rows * (sizeof(float2) + kD * sizeof(float));
 }
 
 cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void* q, const Q4View& pools, void* out,
@@ -493,12 +618,13 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   PageView pages = view;
   uint32_t* err = static_cast<uint32_t*>(ws);
   const int rows = pages.w * (hq / hkv), part_rows = q4_part_rows(dt, pages, hq / hkv), most = q4_most_rows(dt);
-  const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas();
+  const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas(dt, part_rows);
   const long long items = (long long)pages.n_seqs * hkv * chunks;
-  pages.item_units = 12;
-  int split = 48;
-  const long long longest = ((long long)pages.max_pages * pages.page_rows + kPatBlock - 1) / kPatBlock;
-  const int mode = longest <= 32 ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
+  pages.item_units = 10;
+  pages.block_shift = kQaBlockShift;
+  int split = 20;
+  const long long longest = ((long long)pages.max_pages * pages.page_rows + kQaBlock - 1) / kQaBlock;
+  const int mode = longest <= 8 ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
   if (mode == kWholeItems) split = 1 << 30;
   const int descs = items <= ctas ? (int)items : ctas;
   uint8_t* at = static_cast<uint8_t*>(ws) + kQaHead;
@@ -509,7 +635,7 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   auto run = [&](auto zero, auto width) {
     typedef decltype(zero) T;
     constexpr int NT = decltype(width)::value, kParts = std::is_same<T, float>::value ? 2 : 1;
-    static_assert(fits_sm(qa_smem(NT, kParts), kQaCtas), "kQaCtas per SM");
+    static_assert(fits_sm(qa_smem(NT, kParts), qa_ctas(NT, kParts)), "qa_ctas per SM");
     TimingScope ts("paged_attention_q4", st);
     auto kern = k_paged_q4<T, NT>;
     const int smem = qa_smem(NT, kParts);

@@ -1,8 +1,8 @@
 // How attention over paged caches is divided among CTAs.
 //
 // Work is divided by what the sessions hold when the kernel runs.  An item is
-// (session, KV head, chunk of query rows); its cache is cut into blocks of 16
-// rows.  An item counts for its blocks and for some units before them that stand
+// (session, KV head, chunk of query rows); its cache is cut into blocks of
+// 16 (or 32) rows.  An item counts for its blocks and for some units before them that stand
 // for its own costs (queries, merge: launch_paged_attention gives their number);
 // the units of all items, laid end to end, are cut into equal ranges, one per CTA.  A CTA
 // computes the parts of the few items that its range meets: an item whose
@@ -32,7 +32,6 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float
 }
 
 // ---------------------------------------------------------------- the split
-constexpr int kPatBlock = 16;  // cached rows of a block
 
 // Whether any item can be split, and whether what is left for the second
 // kernel is described by CTA or by item.
@@ -51,7 +50,7 @@ __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int first, int f
   w.first = first;
   w.fresh = fresh;
   w.len = max(0, min(len, pg.max_pages * pg.page_rows));
-  w.blocks = (w.len + kPatBlock - 1) / kPatBlock;
+  w.blocks = (w.len + (1 << pg.block_shift) - 1) >> pg.block_shift;
   w.units = pg.item_units + w.blocks;
   const int rows = max(0, min(fresh, pg.w)) * G;
   w.chunks = rows <= chunk_rows ? (rows > 0 ? 1 : 0) : (rows + chunk_rows - 1) / chunk_rows;
@@ -232,8 +231,7 @@ __device__ __forceinline__ void cp_async_wait() {
 __host__ __device__ constexpr bool fits_sm(int smem, int ctas) { return ctas * ((smem + 127) / 128 * 128 + 1024) <= 228 * 1024; }
 template <int WARPS>
 __device__ __forceinline__ int warps_first(int u, int warp) { return u + ((warp - u) & (WARPS - 1)); }
-// HEADS_FIRST: the pools are [n_pages][Hkv][page_rows] rows of a head, else [n_pages][page_rows][Hkv].
-template <int WARPS, bool HEADS_FIRST>
+template <int WARPS, int BLOCK>
 struct RowFinder {
   Cursor at;
   int end;         // of the CTA's range
@@ -248,11 +246,10 @@ struct RowFinder {
     u = f0 = i1 = from;
   }
 
-  // Lane % 16's row of the warp's next block, as a row of the pools seen as
-  // [rows][128]; -1 where it does not count, -2 past the range.
-  __device__ __forceinline__ int next(const PageView& pg, int warp, int G, int chunk_rows, int hkv, uint32_t* err) {
+  // Moves on to the item of the warp's next block; false past the range.
+  __device__ __forceinline__ bool seek(const PageView& pg, int warp, int G, int chunk_rows, int hkv) {
     while (u >= i1) {
-      if (i1 >= end) return -2;
+      if (i1 >= end) return false;
       advance(at, i1, pg, G, chunk_rows, hkv);
       const Item x = item_at(at, i1);
       u = warps_first<WARPS>(max(i1, x.f0), warp);
@@ -260,8 +257,14 @@ struct RowFinder {
       i1 = x.i1;
       head = x.h;
     }
-    if (u >= end) return -2;
-    const int j = (u - f0) * kPatBlock + (threadIdx.x & (kPatBlock - 1));
+    return u < end;
+  }
+
+  // Lane % BLOCK's row of the warp's next block, as a row of 128 elements of the
+  // pools seen as [rows][128]; -1 where it does not count, -2 past the range.
+  __device__ __forceinline__ int next(const PageView& pg, int warp, int G, int chunk_rows, int hkv, uint32_t* err) {
+    if (!seek(pg, warp, G, chunk_rows, hkv)) return -2;
+    const int j = (u - f0) * BLOCK + (threadIdx.x & (BLOCK - 1));
     u += WARPS;
     if (j >= at.w.len) return -1;
     const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
@@ -270,8 +273,7 @@ struct RowFinder {
       record_error(err, kErrInput);
       return -1;
     }
-    const int row = j - i * pg.page_rows;
-    return HEADS_FIRST ? (page * hkv + head) * pg.page_rows + row : (page * pg.page_rows + row) * hkv + head;
+    return (page * pg.page_rows + (j - i * pg.page_rows)) * hkv + head;
   }
 };
 
