@@ -147,7 +147,8 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
         top_a = max(top_a, __shfl_xor_sync(0xffffffffu, top_a, 1));
         top_b = max(top_b, __shfl_xor_sync(0xffffffffu, top_b, 1));
       }
-      const Q4Scale sa = q4_scale(top_a, f), sb = IL ? sa : q4_scale(top_b, f);
+      const Q4Recip by_six(6.f * f);
+      const Q4Scale sa(top_a, by_six, f), sb(top_b, by_six, f);
       if (live && !is_q && at.page >= 0) {
         const size_t row = q4_row(pg, at.page, at.row, h, x.hkv);
         uint8_t *codes = (is_v ? q4.v : q4.k) + row * kQ4Row, *scales = (is_v ? q4.v_scale : q4.k_scale) + row * kQ4Scales;

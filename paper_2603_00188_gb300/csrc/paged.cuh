@@ -91,6 +91,23 @@ __device__ __forceinline__ Place token_place(const PageView& pg, int t) {
   const int row = __shfl_sync(0xffffffffu, len, k) - (__shfl_sync(0xffffffffu, next, k) - t);
   return page_place(pg, lo + k, row);
 }
+// The same by a thread for itself: the sequence is found by halves.
+__device__ __forceinline__ Place thread_token_place(const PageView& pg, int t) {
+  if (!pg.cu) {
+    const int s = t / pg.w;
+    if (s >= pg.n_seqs) return {-1, 0};
+    return page_place(pg, s, pg.len[s] - ((s + 1) * pg.w - t));
+  }
+  int lo = 0, hi = pg.n_seqs;  // cu[lo] <= t < cu[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pg.cu[mid] <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return page_place(pg, lo, pg.len[lo] - (pg.cu[lo + 1] - t));
+}
 __device__ __forceinline__ int token_slot(const PageView& pg, int t) {
   const Place at = token_place(pg, t);
   return at.page >= 0 ? at.page * pg.page_rows + at.row : -1;

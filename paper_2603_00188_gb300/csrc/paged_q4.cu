@@ -6,96 +6,148 @@
 
 namespace stl {
 
+// A group of sixteen elements as they are in memory.
+template <typename T>
+struct Group16 {
+  Vec8<T> x[2];
+  __device__ __forceinline__ void load(const T* p) {
+    x[0].load(p);
+    x[1].load(p + 8);
+  }
+  __device__ __forceinline__ void zero() {
+    const float y[8] = {};
+    x[0].set(y);
+    x[1].set(y);
+  }
+  // The bits of its largest magnitude, as Q4Scale takes them.
+  __device__ __forceinline__ uint32_t top() const;
+};
+template <>
+__device__ __forceinline__ uint32_t Group16<float>::top() const {
+  float y[2][8];
+  x[0].get(y[0]);
+  x[1].get(y[1]);
+  return max(q4_top(y[0]), q4_top(y[1]));
+}
+// Two at a time, the sign of what comes out being of no account.
+template <>
+__device__ __forceinline__ uint32_t Group16<__nv_bfloat16>::top() const {
+  const uint4 &a = x[0].u, &b = x[1].u;
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t most = w[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(most) : "r"(w[i]));
+  return max(most << 16 & 0x7fff0000u, most & 0x7fff0000u);
+}
+
 // ---------------------------------------------------------------- compaction
-// k_gather_paged with the kept rows put into 4 bits on the way.  16 lanes hold a
-// row of a head, 8 elements each, two lanes a group; a CTA takes 16 rows of one
-// head, whose codes are one piece of their page.
+// k_gather_paged with the kept rows put into 4 bits on the way.  A lane takes a
+// group of 16 elements, eight lanes a row of a head, and a CTA 32 rows of one
+// head, whose codes are one piece of each of their pages.
 template <typename T>
 __global__ void __launch_bounds__(256) k_gather_q4(const __grid_constant__ Q4Layers io,
                                                    const __grid_constant__ PageView pg, int seq, int n, int hkv,
                                                    int budget) {
   pdl_trigger();
   pdl_wait();
-  const int l = blockIdx.z, h = blockIdx.y, c = threadIdx.x & 15, r = blockIdx.x * 16 + (threadIdx.x >> 4);
-  int src = -1;
-  Place at = {-1, 0};
-  if (r < budget) {
-    src = io.idx[l][(size_t)h * budget + r];
-    at = page_place(pg, seq, r);
-  }
-  const bool live = at.page >= 0 && src >= 0 && src < n;
+  const int l = blockIdx.z, h = blockIdx.y, c = threadIdx.x & 7, r = blockIdx.x * 32 + (threadIdx.x >> 3);
+  if (r >= budget) return;
+  const int src = io.idx[l][(size_t)h * budget + r];
+  const Place at = page_place(pg, seq, r);
+  if (at.page < 0 || src < 0 || src >= n) return;
   const Q4View& to = io.pools[l];
-  Vec8<T> x[2];
-  float f[2] = {1.f, 1.f};
-  if (live) {
-    const size_t from = ((size_t)src * hkv + h) * kD + 8 * c;
-    x[0].load(static_cast<const T*>(io.k[l]) + from);
-    x[1].load(static_cast<const T*>(io.v[l]) + from);
-    if (to.k_factor) f[0] = to.k_factor[h];
-    if (to.v_factor) f[1] = to.v_factor[h];
-  }
-  const size_t row = live ? q4_row(pg, at.page, at.row, h, hkv) : 0;
+  const size_t from = ((size_t)src * hkv + h) * kD + kQ4Group * c, row = q4_row(pg, at.page, at.row, h, hkv);
+  Group16<T> x[2];
+  x[0].load(static_cast<const T*>(io.k[l]) + from);
+  x[1].load(static_cast<const T*>(io.v[l]) + from);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    float y[8] = {};
-    if (live) x[i].get(y);
-    uint32_t top = q4_top(y);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const Q4Scale s = q4_scale(top, f[i]);
-    const uint32_t w = q4_word(y, s);
-    if (live) {
-      *reinterpret_cast<uint32_t*>((i ? to.v : to.k) + row * kQ4Row + 4 * c) = w;
-      if (!(c & 1)) (i ? to.v_scale : to.k_scale)[row * kQ4Scales + (c >> 1)] = (uint8_t)s.byte;
-    }
+    const float* factor = i ? to.v_factor : to.k_factor;
+    const float f = factor ? factor[h] : 1.f;
+    const Q4Scale s(x[i].top(), Q4Recip(6.f * f), f);
+    float y[2][8];
+    x[i].x[0].get(y[0]);
+    x[i].x[1].get(y[1]);
+    *reinterpret_cast<uint2*>((i ? to.v : to.k) + row * kQ4Row + 8 * c) = make_uint2(q4_word(y[0], s), q4_word(y[1], s));
+    (i ? to.v_scale : to.k_scale)[row * kQ4Scales + c] = (uint8_t)s.byte;
   }
 }
 
 cudaError_t launch_gather_q4(const Problem& p, const Q4Layers& io, int budget, const PageView& pages, int seq,
                              cudaStream_t st) {
   TimingScope ts("gather_q4", st);
-  const dim3 grid((budget + 15) / 16, p.hkv, p.L);
+  const dim3 grid((budget + 31) / 32, p.hkv, p.L);
   const cudaError_t e = launch_after(p.dtype == kBF16 ? k_gather_q4<__nv_bfloat16> : k_gather_q4<float>, grid, 256, 0,
                                      st, io, pages, seq, p.n, p.hkv, budget);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 // --------------------------------------------------------------------- fetch
-// Rows as values: a warp takes a token's heads, a group of 16 elements to a
-// lane, in every layer of its share.
+// Rows as values.  A CTA's first warp finds the places of 32 tokens; then, for
+// every head of its share of the layers' keys and values, a lane takes elements
+// 8 g .. and 64 + 8 g .. of a row, so that what eight lanes write at a time lies
+// together.
+constexpr int kFetchTokens = 32;
 template <typename T>
-__global__ void __launch_bounds__(128) k_fetch_q4(const __grid_constant__ Q4Layers io,
-                                                  const __grid_constant__ PageView pg, int n, int hkv, int layers) {
+__global__ void __launch_bounds__(256) k_fetch_q4(const __grid_constant__ Q4Layers io,
+                                                  const __grid_constant__ PageView pg, int n, int hkv, int units) {
+  __shared__ Place places[kFetchTokens];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, t = blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (t >= (pg.cu ? min(n, pg.cu[pg.n_seqs]) : n)) return;
-  const Place at = token_place(pg, t);
+  const int t0 = blockIdx.x * kFetchTokens;
+  if (threadIdx.x < kFetchTokens) {
+    Place at = {-1, 0};
+    if (t0 + (int)threadIdx.x < (pg.cu ? min(n, pg.cu[pg.n_seqs]) : n)) at = thread_token_place(pg, t0 + threadIdx.x);
+    places[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int g = threadIdx.x & 7, t = t0 + (threadIdx.x >> 3);
+  const Place at = places[threadIdx.x >> 3];
   if (at.page < 0) return;
-  for (int l = blockIdx.y; l < layers; l += gridDim.y) {
-    const Q4View& from = io.pools[l];
-    for (int e = lane; e < 2 * hkv * kQ4Scales; e += 32) {
-      const int g = e & (kQ4Scales - 1), kh = e / kQ4Scales, is_v = kh >= hkv, h = is_v ? kh - hkv : kh;
-      const size_t row = q4_row(pg, at.page, at.row, h, hkv);
-      const uint2 w = *reinterpret_cast<const uint2*>((is_v ? from.v : from.k) + row * kQ4Row + 8 * g);
-      const uint32_t b = (is_v ? from.v_scale : from.k_scale)[row * kQ4Scales + g], s = q4_scales(b | b << 8);
-      const float* factor = is_v ? from.v_factor : from.k_factor;
-      const float f = factor ? factor[h] : 1.f;
-      T* dst = static_cast<T*>(const_cast<void*>(is_v ? io.v[l] : io.k[l])) + ((size_t)t * hkv + h) * kD + kQ4Group * g;
+  // units: layers * 2 (keys, values) * heads
+  constexpr int kAtOnce = 4;
+  for (int u0 = blockIdx.y; u0 < units; u0 += gridDim.y * kAtOnce) {
+    uint32_t w[kAtOnce][2], b[kAtOnce][2];
+    float f[kAtOnce];
+    T* dst[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int u = u0 + i * gridDim.y;
+      if (u >= units) break;
+      const int x = u / hkv, h = u - x * hkv, l = x >> 1;
+      const bool is_v = x & 1;
+      const Q4View& from = io.pools[l];
+      const size_t row = q4_row(pg, at.page, at.row, h, hkv);
+      const uint8_t *codes = (is_v ? from.v : from.k) + row * kQ4Row + 4 * g;
+      const uint8_t* scales = (is_v ? from.v_scale : from.k_scale) + row * kQ4Scales + (g >> 1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        w[i][k] = *reinterpret_cast<const uint32_t*>(codes + 32 * k);
+        b[i][k] = scales[4 * k];
+      }
+      const float* factor = is_v ? from.v_factor : from.k_factor;
+      f[i] = factor ? factor[h] : 1.f;
+      dst[i] = static_cast<T*>(const_cast<void*>(is_v ? io.v[l] : io.k[l])) + ((size_t)t * hkv + h) * kD + 8 * g;
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (u0 + i * (int)gridDim.y >= units) break;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t s2 = q4_scales(b[i][k] | b[i][k] << 8);
         uint32_t p[4];
         float y[8];
-        q4_codes(i ? w.y : w.x, p);
+        q4_codes(w[i][k], p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t v = mul_f16x2(p[j], s);
+          const uint32_t v = mul_f16x2(p[j], s2);
           const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&v));
-          y[2 * j] = z.x * f;
-          y[2 * j + 1] = z.y * f;
+          y[2 * j] = z.x * f[i];
+          y[2 * j + 1] = z.y * f[i];
         }
         Vec8<T> o;
         o.set(y);
-        o.store(dst + 8 * i);
+        o.store(dst[i] + kD / 2 * k);
       }
     }
   }
@@ -104,11 +156,12 @@ __global__ void __launch_bounds__(128) k_fetch_q4(const __grid_constant__ Q4Laye
 cudaError_t launch_fetch_q4(DType dt, const Q4Layers& io, int layers, int n, int hkv, const PageView& pages,
                             cudaStream_t st) {
   TimingScope ts("paged_fetch_q4", st);
-  const int blocks = (n + 3) / 4;
-  int share = 152 * 16 / blocks;  // CTAs to a token's layers, where there are few tokens
-  share = share < 1 ? 1 : (share > layers ? layers : share);
+  const int blocks = (n + kFetchTokens - 1) / kFetchTokens, units = layers * 2 * hkv;
+  // CTAs to the units of a block's tokens: eight to each of the chip's 152 SMs in all, where there are few tokens
+  int share = (152 * 8 + blocks - 1) / blocks;
+  share = share > units ? units : share;
   const cudaError_t e = launch_after(dt == kBF16 ? k_fetch_q4<__nv_bfloat16> : k_fetch_q4<float>, dim3(blocks, share),
-                                     128, 0, st, io, pages, n, hkv, layers);
+                                     256, 0, st, io, pages, n, hkv, units);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -38,7 +38,7 @@ constexpr float kQaLift = 10.f;       // weights are 2^(x - m), m their referenc
 constexpr float kQaSlack = 4.f;       // how far a score may exceed the reference
 // Warps of a CTA: eight where 128 registers hold a warp's state; and CTAs per SM.
 __host__ __device__ constexpr int qa_warps(int nt) { return 4; }
-__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt == 1 ? (parts == 1 ? 4 : 3) : (nt == 2 ? 3 : 2); }
+__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt <= 2 ? 3 : 2; }
 // Bytes of shared memory for queries; none where they are in registers.
 __host__ __device__ constexpr int qa_queries(int nt, int parts) { return nt * parts > 1 ? 8 * nt * parts * kD * 2 : 0; }
 __host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
@@ -47,7 +47,10 @@ __host__ __device__ constexpr int qa_factors(int nt) {
                                                                           : (int)sizeof(RangeScratch<256>);
 }
 __host__ __device__ constexpr int qa_smem(int nt, int parts) {
-  return qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (kQaPitch * 4 + nt * 8) + qa_factors(nt);
+  const int need = qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (kQaPitch * 4 + nt * 8) + qa_factors(nt);
+  // no more CTAs to an SM than dealt to it, however soon another launch's end
+  const int alone = (228 * 1024 / (qa_ctas(nt, parts) + 1) - 1024) / 128 * 128 + 128;
+  return need > alone ? need : alone;
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {

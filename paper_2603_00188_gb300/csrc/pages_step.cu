@@ -11,6 +11,10 @@ namespace stl {
 // go back are on the free list before any is taken, and lengths are written
 // when no CTA reads the old ones.  Latency bounds it: lengths, table, free list.
 constexpr int kStepThreads = 512, kStepCtas = 8;
+// Places of more tokens than this are found by a second kernel on the whole
+// chip: 226,000 tokens of 256 sessions SLOT2 us so and 34 in the cluster, whose
+// threads take 0.5 us for each 4,096 of them.
+constexpr int kStepSlots = 16384;
 
 __device__ __forceinline__ void cluster_wait_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -144,9 +148,43 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
   if (last + tid < s.n_seqs) s.len[last + tid] = new_len;
 }
 
-cudaError_t launch_pages_step(const StepView& s, cudaStream_t st) {
-  TimingScope ts("pages_step", st);
-  const cudaError_t e = launch_after(k_pages_step, dim3(kStepCtas), kStepThreads, 0, st, s);
+// The places of new tokens, as k_pages_step writes them: a token to a thread,
+// its session found by halves in cu.
+__global__ void __launch_bounds__(256) k_step_slots(const __grid_constant__ StepView s) {
+  pdl_trigger();
+  pdl_wait();
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= s.n_tokens) return;
+  int slot = -1;
+  if (t < s.cu[s.n_seqs]) {
+    int lo = 0, hi = s.n_seqs;  // cu[lo] <= t < cu[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s.cu[mid] <= t)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const int row = s.len[lo] - (s.cu[lo + 1] - t), i = row / s.page_rows;
+    const int page = s.table[(size_t)lo * s.max_pages + i];
+    if (page >= 0 && page < s.n_pages) slot = page * s.page_rows + (row - i * s.page_rows);
+  }
+  s.slot[t] = slot;
+}
+
+cudaError_t launch_pages_step(const StepView& step, cudaStream_t st) {
+  StepView s = step;
+  const bool apart = s.slot && s.n_tokens > kStepSlots;
+  cudaError_t e;
+  {
+    TimingScope ts("pages_step", st);
+    if (apart) s.slot = nullptr;
+    e = launch_after(k_pages_step, dim3(kStepCtas), kStepThreads, 0, st, s);
+    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !apart) return e;
+  }
+  TimingScope ts("step_slots", st);
+  s.slot = step.slot;
+  e = launch_after(k_step_slots, dim3((s.n_tokens + 255) / 256), 256, 0, st, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -41,40 +41,52 @@ __device__ __forceinline__ void q4_codes(uint32_t word, uint32_t (&h)[4]) {
 
 // How a group is put into 4 bits: its scale is the largest magnitude over six
 // times the factor, rounded to e4m3, at least the smallest (a group of zeros
-// divides by something) and at most the largest.  top: the bits of the largest
-// magnitude; integer order puts infinities and NaN above every number.
+// divides by something) and at most the largest.
+//
+// Quotients x / t are x r + x r_lo, the first product and the sum rounded
+// together: r is below 1 / t by some 2^-23 of it and r_lo what is missing, to
+// 2^-45.  So a quotient that fp32 holds comes out exact, a border between two
+// codes (or scales) with it, where bf16 elements often lie, for two operations
+// instead of a division.  Both parts have t's sign: zeros keep theirs.
+struct Q4Recip {
+  float r, r_lo;
+  __device__ __forceinline__ explicit Q4Recip(float t) {
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    r *= 0x1.fffffcp-1f;
+    r_lo = fmaf(-r, t, 1.f) * r;
+  }
+  __device__ __forceinline__ float quotient(float x) const { return fmaf(x, r, x * r_lo); }
+};
+
+// top: the bits of the group's largest magnitude as integers order them, which
+// puts infinities and NaN above every number; by_six: of 6 factor.
 struct Q4Scale {
   uint32_t byte;
-  float r, r_lo;  // 1 / (scale * factor) rounded down, and what that cut off
-};
-__device__ __forceinline__ Q4Scale q4_scale(uint32_t top, float factor) {
-  const float want = fminf(fmaxf(__uint_as_float(top) / (6.f * factor), 0x1p-9f), 448.f);
-  unsigned short two;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(want));
-  const uint32_t half = q4_scales(two);
-  const float t = __low2float(*reinterpret_cast<const __half2*>(&half)) * factor;
-  Q4Scale s;
-  s.byte = top >= 0x7f800000u ? kQ4NaN : two & 0xffu;
-  s.r = __frcp_rd(t);  // downwards: both parts have t's sign, and a zero keeps its own below
-  s.r_lo = fmaf(-s.r, t, 1.f) * s.r;
-  return s;
-}
-// Eight elements' codes.  x / t is rounded to fp32 and then to a code; with the
-// reciprocal's two parts a quotient that fp32 holds (a border between two codes,
-// where bf16 elements often lie) comes out exact, for two operations instead of
-// a division.
-__device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& s) {
-  uint32_t b[4], w;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float lo = fmaf(x[2 * i], s.r, x[2 * i] * s.r_lo), hi = fmaf(x[2 * i + 1], s.r, x[2 * i + 1] * s.r_lo);
-    asm("{\n\t.reg .b8 a;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %1, %2;\n\t"
-        "cvt.u32.u8 %0, a;\n\t}"
-        : "=r"(b[i])
-        : "f"(hi), "f"(lo));
+  Q4Recip by;  // of scale * factor
+  __device__ __forceinline__ Q4Scale(uint32_t top, const Q4Recip& by_six, float factor) : by(init(top, by_six, factor)) {}
+
+ private:
+  __device__ __forceinline__ float init(uint32_t top, const Q4Recip& by_six, float factor) {
+    const float want = fminf(fmaxf(by_six.quotient(__uint_as_float(top)), 0x1p-9f), 448.f);
+    unsigned short two;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(want));
+    const uint32_t half = q4_scales(two);
+    byte = top >= 0x7f800000u ? kQ4NaN : two;  // the upper half is zero
+    return __low2float(*reinterpret_cast<const __half2*>(&half)) * factor;
   }
-  w = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+};
+// Eight elements' codes.
+__device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& s) {
+  uint32_t w;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(w)
+      : "f"(s.by.quotient(x[0])), "f"(s.by.quotient(x[1])), "f"(s.by.quotient(x[2])), "f"(s.by.quotient(x[3])),
+        "f"(s.by.quotient(x[4])), "f"(s.by.quotient(x[5])), "f"(s.by.quotient(x[6])), "f"(s.by.quotient(x[7])));
   return s.byte == kQ4NaN ? 0u : w;
 }
 __device__ __forceinline__ uint32_t q4_top(const float (&x)[8]) {
