@@ -42,12 +42,14 @@ __host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt <= 2 ? 
 // Bytes of shared memory for queries; none where they are in registers.
 __host__ __device__ constexpr int qa_queries(int nt, int parts) { return nt * parts > 1 ? 8 * nt * parts * kD * 2 : 0; }
 __host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
+// Groups of queries whose parts the warps merge at a time: all, where that leaves qa_ctas to an SM.
+__host__ __device__ constexpr int qa_pass(int nt, int parts) { return nt == 2 && parts == 2 ? 1 : nt; }
 __host__ __device__ constexpr int qa_factors(int nt) {
   return 8 * nt * 4 * (1 + qa_warps(nt)) > (int)sizeof(RangeScratch<256>) ? 8 * nt * 4 * (1 + qa_warps(nt))
                                                                           : (int)sizeof(RangeScratch<256>);
 }
 __host__ __device__ constexpr int qa_smem(int nt, int parts) {
-  const int need = qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (kQaPitch * 4 + nt * 8) + qa_factors(nt);
+  const int need = qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (qa_pass(nt, parts) * kQaPitch * 4 + nt * 8) + qa_factors(nt) + 8 * nt * 4;
   // no more CTAs to an SM than dealt to it, however soon another launch's end
   const int alone = (228 * 1024 / (qa_ctas(nt, parts) + 1) - 1024) / 128 * 128 + 128;
   return need > alone ? need : alone;
@@ -107,13 +109,22 @@ __device__ __forceinline__ uint32_t lds16(uint32_t at) {
   return x;
 }
 
-// Four neighbouring elements of a query.
-__device__ __forceinline__ float4 load_query4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load_query4(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
+// Four neighbouring elements of a query, as they are in memory.
+template <typename T>
+struct Query4;
+template <>
+struct Query4<float> {
+  float4 x;
+  __device__ __forceinline__ float4 get() const { return x; }
+};
+template <>
+struct Query4<__nv_bfloat16> {
+  uint2 x;
+  __device__ __forceinline__ float4 get() const {
+    return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                       __uint_as_float(x.y & 0xffff0000u));
+  }
+};
 
 // Byte of the 16-byte chunk c of value row r in its block: eight rows' first
 // chunks, which a read takes together, lie in different banks.
@@ -129,15 +140,17 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
                float* part_o, uint32_t* err) {
   constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;  // of a query's elements and of a weight
   constexpr int kRows = 8 * NT, kWarps = qa_warps(NT), kThreads = 32 * kWarps;
+  constexpr int kPass = qa_pass(NT, kParts);
   constexpr bool kRegs = qa_queries(NT, kParts) == 0;  // queries in registers, else in shared memory
   extern __shared__ uint4 pat_smem[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
   uint2* qs = reinterpret_cast<uint2*>(sm + qa_ring(NT));  // [part][NT][step][lane]
   float* wo = reinterpret_cast<float*>(sm + qa_ring(NT) + qa_queries(NT, kParts));
-  float2* wml = reinterpret_cast<float2*>(wo + kWarps * 8 * kQaPitch);
+  float2* wml = reinterpret_cast<float2*>(wo + kWarps * 8 * kPass * kQaPitch);
   RangeScratch<kThreads>* scratch = reinterpret_cast<RangeScratch<kThreads>*>(wml + kWarps * kRows);
   // once an item has ended (the range was found long before): 1 / sum of each
   // query, and the warps' factors
+  float* q_back = reinterpret_cast<float*>(sm + qa_smem(NT, kParts) - kRows * 4);  // what each query's sums are multiplied by
   float* inv = reinterpret_cast<float*>(scratch);  // [kRows]
   float* factor = inv + kRows;                     // [warps][kRows]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
@@ -229,18 +242,82 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     }
     cp_async_commit();
   };
-  auto fill = [&]() {
+  // Queries of an item: its lane takes elements 32 t4 .. of query g8 of group 0
+  // (one group: every warp all of them) or of the warp's number.
+  const int group = kRegs ? 0 : warp;
+  Query4<T> raw[8];
+  // Step ks of the products takes elements 32 t4 + 4 ks .. + 3 of query 8 nt + g8.
+  // sc: what the sums of queries 8 nt + 2 t4 + e are multiplied by.
+  uint2 qr[8];
+  float sc[NT][2];
+  auto load_queries = [&](const Cursor& c, const Item& x) {
+    const int row0 = x.chunk * chunk_rows, rows = min(chunk_rows, min(c.w.fresh, pg.w) * G - row0);
+    const int at = 8 * group + g8, r = row0 + at, t = c.w.first + r / G;
+    const bool there = at < rows && t >= 0 && t < n;
+    const T* from = q + ((size_t)(there ? t : 0) * hq + x.h * G + r % G) * kD + 32 * t4;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      raw[ks].x = {};
+      if (there) raw[ks] = *reinterpret_cast<const Query4<T>*>(from + 4 * ks);
+    }
+  };
+  auto take_queries = [&](int h) {
+    if (!kRegs && warp >= NT) return;
+    uint32_t top = 0;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      const float4 y = raw[ks].get();
+      top = max(max(top, __float_as_uint(y.x) & 0x7fffffffu), max(__float_as_uint(y.y) & 0x7fffffffu, __float_as_uint(y.z) & 0x7fffffffu));
+      top = max(top, __float_as_uint(y.w) & 0x7fffffffu);
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int ex = min((int)(top >> 23), 253);
+    float mul = __uint_as_float((uint32_t)(254 - ex) << 23);  // 2^-exponent
+    const float back = kPatLog2e * rsqrtf((float)kD) * (pools.k_factor ? pools.k_factor[h] : 1.f) / mul;
+    if (top >= 0x7f800000u) mul = CUDART_NAN_F;  // not all are numbers: nor are its scores
+    if constexpr (kRegs) {
+      sc[0][0] = __shfl_sync(0xffffffffu, back, 8 * t4);
+      sc[0][1] = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
+    } else if (t4 == 0) {
+      q_back[8 * warp + g8] = back;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      const float4 y = raw[ks].get(), z = make_float4(y.x * mul, y.y * mul, y.z * mul, y.w * mul);
+      const uint2 hi = make_uint2(pack_f16(z.x, z.y), pack_f16(z.z, z.w));
+      if constexpr (kRegs) {
+        qr[ks] = hi;
+      } else {
+        qs[(warp * 8 + ks) * 32 + lane] = hi;
+        if (kParts == 2) {
+          const float2 a = unpack_f16(hi.x), b = unpack_f16(hi.y);
+          qs[((NT + warp) * 8 + ks) * 32 + lane] =
+              make_uint2(pack_f16(z.x - a.x, z.y - a.y), pack_f16(z.z - b.x, z.w - b.y));
+        }
+      }
+    }
+  };
+  auto fill = [&](auto between) {
     Entry first[kQaStages];  // all table entries on their way before the first copies
     bool any[kQaStages];
 #pragma unroll
     for (int st = 0; st < kQaStages; ++st) any[st] = look_up(first[st]);
+    between();
 #pragma unroll
     for (int st = 0; st < kQaStages; ++st) fetch(ring + st * kQaStage, any[st], first[st]);
   };
   start(rg.at, rg.b0);
-  fill();
-
   Cursor cur = rg.at;
+  int ready = -1;  // the unit that the part begins at whose queries are taken: the first
+  if (rg.b0 < rg.b1) {
+    advance(cur, rg.b0, pg, G, chunk_rows, hkv);
+    const Item x = item_at(cur, rg.b0);
+    fill([&]() { load_queries(cur, x); });
+    take_queries(x.h);
+    ready = rg.b0;
+  }
+
   int stage = 0;  // bytes to the stage at hand
   for (int seg = rg.b0; seg < rg.b1;) {
     // the part of one item that lies in the range: blocks part0 .. seg_end
@@ -266,51 +343,17 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
         desc[cta] = d;
     }
 
-    // Queries: step ks takes elements 32 t4 + 4 ks .. + 3 of query 8 nt + g8.
-    // sc: what the sums of queries 8 nt + 2 t4 + e are multiplied by.
-    uint2 qr[kRegs ? kParts : 1][kRegs ? NT : 1][kRegs ? 8 : 1];
-    float sc[NT][2];
-    const float base_scale = kPatLog2e * rsqrtf((float)kD) * (pools.k_factor ? pools.k_factor[h] : 1.f);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int r = row0 + 8 * nt + g8, t = cur.w.first + r / G;
-      const bool ok = 8 * nt + g8 < rows && t >= 0 && t < n;
-      const T* from = q + ((size_t)(ok ? t : 0) * hq + h * G + r % G) * kD + 32 * t4;
-      float4 y[8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        y[ks] = ok ? load_query4(from + 4 * ks) : make_float4(0.f, 0.f, 0.f, 0.f);
-        top = max(max(top, __float_as_uint(y[ks].x) & 0x7fffffffu), max(__float_as_uint(y[ks].y) & 0x7fffffffu, __float_as_uint(y[ks].z) & 0x7fffffffu));
-        top = max(top, __float_as_uint(y[ks].w) & 0x7fffffffu);
-      }
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int ex = min((int)(top >> 23), 253);
-      float mul = __uint_as_float((uint32_t)(254 - ex) << 23);  // 2^-exponent
-      const float back = base_scale / mul;
-      if (top >= 0x7f800000u) mul = CUDART_NAN_F;  // not all are numbers: nor are its scores
-#pragma unroll
-      for (int e = 0; e < 2; ++e) sc[nt][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * t4 + e));
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const float4 z = make_float4(y[ks].x * mul, y[ks].y * mul, y[ks].z * mul, y[ks].w * mul);
-        const uint2 hi = make_uint2(pack_f16(z.x, z.y), pack_f16(z.z, z.w));
-        uint2 lo = make_uint2(0u, 0u);
-        if (kParts == 2) {
-          const float2 a = unpack_f16(hi.x), b = unpack_f16(hi.y);
-          lo = make_uint2(pack_f16(z.x - a.x, z.y - a.y), pack_f16(z.z - b.x, z.w - b.y));
-        }
-        if constexpr (kRegs) {
-          qr[0][nt][ks] = hi;
-          if (kParts == 2) qr[kParts - 1][nt][ks] = lo;
-        } else if (warp == 0) {
-          qs[(nt * 8 + ks) * 32 + lane] = hi;
-          if (kParts == 2) qs[((NT + nt) * 8 + ks) * 32 + lane] = lo;
-        }
-      }
+    if (ready != seg) {
+      load_queries(cur, item);
+      take_queries(h);
     }
-    if constexpr (!kRegs) __syncthreads();
+    if constexpr (!kRegs) {
+      __syncthreads();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) sc[nt][e] = q_back[8 * nt + 2 * t4 + e];
+    }
 
     // Running state: reference and the lane's part of the sum of queries
     // 8 nt + 2 t4 + e; o[mt][nt][j] is dimension 16 g8 + 2 mt + (j >> 1) of
@@ -364,7 +407,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
               for (int part = 0; part < kParts; ++part) {
                 uint2 b;
                 if constexpr (kRegs)
-                  b = qr[part][nt][2 * i + j];
+                  b = qr[2 * i + j];
                 else
                   b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
 #pragma unroll
@@ -517,7 +560,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     __syncwarp();
     start(cur, part0);
     stage = 0;
-    fill();
+    fill([]() {});
     }
     // The warps' states of this item, merged in shared memory, eight queries at
     // a time.
@@ -554,24 +597,28 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     }
     __syncthreads();
 #pragma unroll
-    for (int n0 = 0; n0 < NT; ++n0) {
+    for (int n0 = 0; n0 < NT; n0 += kPass) {
       if (n0 > 0) __syncthreads();  // the buffer is free again
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int x = 2 * t4 + e;
-        const float a = factor[warp * kRows + 8 * n0 + x];
-        float* w = wo + (warp * 8 + x) * kQaPitch + 16 * g8;
+      for (int i = 0; i < kPass; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          store4(w + 4 * k, o[2 * k][n0][e] * a, o[2 * k][n0][2 + e] * a, o[2 * k + 1][n0][e] * a, o[2 * k + 1][n0][2 + e] * a);
-      }
+        for (int e = 0; e < 2; ++e) {
+          const int x = 8 * i + 2 * t4 + e;
+          const float a = factor[warp * kRows + 8 * n0 + x];
+          float* w = wo + (warp * 8 * kPass + x) * kQaPitch + 16 * g8;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            store4(w + 4 * k, o[2 * k][n0 + i][e] * a, o[2 * k][n0 + i][2 + e] * a, o[2 * k + 1][n0 + i][e] * a,
+                   o[2 * k + 1][n0 + i][2 + e] * a);
+        }
       __syncthreads();
-      for (int y = warp; y < min(8, rows - 8 * n0); y += kWarps) {
+#pragma unroll 2
+      for (int y = warp; y < min(8 * kPass, rows - 8 * n0); y += kWarps) {
         const int x = 8 * n0 + y;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 + y) * kQaPitch + 4 * lane);
+          const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 * kPass + y) * kQaPitch + 4 * lane);
           O.x += z.x;
           O.y += z.y;
           O.z += z.z;
