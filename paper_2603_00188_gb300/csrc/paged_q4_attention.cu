@@ -213,10 +213,11 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
   const uint8_t *k_from = pools.k + 16 * t4, *v_from = pools.v + 16 * t4;
   const uint32_t v_to = kQaCodes + qa_value_off(g8, t4);
   const int page_all = hkv * pg.page_rows;  // rows of all heads
-  // Known to be 64 and 8, addresses become two shifted additions each on the
-  // pipe that the conversions fill; as numbers they are one multiplication.
-  uint32_t code_bytes, scale_bytes;
-  asm volatile("mov.u32 %0, 64;\n\tmov.u32 %1, 8;" : "=r"(code_bytes), "=r"(scale_bytes));
+  const bool whole_tiles = pg.page_rows % 16 == 0;
+  // Known to be powers of two, these become shifts and additions on the pipe that
+  // the conversions fill; as numbers they are multiplications on another.
+  uint32_t code_bytes, scale_bytes, sixteen;
+  asm volatile("mov.u32 %0, 64;\n\tmov.u32 %1, 8;\n\tmov.u32 %2, 16;" : "=r"(code_bytes), "=r"(scale_bytes), "=r"(sixteen));
   auto fetch = [&](uint32_t dst, bool any, const Entry& e) {
     ok = ok_next;
     ok_next = 0;
@@ -225,16 +226,32 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
       if (e.row >= 0 && !good) record_error(err, kErrInput);
       const int row = good ? e.page * page_all + e.row : -1;
       ok_next = __ballot_sync(0xffffffffu, good);
+      const uint32_t k_to = dst + 16 * lane, v_at = dst + v_to;
+      if (whole_tiles && ok_next == 0xffffffffu) {  // 16 rows lie together
 #pragma unroll
-      for (int i = 0; i < kQaBlock / 8; ++i) {
-        const int r = __shfl_sync(0xffffffffu, row, g8 + 8 * i);
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ge.s32 p, %4, 0;\n\t"
-            "@p cp.async.cg.shared.global [%0], [%1], 16;\n\t"
-            "@p cp.async.cg.shared.global [%2], [%3], 16;\n\t}" ::"r"(dst + 512 * i + 16 * lane),
-            "l"(k_from + (uint64_t)(uint32_t)r * code_bytes), "r"(dst + 512 * i + v_to),
-            "l"(v_from + (uint64_t)(uint32_t)r * code_bytes), "r"(r)
-            : "memory");
+        for (int y = 0; y < 2; ++y) {
+          const uint64_t at = (uint64_t)(uint32_t)(__shfl_sync(0xffffffffu, row, 16 * y) + g8) * code_bytes;
+          const uint8_t *ks = k_from + at, *vs = v_from + at;
+          asm volatile(
+              "cp.async.cg.shared.global [%0], [%1], 16;\n\t"
+              "cp.async.cg.shared.global [%0 + 512], [%1 + 512], 16;\n\t"
+              "cp.async.cg.shared.global [%2], [%3], 16;\n\t"
+              "cp.async.cg.shared.global [%2 + 512], [%3 + 512], 16;" ::"r"(k_to + 1024 * y),
+              "l"(ks), "r"(v_at + 1024 * y), "l"(vs)
+              : "memory");
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kQaBlock / 8; ++i) {
+          const int r = __shfl_sync(0xffffffffu, row, g8 + 8 * i);
+          asm volatile(
+              "{\n\t.reg .pred p;\n\tsetp.ge.s32 p, %4, 0;\n\t"
+              "@p cp.async.cg.shared.global [%0], [%1], 16;\n\t"
+              "@p cp.async.cg.shared.global [%2], [%3], 16;\n\t}" ::"r"(k_to + 512 * i),
+              "l"(k_from + (uint64_t)(uint32_t)r * code_bytes), "r"(v_at + 512 * i),
+              "l"(v_from + (uint64_t)(uint32_t)r * code_bytes), "r"(r)
+              : "memory");
+        }
       }
       const uint64_t at = (uint64_t)(uint32_t)max(row, 0) * scale_bytes;
       cp_async8_fill(dst + 2 * kQaCodes + 8 * lane, pools.k_scale + at, row >= 0);
@@ -529,9 +546,9 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
           const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
                          r3 = i ? w[3].y : w[3].x;
           uint32_t even0[4], odd0[4], even1[4], odd1[4];
-          q4_codes((r0 & 0x0f0f0f0fu) | (r1 << 4 & 0xf0f0f0f0u), even0);
+          q4_codes((r0 & 0x0f0f0f0fu) | (r1 * sixteen & 0xf0f0f0f0u), even0);
           q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
-          q4_codes((r2 & 0x0f0f0f0fu) | (r3 << 4 & 0xf0f0f0f0u), even1);
+          q4_codes((r2 & 0x0f0f0f0fu) | (r3 * sixteen & 0xf0f0f0f0u), even1);
           q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
