@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     for (bool look = false;; look = true) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -1e30f;
+      m[nt][0] = m[nt][1] = -3e38f;
       l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
@@ -687,7 +687,7 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   const int rows = pages.w * (hq / hkv), part_rows = q4_part_rows(dt, pages, hq / hkv), most = q4_most_rows(dt);
   const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas(dt, part_rows);
   const long long items = (long long)pages.n_seqs * hkv * chunks;
-  pages.item_units = 10;
+  pages.item_units = 12;
   pages.block_shift = kQaBlockShift;
   int split = 20;
   const long long longest = ((long long)pages.max_pages * pages.page_rows + kQaBlock - 1) / kQaBlock;

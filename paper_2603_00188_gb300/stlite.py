@@ -585,16 +585,17 @@ def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype) -> bytes:
     each token's heads packed."""
     n, hq, d = qs
     nk, hkv, dk = ks
-    sq, sk = q.stride(), k.stride()
-    if (d != 128 or dk != 128 or nk != n or k.dtype != dtype or sq[2] != 1 or sk[2] != 1 or (sq[1] != 128 and hq > 1)
-            or (sk[1] != 128 and hkv > 1)):
+    sq0, sq1, sq2 = q.stride()
+    sk0, sk1, sk2 = k.stride()
+    if not (d == 128 == dk and nk == n and sq2 == 1 == sk2 and (sq1 == 128 or hq == 1) and (sk1 == 128 or hkv == 1)
+            and k.dtype == dtype):
         raise ValueError("q and k are [T][H][128] of one type, each token's heads packed")
     pv = sv0 = 0
     if v is not None:
-        sv, pv = v.stride(), v.data_ptr()
-        if v.shape != ks or v.dtype != dtype or sv[2] != 1 or (sv[1] != 128 and hkv > 1):
+        sv0, sv1, sv2 = v.stride()
+        pv, sv0 = v.data_ptr(), sv0 or 1
+        if not (sv2 == 1 and (sv1 == 128 or hkv == 1) and v.shape == ks and v.dtype == dtype):
             raise ValueError("v is as k")
-        sv0 = sv[0] or 1
     pq = pk = 0
     if q_norm is not None or k_norm is not None:
         for w in (q_norm, k_norm):
@@ -610,7 +611,7 @@ def _tokens(q, k, v, pos, rope, q_norm, k_norm, eps, qs, ks, dtype) -> bytes:
     if n == 1:  # no next token: whatever its distance would be
         return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, 0, 0, 0, pq, pk, eps, pos.data_ptr())
     # 0 stands for packed, so a broadcast token's goes as 1, which the library refuses
-    return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, sq[0] or 1, sk[0] or 1, sv0, pq, pk, eps, pos.data_ptr())
+    return _TOKENS.pack(q.data_ptr(), k.data_ptr(), pv, sq0 or 1, sk0 or 1, sv0, pq, pk, eps, pos.data_ptr())
 
 
 def stlite_rotate_qk(q, k, pos, rope, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
@@ -800,7 +801,8 @@ class Q4Pools:
         self.k, self.v, self.k_scale, self.v_scale, self.k_factor, self.v_factor = k, v, k_scale, v_scale, k_factor, v_factor
         self.c = Q4PoolsC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(k_factor), _ptr(v_factor))
         self.hkv, self._pool, self._device = hkv, (p, r), k.get_device()
-        self._address, self._words = ctypes.addressof(self.c), tuple(getattr(self.c, n) or 0 for n, _ in self.c._fields_)
+        self._kind = (p, r, hkv)
+        self._address, self._bytes = ctypes.addressof(self.c), bytes(self.c)
 
 
 def make_q4_pools(n_pages, page_rows, hkv, k_factor=None, v_factor=None, device="cuda") -> Q4Pools:
@@ -809,6 +811,9 @@ def make_q4_pools(n_pages, page_rows, hkv, k_factor=None, v_factor=None, device=
     k, v = (torch.zeros(shape + (64,), dtype=torch.uint8, device=device) for _ in range(2))
     ks, vs = (torch.zeros(shape + (8,), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
     return Q4Pools(k, v, ks, vs, k_factor, v_factor)
+
+
+_ROWS = struct.Struct("=4Q")  # the rows of stlite_q4_layer, before its pools
 
 
 def _q4_error():
@@ -822,7 +827,7 @@ def stlite_paged_append_q4(q, k, v, pos, rope, pages, q_out, pools, q_norm=None,
     if q_out.shape != qs or q_out.dtype != dtype or not q_out.is_contiguous():
         raise _output_error(qs)
     hkv = ks[1]
-    if pools._pool != pages._pool or pools.hkv != hkv:
+    if pools._kind != (*pages._pool, hkv):
         raise _q4_error()
     if dev < 0 or not (torch._C._cuda_getDevice() == dev == k.get_device() == v.get_device() == pos.get_device()
                        == q_out.get_device() == pools._device == pages._device):
@@ -881,25 +886,25 @@ def stlite_compact_paged_q4(layers, budget, pages, seq, stream=None):
     """The kept rows of every layer into sequence seq's 4-bit pages; layers:
     list of (k, v, pools, idx)."""
     k0 = layers[0][0]
-    shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
+    shape, dtype, dev, parts = k0.shape, k0.dtype, k0.get_device(), []
     n, hkv, d = shape
-    want, index = pages._pool, (hkv, budget)
+    kind, index = (*pages._pool, hkv), (hkv, budget)
     for k, v, pools, ix in layers:
-        if pools._pool != want or pools.hkv != hkv:
+        if pools._kind != kind:
             raise _q4_error()
-        if not (k.shape == shape == v.shape and ix.shape == index and k.dtype == dtype == v.dtype
-                and ix.dtype == torch.int32 and k.is_contiguous() and v.is_contiguous() and ix.is_contiguous()):
+        if not ((k is k0 or (k.shape == shape and k.dtype == dtype)) and v.shape == shape and v.dtype == dtype
+                and ix.shape == index and ix.dtype == torch.int32 and k.is_contiguous() and v.is_contiguous()
+                and ix.is_contiguous()):
             raise ValueError("every layer's k and v are [N][Hkv][128] of one type and idx int32 [Hkv][budget], "
                              "contiguous")
         if not k.get_device() == pools._device == ix.get_device() == dev or (v.get_device() != dev
                                                                              and not v.is_pinned()):
             raise ValueError(_ELSEWHERE)
-        flat += (0, k.data_ptr(), v.data_ptr(), ix.data_ptr(), *pools._words)
+        parts += (_ROWS.pack(0, k.data_ptr(), v.data_ptr(), ix.data_ptr()), pools._bytes)
     if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
         raise ValueError(_ELSEWHERE)
-    arr = array("Q", flat)
     st = _lib.stlite_compact_paged_q4(_SHAPE.pack(n, hkv, hkv, d, 1, _DTYPE[dtype]), budget, pages._address, seq,
-                                      len(layers), _address(arr),
+                                      len(layers), b"".join(parts),
                                       _CURRENT(dev) if stream is None else stream.cuda_stream)
     if st != STLITE_OK:
         raise StliteError(st, "stlite_compact_paged_q4")
@@ -910,10 +915,11 @@ def stlite_compress_layers_paged_q4(layers, frames, params, pages, seq, ws, stre
     pages; layers: list of (q, k, v, pools, idx_out)."""
     q0, k0 = layers[0][:2]
     sh = make_shape(q0, k0)
-    qs, shape, dtype, dev, flat = q0.shape, k0.shape, k0.dtype, k0.get_device(), []
+    qs, shape, dtype, dev, parts = q0.shape, k0.shape, k0.dtype, k0.get_device(), []
     kept = sh.n_kv_heads * stlite_budget(sh.n_tokens, params.beta, params.k_override)
+    kind = (*pages._pool, sh.n_kv_heads)
     for q, k, v, pools, ix in layers:
-        if pools._pool != pages._pool or pools.hkv != sh.n_kv_heads:
+        if pools._kind != kind:
             raise _q4_error()
         if not (q.shape == qs and k.shape == shape == v.shape and q.dtype == dtype == k.dtype and v.dtype == dtype
                 and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
@@ -923,14 +929,13 @@ def stlite_compress_layers_paged_q4(layers, frames, params, pages, seq, ws, stre
         if not q.get_device() == k.get_device() == pools._device == ix.get_device() == dev or (
                 v.get_device() != dev and not v.is_pinned()):
             raise ValueError(_ELSEWHERE)
-        flat += (q.data_ptr(), k.data_ptr(), v.data_ptr(), ix.data_ptr(), *pools._words)
+        parts += (_ROWS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), ix.data_ptr()), pools._bytes)
     if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device == ws.get_device():
         raise ValueError(_ELSEWHERE)
     fs = _frames(frames)
-    arr = array("Q", flat)
     b = ctypes.c_int32(0)
     _check(_lib.stlite_compress_layers_paged_q4(ctypes.byref(sh), ctypes.byref(fs.c), ctypes.byref(params),
-                                                pages._address, int(seq), len(layers), _address(arr), ctypes.byref(b),
+                                                pages._address, int(seq), len(layers), b"".join(parts), ctypes.byref(b),
                                                 _ptr(ws), ws.numel(), _stream(stream)),
            "stlite_compress_layers_paged_q4")
     return int(b.value)
@@ -941,24 +946,23 @@ def stlite_paged_fetch_q4(layers, pages, stream=None):
     - cu_new[s] (or max_new) rows of each sequence; layers: list of (pools, k_out,
     v_out), outputs [T][Hkv][128]."""
     k0 = layers[0][1]
-    shape, dtype, dev, flat = k0.shape, k0.dtype, k0.get_device(), []
+    shape, dtype, dev, parts = k0.shape, k0.dtype, k0.get_device(), []
     n, hkv, d = shape
-    want = pages._pool
+    kind = (*pages._pool, hkv)
     for pools, k, v in layers:
-        if pools._pool != want or pools.hkv != hkv:
+        if pools._kind != kind:
             raise _q4_error()
-        if not (d == 128 and k.shape == shape == v.shape and k.dtype == dtype == v.dtype and k.is_contiguous()
-                and v.is_contiguous()):
+        if not ((k is k0 or (k.shape == shape and k.dtype == dtype)) and v.shape == shape and v.dtype == dtype
+                and d == 128 and k.is_contiguous() and v.is_contiguous()):
             raise ValueError("every layer's outputs are contiguous [T][Hkv][128] of one type")
         if not k.get_device() == v.get_device() == pools._device == dev:
             raise ValueError(_ELSEWHERE)
-        flat += (0, k.data_ptr(), v.data_ptr(), 0, *pools._words)
+        parts += (_ROWS.pack(0, k.data_ptr(), v.data_ptr(), 0), pools._bytes)
     if dev < 0 or not torch._C._cuda_getDevice() == dev == pages._device:
         raise ValueError(_ELSEWHERE)
-    arr = array("Q", flat)
     st = _lib.stlite_paged_fetch_q4(
         _SHAPE.pack(n, hkv, hkv, 128, pages.max_new if pages.cu_new is None else 1, _DTYPE[dtype]), pages._address,
-        len(layers), _address(arr), _CURRENT(dev) if stream is None else stream.cuda_stream)
+        len(layers), b"".join(parts), _CURRENT(dev) if stream is None else stream.cuda_stream)
     if st != STLITE_OK:
         raise StliteError(st, "stlite_paged_fetch_q4")
 
