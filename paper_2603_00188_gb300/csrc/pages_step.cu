@@ -10,7 +10,7 @@ namespace stl {
 // cluster separate what reads the state before from what changes it: pages that
 // go back are on the free list before any is taken, and lengths are written
 // when no CTA reads the old ones.  Latency bounds it: lengths, table, free list.
-constexpr int kStepThreads = 512, kStepCtas = 8;
+constexpr int kStepThreads = 256, kStepCtas = 8;
 // Places of more tokens than this are found by a second kernel on the whole
 // chip: 226,000 tokens of 256 sessions SLOT2 us so and 34 in the cluster, whose
 // threads take 0.5 us for each 4,096 of them.
@@ -20,26 +20,36 @@ __device__ __forceinline__ void cluster_wait_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The sum of x over the threads up to this one; *total: over all.  Whole CTA.
-__device__ __forceinline__ long long scan(long long x, long long* warp_sums, long long* total) {
+// Two sums over the threads up to this one, and over all of them (*total).
+// Sums stop at 2^31 - 1, so that they keep their order however much is asked
+// for.  Whole CTA; calls take turns with two buffers.
+struct Pair {
+  int a, b;
+};
+__device__ __forceinline__ int add_most(int x, int y) { return (int)min((uint32_t)x + (uint32_t)y, 0x7fffffffu); }
+__device__ __forceinline__ Pair scan(Pair x, Pair* warp_sums, Pair* total) {
+  constexpr int kWarps = kStepThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const int ya = __shfl_up_sync(0xffffffffu, x.a, o), yb = __shfl_up_sync(0xffffffffu, x.b, o);
+    if (lane >= o) {
+      x.a = add_most(x.a, ya);
+      x.b = add_most(x.b, yb);
+    }
   }
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  long long before = 0, all = 0;
+  Pair before = {0, 0}, all = {0, 0};
 #pragma unroll
-  for (int w = 0; w < kStepThreads / 32; ++w) {
-    const long long y = warp_sums[w];
-    if (w < warp) before += y;
-    all += y;
+  for (int w = 0; w < kWarps; ++w) {
+    const Pair y = warp_sums[w];
+    if (w == warp) before = all;
+    all.a = add_most(all.a, y.a);
+    all.b = add_most(all.b, y.b);
   }
-  __syncthreads();
   *total = all;
-  return x + before;
+  return {add_most(before.a, x.a), add_most(before.b, x.b)};
 }
 
 // The last of the kStepThreads sessions whose entries begin at or before j.
@@ -54,10 +64,11 @@ __device__ __forceinline__ int session_of(const int* start, int j) {
 __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads)
     k_pages_step(const __grid_constant__ StepView s) {
   __shared__ int start[kStepThreads], tok_start[kStepThreads], kept_of[kStepThreads], keep_of[kStepThreads];
-  __shared__ long long warp_sums[kStepThreads / 32];
+  __shared__ Pair sums[2][kStepThreads / 32];
   pdl_trigger();
   pdl_wait();
-  const int tid = threadIdx.x, rank = blockIdx.x, flat = rank * kStepThreads + tid, all = kStepCtas * kStepThreads;
+  const int tid = threadIdx.x, rank = blockIdx.x, flat = rank * kStepThreads + tid;
+  constexpr int kAll = kStepCtas * kStepThreads, kAtOnce = 4;  // entries that a thread moves at a time
   const int rows_max = s.max_pages * s.page_rows, pr = s.page_rows;
   const int n0 = max(0, min(*s.n_free, s.n_pages));
   int have = 0, keep = 0, fresh = 0, held = 0, kept = 0;
@@ -72,71 +83,91 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
     held = have / pr + (have % pr != 0);
     kept = keep / pr + (keep % pr != 0);
   };
-  // pages past the rows that stay go on top of the free ones
-  long long back = 0, total;
+  // Pages past the rows that stay go on top of the free ones.  The sums of pages
+  // are below 2^31: a table's entries are.
+  int back = 0;
+  Pair total;
   for (int s0 = 0; s0 < s.n_seqs; s0 += kStepThreads) {
     load(s0);
     const int mine = held - kept;
-    const long long incl = scan(mine, warp_sums, &total);
-    start[tid] = (int)incl - mine;
+    start[tid] = scan({mine, 0}, sums[0], &total).a - mine;
     kept_of[tid] = kept;
     __syncthreads();
-    for (int j = flat; j < total; j += all) {
-      const int b = session_of(start, j);
-      const long long to = n0 + back + j;
-      if (to < s.n_pages)
-        s.free_pages[to] = s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]];
+    for (uint32_t j0 = flat; j0 < (uint32_t)total.a; j0 += kAtOnce * kAll) {
+      int page[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t j = j0 + i * kAll;
+        if (j >= (uint32_t)total.a) break;
+        const int b = session_of(start, j);
+        page[i] = s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]];
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t j = j0 + i * kAll;
+        const long long to = (long long)n0 + back + j;
+        if (j < (uint32_t)total.a && to < s.n_pages) s.free_pages[to] = page[i];
+      }
     }
-    back += total;
+    back += total.a;
     if (s0 + kStepThreads < s.n_seqs) __syncthreads();
   }
   cluster_wait_all();
-  const int n_free = (int)min((long long)s.n_pages, n0 + back);
+  const int n_free = (int)min((long long)s.n_pages, (long long)n0 + back);
 
   // who is served, and what it gets
-  long long asked_pages = 0, asked_tokens = 0;
-  int taken = 0, given = 0;  // pages and tokens of the sessions before
+  Pair asked = {0, 0};       // pages and tokens asked for by the sessions before
+  int taken = 0, given = 0;  // what those got
   int new_len = 0;
   if (rank == 0 && tid == 0) s.cu[0] = 0;
   for (int s0 = 0; s0 < s.n_seqs; s0 += kStepThreads) {
     if (s.n_seqs > kStepThreads) load(s0);
     const bool fits = fresh <= rows_max - keep;
     const int rows = fits ? keep + fresh : keep, want = rows / pr + (rows % pr != 0) - kept;
-    long long incl = asked_pages + scan(want, warp_sums, &total);
-    asked_pages += total;
-    const bool may = fits && (want == 0 || incl <= n_free);
-    incl = asked_tokens + scan(may ? fresh : 0, warp_sums, &total);
-    asked_tokens += total;
-    const bool served = may && (fresh == 0 || incl <= s.n_tokens);
+    const int pages_to = add_most(asked.a, scan({want, 0}, sums[1], &total).a);
+    asked.a = add_most(asked.a, total.a);
+    const bool may = fits && (want == 0 || pages_to <= n_free);
+    const int tokens_to = add_most(asked.b, scan({0, may ? fresh : 0}, sums[0], &total).b);
+    asked.b = add_most(asked.b, total.b);
+    // a sum that stopped is too much for any step
+    const bool served = may && (fresh == 0 || (tokens_to <= s.n_tokens && tokens_to < 0x7fffffff));
     const int pages = served ? want : 0, got = served ? fresh : 0;
-    // both sums are below 2^31: pages of the pool, places of the step
-    incl = scan((long long)pages << 32 | got, warp_sums, &total);
-    const int my_pages = (int)(incl >> 32) - pages, my_tokens = (int)(incl & 0xffffffffu) - got;
+    const Pair to = scan({pages, got}, sums[1], &total);
+    const int my_pages = to.a - pages, my_tokens = to.b - got;
     start[tid] = my_pages;
     tok_start[tid] = my_tokens;
     kept_of[tid] = kept;
     keep_of[tid] = keep;
     new_len = keep + got;
-    if (rank == 0 && s0 + tid < s.n_seqs) s.cu[s0 + tid + 1] = given + my_tokens + got;
+    if (rank == 0 && s0 + tid < s.n_seqs) s.cu[s0 + tid + 1] = given + to.b;
     __syncthreads();
-    const int n_pages = (int)(total >> 32), n_tok = (int)(total & 0xffffffffu), top = n_free - 1 - taken;
-    for (int j = flat; j < n_pages; j += all) {
-      const int b = session_of(start, j);
-      s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]] = s.free_pages[top - j];
+    const int top = n_free - 1 - taken;
+    for (uint32_t j0 = flat; j0 < (uint32_t)total.a; j0 += kAtOnce * kAll) {
+      int page[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (j0 + i * kAll < (uint32_t)total.a) page[i] = s.free_pages[top - (int)(j0 + i * kAll)];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t j = j0 + i * kAll;
+        if (j >= (uint32_t)total.a) break;
+        const int b = session_of(start, j);
+        s.table[(size_t)(s0 + b) * s.max_pages + kept_of[b] + j - start[b]] = page[i];
+      }
     }
     if (s.slot)
-      for (int j = flat; j < n_tok; j += all) {
+      for (uint32_t j = flat; j < (uint32_t)total.b; j += kAll) {
         const int b = session_of(tok_start, j), row = keep_of[b] + j - tok_start[b], i = row / pr;
         const int page = i < kept_of[b] ? s.table[(size_t)(s0 + b) * s.max_pages + i]
                                         : s.free_pages[top - (start[b] + i - kept_of[b])];
         s.slot[given + j] = page >= 0 && page < s.n_pages ? page * pr + (row - i * pr) : -1;
       }
-    taken += n_pages;
-    given += n_tok;
+    taken += total.a;
+    given += total.b;
     if (s0 + kStepThreads < s.n_seqs) __syncthreads();
   }
   if (s.slot)
-    for (int j = given + flat; j < s.n_tokens; j += all) s.slot[j] = -1;
+    for (uint32_t j = given + flat; j < (uint32_t)s.n_tokens; j += kAll) s.slot[j] = -1;
   cluster_wait_all();
   if (rank > 0) return;
   if (tid == 0) *s.n_free = n_free - taken;
