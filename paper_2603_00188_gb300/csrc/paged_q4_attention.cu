@@ -77,6 +77,9 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async8_fill(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
 }
@@ -204,6 +207,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
   // A stage: keys' codes, values' codes, keys' scales, values' scales.  Of a row
   // that does not count only the scales are written, zeros: whatever codes lie in
   // its place are numbers.
+  bool bad = false;              // a table entry was no page
   uint32_t ok = 0, ok_next = 0;  // rows that count of the block at hand, and of the one after it
   // where the lane reads in a stage: keys' codes and scales, values' even and odd rows and scales
   const uint32_t k_at = ring + 16 * lane, ks_at = ring + 2 * kQaCodes + kQ4Scales * g8 + 2 * t4;
@@ -223,10 +227,10 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     ok_next = 0;
     if (any) {
       const bool good = e.row >= 0 && (uint32_t)e.page < (uint32_t)pg.n_pages;
-      if (e.row >= 0 && !good) record_error(err, kErrInput);
+      bad |= e.row >= 0 && !good;
       const int row = good ? e.page * page_all + e.row : -1;
       ok_next = __ballot_sync(0xffffffffu, good);
-      const uint32_t k_to = dst + 16 * lane, v_at = dst + v_to;
+      const uint32_t k_to = dst + 16 * lane, v_at = dst + v_to, s_to = dst + 2 * kQaCodes + 8 * lane;
       if (whole_tiles && ok_next == 0xffffffffu) {  // 16 rows lie together
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
@@ -240,6 +244,9 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
               "l"(ks), "r"(v_at + 1024 * y), "l"(vs)
               : "memory");
         }
+        const uint64_t at = (uint64_t)(uint32_t)row * scale_bytes;
+        cp_async8(s_to, pools.k_scale + at);
+        cp_async8(s_to + kQaScales, pools.v_scale + at);
       } else {
 #pragma unroll
         for (int i = 0; i < kQaBlock / 8; ++i) {
@@ -252,10 +259,10 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
               "l"(v_from + (uint64_t)(uint32_t)r * code_bytes), "r"(r)
               : "memory");
         }
+        const uint64_t at = (uint64_t)(uint32_t)max(row, 0) * scale_bytes;
+        cp_async8_fill(s_to, pools.k_scale + at, row >= 0);
+        cp_async8_fill(s_to + kQaScales, pools.v_scale + at, row >= 0);
       }
-      const uint64_t at = (uint64_t)(uint32_t)max(row, 0) * scale_bytes;
-      cp_async8_fill(dst + 2 * kQaCodes + 8 * lane, pools.k_scale + at, row >= 0);
-      cp_async8_fill(dst + 2 * kQaCodes + kQaScales + 8 * lane, pools.v_scale + at, row >= 0);
     }
     cp_async_commit();
   };
@@ -381,190 +388,192 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     // group's results so for the tokens that see its row, and a weight of 0 would
     // carry it to the others too: a warp whose sums are not numbers at the part's
     // end takes its blocks again and looks for them.
-    for (bool look = false;; look = true) {
+    auto take = [&](auto look) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      m[nt][0] = m[nt][1] = -3e38f;
-      l[nt][0] = l[nt][1] = 0.f;
+      for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = -3e38f;
+        l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-      for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
-    }
-    for (int u = warps_first<kWarps>(part0, warp); u < seg_end; u += kWarps) {
-      cp_async_wait<kQaStages - 1>();
-      __syncwarp();
-      Entry next;  // of the block that will take this stage
-      const bool any = look_up(next);
-      const int base = (u - item.f0) * kQaBlock;
-      float c[2][NT][4];
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) c[y][nt][0] = c[y][nt][1] = c[y][nt][2] = c[y][nt][3] = 0.f;
-      {
-        const uint32_t kt = k_at + stage, st = ks_at + stage;
-        // rows g8, g8 + 8, g8 + 16 and g8 + 24
-        const uint4 w[4] = {lds128<0>(kt), lds128<8 * kQ4Row>(kt), lds128<16 * kQ4Row>(kt), lds128<24 * kQ4Row>(kt)};
-        const __half2 s[4] = {as_half2(q4_scales(lds16<0>(st))), as_half2(q4_scales(lds16<8 * kQ4Scales>(st))),
-                              as_half2(q4_scales(lds16<16 * kQ4Scales>(st))), as_half2(q4_scales(lds16<24 * kQ4Scales>(st)))};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[4][4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            q4_codes(i == 0 ? w[x].x : (i == 1 ? w[x].y : (i == 2 ? w[x].z : w[x].w)), p[x]);
-            const __half2 f = i < 2 ? __low2half2(s[x]) : __high2half2(s[x]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[x][j] = mul_half2(p[x][j], f);
-          }
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int part = 0; part < kParts; ++part) {
-                uint2 b;
-                if constexpr (kRegs)
-                  b = qr[2 * i + j];
-                else
-                  b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {  // two sums that do not wait for one another
-                  const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
-                  mma_f16(c[y][nt], a, b.x, b.y);
-                }
-              }
-        }
+        for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
       }
-      if (ok != 0xffffffffu || base + kQaBlock > all_see) {  // some rows do not count for some queries
+      for (int u = warps_first<kWarps>(part0, warp); u < seg_end; u += kWarps) {
+        cp_async_wait<kQaStages - 1>();
+        __syncwarp();
+        Entry next;  // of the block that will take this stage
+        const bool any = look_up(next);
+        const int base = (u - item.f0) * kQaBlock;
+        float c[2][NT][4];
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) c[y][nt][0] = c[y][nt][1] = c[y][nt][2] = c[y][nt][3] = 0.f;
+        {
+          const uint32_t kt = k_at + stage, st = ks_at + stage;
+          // rows g8, g8 + 8, g8 + 16 and g8 + 24
+          const uint4 w[4] = {lds128<0>(kt), lds128<8 * kQ4Row>(kt), lds128<16 * kQ4Row>(kt), lds128<24 * kQ4Row>(kt)};
+          const __half2 s[4] = {as_half2(q4_scales(lds16<0>(st))), as_half2(q4_scales(lds16<8 * kQ4Scales>(st))),
+                                as_half2(q4_scales(lds16<16 * kQ4Scales>(st))), as_half2(q4_scales(lds16<24 * kQ4Scales>(st)))};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t p[4][4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              q4_codes(i == 0 ? w[x].x : (i == 1 ? w[x].y : (i == 2 ? w[x].z : w[x].w)), p[x]);
+              const __half2 f = i < 2 ? __low2half2(s[x]) : __high2half2(s[x]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) p[x][j] = mul_half2(p[x][j], f);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) {
+                  uint2 b;
+                  if constexpr (kRegs)
+                    b = qr[2 * i + j];
+                  else
+                    b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
+#pragma unroll
+                  for (int y = 0; y < 2; ++y) {  // two sums that do not wait for one another
+                    const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
+                    mma_f16(c[y][nt], a, b.x, b.y);
+                  }
+                }
+          }
+        }
+        if (ok != 0xffffffffu || base + kQaBlock > all_see) {  // some rows do not count for some queries
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int r = 16 * y + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
+                const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+                // times a factor above zero
+                if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
+              }
+        }
+        // Scores over their references, in powers of two.  A product and a difference,
+        // each rounded: fused, a huge score would exceed itself.
+        float d[2][NT][4];
+        float most = -CUDART_INF_F;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int r = 16 * y + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
-              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
-              // times a factor above zero
-              if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
+              c[y][nt][j] = __fmul_rn(c[y][nt][j], sc[nt][j & 1]);
+              d[y][nt][j] = __fsub_rn(c[y][nt][j], m[nt][j & 1]);
             }
-      }
-      // Scores over their references, in powers of two.  A product and a difference,
-      // each rounded: fused, a huge score would exceed itself.
-      float d[2][NT][4];
-      float most = -CUDART_INF_F;
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            c[y][nt][j] = __fmul_rn(c[y][nt][j], sc[nt][j & 1]);
-            d[y][nt][j] = __fsub_rn(c[y][nt][j], m[nt][j & 1]);
+            most = max3(max3(most, d[y][nt][0], d[y][nt][1]), d[y][nt][2], d[y][nt][3]);
           }
-          most = max3(max3(most, d[y][nt][0], d[y][nt][1]), d[y][nt][2], d[y][nt][3]);
-        }
-      if (__any_sync(0xffffffffu, most > kQaLift + kQaSlack)) {  // rare once the references have settled
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
-#pragma unroll
-            for (int y = 1; y < 2; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
-            mx -= kQaLift;
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            mx = fmaxf(m[nt][e], mx);
-            const float alpha = ex2_approx(m[nt][e] - mx);
-            m[nt][e] = mx;
-            l[nt][e] *= alpha;
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              d[y][nt][e] = __fsub_rn(c[y][nt][e], mx);
-              d[y][nt][2 + e] = __fsub_rn(c[y][nt][2 + e], mx);
-            }
-#pragma unroll
-            for (int mt = 0; mt < 8; ++mt) {
-              o[mt][nt][e] *= alpha;
-              o[mt][nt][2 + e] *= alpha;
-            }
-          }
-      }
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        uint32_t p[kParts][NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float z[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {  // scores become weights
-            z[j] = ex2_approx(d[y][nt][j]);
-            l[nt][j & 1] += z[j];
-          }
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
-            p[0][nt][x] = turn8x8(hi);
-            if (kParts == 2) {
-              const float2 t = unpack_f16(hi);
-              p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
-            }
-          }
-        }
-        const uint32_t vt = v_at + stage + 16 * kQ4Row * y, vo = v_odd + stage + 16 * kQ4Row * y;
-        const uint32_t st = vs_at + stage + 16 * kQ4Scales * y;
-        // scales of rows 2 t4, 2 t4 + 1 of the tile, and of those + 8
-        uint32_t b[2] = {__byte_perm(lds32<0>(st), lds32<kQ4Scales>(st), pick),
-                         __byte_perm(lds32<8 * kQ4Scales>(st), lds32<9 * kQ4Scales>(st), pick)};
-        if (look) {
-          uint32_t which = 0;  // rows of the tile, of the lane's four
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
-              which |= 1u << (2 * t4 + 8 * (i >> 1) + (i & 1));
-              b[i >> 1] &= ~(0xffu << (8 * (i & 1)));
-            }
-          which |= __shfl_xor_sync(0xffffffffu, which, 1);
-          which |= __shfl_xor_sync(0xffffffffu, which, 2);
-          which &= ok >> (16 * y);
+        if (__any_sync(0xffffffffu, most > kQaLift + kQaSlack)) {  // rare once the references have settled
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * y;  // of the tile's rows
-              if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
+              float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
 #pragma unroll
-                for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
+              for (int y = 1; y < 2; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
+              mx -= kQaLift;
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+              mx = fmaxf(m[nt][e], mx);
+              const float alpha = ex2_approx(m[nt][e] - mx);
+              m[nt][e] = mx;
+              l[nt][e] *= alpha;
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                d[y][nt][e] = __fsub_rn(c[y][nt][e], mx);
+                d[y][nt][2 + e] = __fsub_rn(c[y][nt][2 + e], mx);
+              }
+#pragma unroll
+              for (int mt = 0; mt < 8; ++mt) {
+                o[mt][nt][e] *= alpha;
+                o[mt][nt][2 + e] *= alpha;
+              }
             }
         }
-        const __half2 f0 = as_half2(q4_scales(b[0])), f1 = as_half2(q4_scales(b[1]));
-        const uint2 w[4] = {lds64<0>(vt), lds64<0>(vo), lds64<8 * kQ4Row>(vt), lds64<8 * kQ4Row>(vo)};
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          // bytes of two rows' codes of one dimension: even dimensions, odd ones
-          const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
-                         r3 = i ? w[3].y : w[3].x;
-          uint32_t even0[4], odd0[4], even1[4], odd1[4];
-          q4_codes((r0 & 0x0f0f0f0fu) | (r1 * sixteen & 0xf0f0f0f0u), even0);
-          q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
-          q4_codes((r2 & 0x0f0f0f0fu) | (r3 * sixteen & 0xf0f0f0f0u), even1);
-          q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
+        for (int y = 0; y < 2; ++y) {
+          uint32_t p[kParts][NT][2];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t a[4] = {mul_half2(even0[j], f0), mul_half2(odd0[j], f0), mul_half2(even1[j], f1),
-                                   mul_half2(odd1[j], f1)};
+          for (int nt = 0; nt < NT; ++nt) {
+            float z[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {  // scores become weights
+              z[j] = ex2_approx(d[y][nt][j]);
+              l[nt][j & 1] += z[j];
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
+              p[0][nt][x] = turn8x8(hi);
+              if (kParts == 2) {
+                const float2 t = unpack_f16(hi);
+                p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
+              }
+            }
+          }
+          const uint32_t vt = v_at + stage + 16 * kQ4Row * y, vo = v_odd + stage + 16 * kQ4Row * y;
+          const uint32_t st = vs_at + stage + 16 * kQ4Scales * y;
+          // scales of rows 2 t4, 2 t4 + 1 of the tile, and of those + 8
+          uint32_t b[2] = {__byte_perm(lds32<0>(st), lds32<kQ4Scales>(st), pick),
+                           __byte_perm(lds32<8 * kQ4Scales>(st), lds32<9 * kQ4Scales>(st), pick)};
+          if constexpr (decltype(look)::value) {
+            uint32_t which = 0;  // rows of the tile, of the lane's four
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
+                which |= 1u << (2 * t4 + 8 * (i >> 1) + (i & 1));
+                b[i >> 1] &= ~(0xffu << (8 * (i & 1)));
+              }
+            which |= __shfl_xor_sync(0xffffffffu, which, 1);
+            which |= __shfl_xor_sync(0xffffffffu, which, 2);
+            which &= ok >> (16 * y);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+              for (int e = 0; e < 2; ++e) {
+                const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * y;  // of the tile's rows
+                if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
+#pragma unroll
+                  for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
+              }
+          }
+          const __half2 f0 = as_half2(q4_scales(b[0])), f1 = as_half2(q4_scales(b[1]));
+          const uint2 w[4] = {lds64<0>(vt), lds64<0>(vo), lds64<8 * kQ4Row>(vt), lds64<8 * kQ4Row>(vo)};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            // bytes of two rows' codes of one dimension: even dimensions, odd ones
+            const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
+                           r3 = i ? w[3].y : w[3].x;
+            uint32_t even0[4], odd0[4], even1[4], odd1[4];
+            q4_codes((r0 & 0x0f0f0f0fu) | (r1 * sixteen & 0xf0f0f0f0u), even0);
+            q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
+            q4_codes((r2 & 0x0f0f0f0fu) | (r3 * sixteen & 0xf0f0f0f0u), even1);
+            q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t a[4] = {mul_half2(even0[j], f0), mul_half2(odd0[j], f0), mul_half2(even1[j], f1),
+                                     mul_half2(odd1[j], f1)};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+            }
           }
         }
+        __syncwarp();
+        fetch(ring + stage, any, next);
+        stage = kQaStage - stage;
       }
-      __syncwarp();
-      fetch(ring + stage, any, next);
-      stage = kQaStage - stage;
-    }
+    };
+    take(std::false_type());
     float none = 0.f;  // or a NaN, where a sum is one
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt)
@@ -572,12 +581,13 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 4; ++j) none = fmaf(o[mt][nt][j], 0.f, none);
-    if (look || !__any_sync(0xffffffffu, none != 0.f)) break;
-    cp_async_wait<0>();  // no copy is on its way to the stages
-    __syncwarp();
-    start(cur, part0);
-    stage = 0;
-    fill([]() {});
+    if (__any_sync(0xffffffffu, none != 0.f)) {
+      cp_async_wait<0>();  // no copy is on its way to the stages
+      __syncwarp();
+      start(cur, part0);
+      stage = 0;
+      fill([]() {});
+      take(std::true_type());
     }
     // The warps' states of this item, merged in shared memory, eight queries at
     // a time.
@@ -655,6 +665,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     if (seg < rg.b1) __syncthreads();  // the merge buffer (and the queries) are free again
   }
   cp_async_wait<0>();
+  if (bad) record_error(err, kErrInput);
 }
 
 // -------------------------------------------------------------------- launch
