@@ -38,7 +38,7 @@ constexpr float kQaLift = 10.f;       // weights are 2^(x - m), m their referenc
 constexpr float kQaSlack = 4.f;       // how far a score may exceed the reference
 // Warps of a CTA: eight where 128 registers hold a warp's state; and CTAs per SM.
 __host__ __device__ constexpr int qa_warps(int nt) { return 4; }
-__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt <= 2 ? 3 : 2; }
+__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt == 1 ? 3 : 2; }
 // Bytes of shared memory for queries; none where they are in registers.
 __host__ __device__ constexpr int qa_queries(int nt, int parts) { return nt * parts > 1 ? 8 * nt * parts * kD * 2 : 0; }
 __host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
   constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;  // of a query's elements and of a weight
   constexpr int kRows = 8 * NT, kWarps = qa_warps(NT), kThreads = 32 * kWarps;
   constexpr int kPass = qa_pass(NT, kParts);
+  constexpr int kTiles = NT * kParts >= 4 ? 1 : 2;  // of 16 rows, whose scores are formed together
   constexpr bool kRegs = qa_queries(NT, kParts) == 0;  // queries in registers, else in shared memory
   extern __shared__ uint4 pat_smem[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
@@ -402,169 +403,180 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
         Entry next;  // of the block that will take this stage
         const bool any = look_up(next);
         const int base = (u - item.f0) * kQaBlock;
-        float c[2][NT][4];
+#pragma unroll 1
+        for (int y0 = 0; y0 < 2; y0 += kTiles) {
+          float c[kTiles][NT][4];
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) c[y][nt][0] = c[y][nt][1] = c[y][nt][2] = c[y][nt][3] = 0.f;
-        {
-          const uint32_t kt = k_at + stage, st = ks_at + stage;
-          // rows g8, g8 + 8, g8 + 16 and g8 + 24
-          const uint4 w[4] = {lds128<0>(kt), lds128<8 * kQ4Row>(kt), lds128<16 * kQ4Row>(kt), lds128<24 * kQ4Row>(kt)};
-          const __half2 s[4] = {as_half2(q4_scales(lds16<0>(st))), as_half2(q4_scales(lds16<8 * kQ4Scales>(st))),
-                                as_half2(q4_scales(lds16<16 * kQ4Scales>(st))), as_half2(q4_scales(lds16<24 * kQ4Scales>(st)))};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t p[4][4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              q4_codes(i == 0 ? w[x].x : (i == 1 ? w[x].y : (i == 2 ? w[x].z : w[x].w)), p[x]);
-              const __half2 f = i < 2 ? __low2half2(s[x]) : __high2half2(s[x]);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) p[x][j] = mul_half2(p[x][j], f);
+            for (int nt = 0; nt < NT; ++nt) c[y][nt][0] = c[y][nt][1] = c[y][nt][2] = c[y][nt][3] = 0.f;
+          {
+            const uint32_t kt = k_at + stage + 16 * kQ4Row * y0, st = ks_at + stage + 16 * kQ4Scales * y0;
+            uint4 w[2 * kTiles];      // rows g8, g8 + 8, ...
+            __half2 s[2 * kTiles];
+            w[0] = lds128<0>(kt);
+            w[1] = lds128<8 * kQ4Row>(kt);
+            s[0] = as_half2(q4_scales(lds16<0>(st)));
+            s[1] = as_half2(q4_scales(lds16<8 * kQ4Scales>(st)));
+            if constexpr (kTiles == 2) {
+              w[2] = lds128<16 * kQ4Row>(kt);
+              w[3] = lds128<24 * kQ4Row>(kt);
+              s[2] = as_half2(q4_scales(lds16<16 * kQ4Scales>(st)));
+              s[3] = as_half2(q4_scales(lds16<24 * kQ4Scales>(st)));
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int i = 0; i < 4; ++i) {
+              uint32_t p[2 * kTiles][4];
+#pragma unroll
+              for (int x = 0; x < 2 * kTiles; ++x) {
+                q4_codes(i == 0 ? w[x].x : (i == 1 ? w[x].y : (i == 2 ? w[x].z : w[x].w)), p[x]);
+                const __half2 f = i < 2 ? __low2half2(s[x]) : __high2half2(s[x]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[x][j] = mul_half2(p[x][j], f);
+              }
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int part = 0; part < kParts; ++part) {
+                    uint2 b;
+                    if constexpr (kRegs)
+                      b = qr[2 * i + j];
+                    else
+                      b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
+#pragma unroll
+                    for (int y = 0; y < kTiles; ++y) {  // two sums that do not wait for one another
+                      const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
+                      mma_f16(c[y][nt], a, b.x, b.y);
+                    }
+                  }
+            }
+          }
+          if (ok != 0xffffffffu || base + kQaBlock > all_see) {  // some rows do not count for some queries
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int part = 0; part < kParts; ++part) {
-                  uint2 b;
-                  if constexpr (kRegs)
-                    b = qr[2 * i + j];
-                  else
-                    b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
-#pragma unroll
-                  for (int y = 0; y < 2; ++y) {  // two sums that do not wait for one another
-                    const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
-                    mma_f16(c[y][nt], a, b.x, b.y);
-                  }
+                for (int j = 0; j < 4; ++j) {
+                  const int r = 16 * (y0 + y) + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
+                  const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
+                  // times a factor above zero
+                  if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
                 }
           }
-        }
-        if (ok != 0xffffffffu || base + kQaBlock > all_see) {  // some rows do not count for some queries
+          // Scores over their references, in powers of two.  A product and a difference,
+          // each rounded: fused, a huge score would exceed itself.
+          float d[kTiles][NT][4];
+          float most = -CUDART_INF_F;
 #pragma unroll
-          for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const int r = 16 * y + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
-                const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
-                // times a factor above zero
-                if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
+                c[y][nt][j] = __fmul_rn(c[y][nt][j], sc[nt][j & 1]);
+                d[y][nt][j] = __fsub_rn(c[y][nt][j], m[nt][j & 1]);
               }
-        }
-        // Scores over their references, in powers of two.  A product and a difference,
-        // each rounded: fused, a huge score would exceed itself.
-        float d[2][NT][4];
-        float most = -CUDART_INF_F;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              c[y][nt][j] = __fmul_rn(c[y][nt][j], sc[nt][j & 1]);
-              d[y][nt][j] = __fsub_rn(c[y][nt][j], m[nt][j & 1]);
+              most = max3(max3(most, d[y][nt][0], d[y][nt][1]), d[y][nt][2], d[y][nt][3]);
             }
-            most = max3(max3(most, d[y][nt][0], d[y][nt][1]), d[y][nt][2], d[y][nt][3]);
-          }
-        if (__any_sync(0xffffffffu, most > kQaLift + kQaSlack)) {  // rare once the references have settled
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
-#pragma unroll
-              for (int y = 1; y < 2; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
-              mx -= kQaLift;
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-              mx = fmaxf(m[nt][e], mx);
-              const float alpha = ex2_approx(m[nt][e] - mx);
-              m[nt][e] = mx;
-              l[nt][e] *= alpha;
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                d[y][nt][e] = __fsub_rn(c[y][nt][e], mx);
-                d[y][nt][2 + e] = __fsub_rn(c[y][nt][2 + e], mx);
-              }
-#pragma unroll
-              for (int mt = 0; mt < 8; ++mt) {
-                o[mt][nt][e] *= alpha;
-                o[mt][nt][2 + e] *= alpha;
-              }
-            }
-        }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          uint32_t p[kParts][NT][2];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float z[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {  // scores become weights
-              z[j] = ex2_approx(d[y][nt][j]);
-              l[nt][j & 1] += z[j];
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
-              p[0][nt][x] = turn8x8(hi);
-              if (kParts == 2) {
-                const float2 t = unpack_f16(hi);
-                p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
-              }
-            }
-          }
-          const uint32_t vt = v_at + stage + 16 * kQ4Row * y, vo = v_odd + stage + 16 * kQ4Row * y;
-          const uint32_t st = vs_at + stage + 16 * kQ4Scales * y;
-          // scales of rows 2 t4, 2 t4 + 1 of the tile, and of those + 8
-          uint32_t b[2] = {__byte_perm(lds32<0>(st), lds32<kQ4Scales>(st), pick),
-                           __byte_perm(lds32<8 * kQ4Scales>(st), lds32<9 * kQ4Scales>(st), pick)};
-          if constexpr (decltype(look)::value) {
-            uint32_t which = 0;  // rows of the tile, of the lane's four
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
-                which |= 1u << (2 * t4 + 8 * (i >> 1) + (i & 1));
-                b[i >> 1] &= ~(0xffu << (8 * (i & 1)));
-              }
-            which |= __shfl_xor_sync(0xffffffffu, which, 1);
-            which |= __shfl_xor_sync(0xffffffffu, which, 2);
-            which &= ok >> (16 * y);
+          if (__any_sync(0xffffffffu, most > kQaLift + kQaSlack)) {  // rare once the references have settled
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * y;  // of the tile's rows
-                if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
+                float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
 #pragma unroll
-                  for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
+                for (int y = 1; y < kTiles; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
+                mx -= kQaLift;
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                mx = fmaxf(m[nt][e], mx);
+                const float alpha = ex2_approx(m[nt][e] - mx);
+                m[nt][e] = mx;
+                l[nt][e] *= alpha;
+#pragma unroll
+                for (int y = 0; y < kTiles; ++y) {
+                  d[y][nt][e] = __fsub_rn(c[y][nt][e], mx);
+                  d[y][nt][2 + e] = __fsub_rn(c[y][nt][2 + e], mx);
+                }
+#pragma unroll
+                for (int mt = 0; mt < 8; ++mt) {
+                  o[mt][nt][e] *= alpha;
+                  o[mt][nt][2 + e] *= alpha;
+                }
               }
           }
-          const __half2 f0 = as_half2(q4_scales(b[0])), f1 = as_half2(q4_scales(b[1]));
-          const uint2 w[4] = {lds64<0>(vt), lds64<0>(vo), lds64<8 * kQ4Row>(vt), lds64<8 * kQ4Row>(vo)};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            // bytes of two rows' codes of one dimension: even dimensions, odd ones
-            const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
-                           r3 = i ? w[3].y : w[3].x;
-            uint32_t even0[4], odd0[4], even1[4], odd1[4];
-            q4_codes((r0 & 0x0f0f0f0fu) | (r1 * sixteen & 0xf0f0f0f0u), even0);
-            q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
-            q4_codes((r2 & 0x0f0f0f0fu) | (r3 * sixteen & 0xf0f0f0f0u), even1);
-            q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
+          for (int y = 0; y < kTiles; ++y) {
+            uint32_t p[kParts][NT][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t a[4] = {mul_half2(even0[j], f0), mul_half2(odd0[j], f0), mul_half2(even1[j], f1),
-                                     mul_half2(odd1[j], f1)};
+            for (int nt = 0; nt < NT; ++nt) {
+              float z[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {  // scores become weights
+                z[j] = ex2_approx(d[y][nt][j]);
+                l[nt][j & 1] += z[j];
+              }
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
+                p[0][nt][x] = turn8x8(hi);
+                if (kParts == 2) {
+                  const float2 t = unpack_f16(hi);
+                  p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
+                }
+              }
+            }
+            const uint32_t vt = v_at + stage + 16 * kQ4Row * (y0 + y), vo = v_odd + stage + 16 * kQ4Row * (y0 + y);
+            const uint32_t st = vs_at + stage + 16 * kQ4Scales * (y0 + y);
+            // scales of rows 2 t4, 2 t4 + 1 of the tile, and of those + 8
+            uint32_t b[2] = {__byte_perm(lds32<0>(st), lds32<kQ4Scales>(st), pick),
+                             __byte_perm(lds32<8 * kQ4Scales>(st), lds32<9 * kQ4Scales>(st), pick)};
+            if constexpr (decltype(look)::value) {
+              uint32_t which = 0;  // rows of the tile, of the lane's four
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if ((b[i >> 1] >> (8 * (i & 1)) & 0x7fu) == kQ4NaN) {
+                  which |= 1u << (2 * t4 + 8 * (i >> 1) + (i & 1));
+                  b[i >> 1] &= ~(0xffu << (8 * (i & 1)));
+                }
+              which |= __shfl_xor_sync(0xffffffffu, which, 1);
+              which |= __shfl_xor_sync(0xffffffffu, which, 2);
+              which &= ok >> (16 * (y0 + y));
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+                for (int e = 0; e < 2; ++e) {
+                  const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * (y0 + y);  // of the tile's rows
+                  if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
+#pragma unroll
+                    for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
+                }
+            }
+            const __half2 f0 = as_half2(q4_scales(b[0])), f1 = as_half2(q4_scales(b[1]));
+            const uint2 w[4] = {lds64<0>(vt), lds64<0>(vo), lds64<8 * kQ4Row>(vt), lds64<8 * kQ4Row>(vo)};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              // bytes of two rows' codes of one dimension: even dimensions, odd ones
+              const uint32_t r0 = i ? w[0].y : w[0].x, r1 = i ? w[1].y : w[1].x, r2 = i ? w[2].y : w[2].x,
+                             r3 = i ? w[3].y : w[3].x;
+              uint32_t even0[4], odd0[4], even1[4], odd1[4];
+              q4_codes((r0 & 0x0f0f0f0fu) | (r1 * sixteen & 0xf0f0f0f0u), even0);
+              q4_codes((r0 >> 4 & 0x0f0f0f0fu) | (r1 & 0xf0f0f0f0u), odd0);
+              q4_codes((r2 & 0x0f0f0f0fu) | (r3 * sixteen & 0xf0f0f0f0u), even1);
+              q4_codes((r2 >> 4 & 0x0f0f0f0fu) | (r3 & 0xf0f0f0f0u), odd1);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t a[4] = {mul_half2(even0[j], f0), mul_half2(odd0[j], f0), mul_half2(even1[j], f1),
+                                       mul_half2(odd1[j], f1)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+              }
             }
           }
         }
