@@ -151,7 +151,8 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
       const Q4Scale sa(top_a, by_six, f), sb(top_b, by_six, f);
       if (live && !is_q && at.page >= 0) {
         const size_t row = q4_row(pg, at.page, at.row, h, x.hkv);
-        uint8_t *codes = (is_v ? q4.v : q4.k) + row * kQ4Row, *scales = (is_v ? q4.v_scale : q4.k_scale) + row * kQ4Scales;
+        uint8_t* codes = (is_v ? q4.v : q4.k) + row * kQ4Row;
+        uint8_t* scales = (is_v ? q4.v_scale : q4.k_scale) + row * kQ4Scales;
         *reinterpret_cast<uint32_t*>(codes + off0 / 2) = q4_word(a, sa);
         *reinterpret_cast<uint32_t*>(codes + off1 / 2) = q4_word(b, sb);
         if (IL || !(c & 1)) scales[off0 / kQ4Group] = (uint8_t)sa.byte;

@@ -58,7 +58,8 @@ struct Place {
 };
 __device__ __forceinline__ Place page_place(const PageView& pg, int s, int r) {
   if (r < 0 || r >= pg.max_pages * pg.page_rows) return {-1, 0};
-  const int i = pg.page_shift >= 0 ? r >> pg.page_shift : r / pg.page_rows, page = pg.table[(size_t)s * pg.max_pages + i];
+  const int i = pg.page_shift >= 0 ? r >> pg.page_shift : r / pg.page_rows;
+  const int page = pg.table[(size_t)s * pg.max_pages + i];
   return {page >= 0 && page < pg.n_pages ? page : -1, r - i * pg.page_rows};
 }
 // Slot (page * page_rows + row of the page) of row r of sequence s, or -1.

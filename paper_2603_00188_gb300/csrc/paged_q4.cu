@@ -68,7 +68,8 @@ __global__ void __launch_bounds__(256) k_gather_q4(const __grid_constant__ Q4Lay
     float y[2][8];
     x[i].x[0].get(y[0]);
     x[i].x[1].get(y[1]);
-    *reinterpret_cast<uint2*>((i ? to.v : to.k) + row * kQ4Row + 8 * c) = make_uint2(q4_word(y[0], s), q4_word(y[1], s));
+    const uint2 w = make_uint2(q4_word(y[0], s), q4_word(y[1], s));
+    *reinterpret_cast<uint2*>((i ? to.v : to.k) + row * kQ4Row + 8 * c) = w;
     (i ? to.v_scale : to.k_scale)[row * kQ4Scales + c] = (uint8_t)s.byte;
   }
 }

@@ -36,22 +36,25 @@ constexpr int kQaStage = 2 * (kQaCodes + kQaScales);
 constexpr int kQaPitch = kD + 4;      // floats from row to row of the merge buffer
 constexpr float kQaLift = 10.f;       // weights are 2^(x - m), m their reference less this
 constexpr float kQaSlack = 4.f;       // how far a score may exceed the reference
-// Warps of a CTA: eight where 128 registers hold a warp's state; and CTAs per SM.
-__host__ __device__ constexpr int qa_warps(int nt) { return 4; }
-__host__ __device__ constexpr int qa_ctas(int nt, int parts) { return nt == 1 ? 3 : 2; }
+constexpr int kQaWarps = 4, kQaThreads = 32 * kQaWarps;
+// CTAs per SM.  12 warps of one group of queries keep their state in 168
+// registers (16 in 128: 61 us where 12 take 56), eight of more in 255.
+__host__ __device__ constexpr int qa_ctas(int nt) { return nt == 1 ? 3 : 2; }
 // Bytes of shared memory for queries; none where they are in registers.
 __host__ __device__ constexpr int qa_queries(int nt, int parts) { return nt * parts > 1 ? 8 * nt * parts * kD * 2 : 0; }
-__host__ __device__ constexpr int qa_ring(int nt) { return qa_warps(nt) * kQaStages * kQaStage; }
-// Groups of queries whose parts the warps merge at a time: all, where that leaves qa_ctas to an SM.
-__host__ __device__ constexpr int qa_pass(int nt, int parts) { return nt == 2 && parts == 2 ? 1 : nt; }
+constexpr int kQaRing = kQaWarps * kQaStages * kQaStage;
+// Once an item has ended: 1 / sum of each query, and the warps' factors; the split's scratch before.
 __host__ __device__ constexpr int qa_factors(int nt) {
-  return 8 * nt * 4 * (1 + qa_warps(nt)) > (int)sizeof(RangeScratch<256>) ? 8 * nt * 4 * (1 + qa_warps(nt))
-                                                                          : (int)sizeof(RangeScratch<256>);
+  return 8 * nt * 4 * (1 + kQaWarps) > (int)sizeof(RangeScratch<kQaThreads>) ? 8 * nt * 4 * (1 + kQaWarps)
+                                                                            : (int)sizeof(RangeScratch<kQaThreads>);
 }
 __host__ __device__ constexpr int qa_smem(int nt, int parts) {
-  const int need = qa_ring(nt) + qa_queries(nt, parts) + qa_warps(nt) * 8 * (qa_pass(nt, parts) * kQaPitch * 4 + nt * 8) + qa_factors(nt) + 8 * nt * 4;
-  // no more CTAs to an SM than dealt to it, however soon another launch's end
-  const int alone = (228 * 1024 / (qa_ctas(nt, parts) + 1) - 1024) / 128 * 128 + 128;
+  const int merge = kQaWarps * 8 * nt * (kQaPitch * 4 + 8);  // the warps' sums, maxima and weights
+  const int need = kQaRing + qa_queries(nt, parts) + merge + qa_factors(nt) + 8 * nt * 4;
+  // No more CTAs share an SM than are dealt to it: otherwise those of a launch
+  // that starts while another ends gather on the SMs that are free first (16
+  // sessions of 25,000 rows: up to 75 us in place of 53).
+  const int alone = (228 * 1024 / (qa_ctas(nt) + 1) - 1024) / 128 * 128 + 128;
   return need > alone ? need : alone;
 }
 
@@ -70,7 +73,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(as_half2(x)); }
 // The 8 x 8 matrix of 16-bit values held two to a lane, transposed.
 __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   uint32_t y;
@@ -137,24 +140,22 @@ __device__ __forceinline__ uint32_t qa_value_off(int r, int c) {
 
 // NT: groups of eight queries that share one read of the cache.
 template <typename T, int NT>
-__global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T, float>::value ? 2 : 1))
+__global__ void __launch_bounds__(kQaThreads, qa_ctas(NT))
     k_paged_q4(const __grid_constant__ PageView pg, const __grid_constant__ Q4View pools, const T* q, T* out, int n,
                int hq, int hkv, int mode, int split, int chunks, int chunk_rows, PartDesc* desc, float2* part_ml,
                float* part_o, uint32_t* err) {
   constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;  // of a query's elements and of a weight
-  constexpr int kRows = 8 * NT, kWarps = qa_warps(NT), kThreads = 32 * kWarps;
-  constexpr int kPass = qa_pass(NT, kParts);
+  constexpr int kRows = 8 * NT;
   constexpr int kTiles = NT * kParts >= 4 ? 1 : 2;  // of 16 rows, whose scores are formed together
   constexpr bool kRegs = qa_queries(NT, kParts) == 0;  // queries in registers, else in shared memory
   extern __shared__ uint4 pat_smem[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(pat_smem);
-  uint2* qs = reinterpret_cast<uint2*>(sm + qa_ring(NT));  // [part][NT][step][lane]
-  float* wo = reinterpret_cast<float*>(sm + qa_ring(NT) + qa_queries(NT, kParts));
-  float2* wml = reinterpret_cast<float2*>(wo + kWarps * 8 * kPass * kQaPitch);
-  RangeScratch<kThreads>* scratch = reinterpret_cast<RangeScratch<kThreads>*>(wml + kWarps * kRows);
-  // once an item has ended (the range was found long before): 1 / sum of each
-  // query, and the warps' factors
-  float* q_back = reinterpret_cast<float*>(sm + qa_smem(NT, kParts) - kRows * 4);  // what each query's sums are multiplied by
+  uint2* qs = reinterpret_cast<uint2*>(sm + kQaRing);  // [part][NT][step][lane]
+  float* wo = reinterpret_cast<float*>(sm + kQaRing + qa_queries(NT, kParts));
+  float2* wml = reinterpret_cast<float2*>(wo + kQaWarps * kRows * kQaPitch);
+  RangeScratch<kQaThreads>* scratch = reinterpret_cast<RangeScratch<kQaThreads>*>(wml + kQaWarps * kRows);
+  // [kRows]: what each query's sums are multiplied by
+  float* q_back = reinterpret_cast<float*>(sm + qa_smem(NT, kParts) - kRows * 4);
   float* inv = reinterpret_cast<float*>(scratch);  // [kRows]
   float* factor = inv + kRows;                     // [warps][kRows]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, t4 = lane & 3;
@@ -163,8 +164,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
   const uint32_t ring = smem_u32(sm) + warp * kQaStages * kQaStage;
   pdl_trigger();
   pdl_wait();
-  const Range rg = find_range<kThreads>(pg, G, chunk_rows, hkv, kWarps, split, err, scratch);
-  const bool describes = tid == kThreads - 32;  // the thread that writes the CTA's descriptor
+  const Range rg = find_range<kQaThreads>(pg, G, chunk_rows, hkv, kQaWarps, split, err, scratch);
+  const bool describes = tid == kQaThreads - 32;  // the thread that writes the CTA's descriptor
   if (mode == kDescByCta && describes) desc[cta].item = -1;
   if (cta >= rg.ctas) return;
 
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
       if (find.i1 >= rg.b1) return false;
       advance(find.at, find.i1, pg, G, chunk_rows, hkv);
       const Item x = item_at(find.at, find.i1);
-      find.u = warps_first<kWarps>(max(find.i1, x.f0), warp);
+      find.u = warps_first<kQaWarps>(max(find.i1, x.f0), warp);
       find.f0 = x.f0;
       find.i1 = x.i1;
       find.entries = pg.table + (size_t)find.at.s * pg.max_pages;
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     }
     if (find.u >= rg.b1) return false;
     const int j = (find.u - find.f0) * kQaBlock + lane;
-    find.u += kWarps;
+    find.u += kQaWarps;
     const int i = pg.page_shift >= 0 ? j >> pg.page_shift : j / pg.page_rows;
     e.row = find.head_row + j - i * pg.page_rows;
     if (j < find.at.w.len)
@@ -222,7 +223,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
   // Known to be powers of two, these become shifts and additions on the pipe that
   // the conversions fill; as numbers they are multiplications on another.
   uint32_t code_bytes, scale_bytes, sixteen;
-  asm volatile("mov.u32 %0, 64;\n\tmov.u32 %1, 8;\n\tmov.u32 %2, 16;" : "=r"(code_bytes), "=r"(scale_bytes), "=r"(sixteen));
+  asm volatile("mov.u32 %0, 64;\n\tmov.u32 %1, 8;\n\tmov.u32 %2, 16;"
+               : "=r"(code_bytes), "=r"(scale_bytes), "=r"(sixteen));
   auto fetch = [&](uint32_t dst, bool any, const Entry& e) {
     ok = ok_next;
     ok_next = 0;
@@ -292,8 +294,9 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
       const float4 y = raw[ks].get();
-      top = max(max(top, __float_as_uint(y.x) & 0x7fffffffu), max(__float_as_uint(y.y) & 0x7fffffffu, __float_as_uint(y.z) & 0x7fffffffu));
-      top = max(top, __float_as_uint(y.w) & 0x7fffffffu);
+      const float x[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -354,7 +357,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     if (cur.w.blocks == 0 || part0 >= seg_end) {
       if (cur.w.blocks == 0 && seg == item.i0) {  // an empty session, begun in this range
         if (mode == kDescByItem && describes) desc[(cur.s * hkv + h) * chunks + chunk].item = -1;
-        zero_rows<kThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
+        zero_rows<kQaThreads>(out, cur.w.first, n, hq, h * G, G, row0, rows);
       }
       seg = seg_end;
       continue;
@@ -397,7 +400,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) o[mt][nt][0] = o[mt][nt][1] = o[mt][nt][2] = o[mt][nt][3] = 0.f;
       }
-      for (int u = warps_first<kWarps>(part0, warp); u < seg_end; u += kWarps) {
+      for (int u = warps_first<kQaWarps>(part0, warp); u < seg_end; u += kQaWarps) {
         cp_async_wait<kQaStages - 1>();
         __syncwarp();
         Entry next;  // of the block that will take this stage
@@ -447,7 +450,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
                       b = qs[((part * NT + nt) * 8 + 2 * i + j) * 32 + lane];
 #pragma unroll
                     for (int y = 0; y < kTiles; ++y) {  // two sums that do not wait for one another
-                      const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1], p[2 * y + 1][2 * j + 1]};
+                      const uint32_t a[4] = {p[2 * y][2 * j], p[2 * y + 1][2 * j], p[2 * y][2 * j + 1],
+                                             p[2 * y + 1][2 * j + 1]};
                       mma_f16(c[y][nt], a, b.x, b.y);
                     }
                   }
@@ -550,7 +554,9 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                  const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base - 16 * (y0 + y);  // of the tile's rows
+                  // of the tile's rows
+                  const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + 8 * nt + 2 * t4 + e) / G) - base -
+                                   16 * (y0 + y);
                   if (which & (sees >= 16 ? 0xffffu : (1u << max(sees, 0)) - 1u))
 #pragma unroll
                     for (int mt = 0; mt < 8; ++mt) o[mt][nt][e] = o[mt][nt][2 + e] = CUDART_NAN_F;
@@ -575,7 +581,8 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                  for (int part = 0; part < kParts; ++part) mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
+                  for (int part = 0; part < kParts; ++part)
+                    mma_f16(o[4 * i + j][nt], a, p[part][nt][0], p[part][nt][1]);
               }
             }
           }
@@ -601,8 +608,7 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
       fill([]() {});
       take(std::true_type());
     }
-    // The warps' states of this item, merged in shared memory, eight queries at
-    // a time.
+    // The warps' states of this item, merged in shared memory.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -618,16 +624,16 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     const float vf = pools.v_factor ? pools.v_factor[h] : 1.f;
     // a thread for each warp's query: its factor, and, from the first warp's
     // thread, the query's maximum and sum over the warps
-    for (int e = tid; e < kWarps * kRows; e += kThreads) {
+    for (int e = tid; e < kQaWarps * kRows; e += kQaThreads) {
       const int x = e % kRows;
       float M = -CUDART_INF_F;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
+      for (int w = 0; w < kQaWarps; ++w) M = fmaxf(M, wml[w * kRows + x].x);
       factor[e] = pat_weight(wml[e].x, M) * vf;
       if (e < rows) {
         float L = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) L = fmaf(wml[w * kRows + x].y, pat_weight(wml[w * kRows + x].x, M), L);
+        for (int w = 0; w < kQaWarps; ++w) L = fmaf(wml[w * kRows + x].y, pat_weight(wml[w * kRows + x].x, M), L);
         if (whole)
           inv[x] = L == 0.f ? 0.f : 1.f / L;
         else
@@ -636,41 +642,36 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
     }
     __syncthreads();
 #pragma unroll
-    for (int n0 = 0; n0 < NT; n0 += kPass) {
-      if (n0 > 0) __syncthreads();  // the buffer is free again
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < kPass; ++i)
+      for (int e = 0; e < 2; ++e) {
+        const int x = 8 * nt + 2 * t4 + e;
+        const float a = factor[warp * kRows + x];
+        float* w = wo + (warp * kRows + x) * kQaPitch + 16 * g8;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int x = 8 * i + 2 * t4 + e;
-          const float a = factor[warp * kRows + 8 * n0 + x];
-          float* w = wo + (warp * 8 * kPass + x) * kQaPitch + 16 * g8;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            store4(w + 4 * k, o[2 * k][n0 + i][e] * a, o[2 * k][n0 + i][2 + e] * a, o[2 * k + 1][n0 + i][e] * a,
-                   o[2 * k + 1][n0 + i][2 + e] * a);
-        }
-      __syncthreads();
+        for (int k = 0; k < 4; ++k)
+          store4(w + 4 * k, o[2 * k][nt][e] * a, o[2 * k][nt][2 + e] * a, o[2 * k + 1][nt][e] * a,
+                 o[2 * k + 1][nt][2 + e] * a);
+      }
+    __syncthreads();
 #pragma unroll 2
-      for (int y = warp; y < min(8 * kPass, rows - 8 * n0); y += kWarps) {
-        const int x = 8 * n0 + y;
-        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x = warp; x < rows; x += kQaWarps) {
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float4 z = *reinterpret_cast<const float4*>(wo + (w * 8 * kPass + y) * kQaPitch + 4 * lane);
-          O.x += z.x;
-          O.y += z.y;
-          O.z += z.z;
-          O.w += z.w;
-        }
-        if (whole) {
-          const int r = row0 + x, t = cur.w.first + r / G;
-          const float f = inv[x];
-          if (t >= 0 && t < n)
-            store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * f, O.y * f, O.z * f, O.w * f);
-        } else {
-          store4(part_o + ((size_t)part * kRows + x) * kD + 4 * lane, O.x, O.y, O.z, O.w);
-        }
+      for (int w = 0; w < kQaWarps; ++w) {
+        const float4 z = *reinterpret_cast<const float4*>(wo + (w * kRows + x) * kQaPitch + 4 * lane);
+        O.x += z.x;
+        O.y += z.y;
+        O.z += z.z;
+        O.w += z.w;
+      }
+      if (whole) {
+        const int r = row0 + x, t = cur.w.first + r / G;
+        const float f = inv[x];
+        if (t >= 0 && t < n)
+          store4(out + ((size_t)t * hq + h * G + r % G) * kD + 4 * lane, O.x * f, O.y * f, O.z * f, O.w * f);
+      } else {
+        store4(part_o + ((size_t)part * kRows + x) * kD + 4 * lane, O.x, O.y, O.z, O.w);
       }
     }
     seg = seg_end;
@@ -681,10 +682,10 @@ __global__ void __launch_bounds__(32 * qa_warps(NT), qa_ctas(NT, std::is_same<T,
 }
 
 // -------------------------------------------------------------------- launch
-static int q4_ctas(DType dt, int part_rows) {
+static int q4_ctas(int part_rows) {
   int dev = 0, sms = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  const int ctas = qa_ctas(part_rows / 8, dt == kF32 ? 2 : 1) * sms;
+  const int ctas = qa_ctas(part_rows / 8) * sms;
   return ctas < kPatMaxCtas ? ctas : kPatMaxCtas;
 }
 
@@ -700,7 +701,7 @@ static int q4_part_rows(DType dt, const PageView& pages, int G) {
 constexpr size_t kQaHead = 256, kQaDescs = kPatMaxCtas * sizeof(PartDesc);
 size_t paged_q4_workspace_bytes(DType dt, const PageView& pages, int hq, int hkv) {
   const int rows = q4_part_rows(dt, pages, hq / hkv);
-  return kQaHead + kQaDescs + (size_t)2 * q4_ctas(dt, rows) * rows * (sizeof(float2) + kD * sizeof(float));
+  return kQaHead + kQaDescs + (size_t)2 * q4_ctas(rows) * rows * (sizeof(float2) + kD * sizeof(float));
 }
 
 cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void* q, const Q4View& pools, void* out,
@@ -708,7 +709,7 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   PageView pages = view;
   uint32_t* err = static_cast<uint32_t*>(ws);
   const int rows = pages.w * (hq / hkv), part_rows = q4_part_rows(dt, pages, hq / hkv), most = q4_most_rows(dt);
-  const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas(dt, part_rows);
+  const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas(part_rows);
   const long long items = (long long)pages.n_seqs * hkv * chunks;
   pages.item_units = 12;
   pages.block_shift = kQaBlockShift;
@@ -725,13 +726,13 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   auto run = [&](auto zero, auto width) {
     typedef decltype(zero) T;
     constexpr int NT = decltype(width)::value, kParts = std::is_same<T, float>::value ? 2 : 1;
-    static_assert(fits_sm(qa_smem(NT, kParts), qa_ctas(NT, kParts)), "qa_ctas per SM");
+    static_assert(fits_sm(qa_smem(NT, kParts), qa_ctas(NT)), "qa_ctas per SM");
     TimingScope ts("paged_attention_q4", st);
     auto kern = k_paged_q4<T, NT>;
     const int smem = qa_smem(NT, kParts);
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return;
-    e = launch_after(kern, dim3(ctas), 32 * qa_warps(NT), smem, st, pages, pools, static_cast<const T*>(q),
+    e = launch_after(kern, dim3(ctas), kQaThreads, smem, st, pages, pools, static_cast<const T*>(q),
                      static_cast<T*>(out), n, hq, hkv, mode, split, chunks, chunk_rows, desc, part_ml, part_o, err);
   };
   if (dt == kF32)

@@ -63,7 +63,8 @@ struct Q4Recip {
 struct Q4Scale {
   uint32_t byte;
   Q4Recip by;  // of scale * factor
-  __device__ __forceinline__ Q4Scale(uint32_t top, const Q4Recip& by_six, float factor) : by(init(top, by_six, factor)) {}
+  __device__ __forceinline__ Q4Scale(uint32_t top, const Q4Recip& by_six, float factor)
+      : by(init(top, by_six, factor)) {}
 
  private:
   __device__ __forceinline__ float init(uint32_t top, const Q4Recip& by_six, float factor) {
