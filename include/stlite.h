@@ -571,7 +571,7 @@ typedef struct {
   void* v;               /* 16-byte aligned */
   void* k_scale;         /* 8-byte aligned */
   void* v_scale;         /* 8-byte aligned */
-  const float* k_factor; /* device [Hkv], each finite and > 0, or NULL: 1 */
+  const float* k_factor; /* device [Hkv], each within 2^-60 .. 2^60, or NULL: 1 */
   const float* v_factor; /* the same for values */
 } stlite_q4_pools;
 
@@ -601,7 +601,8 @@ STLITE_API stlite_status stlite_paged_q4_workspace_size(const stlite_shape* shap
  * stlite_compact_paged_q4: k and v are the layer's cache [N][Hkv][d] (v may be
  *   page-locked host memory), idx its indices [Hkv][budget] (read; 4-byte
  *   aligned); q is not used.
- * stlite_compress_layers_paged_q4: as for stlite_layer_io, idx is written.
+ * stlite_compress_layers_paged_q4: as for stlite_layer_io, idx is written (16-
+ *   byte aligned).
  * stlite_paged_fetch_q4: k and v are written; q and idx are not used. */
 typedef struct {
   const void* q;

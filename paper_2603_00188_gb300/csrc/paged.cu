@@ -31,6 +31,10 @@ namespace stl {
 // of a plain copy's rate; groups of a loop without loading ahead 27.1, eight
 // groups ahead 22.8, a CTA to 32 heads with shared sines 29.8), 8,616 tokens
 // with 4 value heads into pages 26.0 (eight groups 34.0, four 27.2, two 28.0).
+//
+// Into 4-bit pages keys and values go as they are here, in fp32, before they
+// would be rounded: two neighbouring lanes share a group of 16 elements (one
+// lane has it where pairs are interleaved).
 constexpr int kRotThreads = 128, kRotWarps = kRotThreads / 32;
 constexpr int kRotHeads = 4;   // heads of a group
 
