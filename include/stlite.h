@@ -559,7 +559,7 @@ STLITE_API stlite_status stlite_compress_layers_paged(const stlite_shape* shape,
  *     element = code * scale * factor.
  * Rows are put in so: top = the largest magnitude of the group / (6 factor),
  * scale = top within 2^-9 .. 448, rounded to e4m3, code = element / (scale *
- * factor), rounded to e2m1 (each to nearest, ties to even, in fp32).  So zeros
+ * factor), rounded to e2m1 (each to nearest, ties to even).  So zeros
  * stay zeros, magnitudes beyond 2688 factors become that, and groups whose
  * largest is below 0.012 factors lose precision: a factor near the head's usual
  * magnitude keeps them within.  A group that holds an infinity or a NaN gets a
@@ -575,9 +575,10 @@ typedef struct {
   const float* v_factor; /* the same for values */
 } stlite_q4_pools;
 
-/* stlite_paged_append into 4-bit pages: keys are put in as they leave the
- * rotation, in fp32, values as they are; q_out as there.  Everything else as
- * for stlite_paged_append. */
+/* stlite_paged_append into 4-bit pages: values are put in as they are, keys with
+ * the codes and scales of their rotation in 64 bits (its inputs' bits, angles to
+ * 2^-64 of a turn); q_out as there.  Everything else as for
+ * stlite_paged_append. */
 STLITE_API stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope,
                                                 const stlite_tokens* x, const stlite_pages* pages, void* q_out,
                                                 const stlite_q4_pools* pools, void* stream);

@@ -1,11 +1,8 @@
 // Paged caches: new tokens' heads normed, rotated and written (packed, or keys
-// and values into pages of 16 or 32 bits or of 4), and the compaction's rows
-// moved into pages.
-#include <type_traits>
-
+// and values into pages), and the compaction's rows moved into pages.
 #include "kernels.cuh"
 #include "paged.cuh"
-#include "q4.cuh"
+#include "rotate.cuh"
 
 namespace stl {
 
@@ -31,25 +28,13 @@ namespace stl {
 // of a plain copy's rate; groups of a loop without loading ahead 27.1, eight
 // groups ahead 22.8, a CTA to 32 heads with shared sines 29.8), 8,616 tokens
 // with 4 value heads into pages 26.0 (eight groups 34.0, four 27.2, two 28.0).
-//
-// Into 4-bit pages keys and values go as they are here, in fp32, before they
-// would be rounded: two neighbouring lanes share a group of 16 elements (one
-// lane has it where pairs are interleaved).
-constexpr int kRotThreads = 128, kRotWarps = kRotThreads / 32;
-constexpr int kRotHeads = 4;   // heads of a group
-
 // One warp per unit: segment `u % segs` of the head groups of token u / segs, `base` of them or, in the first
 // `extra` segments, one more.
-// To packed rows, to pages, or to pages in 4 bits.
-enum RotateTo { kToRows = 0, kToPages = 1, kToQ4 = 2 };
-
-template <typename T, int NB, bool IL, int TO>
+template <typename T, int NB, bool IL, bool PAGED>
 __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ TokenView x,
                                                         const __grid_constant__ RopeView rope,
-                                                        const __grid_constant__ PageView pg,
-                                                        const __grid_constant__ Q4View q4, T* q_out, T* k_out,
+                                                        const __grid_constant__ PageView pg, T* q_out, T* k_out,
                                                         T* v_out, int base, int extra, int segs) {
-  constexpr bool PAGED = TO != kToRows;
   __shared__ uint64_t turn[kD / 2];
   // [warp][four of a lane's eight pairs][lane][pair], so that eight lanes' vectors are adjacent
   __shared__ float4 cs[kRotWarps][2][8], sn[kRotWarps][2][8];
@@ -84,9 +69,8 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
               reinterpret_cast<float*>(cs[warp]) + at);
   }
   if (t >= end) return;  // padding behind the last sequence
-  Place at = {-1, 0};
-  if (PAGED && kRotHeads * g1 > x.hq) at = token_place(pg, t);  // keys or values among the segment's heads
-  const int slot = at.page >= 0 ? at.page * pg.page_rows + at.row : -1;
+  int slot = -1;
+  if (PAGED && kRotHeads * g1 > x.hq) slot = token_slot(pg, t);  // keys or values among the segment's heads
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
@@ -140,30 +124,6 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
       va[i].set(a);
       vb[i].set(b);
     }
-    if (TO == kToQ4 && kRotHeads * (g0 + i + 1) > x.hq) {  // a key or value in the group
-      const int h = min(max(head - x.hq - (is_v ? x.hkv : 0), 0), x.hkv - 1);
-      const float* factor = is_v ? q4.v_factor : q4.k_factor;
-      const float f = factor ? factor[h] : 1.f;
-      uint32_t top_a = q4_top(a), top_b = q4_top(b);
-      if (IL) {  // a and b are one group
-        top_a = top_b = max(top_a, top_b);
-      } else {
-        top_a = max(top_a, __shfl_xor_sync(0xffffffffu, top_a, 1));
-        top_b = max(top_b, __shfl_xor_sync(0xffffffffu, top_b, 1));
-      }
-      const Q4Recip by_six(6.f * f);
-      const Q4Scale sa(top_a, by_six, f), sb(top_b, by_six, f);
-      if (live && !is_q && at.page >= 0) {
-        const size_t row = q4_row(pg, at.page, at.row, h, x.hkv);
-        uint8_t* codes = (is_v ? q4.v : q4.k) + row * kQ4Row;
-        uint8_t* scales = (is_v ? q4.v_scale : q4.k_scale) + row * kQ4Scales;
-        *reinterpret_cast<uint32_t*>(codes + off0 / 2) = q4_word(a, sa);
-        *reinterpret_cast<uint32_t*>(codes + off1 / 2) = q4_word(b, sb);
-        if (IL || !(c & 1)) scales[off0 / kQ4Group] = (uint8_t)sa.byte;
-        if (!IL && !(c & 1)) scales[off1 / kQ4Group] = (uint8_t)sb.byte;
-      }
-    }
-    if (TO == kToQ4 && !is_q) continue;
     T* dst = q_out + ((size_t)t * x.hq + head) * kD;
     if (!is_q) {
       const int h = head - x.hq - (is_v ? x.hkv : 0);
@@ -176,58 +136,22 @@ __global__ void __launch_bounds__(kRotThreads) k_rotate(const __grid_constant__ 
   }
 }
 
-static cudaError_t run_rotate(DType dt, const TokenView& x, const RopeView& rope, RotateTo to, const PageView& pg,
-                              const Q4View& q4, void* q_out, void* k_out, void* v_out, cudaStream_t st) {
-  const int groups = (x.hq + (to != kToRows ? 2 : 1) * x.hkv + kRotHeads - 1) / kRotHeads;
-  // groups of a warp: three, fewer where there are few tokens: 32 warps for each of the chip's 152 SMs (the grid's
-  // shape alone depends on it)
-  constexpr int most = 3;
-  long long segs = (152 * 32 + x.n - 1) / x.n;
-  if (segs < (groups + most - 1) / most) segs = (groups + most - 1) / most;
-  if (segs > groups) segs = groups;
-  const int base = (int)(groups / segs), extra = (int)(groups % segs), each = base + (extra > 0);
-  const dim3 grid((unsigned)((x.n * segs + kRotWarps - 1) / kRotWarps));
-  TimingScope ts(to == kToRows ? "rotate_qk" : (to == kToPages ? "paged_append" : "paged_append_q4"), st);
+cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, const PageView* pages, void* q_out,
+                          void* k_out, void* v_out, cudaStream_t st) {
+  const RotateShare s = rotate_share(x.n, (x.hq + (pages ? 2 : 1) * x.hkv + kRotHeads - 1) / kRotHeads);
+  const dim3 grid((unsigned)(((long long)x.n * s.segs + kRotWarps - 1) / kRotWarps));
+  const PageView pg = pages ? *pages : PageView{};
+  TimingScope ts(pages ? "paged_append" : "rotate_qk", st);
   cudaError_t e = cudaSuccess;
-  auto run = [&](auto zero, auto nb) {
+  with_rotate_type(dt, s, [&](auto zero, auto nb) {
     typedef decltype(zero) T;
     constexpr int NB = decltype(nb)::value;
     T *qo = static_cast<T*>(q_out), *ko = static_cast<T*>(k_out), *vo = static_cast<T*>(v_out);
-    auto pick = [&](auto il) {
-      constexpr bool IL = decltype(il)::value;
-      auto kern = to == kToRows ? k_rotate<T, NB, IL, kToRows>
-                                : (to == kToPages ? k_rotate<T, NB, IL, kToPages> : k_rotate<T, NB, IL, kToQ4>);
-      e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, q4, qo, ko, vo, base, extra, (int)segs);
-    };
-    if (rope.interleaved)
-      pick(std::true_type());
-    else
-      pick(std::false_type());
-  };
-  auto pick = [&](auto zero) {
-    if (each <= 1)
-      run(zero, std::integral_constant<int, 1>());
-    else if (each <= 2)
-      run(zero, std::integral_constant<int, 2>());
-    else
-      run(zero, std::integral_constant<int, most>());
-  };
-  if (dt == kBF16)
-    pick(__nv_bfloat16());
-  else
-    pick(float());
+    auto kern = rope.interleaved ? (pages ? k_rotate<T, NB, true, true> : k_rotate<T, NB, true, false>)
+                                 : (pages ? k_rotate<T, NB, false, true> : k_rotate<T, NB, false, false>);
+    e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pg, qo, ko, vo, s.base, s.extra, s.segs);
+  });
   return e != cudaSuccess ? e : cudaGetLastError();
-}
-
-cudaError_t launch_rotate(DType dt, const TokenView& x, const RopeView& rope, const PageView* pages, void* q_out,
-                          void* k_out, void* v_out, cudaStream_t st) {
-  return run_rotate(dt, x, rope, pages ? kToPages : kToRows, pages ? *pages : PageView{}, Q4View{}, q_out, k_out, v_out,
-                    st);
-}
-
-cudaError_t launch_append_q4(DType dt, const TokenView& x, const RopeView& rope, const PageView& pages,
-                             const Q4View& pools, void* q_out, cudaStream_t st) {
-  return run_rotate(dt, x, rope, kToQ4, pages, pools, q_out, nullptr, nullptr, st);
 }
 
 // ---------------------------------------------------------------- compaction

@@ -52,30 +52,20 @@ struct Vec8<float> {
   }
 };
 
-// Page and row of the page of row r of sequence s; page -1 where there is none.
-struct Place {
-  int page, row;
-};
-__device__ __forceinline__ Place page_place(const PageView& pg, int s, int r) {
-  if (r < 0 || r >= pg.max_pages * pg.page_rows) return {-1, 0};
-  const int i = pg.page_shift >= 0 ? r >> pg.page_shift : r / pg.page_rows;
-  const int page = pg.table[(size_t)s * pg.max_pages + i];
-  return {page >= 0 && page < pg.n_pages ? page : -1, r - i * pg.page_rows};
-}
 // Slot (page * page_rows + row of the page) of row r of sequence s, or -1.
 __device__ __forceinline__ int page_slot(const PageView& pg, int s, int r) {
-  const Place at = page_place(pg, s, r);
-  return at.page >= 0 ? at.page * pg.page_rows + at.row : -1;
+  if (r < 0 || r >= pg.max_pages * pg.page_rows) return -1;
+  const int i = pg.page_shift >= 0 ? r >> pg.page_shift : r / pg.page_rows, page = pg.table[(size_t)s * pg.max_pages + i];
+  return page >= 0 && page < pg.n_pages ? page * pg.page_rows + (r - i * pg.page_rows) : -1;
 }
 
-// The place of packed new token t, which is not padding.  A whole warp
+// The slot of packed new token t, which is not padding, or -1.  A whole warp
 // calls it; 32 sequences are compared at a time, so that up to 32 take two
 // memory latencies: their cu and len, then the table.
-__device__ __forceinline__ Place token_place(const PageView& pg, int t) {
+__device__ __forceinline__ int token_slot(const PageView& pg, int t) {
   if (!pg.cu) {
     const int s = t / pg.w;
-    if (s >= pg.n_seqs) return {-1, 0};
-    return page_place(pg, s, pg.len[s] - ((s + 1) * pg.w - t));
+    return s < pg.n_seqs ? page_slot(pg, s, pg.len[s] - ((s + 1) * pg.w - t)) : -1;
   }
   const int lane = threadIdx.x & 31;
   int lo = 0, count = pg.n_seqs;  // cu[lo] <= t, and the sequence is one of the `count` from lo on
@@ -90,8 +80,28 @@ __device__ __forceinline__ Place token_place(const PageView& pg, int t) {
   const uint32_t le = __ballot_sync(0xffffffffu, lane < count && first <= t);
   const int k = le ? 31 - __clz(le) : 0;
   const int row = __shfl_sync(0xffffffffu, len, k) - (__shfl_sync(0xffffffffu, next, k) - t);
-  return page_place(pg, lo + k, row);
+  return page_slot(pg, lo + k, row);
 }
+
+// Page and row of the page of row r of sequence s; page -1 where there is none.
+struct Place {
+  int page, row;
+};
+__device__ __forceinline__ Place page_place(const PageView& pg, int s, int r) {
+  if (r < 0 || r >= pg.max_pages * pg.page_rows) return {-1, 0};
+  const int i = pg.page_shift >= 0 ? r >> pg.page_shift : r / pg.page_rows;
+  const int page = pg.table[(size_t)s * pg.max_pages + i];
+  return {page >= 0 && page < pg.n_pages ? page : -1, r - i * pg.page_rows};
+}
+
+// token_slot's page and row.
+__device__ __forceinline__ Place token_place(const PageView& pg, int t) {
+  const int slot = token_slot(pg, t);
+  if (slot < 0) return {-1, 0};
+  const int page = pg.page_shift >= 0 ? slot >> pg.page_shift : slot / pg.page_rows;
+  return {page, slot - page * pg.page_rows};
+}
+
 // The same by a thread for itself: the sequence is found by halves.
 __device__ __forceinline__ Place thread_token_place(const PageView& pg, int t) {
   if (!pg.cu) {
@@ -108,10 +118,6 @@ __device__ __forceinline__ Place thread_token_place(const PageView& pg, int t) {
       hi = mid;
   }
   return page_place(pg, lo, pg.len[lo] - (pg.cu[lo + 1] - t));
-}
-__device__ __forceinline__ int token_slot(const PageView& pg, int t) {
-  const Place at = token_place(pg, t);
-  return at.page >= 0 ? at.page * pg.page_rows + at.row : -1;
 }
 
 }  // namespace stl

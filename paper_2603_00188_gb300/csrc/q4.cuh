@@ -56,7 +56,19 @@ struct Q4Recip {
     r_lo = fmaf(-r, t, 1.f) * r;
   }
   __device__ __forceinline__ float quotient(float x) const { return fmaf(x, r, x * r_lo); }
+  __device__ __forceinline__ float nearest() const { return r + r_lo; }  // 1 / t in fp32
 };
+
+// The e4m3 number nearest to one within 2^-9 .. 448, and its value.
+__device__ __forceinline__ uint32_t q4_scale_byte(float want) {
+  unsigned short two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(want));
+  return two;  // the upper half is zero
+}
+__device__ __forceinline__ float q4_scale_value(uint32_t byte) {
+  const uint32_t half = q4_scales(byte);
+  return __low2float(*reinterpret_cast<const __half2*>(&half));
+}
 
 // top: the bits of the group's largest magnitude as integers order them, which
 // puts infinities and NaN above every number; by_six: of 6 factor.
@@ -68,16 +80,13 @@ struct Q4Scale {
 
  private:
   __device__ __forceinline__ float init(uint32_t top, const Q4Recip& by_six, float factor) {
-    const float want = fminf(fmaxf(by_six.quotient(__uint_as_float(top)), 0x1p-9f), 448.f);
-    unsigned short two;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.f), "f"(want));
-    const uint32_t half = q4_scales(two);
-    byte = top >= 0x7f800000u ? kQ4NaN : two;  // the upper half is zero
-    return __low2float(*reinterpret_cast<const __half2*>(&half)) * factor;
+    const uint32_t nearest = q4_scale_byte(fminf(fmaxf(by_six.quotient(__uint_as_float(top)), 0x1p-9f), 448.f));
+    byte = top >= 0x7f800000u ? kQ4NaN : nearest;
+    return q4_scale_value(nearest) * factor;
   }
 };
-// Eight elements' codes.
-__device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& s) {
+// The codes of eight quotients, and of eight elements.
+__device__ __forceinline__ uint32_t q4_codes_of(const float (&x)[8]) {
   uint32_t w;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -86,9 +95,14 @@ __device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& 
       "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
       "mov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(w)
-      : "f"(s.by.quotient(x[0])), "f"(s.by.quotient(x[1])), "f"(s.by.quotient(x[2])), "f"(s.by.quotient(x[3])),
-        "f"(s.by.quotient(x[4])), "f"(s.by.quotient(x[5])), "f"(s.by.quotient(x[6])), "f"(s.by.quotient(x[7])));
-  return s.byte == kQ4NaN ? 0u : w;
+      : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return w;
+}
+__device__ __forceinline__ uint32_t q4_word(const float (&x)[8], const Q4Scale& s) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = s.by.quotient(x[i]);
+  return s.byte == kQ4NaN ? 0u : q4_codes_of(y);
 }
 __device__ __forceinline__ uint32_t q4_top(const float (&x)[8]) {
   uint32_t top = 0;

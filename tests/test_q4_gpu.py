@@ -51,9 +51,18 @@ def _special(g, *shape, dtype):
     return x.to(dtype)
 
 
-def _equal(p, x, codes, scales, at):
+def _unsigned_zeros(c):
+    """Codes with that of -0 (8) as that of 0: both stand for 0, and which of them a turned key of less than any code's
+    half gets is a matter of its sign alone."""
+    lo, hi = c & 15, c >> 4
+    return torch.where(lo == 8, 0, lo) | torch.where(hi == 8, 0, hi) << 4
+
+
+def _equal(p, x, codes, scales, at, turned=False):
     """Codes and scales of pool x at index `at` of [pages][hkv][page]."""
     c, s = getattr(p, x).cpu()[at], getattr(p, x + "_scale").view(torch.uint8).cpu()[at]
+    if turned:
+        c, codes = _unsigned_zeros(c), _unsigned_zeros(codes)
     assert torch.equal(s, scales), (x, (s != scales).sum(), (s != scales).nonzero()[:3])
     assert torch.equal(c, codes), (x, (c != codes).sum(), (c != codes).nonzero()[:3])
 
@@ -129,7 +138,7 @@ def test_groups_that_hold_no_number(st):
     (28, 4, BF, False, 1, False, True, False), (12, 2, BF, True, 3, True, True, True), (7, 1, F32, False, 3, True, False, True),
     (3, 3, F32, True, 1, False, False, False)])
 def test_append_bits(st, page, hq, hkv, dtype, interleaved, axes, norm, fused, factors):
-    """q as stlite_rotate_qk leaves it; keys as its fp32 results put into 4 bits; values as they are."""
+    """q as stlite_rotate_qk leaves it; keys as the rotation in 64 bits put into 4; values as they are."""
     g = _gen(page + hq)
     new, old = [3, 0, 1, 9, 2], [0, 5, 16, 30, 1]
     rows, T, pad = [o + m for o, m in zip(old, new)], sum(new), 4
@@ -150,16 +159,17 @@ def test_append_bits(st, page, hq, hkv, dtype, interleaved, axes, norm, fused, f
     st.stlite_paged_append_q4(q, k, v, pos, rope, pt, qo, p, *w, 1e-5)
     want_q, _ = st.rotate_qk(q, k, pos, rope, *w, 1e-5)
     assert torch.equal(qo[:T], want_q[:T]) and (qo[T:] == 7).all()
-    _, y = st.rotate_qk(q.float(), k.float(), pos, rope, *[z if z is None else z.float() for z in w], 1e-5)
+    eps = torch.tensor(1e-5, dtype=F32).double().item()
+    y, _ = paged_ref.rotate(k, pos, paged_ref.default_freq(1e6), section, interleaved, w[1], eps)
     seq = [s for s, m in enumerate(new) for _ in range(m)]
     row = [old[s] + i for s, m in enumerate(new) for i in range(m)]
     at = (torch.tensor([int(table[s, r // page]) for s, r in zip(seq, row)]), slice(None), torch.tensor([r % page for r in row]))
     for name, src in (("k", y), ("v", v)):
         f = getattr(p, name + "_factor")
-        c, s = ref.encode(src[:T].float(), 1.0 if f is None else f[:, None])
-        _equal(p, name, c, s, at)
+        c, s = ref.encode(src[:T], 1.0 if f is None else f[:, None])
+        _equal(p, name, c, s, at, name == "k")
         before[name][at] = c
-        assert torch.equal(getattr(p, name).cpu(), before[name])
+        assert torch.equal(_unsigned_zeros(getattr(p, name).cpu()), _unsigned_zeros(before[name]))
     # and out again
     ko, vo = st.paged_fetch_q4(p, pt, T + pad, dtype)
     for name, got in (("k", ko), ("v", vo)):
@@ -168,6 +178,42 @@ def test_append_bits(st, page, hq, hkv, dtype, interleaved, axes, norm, fused, f
                           1.0 if f is None else f[:, None])
         paged_ref.within(got[:T], want, want.abs() * paged_ref.U)
         assert not got[T:].any()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_keys_at_borders(st, interleaved):
+    """Keys turned by tiny angles, elements at borders between codes and scales: each has the code of 64 bits.
+
+    Within 2^-50 of its pair's magnitude of a border it may have that of either side: angles are held to 2^-65 of a
+    turn a position (1,000 of them 2^-52.4), and the reference, rounded four times, may be off by 2^-51 itself.
+    """
+    g, T, hkv, page = _gen(31), 200, 4, 16
+    k = _special(g, T, hkv, 128, dtype=BF)
+    q = _randn(g, T, hkv, 128)
+    pos = torch.randint(1, 1000, (T,), generator=g, dtype=I32)
+    freq = [2.0 ** -(20 + i % 12) for i in range(64)]  # an element moves by some of its half steps in fp32
+    rope = st.make_rope(interleaved=interleaved, inv_freq=freq)
+    table, pages = _table([T], page, 3)
+    pt = st.make_pages(pages, page, table.cuda(), _ints([T]), max_new=T)
+    p, w = st.make_q4_pools(pages, page, hkv), (1 + 0.2 * torch.randn(128, generator=g)).to(BF)
+    r = torch.arange(T)
+    at = (table[0].long()[r // page], slice(None), r % page)
+    eps = torch.tensor(1e-6, dtype=F32).double().item()
+    for norm in (None, w.cuda()):
+        st.stlite_paged_append_q4(q, k.cuda(), k.cuda(), pos.cuda(), rope, pt, q.clone(), p, None, norm, 1e-6)
+        y, _ = paged_ref.rotate(k, pos[None], freq, (64, 0, 0), interleaved, norm, eps)
+        pairs = y.unflatten(-1, (64, 2) if interleaved else (2, 64))
+        off = pairs.norm(dim=-1 if interleaved else -2, keepdim=True).expand_as(pairs).flatten(-2) * 2.0 ** -50
+        ends = [(y.abs() - off).clamp_min(0), y.abs() + off]
+        scale = p.k_scale.view(torch.uint8).cpu()[at]
+        low, high = (ref.encode(e)[1] for e in ends)
+        assert ((low <= scale) & (scale <= high)).all() and (low != high).sum() < 10
+        step = ref.SCALES[scale.long()].repeat_interleave(16, -1)
+        low, high = (ref.nearest((e / step).clamp_max(6.0), ref.VALUES[:8]) for e in ends)
+        code = torch.stack([p.k.cpu()[at] & 15, p.k.cpu()[at] >> 4], -1).flatten(-2)
+        assert ((low <= code % 8) & (code % 8 <= high)).all() and (low != high).sum() < 100
+        assert ((code % 8 == 0) | ((code >= 8) == y.signbit())).all()
+        _equal(p, "v", *ref.encode(k), at)
 
 
 @pytest.mark.parametrize("layers", [1, 5, 33])
