@@ -576,8 +576,8 @@ typedef struct {
 } stlite_q4_pools;
 
 /* stlite_paged_append into 4-bit pages: values are put in as they are, keys with
- * the codes and scales of their rotation in 64 bits (its inputs' bits, angles to
- * 2^-64 of a turn); q_out as there.  Everything else as for
+ * the codes and scales of their rotation in 64 bits (angles to 2^-64 of a turn for
+ * each position), not of its fp32 form; q_out as there.  Everything else as for
  * stlite_paged_append. */
 STLITE_API stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope,
                                                 const stlite_tokens* x, const stlite_pages* pages, void* q_out,

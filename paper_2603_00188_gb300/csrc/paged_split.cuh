@@ -224,13 +224,14 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The rows of a warp's blocks, one block after the other.  The block of unit u
-// is warp u % WARPS's.
 // Whether `ctas` CTAs of so much dynamic shared memory share an SM's 228 KB
 // (1 KB of it each is reserved).
 __host__ __device__ constexpr bool fits_sm(int smem, int ctas) {
   return ctas * ((smem + 127) / 128 * 128 + 1024) <= 228 * 1024;
 }
+
+// The rows of a warp's blocks, one block after the other.  The block of unit u
+// is warp u % WARPS's.
 template <int WARPS>
 __device__ __forceinline__ int warps_first(int u, int warp) { return u + ((warp - u) & (WARPS - 1)); }
 template <int WARPS, int BLOCK>
