@@ -1,6 +1,8 @@
 """Caches in 4 bits on the GPU: rows in (append, compaction, the fused pass) and
 out, and attention over them, through the public entry points, against plain
 64-bit forms (q4_ref.py)."""
+import math
+
 import pytest
 import torch
 
@@ -180,13 +182,26 @@ def test_append_bits(st, page, hq, hkv, dtype, interleaved, axes, norm, fused, f
         assert not got[T:].any()
 
 
+def _turned_equal(p, y, interleaved, at, factor=1.0):
+    """Keys of pool p have the codes and scales of y, but within 2^-50 of its pair's magnitude of a border an element
+    may have the code of either side: angles are held to 2^-65 of a turn a position (1,000 of them 2^-52.4), and the
+    reference, rounded four times, may be off by 2^-51 itself."""
+    pairs = y.unflatten(-1, (64, 2) if interleaved else (2, 64))
+    off = pairs.norm(dim=-1 if interleaved else -2, keepdim=True).expand_as(pairs).flatten(-2) * 2.0 ** -50
+    ends = [(y.abs() - off).clamp_min(0), y.abs() + off]
+    scale = p.k_scale.view(torch.uint8).cpu()[at]
+    low, high = (ref.encode(e, factor)[1] for e in ends)
+    assert ((low <= scale) & (scale <= high)).all() and (low != high).sum() < 10
+    step = ref.SCALES[scale.long()].repeat_interleave(16, -1) * factor
+    low, high = (ref.nearest((e / step).clamp_max(6.0), ref.VALUES[:8]) for e in ends)
+    code = torch.stack([p.k.cpu()[at] & 15, p.k.cpu()[at] >> 4], -1).flatten(-2)
+    assert ((low <= code % 8) & (code % 8 <= high)).all() and (low != high).sum() < 100
+    assert ((code % 8 == 0) | ((code >= 8) == y.signbit())).all()
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_keys_at_borders(st, interleaved):
-    """Keys turned by tiny angles, elements at borders between codes and scales: each has the code of 64 bits.
-
-    Within 2^-50 of its pair's magnitude of a border it may have that of either side: angles are held to 2^-65 of a
-    turn a position (1,000 of them 2^-52.4), and the reference, rounded four times, may be off by 2^-51 itself.
-    """
+    """Keys turned by tiny angles, elements at borders between codes and scales: each has the code of 64 bits."""
     g, T, hkv, page = _gen(31), 200, 4, 16
     k = _special(g, T, hkv, 128, dtype=BF)
     q = _randn(g, T, hkv, 128)
@@ -202,18 +217,53 @@ def test_keys_at_borders(st, interleaved):
     for norm in (None, w.cuda()):
         st.stlite_paged_append_q4(q, k.cuda(), k.cuda(), pos.cuda(), rope, pt, q.clone(), p, None, norm, 1e-6)
         y, _ = paged_ref.rotate(k, pos[None], freq, (64, 0, 0), interleaved, norm, eps)
-        pairs = y.unflatten(-1, (64, 2) if interleaved else (2, 64))
-        off = pairs.norm(dim=-1 if interleaved else -2, keepdim=True).expand_as(pairs).flatten(-2) * 2.0 ** -50
-        ends = [(y.abs() - off).clamp_min(0), y.abs() + off]
-        scale = p.k_scale.view(torch.uint8).cpu()[at]
-        low, high = (ref.encode(e)[1] for e in ends)
-        assert ((low <= scale) & (scale <= high)).all() and (low != high).sum() < 10
-        step = ref.SCALES[scale.long()].repeat_interleave(16, -1)
-        low, high = (ref.nearest((e / step).clamp_max(6.0), ref.VALUES[:8]) for e in ends)
-        code = torch.stack([p.k.cpu()[at] & 15, p.k.cpu()[at] >> 4], -1).flatten(-2)
-        assert ((low <= code % 8) & (code % 8 <= high)).all() and (low != high).sum() < 100
-        assert ((code % 8 == 0) | ((code >= 8) == y.signbit())).all()
+        _turned_equal(p, y, interleaved, at)
         _equal(p, "v", *ref.encode(k), at)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_keys_that_cancel(st, dtype, interleaved):
+    """Pairs of one size turned by almost an eighth of a turn: one half of each, of either sign, is 2^-17 of what it is
+    the difference of, all of it below the fp32 rotation's error, and the factor makes codes of it."""
+    g, T, hkv, page = _gen(41), 40, 4, 16
+    size = (0.5 + torch.rand((T, hkv, 64), generator=g)).to(dtype)
+    sign = torch.tensor([1.0, -1.0])[torch.randint(0, 2, (2, T, hkv, 64), generator=g)]
+    sign[1, :, 0], sign[1, :, 1] = sign[0, :, 0], -sign[0, :, 1]  # heads whose first halves, or second ones, cancel
+    pair = (size * sign[0], size * sign[1])
+    k = torch.stack(pair, -1).flatten(-2).to(dtype) if interleaved else torch.cat(pair, -1).to(dtype)
+    freq = [2 * math.pi * (0.125 + (-1) ** i * (1 + i / 64) * 2.0 ** -20) for i in range(64)]
+    factor = torch.tensor([1.0, 1.25, 1.5, 0.7]) * 2.0 ** -25
+    table, pages = _table([T], page, 3)
+    pt = st.make_pages(pages, page, table.cuda(), _ints([T]), max_new=T)
+    p, q, pos = st.make_q4_pools(pages, page, hkv, factor.cuda()), _randn(g, T, 4, 128, dtype=dtype), torch.ones(T, dtype=I32)
+    rope = st.make_rope(interleaved=interleaved, inv_freq=freq)
+    st.stlite_paged_append_q4(q, k.cuda(), k.cuda(), pos.cuda(), rope, pt, q.clone(), p)
+    y, _ = paged_ref.rotate(k, pos[None], freq, (64, 0, 0), interleaved)
+    r = torch.arange(T)
+    _turned_equal(p, y, interleaved, (table[0].long()[r // page], slice(None), r % page), factor.double()[:, None])
+
+
+@pytest.mark.parametrize("tokens,hq,hkv,dtype", [(5003, 12, 2, BF), (2433, 3, 1, F32), (4868, 28, 4, BF)])
+def test_long_prompts_as_short_ones(st, tokens, hq, hkv, dtype):
+    """A call's tokens as calls of at most 1,000 of them leave them, padding unwritten."""
+    g, page, pad = _gen(tokens), 64, 5
+    q, k, v = (_randn(g, tokens + pad, h, 128, dtype=dtype) for h in (hq, hkv, hkv))
+    pos, rope = torch.randint(0, 30000, (tokens + pad,), generator=g, dtype=I32).cuda(), st.make_rope(1e6)
+    cut = tokens // 3
+    table, pages = _table([cut, tokens - cut], page, tokens)
+    out, pools = [torch.full_like(q, 7) for _ in range(2)], [st.make_q4_pools(pages, page, hkv) for _ in range(2)]
+    pt = st.make_pages(pages, page, table.cuda(), _ints([cut, tokens - cut]), _ints([0, cut, tokens]), max_new=tokens)
+    st.stlite_paged_append_q4(q, k, v, pos, rope, pt, out[0], pools[0])
+    assert (out[0][tokens:] == 7).all()
+    for s, (first, end) in enumerate(((0, cut), (cut, tokens))):
+        for t in range(first, end, 1000):
+            u = min(end, t + 1000)
+            pt = st.make_pages(pages, page, table[s:s + 1].cuda(), _ints([u - first]), max_new=u - t)
+            st.stlite_paged_append_q4(q[t:u], k[t:u], v[t:u], pos[t:u], rope, pt, out[1][t:u], pools[1])
+    assert torch.equal(*out)
+    for x in ("k", "v", "k_scale", "v_scale"):
+        assert torch.equal(*(getattr(p, x).view(torch.uint8) for p in pools)), x
 
 
 @pytest.mark.parametrize("layers", [1, 5, 33])
