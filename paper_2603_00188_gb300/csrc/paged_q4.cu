@@ -90,10 +90,11 @@ cudaError_t launch_gather_q4(const Problem& p, const Q4Layers& io, int budget, c
 // Rows as values.  A CTA's first warp finds the places of 32 tokens; then, for
 // every head of its share of the layers' keys and values, a lane takes elements
 // 8 g .. and 64 + 8 g .. of a row, so that what eight lanes write at a time lies
-// together.  24 sessions, 65,000 rows of 12 layers: 336 us, 0.93 of a copy's rate
+// together.  24 sessions, 65,000 rows of 12 layers: 324 us, 0.96 of a copy's rate
 // (a warp to a token, its place found by the whole warp and a group of 16
-// elements to a lane: 403).
-constexpr int kFetchTokens = 32;
+// elements to a lane: 403).  Four heads are taken at once, of layers apart: three
+// take 355 us, two 331, six 335, neighbours 362.
+constexpr int kFetchTokens = 32, kFetchAtOnce = 4;
 template <typename T>
 __global__ void __launch_bounds__(256) k_fetch_q4(const __grid_constant__ Q4Layers io,
                                                   const __grid_constant__ PageView pg, int n, int hkv, int units) {
@@ -111,13 +112,12 @@ __global__ void __launch_bounds__(256) k_fetch_q4(const __grid_constant__ Q4Laye
   const Place at = places[threadIdx.x >> 3];
   if (at.page < 0) return;
   // units: layers * 2 (keys, values) * heads
-  constexpr int kAtOnce = 4;
-  for (int u0 = blockIdx.y; u0 < units; u0 += gridDim.y * kAtOnce) {
-    uint32_t w[kAtOnce][2], b[kAtOnce][2];
-    float f[kAtOnce];
-    T* dst[kAtOnce];
+  for (int u0 = blockIdx.y; u0 < units; u0 += gridDim.y * kFetchAtOnce) {
+    uint32_t w[kFetchAtOnce][2], b[kFetchAtOnce][2];
+    float f[kFetchAtOnce];
+    T* dst[kFetchAtOnce];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kFetchAtOnce; ++i) {
       const int u = u0 + i * gridDim.y;
       if (u >= units) break;
       const int x = u / hkv, h = u - x * hkv, l = x >> 1;
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(256) k_fetch_q4(const __grid_constant__ Q4Laye
       dst[i] = static_cast<T*>(const_cast<void*>(is_v ? io.v[l] : io.k[l])) + ((size_t)t * hkv + h) * kD + 8 * g;
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
+    for (int i = 0; i < kFetchAtOnce; ++i) {
       if (u0 + i * (int)gridDim.y >= units) break;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -163,9 +163,13 @@ cudaError_t launch_fetch_q4(DType dt, const Q4Layers& io, int layers, int n, int
                             cudaStream_t st) {
   TimingScope ts("paged_fetch_q4", st);
   const int blocks = (n + kFetchTokens - 1) / kFetchTokens, units = layers * 2 * hkv;
-  // CTAs to the units of a block's tokens: eight to each of the chip's 152 SMs in all, where there are few tokens
-  int share = (152 * 8 + blocks - 1) / blocks;
+  // CTAs to the units of a block's tokens: one to those that it takes at once (24 sessions, 12 layers: 324 us; one to
+  // all of them 337, one to two 331), and eight to each of the chip's 152 SMs in all where there are few tokens
+  int share = (units + kFetchAtOnce - 1) / kFetchAtOnce;
+  const int few = (152 * 8 + blocks - 1) / blocks;
+  share = few > share ? few : share;
   share = share > units ? units : share;
+  share = share > 65535 ? 65535 : share;
   const cudaError_t e = launch_after(dt == kBF16 ? k_fetch_q4<__nv_bfloat16> : k_fetch_q4<float>, dim3(blocks, share),
                                      256, 0, st, io, pages, n, hkv, units);
   return e != cudaSuccess ? e : cudaGetLastError();
