@@ -16,9 +16,9 @@ namespace stl {
 // A unit is a warp's: a segment of a token's query heads, as k_rotate's, or four of
 // its key and value heads, whose lanes share a group of 16 elements by twos (one
 // lane has it where pairs are interleaved).  The bytes moved bound long prompts
-// (8,616 tokens of 28 + 4 bf16 heads 38.2 us, 0.65 of a plain copy's rate; 34.4
+// (8,616 tokens of 28 + 4 bf16 heads 37.4 us, 0.66 of a plain copy's rate; 34.4
 // without the second end and what it decides, with wrong codes), latency the rest
-// (2,096 tokens of 12 + 2 heads 9.2 us with a fetch of 2).  Keys are most of a
+// (2,096 tokens of 12 + 2 heads 9.1 us with a fetch of 2).  Keys are most of a
 // warp's work, so that warps of four tokens' keys share a CTA and those of the
 // first kAhead tokens come before anything else.
 // A lane's elements of a key: as they are in memory, the norm's weights, rotated in fp32 and how far (each pair, and
@@ -245,19 +245,44 @@ __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps
 // Measured at 2,096 and 8,616 tokens, each token's units together: 11.6 and 40.1 us;
 // with kAhead 0: 10.5 and 37.8; 1,216: 9.5 and 37.8; 2,432: 9.2 and 38.2; all: 9.2 and 40.6.
 constexpr int kAhead = 2432;
+// Divides numbers below 2^31 by d: the product with 2^shift / d, rounded up, is off by
+// less than a quotient's step (Granlund and Montgomery, 1994).  Three instructions for
+// some thirty, of a warp's 500: 38.2 to 37.4 us.
+struct Divisor {
+  uint32_t mul;
+  int shift, d;
+  explicit Divisor(int by) : shift(31), d(by) {
+    while ((1LL << (shift - 31)) < d) ++shift;
+    mul = (uint32_t)(((1ULL << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ int of(int x) const { return (int)((uint64_t)(uint32_t)x * mul >> shift); }
+};
+struct Order {
+  int q_segs, first, rest;  // first: units of the keys and values that come first; rest: other tokens, in fours
+  Divisor ahead, four, q;   // four: units of four tokens
+  Order(int n, int q_segs, int segs)
+      : q_segs(q_segs), ahead(n < kAhead ? n : kAhead), four(4 * segs), q(q_segs) {
+    first = (segs - q_segs) * ahead.d;
+    rest = (n - ahead.d + 3) / 4 * 4;
+  }
+};
 struct Unit {
   int t, seg;
 };
-__device__ __forceinline__ Unit unit_of(int u, int n, int q_segs, int segs) {
-  const int ahead = min(n, kAhead), first = (segs - q_segs) * ahead, rest = (n - ahead + 3) & ~3;
-  if (u < first) return {u % ahead, q_segs + u / ahead};
-  u -= first;
-  if (u < rest * segs) {
-    const int four = u / (4 * segs), i = u - four * 4 * segs, seg = segs - 1 - (i >> 2);
-    return {4 * four + (i & 3) + (seg < q_segs ? 0 : ahead), seg};
+__device__ __forceinline__ Unit unit_of(int u, const Order& o) {
+  if (u < o.first) {
+    const int seg = o.ahead.of(u);
+    return {u - seg * o.ahead.d, o.q_segs + seg};
   }
-  u -= rest * segs;
-  return {rest + u / q_segs, u % q_segs};
+  u -= o.first;
+  const int fours = o.four.of(u);
+  if (4 * fours < o.rest) {
+    const int i = u - fours * o.four.d, seg = (o.four.d >> 2) - 1 - (i >> 2);
+    return {4 * fours + (i & 3) + (seg < o.q_segs ? 0 : o.ahead.d), seg};
+  }
+  u -= (o.rest >> 2) * o.four.d;
+  const int t = o.q.of(u);
+  return {o.rest + t, u - t * o.q.d};
 }
 
 // Registers for eight CTAs an SM, seven of fp32 (few are spilled): 8,616 tokens of bf16 take 41.0 / 40.6 / 39.9 us
@@ -266,7 +291,7 @@ template <typename T, int NB, bool IL>
 __global__ void __launch_bounds__(kRotThreads, sizeof(T) == 2 ? 8 : 7)
     k_append_q4(const __grid_constant__ TokenView x, const __grid_constant__ RopeView rope,
                 const __grid_constant__ PageView pg, const __grid_constant__ Q4View q4, T* q_out, int base, int extra,
-                int q_segs, int segs) {
+                const __grid_constant__ Order order) {
   __shared__ uint64_t turn[kD / 2];
   __shared__ float4 cs[kRotWarps][2][8], sn[kRotWarps][2][8];  // as in k_rotate
   if (threadIdx.x < kD / 2) turn[threadIdx.x] = rope.turn[threadIdx.x];
@@ -274,8 +299,8 @@ __global__ void __launch_bounds__(kRotThreads, sizeof(T) == 2 ? 8 : 7)
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, c = lane & 7;
-  const Unit unit = unit_of(blockIdx.x * kRotWarps + warp, x.n, q_segs, segs);
-  const int t = unit.t, seg = unit.seg;
+  const Unit unit = unit_of(blockIdx.x * kRotWarps + warp, order);
+  const int t = unit.t, seg = unit.seg, q_segs = order.q_segs;
   if (t >= x.n) return;
   const int off0 = IL ? 16 * c : 8 * c, off1 = IL ? 16 * c + 8 : kD / 2 + 8 * c;
   const int end = pg.cu ? pg.cu[pg.n_seqs] : x.n;
@@ -441,7 +466,7 @@ cudaError_t launch_append_q4(DType dt, const TokenView& x, const RopeView& rope,
     constexpr int NB = decltype(nb)::value;
     auto kern = rope.interleaved ? k_append_q4<T, NB, true> : k_append_q4<T, NB, false>;
     e = launch_after(kern, grid, kRotThreads, 0, st, x, rope, pages, pools, static_cast<T*>(q_out), s.base, s.extra,
-                     s.segs, segs);
+                     Order(x.n, s.segs, segs));
   });
   return e != cudaSuccess ? e : cudaGetLastError();
 }
