@@ -314,7 +314,10 @@ __global__ void __launch_bounds__(kQaThreads, qa_ctas(NT))
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int ex = min((int)(top >> 23), 253);
     float mul = __uint_as_float((uint32_t)(254 - ex) << 23);  // 2^-exponent
-    const float back = kPatLog2e * rsqrtf((float)kD) * (pools.k_factor ? pools.k_factor[h] : 1.f) / mul;
+    // What the products, below 2^21 and multiples of 2^-34, become scores by.  Below 2^-100 every weight is 1, above
+    // 2^100 the largest score's alone counts, whatever it is: held there, no score is an infinity, nor 0 times one.
+    float back = kPatLog2e * rsqrtf((float)kD) * (pools.k_factor ? pools.k_factor[h] : 1.f) / mul;
+    back = fminf(fmaxf(back, 0x1p-100f), 0x1p100f);
     if (top >= 0x7f800000u) mul = CUDART_NAN_F;  // not all are numbers: nor are its scores
     if constexpr (kRegs) {
       sc[0][0] = __shfl_sync(0xffffffffu, back, 8 * t4);
@@ -478,7 +481,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_ctas(NT))
                 for (int j = 0; j < 4; ++j) {
                   const int r = 16 * (y0 + y) + g8 + 8 * (j >> 1), x = 8 * nt + 2 * t4 + (j & 1);
                   const int sees = cur.w.len - (cur.w.fresh - 1 - (row0 + x) / G);
-                  // times a factor above zero
+                  // times a factor of 2^-100 at least
                   if (!(ok >> r & 1u) || base + r >= sees) c[y][nt][j] = -CUDART_INF_F;
                 }
           }
