@@ -19,9 +19,10 @@
 // result's own rounding).  fp32 queries and their weights are taken as hi + lo,
 // two parts of 11 bits, which is twice the products.
 //
-// Weights are 2^(x - m) with m moved only when a score exceeds it by more than
-// 2^4, at most 2^14 (fp16 goes to 2^16): no maximum is formed for blocks that do
-// not exceed it.
+// Weights are 2^(x - m), m the largest score so far less 10, moved only when one
+// exceeds it by more than 14: no maximum is formed for blocks that do not.  So they
+// are at most 2^14 (fp16 goes to 2^16).  Scores of 2^27 and more, whose difference
+// to m fp32 cannot hold within that, have the largest itself as m.
 //
 // What bounds it.  16 sessions of 25,000 rows, one token of 7 queries to a KV
 // head, take 48 to 51 us with start (4 us) and merge, 4.8 TB/s, 0.70 of a copy's
@@ -508,11 +509,11 @@ __global__ void __launch_bounds__(kQaThreads, qa_ctas(NT))
                 float mx = fmaxf(c[0][nt][e], c[0][nt][2 + e]);
 #pragma unroll
                 for (int y = 1; y < kTiles; ++y) mx = max3(mx, c[y][nt][e], c[y][nt][2 + e]);
-                mx -= kQaLift;
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                mx = fmaxf(m[nt][e], mx);
+                const float lifted = __fsub_rn(mx, kQaLift);  // 16 below where fp32's numbers are 16 apart
+                mx = fmaxf(m[nt][e], __fsub_rn(mx, lifted) > kQaLift + kQaSlack ? mx : lifted);
                 const float alpha = ex2_approx(m[nt][e] - mx);
                 m[nt][e] = mx;
                 l[nt][e] *= alpha;

@@ -1,6 +1,8 @@
 """Attention over 4-bit pages at the ends of what factors and scores may be:
 against plain 64-bit forms (q4_ref.py), or against what scores that are all
 equal, or far apart, leave of the softmax."""
+import math
+
 import pytest
 import torch
 
@@ -70,3 +72,41 @@ def test_largest_scores(st, dtype, factor):
     for h in range(hkv):
         kept = paged_ref.rows_of(v, table[2], 50)[:, h]
         paged_ref.within(got[2, 4 * h:4 * h + 4], kept.mean(0).expand(4, 128), _mean_bound(kept, dtype == F32).expand(4, 128))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("hq,hkv,new", [(7, 1, 1), (8, 1, 3), (16, 2, 4)])
+def test_scores_of_any_magnitude(st, dtype, sign, hq, hkv, new):
+    """Scores of 2^18 to 2^33 (as powers of two), where fp32's numbers are 2^-5 to 2^10 apart: those of the rows that
+    have the largest are all equal, the others' half of them or twice, so that the result is a mean."""
+    g, page, n, S = _gen(hq + new), 16, 93, 64
+    table, pages = _table([n], page, 3)
+    p = st.make_q4_pools(pages, page, hkv)
+    v = torch.randn((pages, hkv, page, 128), generator=g)
+    large = torch.rand(n, generator=g) < 0.5
+    large[:40] = False  # the largest come later
+    large[n - new:] = False  # every token sees the same ones of them
+    large[0] = sign < 0
+    key = torch.zeros((pages, hkv, page, 128))
+    for r in range(n):  # the larger score is that of 6, or of -3
+        key[int(table[0, r // page]), :, r % page, 5] = 6.0 if large[r] else 3.0
+    for x, src in (("k", key), ("v", v)):
+        c, s = ref.encode(src)
+        getattr(p, x).copy_(c)
+        getattr(p, x + "_scale").view(torch.uint8).copy_(s)
+    vd = paged_ref.rows_of(ref.dense(p, "v"), table[0], n)
+    assert torch.equal(paged_ref.rows_of(ref.dense(p, "k"), table[0], n)[:, 0, 5], torch.where(large, 6.0, 3.0).double())
+    size = torch.exp2(18 + 15 * torch.arange(S) / (S - 1)) / 6  # of the query that makes such a score of a 6
+    q = torch.zeros((S, new, hq, 128))
+    q[..., 5] = (sign * size * math.sqrt(128) / math.log2(math.e))[:, None, None]
+    pt = st.make_pages(pages, page, table.repeat(S, 1).cuda(), _ints([n] * S), max_new=new)
+    got = st.paged_attention_q4(q.view(S * new, hq, 128).to(dtype).cuda(), p, pt).view(S, new, hq, 128)
+    for i in range(new):
+        for h in range(hkv):
+            rows = large if sign > 0 else ~large
+            kept = vd[:, h][rows & (torch.arange(n) < n - (new - 1 - i))]
+            G = hq // hkv
+            shape = (S, G, 128)
+            paged_ref.within(got[:, i, G * h:G * h + G], kept.mean(0).expand(shape),
+                             _mean_bound(kept, dtype == F32).expand(shape), (i, h))
