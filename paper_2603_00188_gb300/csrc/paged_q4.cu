@@ -54,24 +54,36 @@ __global__ void __launch_bounds__(256) k_gather_q4(const __grid_constant__ Q4Lay
   pdl_trigger();
   pdl_wait();
   const int l = blockIdx.z, h = blockIdx.y, c = threadIdx.x & 7, r = blockIdx.x * 32 + (threadIdx.x >> 3);
+  const Q4View& to = io.pools[l];
+  const float fk = to.k_factor ? to.k_factor[h] : 1.f, fv = to.v_factor ? to.v_factor[h] : 1.f;
+  Q4Factor factors[2] = {{fk, sizeof(T) == 4 && q4_long(fk)}, {fv, sizeof(T) == 4 && q4_long(fv)}};
+  if (sizeof(T) == 2 && (q4_long(fk) || q4_long(fv))) {  // the same for the whole CTA
+    __shared__ float moved[2];
+    const int warp = threadIdx.x >> 5;
+    if (warp < 2) {
+      const float f = q4_factor<T, 32>(warp ? fv : fk).f;
+      if ((threadIdx.x & 31) == 0) moved[warp] = f;
+    }
+    __syncthreads();
+    factors[0].f = moved[0];
+    factors[1].f = moved[1];
+  }
   if (r >= budget) return;
   const int src = io.idx[l][(size_t)h * budget + r];
   const Place at = page_place(pg, seq, r);
   if (at.page < 0 || src < 0 || src >= n) return;
-  const Q4View& to = io.pools[l];
   const size_t from = ((size_t)src * hkv + h) * kD + kQ4Group * c, row = q4_row(pg, at.page, at.row, h, hkv);
   Group16<T> x[2];
   x[0].load(static_cast<const T*>(io.k[l]) + from);
   x[1].load(static_cast<const T*>(io.v[l]) + from);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float* factor = i ? to.v_factor : to.k_factor;
-    const float f = factor ? factor[h] : 1.f;
-    const Q4Scale s(x[i].top(), Q4Recip(6.f * f), f);
+    const Q4Factor f = factors[i];
+    const Q4Scale s(x[i].top(), Q4Recip(6.f, f.f), f);
     float y[2][8];
     x[i].x[0].get(y[0]);
     x[i].x[1].get(y[1]);
-    const uint2 w = make_uint2(q4_word(y[0], s), q4_word(y[1], s));
+    const uint2 w = make_uint2(q4_word(y[0], s, f), q4_word(y[1], s, f));
     *reinterpret_cast<uint2*>((i ? to.v : to.k) + row * kQ4Row + 8 * c) = w;
     (i ? to.v_scale : to.k_scale)[row * kQ4Scales + c] = (uint8_t)s.byte;
   }

@@ -215,7 +215,7 @@ __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps
         if (!misses(top[e], border, at)) break;
       }
       part->scale[e] = at;
-      const Q4Recip by(q4_scale_value(at) * factor);
+      const Q4Recip by(q4_scale_value(at), factor);
       part->code[e] = codes_within<IL>(part->y[e], e, part->off, part->most, by, &part->open[e]);
     }
   }
@@ -370,6 +370,11 @@ __global__ void __launch_bounds__(kRotThreads, sizeof(T) == 2 ? 8 : 7)
   }
   const float* factor = is_v ? q4.v_factor : q4.k_factor;
   const float f = factor ? factor[h] : 1.f;
+  Q4Factor by = {f, false};  // keys' borders are settled below, with the factor as it is
+  if (q4.v_factor) {
+    const Q4Factor moved = q4_factor<T, 8>(f);
+    if (is_v) by = moved;
+  }
   // How far a rotated key's elements may be off, 8 half steps of the magnitudes
   // of their pair (its angle and sines 2.6, products and sum 2.4, the ends of what
   // it may be and their quotients 3), 24 with a norm (16 more: 19 additions halved
@@ -395,13 +400,13 @@ __global__ void __launch_bounds__(kRotThreads, sizeof(T) == 2 ? 8 : 7)
     for (int e = 0; e < 2; ++e) top[e] = max(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
   }
-  const Q4Recip by_six(6.f * f);
-  const Q4Scale sa(top[0], by_six, f), sb(top[1], by_six, f);
+  const Q4Recip by_six(6.f, by.f);
+  const Q4Scale sa(top[0], by_six, by), sb(top[1], by_six, by);
   uint32_t code[2], scale[2] = {sa.byte, sb.byte}, open[2] = {0u, 0u};
   bool open_a = false, open_b = false;
   if (is_v) {
-    code[0] = q4_word(a, sa);
-    code[1] = q4_word(b, sb);
+    code[0] = q4_word(a, sa, by);
+    code[1] = q4_word(b, sb, by);
   } else {
     code[0] = codes_within<IL>(a, 0, off, most, sa.by, &open[0]);
     code[1] = codes_within<IL>(b, 1, off, most, sb.by, &open[1]);
