@@ -65,43 +65,43 @@ __device__ __forceinline__ bool open_scale(uint32_t top, float off, const Q4Reci
 
 // What is open is formed in pairs of fp32, some 45 bits: in fp64, whose operations
 // are few a clock on this chip, the same took 2.9 us longer.
-struct Pair {
+struct TwoFloats {
   float h, l;  // h + l, l no more than half a step of h
 };
-__device__ __forceinline__ Pair joined(float h, float l) {  // |h| >= |l|
+__device__ __forceinline__ TwoFloats joined(float h, float l) {  // |h| >= |l|
   const float s = h + l;
   return {s, l - (s - h)};
 }
-__device__ __forceinline__ Pair sum_of(float a, float b) {
+__device__ __forceinline__ TwoFloats sum_of(float a, float b) {
   const float s = a + b, t = s - a;
   return {s, (a - (s - t)) + (b - t)};
 }
-__device__ __forceinline__ Pair product_of(float a, float b) {
+__device__ __forceinline__ TwoFloats product_of(float a, float b) {
   const float p = __fmul_rn(a, b);
   return {p, fmaf(a, b, -p)};
 }
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
-  const Pair s = sum_of(a.h, b.h);
+__device__ __forceinline__ TwoFloats operator+(TwoFloats a, TwoFloats b) {
+  const TwoFloats s = sum_of(a.h, b.h);
   return joined(s.h, s.l + (a.l + b.l));
 }
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-  const Pair p = product_of(a.h, b.h);
+__device__ __forceinline__ TwoFloats operator*(TwoFloats a, TwoFloats b) {
+  const TwoFloats p = product_of(a.h, b.h);
   return joined(p.h, fmaf(a.h, b.l, fmaf(a.l, b.h, p.l)));
 }
-__device__ __forceinline__ Pair operator-(Pair a) { return {-a.h, -a.l}; }
+__device__ __forceinline__ TwoFloats operator-(TwoFloats a) { return {-a.h, -a.l}; }
 // A rotated element: what it is at the nearest 64th of a turn, and the rest.  (Of
 // keys at the first positions the first part is the key itself, and a rest below
 // every bit of it still tells the side of a border.)
 struct Turned {
-  Pair near, rest;
-  __device__ __forceinline__ float sign_of_less(Pair b) const { return (near + -b + rest).h; }  // of this - b
+  TwoFloats near, rest;
+  __device__ __forceinline__ float sign_of_less(TwoFloats b) const { return (near + -b + rest).h; }  // of this - b
 };
 __device__ __forceinline__ Turned magnitude(Turned a) {
   return a.sign_of_less({0.f, 0.f}) < 0.f ? Turned{-a.near, -a.rest} : a;
 }
 __device__ __forceinline__ bool below(Turned a, Turned b) { return (a.near + -b.near + (a.rest + -b.rest)).h < 0.f; }
 // Whether the code (scale) behind a border is not that of a magnitude; on it, the even one is.
-__device__ __forceinline__ bool misses(Turned a, Pair border, uint32_t code) {
+__device__ __forceinline__ bool misses(Turned a, TwoFloats border, uint32_t code) {
   const float d = a.sign_of_less(border);
   return d < 0.f || (d == 0.f && (code & 1));
 }
@@ -117,18 +117,19 @@ __device__ const float2 kSin64[17] = {  // of 0 .. 16 64ths, as pairs
     {0.773010433f, 2.06425526e-08f}, {0.831469595f, 1.68702634e-08f}, {0.881921291f, -2.70029634e-08f},
     {0.923879504f, 2.83074897e-08f}, {0.956940353f, -1.7184508e-08f}, {0.980785251f, 2.97394731e-08f},
     {0.99518472f, 7.10966619e-09f}, {1.0f, 0.0f}};
-__device__ __forceinline__ void turn_sincos(uint64_t a, Pair (&sn)[2], Pair (&cs)[2]) {
+__device__ __forceinline__ void turn_sincos(uint64_t a, TwoFloats (&sn)[2], TwoFloats (&cs)[2]) {
   const uint32_t k = (uint32_t)((a + (1ull << 57)) >> 58);
   const long long left = (long long)(a - ((uint64_t)k << 58));
   const float h = (float)left;
-  const Pair x = Pair{h, (float)(left - (long long)h)} * Pair{3.40612167e-19f, -9.47839643e-27f};  // 2 pi 2^-64
-  const Pair x2 = product_of(x.h, x.h);
-  const Pair s = {x.h, fmaf(x.h * x2.h, fmaf(x2.h, fmaf(x2.h, -1.f / 5040, 1.f / 120), -1.f / 6), x.l)};
-  const Pair c = {-0.5f * x2.h,
-                  fmaf(x2.h * x2.h, fmaf(x2.h, -1.f / 720, 1.f / 24), -fmaf(x.h, x.l, 0.5f * x2.l))};
+  const TwoFloats two_pi = {3.40612167e-19f, -9.47839643e-27f};  // times 2^-64
+  const TwoFloats x = TwoFloats{h, (float)(left - (long long)h)} * two_pi;
+  const TwoFloats x2 = product_of(x.h, x.h);
+  const TwoFloats s = {x.h, fmaf(x.h * x2.h, fmaf(x2.h, fmaf(x2.h, -1.f / 5040, 1.f / 120), -1.f / 6), x.l)};
+  const TwoFloats c = {-0.5f * x2.h,
+                       fmaf(x2.h * x2.h, fmaf(x2.h, -1.f / 720, 1.f / 24), -fmaf(x.h, x.l, 0.5f * x2.l))};
   const float2 s0 = kSin64[k & 15], c0 = kSin64[16 - (k & 15)];
-  sn[0] = k & 16 ? Pair{c0.x, c0.y} : Pair{s0.x, s0.y};
-  cs[0] = k & 16 ? Pair{-s0.x, -s0.y} : Pair{c0.x, c0.y};
+  sn[0] = k & 16 ? TwoFloats{c0.x, c0.y} : TwoFloats{s0.x, s0.y};
+  cs[0] = k & 16 ? TwoFloats{-s0.x, -s0.y} : TwoFloats{c0.x, c0.y};
   if (k & 32) {
     sn[0] = -sn[0];
     cs[0] = -cs[0];
@@ -144,31 +145,31 @@ template <bool IL>
 __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps, const int32_t* pos, int n, int t,
                                          int end0, int end1, const uint64_t* turn, float factor) {
   const int c = threadIdx.x & 7;
-  Pair r = {1.f, 0.f};
+  TwoFloats r = {1.f, 0.f};
   if (has_norm) {
-    Pair ss = {0.f, 0.f};
+    TwoFloats ss = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float x = part->x[i >> 3][i & 7];
-      const Pair sq = product_of(x, x), s = sum_of(ss.h, sq.h);
+      const TwoFloats sq = product_of(x, x), s = sum_of(ss.h, sq.h);
       ss = {s.h, ss.l + (s.l + sq.l)};
     }
     ss = joined(ss.h, ss.l);
     for (int o = 1; o < 8; o <<= 1)
-      ss = ss + Pair{__shfl_xor_sync(0xffffffffu, ss.h, o), __shfl_xor_sync(0xffffffffu, ss.l, o)};
-    const Pair mean = Pair{ss.h * (1.f / kD), ss.l * (1.f / kD)} + Pair{eps, 0.f};
+      ss = ss + TwoFloats{__shfl_xor_sync(0xffffffffu, ss.h, o), __shfl_xor_sync(0xffffffffu, ss.l, o)};
+    const TwoFloats mean = TwoFloats{ss.h * (1.f / kD), ss.l * (1.f / kD)} + TwoFloats{eps, 0.f};
     const float r0 = rsqrtf(mean.h);  // and a step of Newton's iteration
-    const Pair one = mean * Pair{r0, 0.f} * Pair{r0, 0.f};
+    const TwoFloats one = mean * TwoFloats{r0, 0.f} * TwoFloats{r0, 0.f};
     r = joined(r0, 0.5f * r0 * ((1.f - one.h) - one.l));
   }
   auto exact = [&](int e, int j) {
     const int i = pair_of<IL>(e, j), pair = 8 * c + i, axis = pair < end0 ? 0 : (pair < end1 ? 1 : 2);
     const bool second = IL ? j & 1 : e;
     const int e0 = IL ? e : 0, j0 = IL ? j & ~1 : j, e1 = IL ? e : 1, j1 = IL ? j | 1 : j;
-    Pair p = {part->x[e0][j0], 0.f}, q = {part->x[e1][j1], 0.f}, sn[2], cs[2];
+    TwoFloats p = {part->x[e0][j0], 0.f}, q = {part->x[e1][j1], 0.f}, sn[2], cs[2];
     if (has_norm) {
-      p = r * p * Pair{part->w[e0][j0], 0.f};
-      q = r * q * Pair{part->w[e1][j1], 0.f};
+      p = r * p * TwoFloats{part->w[e0][j0], 0.f};
+      q = r * q * TwoFloats{part->w[e1][j1], 0.f};
     }
     turn_sincos((uint64_t)(int64_t)pos[(size_t)axis * n + t] * turn[pair], sn, cs);
     if (second) return Turned{q * cs[0] + p * sn[0], q * cs[1] + p * sn[1]};
@@ -201,8 +202,8 @@ __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps
       __syncwarp();
     }
     for (int e = 0; e < 2; ++e) {
-      auto swap = [](Pair a) {
-        return Pair{__shfl_xor_sync(0xffffffffu, a.h, 1), __shfl_xor_sync(0xffffffffu, a.l, 1)};
+      auto swap = [](TwoFloats a) {
+        return TwoFloats{__shfl_xor_sync(0xffffffffu, a.h, 1), __shfl_xor_sync(0xffffffffu, a.l, 1)};
       };
       const Turned other = IL ? top[1 - e] : Turned{swap(top[e].near), swap(top[e].rest)};
       if (below(top[e], other)) top[e] = other;
@@ -211,7 +212,7 @@ __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps
       if (!part->open_scale[e]) continue;
       uint32_t at = part->scale[e];
       for (; at > 1; --at) {  // the border to the scale before, six times and by the factor
-        const Pair border = product_of(3.f * (q4_scale_value(at - 1) + q4_scale_value(at)), factor);
+        const TwoFloats border = product_of(3.f * (q4_scale_value(at - 1) + q4_scale_value(at)), factor);
         if (!misses(top[e], border, at)) break;
       }
       part->scale[e] = at;

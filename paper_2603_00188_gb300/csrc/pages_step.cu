@@ -26,11 +26,11 @@ __device__ __forceinline__ void cluster_wait_all() {
 // Two sums over the threads up to this one, and over all of them (*total).
 // Sums stop at 2^31 - 1, so that they keep their order however much is asked
 // for.  Whole CTA; calls take turns with two buffers.
-struct Pair {
+struct Sums {
   int a, b;
 };
 __device__ __forceinline__ int add_most(int x, int y) { return (int)min((uint32_t)x + (uint32_t)y, 0x7fffffffu); }
-__device__ __forceinline__ Pair scan(Pair x, Pair* warp_sums, Pair* total) {
+__device__ __forceinline__ Sums scan(Sums x, Sums* warp_sums, Sums* total) {
   constexpr int kWarps = kStepThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -43,10 +43,10 @@ __device__ __forceinline__ Pair scan(Pair x, Pair* warp_sums, Pair* total) {
   }
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  Pair before = {0, 0}, all = {0, 0};
+  Sums before = {0, 0}, all = {0, 0};
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    const Pair y = warp_sums[w];
+    const Sums y = warp_sums[w];
     if (w == warp) before = all;
     all.a = add_most(all.a, y.a);
     all.b = add_most(all.b, y.b);
@@ -67,7 +67,7 @@ __device__ __forceinline__ int session_of(const int* start, int j) {
 __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads)
     k_pages_step(const __grid_constant__ StepView s) {
   __shared__ int start[kStepThreads], tok_start[kStepThreads], kept_of[kStepThreads], keep_of[kStepThreads];
-  __shared__ Pair sums[2][kStepThreads / 32];
+  __shared__ Sums sums[2][kStepThreads / 32];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, rank = blockIdx.x, flat = rank * kStepThreads + tid;
@@ -89,7 +89,7 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
   // Pages past the rows that stay go on top of the free ones.  The sums of pages
   // are below 2^31: a table's entries are.
   int back = 0;
-  Pair total;
+  Sums total;
   for (int s0 = 0; s0 < s.n_seqs; s0 += kStepThreads) {
     load(s0);
     const int mine = held - kept;
@@ -119,7 +119,7 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
   const int n_free = (int)min((long long)s.n_pages, (long long)n0 + back);
 
   // who is served, and what it gets
-  Pair asked = {0, 0};       // pages and tokens asked for by the sessions before
+  Sums asked = {0, 0};       // pages and tokens asked for by the sessions before
   int taken = 0, given = 0;  // what those got
   int new_len = 0;
   if (rank == 0 && tid == 0) s.cu[0] = 0;
@@ -135,7 +135,7 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
     // a sum that stopped is too much for any step
     const bool served = may && (fresh == 0 || (tokens_to <= s.n_tokens && tokens_to < 0x7fffffff));
     const int pages = served ? want : 0, got = served ? fresh : 0;
-    const Pair to = scan({pages, got}, sums[1], &total);
+    const Sums to = scan({pages, got}, sums[1], &total);
     const int my_pages = to.a - pages, my_tokens = to.b - got;
     start[tid] = my_pages;
     tok_start[tid] = my_tokens;

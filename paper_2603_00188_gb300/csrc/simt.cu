@@ -99,7 +99,7 @@ constexpr int kCssBudget = 100 * 1024;  // shared-memory bytes per CTA
 constexpr int kCssMaxCols = 64;         // output columns per tile
 
 template <typename T>
-struct CssGeom {
+struct CssTile {
   static constexpr int kStride = kD * (int)sizeof(T) + 16;   // padded key row
   static constexpr int kCellBytes = kStride + 5 * 4;         // key + rn + 4 pair dots
   static constexpr int kCap = kCssBudget / kCellBytes;       // cells per CTA
@@ -121,7 +121,7 @@ template <typename T>
 __global__ void __launch_bounds__(kCssThreads) k_css(const __grid_constant__ LayerPtrs io,
                                                      const __grid_constant__ FrameTable ft, int hkv,
                                                      Strided<float> phi_all, NormsOut norms) {
-  using Gm = CssGeom<T>;
+  using Gm = CssTile<T>;
   constexpr int kChunks = kD * (int)sizeof(T) / 16;
   constexpr int kPer = 16 / (int)sizeof(T);
   extern __shared__ float4 css_smem[];
@@ -237,7 +237,7 @@ __global__ void k_fill_text_nan(const __grid_constant__ FrameTable ft, int hkv, 
 template <typename T>
 static cudaError_t css_launch_t(const Problem& p, const FrameTable& ft, const LayerPtrs& io,
                                 Strided<float> phi, const NormsOut& norms, cudaStream_t st) {
-  using Gm = CssGeom<T>;
+  using Gm = CssTile<T>;
   int tmax = 0, cmax = 0;
   for (int f = 0; f < ft.n_frames; ++f) {
     int RB, CB;
