@@ -187,8 +187,8 @@ __global__ void __cluster_dims__(kStepCtas, 1, 1) __launch_bounds__(kStepThreads
 __global__ void __launch_bounds__(256) k_step_slots(const __grid_constant__ StepView s) {
   pdl_trigger();
   pdl_wait();
+  if (blockIdx.x * 256u + threadIdx.x >= (uint32_t)s.n_tokens) return;
   const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= s.n_tokens) return;
   int slot = -1;
   if (t < s.cu[s.n_seqs]) {
     int lo = 0, hi = s.n_seqs;  // cu[lo] <= t < cu[hi]
@@ -218,7 +218,7 @@ cudaError_t launch_pages_step(const StepView& step, cudaStream_t st) {
   }
   TimingScope ts("step_slots", st);
   s.slot = step.slot;
-  e = launch_after(k_step_slots, dim3((s.n_tokens + 255) / 256), 256, 0, st, s);
+  e = launch_after(k_step_slots, dim3(((unsigned)s.n_tokens + 255) / 256), 256, 0, st, s);
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
