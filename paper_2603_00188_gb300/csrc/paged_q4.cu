@@ -1,5 +1,5 @@
-// Rows into 4-bit pages (the compaction's, see k_rotate for a step's tokens)
-// and out of them.
+// Rows into 4-bit pages (the compaction's; a step's tokens: k_append_q4) and out of
+// them.
 #include "kernels.cuh"
 #include "paged.cuh"
 #include "q4.cuh"
@@ -44,9 +44,9 @@ __device__ __forceinline__ uint32_t Group16<__nv_bfloat16>::top() const {
 // k_gather_paged with the kept rows put into 4 bits on the way.  A lane takes a
 // group of 16 elements, eight lanes a row of a head, and a CTA 32 rows of one
 // head, whose codes are one piece of each of their pages.  28 layers of 10,720
-// rows: 124 us, 0.93 of a copy's rate for the bytes (a lane to 8 elements, whose
-// scales two lanes then form, and a division for each element: 208).  HBM bounds
-// it, with the integer pipe half busy.
+// rows: 115 us, a plain copy's rate for the bytes (a lane to 8 elements, whose
+// scales two lanes then form, and a division for each element: some 200).  HBM
+// bounds it, with the integer pipe half busy.
 template <typename T>
 __global__ void __launch_bounds__(256) k_gather_q4(const __grid_constant__ Q4Layers io,
                                                    const __grid_constant__ PageView pg, int seq, int n, int hkv,

@@ -15,12 +15,17 @@ namespace stl {
 //
 // A unit is a warp's: a segment of a token's query heads, as k_rotate's, or four of
 // its key and value heads, whose lanes share a group of 16 elements by twos (one
-// lane has it where pairs are interleaved).  The bytes moved bound long prompts
-// (8,616 tokens of 28 + 4 bf16 heads 37.4 us, 0.66 of a plain copy's rate; 34.4
-// without the second end and what it decides, with wrong codes), latency the rest
-// (2,096 tokens of 12 + 2 heads 9.1 us with a fetch of 2).  Keys are most of a
-// warp's work, so that warps of four tokens' keys share a CTA and those of the
-// first kAhead tokens come before anything else.
+// lane has it where pairs are interleaved).  Instructions bound long prompts of
+// bf16: 8,616 tokens of 28 + 4 heads take 31 us, 0.70 of a plain copy's rate, where
+// the append in 16 bits, with the same rotation, has 0.89.  They execute 22 million
+// warp instructions, 62 % of the cycles that could issue one, with the integer pipe
+// (conversions, comparisons of codes, masks) busy for 57 % and 44 % of the warps
+// resident; a norm adds 4 us, the keys' second end and what it decides 3.  fp32 has
+// twice the bytes for them: 46 us, 0.92.  Latency bounds the rest (2,096 tokens of
+// 12 + 2 heads 6.7 us, one 2.3).  Keys are most of a warp's work, so that warps of
+// four tokens' keys share a CTA and those of the first kAhead tokens come before
+// anything else.
+//
 // A lane's elements of a key: as they are in memory, the norm's weights, rotated in fp32 and how far (each pair, and
 // all pairs of the groups) they may be off by that; codes, the scales of their groups, and which codes (nibbles that
 // are not 0) and scales are open.
@@ -243,12 +248,13 @@ __device__ __noinline__ void settle_keys(KeyPart* part, bool has_norm, float eps
 
 // A token's units in order: the keys and values of the first kAhead tokens; then by
 // fours of tokens keys and values kAhead tokens ahead, and queries; the last queries.
-// Measured at 2,096 and 8,616 tokens, each token's units together: 11.6 and 40.1 us;
-// with kAhead 0: 10.5 and 37.8; 1,216: 9.5 and 37.8; 2,432: 9.2 and 38.2; all: 9.2 and 40.6.
+// Measured at 2,096 tokens of 12 + 2 heads with norms and 8,616 of 28 + 4, in bf16, and
+// the latter in fp32: kAhead 0: 8.4, 32.2 and 45.5 us; 1,216: 7.0, 30.7, 44.9; 2,432: 6.7,
+// 31.1, 46.0; all: 6.7, 33.1, 49.6.  (Each token's units together: 2 us more than with 2,432.)
 constexpr int kAhead = 2432;
 // Divides numbers below 2^31 by d: the product with 2^shift / d, rounded up, is off by
 // less than a quotient's step (Granlund and Montgomery, 1994).  Three instructions for
-// some thirty, of a warp's 500: 38.2 to 37.4 us.
+// some thirty, of a warp's 500: 0.8 us of 8,616 tokens'.
 struct Divisor {
   uint32_t mul;
   int shift, d;
@@ -286,8 +292,9 @@ __device__ __forceinline__ Unit unit_of(int u, const Order& o) {
   return {o.rest + t, u - t * o.q.d};
 }
 
-// Registers for eight CTAs an SM, seven of fp32 (few are spilled): 8,616 tokens of bf16 take 41.0 / 40.6 / 39.9 us
-// with seven / eight / nine, one 4.4 / 4.4 / 4.5; fp32 with norms 59.6 / 62.5 / 68.3.
+// Registers for eight CTAs an SM, seven of fp32 (few are spilled): 8,616 tokens of bf16 take 31.3 / 31.1 / 30.2 us
+// with seven / eight / nine, one 2.3 / 2.3 / 2.5, 64 3.9 / 3.9 / 4.0; 8,616 of fp32 with norms 49.7 / 49.1 / 53.2 with
+// six / seven / eight.
 template <typename T, int NB, bool IL>
 __global__ void __launch_bounds__(kRotThreads, sizeof(T) == 2 ? 8 : 7)
     k_append_q4(const __grid_constant__ TokenView x, const __grid_constant__ RopeView rope,

@@ -15,9 +15,12 @@
 // code * scale is exact in fp16. What is rounded: queries, scaled by a power of
 // two so that the largest element of each is in [1, 2), to fp16, which holds
 // bf16 ones exactly down to 2^-17 of the largest and loses less than 2^-25 of
-// it below; and weights, to fp16's 11 bits (2^-12, an eighth of the bf16
-// result's own rounding).  fp32 queries and their weights are taken as hi + lo,
-// two parts of 11 bits, which is twice the products.
+// it below; and weights, to fp16's 11 bits (2^-12, an eighth of the bf16 result's
+// own rounding: 32 sessions of 1,000 to 53,600 rows are off from 64 bits by 1.685e-3
+// of the result where that rounding alone makes 1.673e-3; with weights in two parts,
+// also 1.673e-3, they take 61.7 us and not 55.9, 28 queries to a head 130 and not
+// 100).  fp32 queries and their weights are taken as hi + lo, two parts of 11 bits,
+// which is twice the products (off by 4.6e-7, as fp32 throughout).
 //
 // Weights are 2^(x - m), m the largest score so far less 10, moved only when one
 // exceeds it by more than 14: no maximum is formed for blocks that do not.  So they
@@ -727,9 +730,15 @@ cudaError_t launch_paged_attention_q4(DType dt, const PageView& view, const void
   const int rows = pages.w * (hq / hkv), part_rows = q4_part_rows(dt, pages, hq / hkv), most = q4_most_rows(dt);
   const int chunks = (rows + most - 1) / most, chunk_rows = (rows + chunks - 1) / chunks, ctas = q4_ctas(part_rows);
   const long long items = (long long)pages.n_seqs * hkv * chunks;
-  pages.item_units = 12;
   pages.block_shift = kQaBlockShift;
+  // Blocks that an item's own costs take: 6 / 12 / 18 / 24 make 58.4 / 55.7 / 54.7 / 55.5 us of 32 sessions of 1,000 to
+  // 53,600 rows, 27.7 / 27.1 / 27.9 / 28.5 of 64 of 2,000, 15.7 / 15.6 / 15.6 / 16.7 of five tokens each of eight.
+  pages.item_units = 12;
+  // And those that splitting one takes: 0 and 10 as 20; 40 makes 11.9 us and not 8.3 of one session of 1,000 rows, 30.7
+  // and not 27.2 of 64 of 2,000.
   int split = 20;
+  // Tables of at most eight blocks: their items stay whole, which saves the second launch (64 sessions of 256 rows
+  // 9.1 us, 11.2 split; up to 32 blocks one of 1,000 rows would: 11.2, 8.3 split).
   const long long longest = ((long long)pages.max_pages * pages.page_rows + kQaBlock - 1) / kQaBlock;
   const int mode = longest <= 8 ? kWholeItems : (items <= ctas ? kDescByItem : kDescByCta);
   if (mode == kWholeItems) split = 1 << 30;

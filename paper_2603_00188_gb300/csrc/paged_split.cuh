@@ -113,8 +113,9 @@ __device__ __forceinline__ Item item_at(const Cursor& c, int u) {
 // (writing them, a second part in the CTA, the merge).  Where CTAs with whole
 // items, each the CTA's where its first unit falls, are sure to take no longer
 // than the even ranges and this, the range's ends move on to the next item's
-// start: 64 sessions of 2,000 rows on 304 CTAs take 45 us so and 53 split; 8 of
-// 256 rows 7.8 and 8.2; 8 of 500 rows, a tenth of the CTAs, 11.2 and 9.0.
+// start: of 16-bit rows, 64 sessions of 2,000 on 304 CTAs take 45 us so and 53
+// split; 8 of 256 rows 7.8 and 8.2; 8 of 500 rows, a tenth of the CTAs, 11.2 and 9.0.
+// (4-bit rows: see their launch.)
 template <int THREADS>
 struct RangeScratch {
   int warp_sum[THREADS / 32], warp_most[THREADS / 32], warp_least[THREADS / 32];
