@@ -76,12 +76,6 @@ __device__ __forceinline__ void pm_mma(float (&d)[4], const uint32_t (&a)[4], ui
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// The 8 x 8 matrix of 16-bit values held two to a lane, transposed.
-__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
-  uint32_t y;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
 
 // Whether either of two bf16 is an infinity or a NaN.
 __device__ __forceinline__ bool has_odd_bf16(uint32_t x) {

@@ -152,14 +152,13 @@ __global__ void __launch_bounds__(256) k_fetch_q4(const __grid_constant__ Q4Laye
       if (u0 + i * (int)gridDim.y >= units) break;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint32_t s2 = q4_scales(b[i][k] | b[i][k] << 8);
+        const __half2 s2 = as_half2(q4_scales(b[i][k] | b[i][k] << 8));
         uint32_t p[4];
         float y[8];
         q4_codes(w[i][k], p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t v = mul_f16x2(p[j], s2);
-          const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&v));
+          const float2 z = __half22float2(as_half2(mul_half2(p[j], s2)));
           y[2 * j] = z.x * f[i];
           y[2 * j + 1] = z.y * f[i];
         }

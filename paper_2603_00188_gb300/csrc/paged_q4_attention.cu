@@ -80,22 +80,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
-__device__ __forceinline__ uint32_t mul_half2(uint32_t x, __half2 y) {
-  const __half2 z = __hmul2(as_half2(x), y);
-  return *reinterpret_cast<const uint32_t*>(&z);
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(as_half2(x)); }
-// The 8 x 8 matrix of 16-bit values held two to a lane, transposed.
-__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
-  uint32_t y;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -546,10 +535,10 @@ __global__ void __launch_bounds__(kQaThreads, qa_ctas(NT))
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 const uint32_t hi = pack_f16(z[2 * x], z[2 * x + 1]);
-                p[0][nt][x] = turn8x8(hi);
+                p[0][nt][x] = transpose8x8(hi);
                 if (kParts == 2) {
                   const float2 t = unpack_f16(hi);
-                  p[kParts - 1][nt][x] = turn8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
+                  p[kParts - 1][nt][x] = transpose8x8(pack_f16(z[2 * x] - t.x, z[2 * x + 1] - t.y));
                 }
               }
             }

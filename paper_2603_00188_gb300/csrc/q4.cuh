@@ -16,10 +16,10 @@ constexpr int kQ4Group = 16;           // elements of a scale
 constexpr int kQ4Scales = kD / kQ4Group;
 constexpr uint32_t kQ4NaN = 0x7f;      // the scale of a group that holds an infinity or a NaN
 
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t mul_half2(uint32_t x, __half2 y) {
+  const __half2 z = __hmul2(as_half2(x), y);
+  return *reinterpret_cast<const uint32_t*>(&z);
 }
 // The two e4m3 scales of the low 16 bits, as fp16.
 __device__ __forceinline__ uint32_t q4_scales(uint32_t two) {
@@ -126,8 +126,7 @@ __device__ __forceinline__ uint32_t q4_scale_byte(float want) {
   return two;  // the upper half is zero
 }
 __device__ __forceinline__ float q4_scale_value(uint32_t byte) {
-  const uint32_t half = q4_scales(byte);
-  return __low2float(*reinterpret_cast<const __half2*>(&half));
+  return __low2float(as_half2(q4_scales(byte)));
 }
 
 // top: the bits of the group's largest magnitude as integers order them, which
