@@ -577,17 +577,22 @@ typedef struct {
 
 /* stlite_paged_append into 4-bit pages: values are put in as they are, keys with
  * the codes and scales of their rotation in 64 bits (angles to 2^-64 of a turn for
- * each position), not of its fp32 form; q_out as there.  Everything else as for
- * stlite_paged_append. */
+ * each position), not of its fp32 form; q_out as there.  Keys' magnitudes are below
+ * 2^126, and with a norm the mean of a head's squares and eps together within
+ * 2^-80 .. 2^120: beyond, fp32 does not hold the rotation or the sum.  Everything
+ * else as for stlite_paged_append. */
 STLITE_API stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope,
                                                 const stlite_tokens* x, const stlite_pages* pages, void* q_out,
                                                 const stlite_q4_pools* pools, void* stream);
 
 /* stlite_paged_attention over 4-bit pages: the same result for the elements'
- * values above.  bf16 queries: weights are rounded to 11 bits.  A row that a
- * token sees and whose key has a NaN scale makes the token's head's output NaN;
- * one whose value has makes its 16 elements NaN.  Rows that a token does not see
- * take no part, whatever they hold.
+ * values above.  A row's weight is rounded to 11 bits for bf16 queries; for fp32
+ * ones weights and queries are rounded to 22 bits.  What is below 2^-25 of a query's
+ * largest element may be lost, and weights below 2^-34 of a token's largest may
+ * count in their sum alone.  Finite queries and elements have finite results.  A
+ * row that a token sees and whose key has a NaN scale makes the token's head's
+ * output NaN; one whose value has makes its 16 elements NaN.  Rows that a token
+ * does not see take no part, whatever they hold.
  * q, out [T][Hq][d] (shape->dtype), packed.  shape, ws, T = 0 and errors as for
  * stlite_paged_attention; ws: at least stlite_paged_q4_workspace_size bytes. */
 STLITE_API stlite_status stlite_paged_attention_q4(const stlite_shape* shape, const stlite_pages* pages, const void* q,
@@ -663,7 +668,12 @@ STLITE_API stlite_status stlite_paged_fetch_q4(const stlite_shape* shape, const 
  *   3. len[s] = rows that stay + new tokens, cu_new[S + 1] the sums of the new
  *      tokens, *n_free the pages that are left.  slot[i], i < n_tokens: page *
  *      page_rows + row of the page of packed new token i, -1 for those behind
- *      cu_new[S] and where the table names a page outside the pool.
+ *      cu_new[S] and where the table names a page outside the pool.  (For kernels
+ *      of the caller's that write or read rows; stlite_paged_append and the other
+ *      calls find places from the table, and slot may be NULL for them.)
+ * fresh has no upper bound but these: a step whose tokens are attended from asks
+ * for no more of a session than that call's window, as stlite_paged_attention
+ * leaves the tokens past it unwritten.
  * pages: all fields as above, cu_new given.  keep, fresh: device [S].
  * free_pages: device [n_pages], its first *n_free entries (0 .. n_pages) pages
  * that no session holds; entries past *n_free are room.  n_free: device.
