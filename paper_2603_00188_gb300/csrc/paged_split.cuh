@@ -56,7 +56,7 @@ __device__ __forceinline__ SeqWork seq_work(const PageView& pg, int first, int f
   w.first = first;
   w.fresh = fresh;
   w.len = max(0, min(len, pg.max_pages * pg.page_rows));
-  w.blocks = (w.len + (1 << pg.block_shift) - 1) >> pg.block_shift;
+  w.blocks = (int)(((uint32_t)w.len + (1u << pg.block_shift) - 1u) >> pg.block_shift);  // len may be 2^31 - 1
   w.units = pg.item_units + w.blocks;
   const int rows = max(0, min(fresh, pg.w)) * G;
   w.chunks = rows <= chunk_rows ? (rows > 0 ? 1 : 0) : (rows + chunk_rows - 1) / chunk_rows;
