@@ -577,10 +577,11 @@ typedef struct {
 
 /* stlite_paged_append into 4-bit pages: values are put in as they are, keys with
  * the codes and scales of their rotation in 64 bits (angles to 2^-64 of a turn for
- * each position), not of its fp32 form; q_out as there.  Keys' magnitudes are below
- * 2^126, and with a norm the mean of a head's squares and eps together within
- * 2^-80 .. 2^120: beyond, fp32 does not hold the rotation or the sum.  Everything
- * else as for stlite_paged_append. */
+ * each position), not of its fp32 form (an element within 2^-38 of its pair's
+ * magnitude of a border between two codes may have either); q_out as there.  Keys'
+ * magnitudes are below 2^126, and with a norm the mean of a head's squares and eps
+ * together within 2^-80 .. 2^120: beyond, fp32 does not hold the rotation or the
+ * sum.  Everything else as for stlite_paged_append. */
 STLITE_API stlite_status stlite_paged_append_q4(const stlite_shape* shape, const stlite_rope* rope,
                                                 const stlite_tokens* x, const stlite_pages* pages, void* q_out,
                                                 const stlite_q4_pools* pools, void* stream);
