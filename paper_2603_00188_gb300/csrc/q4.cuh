@@ -85,7 +85,7 @@ struct Q4Factor {
 __device__ __forceinline__ float q4_beside(float y, float x, float a, float b) {  // y: of x and a b
   const float t = __fmul_rn(a, b), left = fmaf(-y, fmaf(a, b, -t), fmaf(-y, t, x));
   const int bits = __float_as_int(y);
-  if ((bits & 0x7ffff) != 0 || left == 0.f) return y;
+  if ((bits & 0x7ffff) != 0 || left == 0.f || fabsf(y) > 448.f) return y;  // no border above (y may be an infinity)
   return __int_as_float(bits + ((__float_as_int(left) ^ bits) < 0 ? -1 : 1));
 }
 __device__ __forceinline__ bool q4_long(float f) { return (__float_as_uint(f) & 0x7ffu) != 0u; }

@@ -93,3 +93,30 @@ def test_factors_of_a_few_digits(st, factor):
     st.stlite_compact_paged_q4([(x.cuda(), x.cuda(), p, torch.arange(n, dtype=I32, device="cuda")[None])], n, pt, 0)
     for y in "kv":
         _equal(p, y, *ref.encode(x, f[:, None]), (table[0].long()[r // page], slice(None), r % page))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("exponent", [-60, -30, 30, 59])
+def test_elements_far_from_their_factor(st, dtype, exponent):
+    """Magnitudes from 2^-126 to 2^126 of either sign: quotients past fp32's ends become the largest code, or 0."""
+    g, page, n, hkv = _gen(exponent + 99), 16, 40, 4
+    f = 2.0 ** exponent * torch.tensor([1.0, 1.0 + 2 ** -23, 1.37, 1.99])
+    x = torch.randn((n, hkv, 8, 16), generator=g).clamp(-1, 1) * torch.exp2(torch.randint(-126, 127, (n, hkv, 8, 1), generator=g).float())
+    x[::3] *= torch.exp2(torch.randint(-40, 1, x[::3].shape, generator=g).float())
+    x[:, :, :, 3] = torch.exp2(torch.randint(-126, 127, (n, hkv, 8), generator=g).float())  # few bits, as a border
+    x[:, :, :, 4] = -x[:, :, :, 3]
+    x = x.flatten(-2).to(dtype)
+    want = ref.encode(x, f[:, None])
+    table, pages = _table([n], page, 7)
+    r = torch.arange(n)
+    at = (table[0].long()[r // page], slice(None), r % page)
+    pt = st.make_pages(pages, page, table.cuda(), _ints([n]), max_new=n)
+    p = st.make_q4_pools(pages, page, hkv, f.cuda(), f.cuda())
+    st.stlite_compact_paged_q4([(x.cuda(), x.cuda(), p, torch.arange(n, dtype=I32).repeat(hkv, 1).cuda())], n, pt, 0)
+    for y in "kv":
+        _equal(p, y, *want, at)
+    p = st.make_q4_pools(pages, page, hkv, f.cuda(), f.cuda())
+    q, pos = _randn(g, n, hkv, 128, dtype=dtype), torch.zeros(n, dtype=I32, device="cuda")
+    st.stlite_paged_append_q4(q, x.cuda(), x.cuda(), pos, st.make_rope(), pt, q.clone(), p)
+    for y in "kv":
+        _equal(p, y, *want, at, y == "k")
